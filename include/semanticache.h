@@ -355,6 +355,130 @@ sc_status sc_multi_attn(const void *Q, sc_dtype q_dtype, int nq,
                         void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * A cache held in pages.  A serving program that keeps the caches of many sequences gives each of them
+ * pages of a pool instead of an array of its largest length.  Three calls work on such a cache: new rows
+ * go to it (sc_paged_append), one new token of every sequence attends to it (sc_paged_decode_attn), or to
+ * the pages of it that a bound on the logits selects (sc_paged_select).  Rows may be tokens, or merged
+ * rows with their sizes as sc_gsc_merge leaves them (then every KV head has its own number of rows).
+ *
+ *   pools       K, V     [num_pages, page_heads, page_rows, d] of dtype, addressed as
+ *                        base + page*stride_page + head*stride_head + row*stride_row (+ e), strides in
+ *                        ELEMENTS, the same for K and V, multiples of 16 bytes; 16-byte aligned
+ *               counts   i32 [num_pages, page_heads, page_rows], contiguous, or NULL: sizes of the rows
+ *               k_min, k_max   [num_pages, page_heads, d] of dtype, contiguous, 16-byte aligned, or both
+ *                        NULL: per page the minimum and maximum of the keys that it holds
+ *   page_heads           Hkv: a page holds its rows for all KV heads, table [B, table_len];
+ *                        1 (with Hkv > 1, or if table_per_head is set): every KV head has pages of its
+ *                        own, table [B, Hkv, table_len]
+ *   page_rows            a power of two, 16 .. 1024
+ *   table       i32, contiguous: row t of a sequence (and head) is row t % page_rows of page
+ *               table[.., t / page_rows].  Entries behind the last page that holds a row are never read.
+ *
+ * Lengths (base_lens, new_lens, lens) are i32 [B], or [B, Hkv] where per_head is set.  A page number
+ * outside [0, num_pages) is found on the device and never followed (see the calls).  Two sequences may
+ * name the same page (a common prefix), but rows are appended only to pages that one of them names.
+ *
+ * Common host errors: NULL or misaligned pointers, sizes <= 0, page_rows not a power of two or out of
+ * range, page_heads neither Hkv nor 1, strides that let rows overlap or reach 2 GiB inside a page
+ * (SC_ERR_INVALID_ARG); d not in {64, 128}, bad dtype, B or Hkv > 65535, B * Hkv > 2^20, table_len *
+ * page_rows >= 2^31 (SC_ERR_UNSUPPORTED).
+ */
+typedef struct {
+    void *K, *V;
+    int32_t *counts;
+    void *k_min, *k_max;
+    const int32_t *table;
+    int64_t stride_page, stride_head, stride_row;
+    int32_t dtype;             /* sc_dtype */
+    int32_t num_pages, page_heads, page_rows;
+    int32_t table_len, table_per_head;
+    int32_t B, Hkv, d;
+} sc_paged_cache;
+
+/* sc_paged_append — rows that arrive go to the pages of their sequences, and the rotation of positions is
+ * applied on the way: for n < new_lens[b] (or [b,h]), with t = base_lens[b] + n,
+ *     K page row t = rot(K[b,h,n], positions[b] + n),  V page row t = V[b,h,n],  counts page row t = counts[b,h,n],
+ *     lens[b] = base_lens[b] + new_lens[b],   Q_out[b,hq,n] = rot(Q[b,hq,n], positions[b] + n)  for every n < N.
+ * rot turns the first `rot` elements of a row: element pairs (i, i + rot/2), or (2i, 2i + 1) if interleaved,
+ * with cos and sin of the row's position:  a' = a cos - b sin, b' = b cos + a sin, in fp32, rounded once.
+ * k_min / k_max of every page that receives a row are computed over all keys that the page holds after the
+ * call (as stored; rows behind the length, left there by an earlier and longer one, do not count; a NaN in a column shows).
+ *
+ *   K, V            device [B, Hkv, N, d] of the cache's dtype; strides (b, h, n) of each in ELEMENTS,
+ *                   multiples of 16 bytes, the last dimension contiguous, 16-byte aligned
+ *   counts          device i32 [B, Hkv, N], contiguous; required if and only if the cache has counts
+ *   base_lens       device i32: rows that the cache holds
+ *   new_lens        device i32 or NULL (= N for all): rows to append, 0 .. N
+ *   lens            device i32: the new lengths; not the same array as base_lens or new_lens.  Set to -1, with nothing
+ *                   written to the cache for it, if base_lens is negative, new_lens outside [0, N], the sum
+ *                   beyond table_len * page_rows, or a position of a row outside the angles; set to -1
+ *                   if a page it needs has a number outside the pool (rows of its other pages are written)
+ *   cos_sin         device f32 [max_position, rot]: rot/2 cosines, then rot/2 sines; or NULL: no rotation
+ *   rot             0 without cos_sin, else a multiple of 16 up to d
+ *   positions       device i32 [B]: position of row 0 of the call, or NULL: base_lens (not with per_head)
+ *   Q, Q_out        device [B, Hq, N, d] of q_dtype (strides as for K and V), or both NULL; only with cos_sin.  Q_out may
+ *                   be Q itself.  A query whose position lies outside the angles comes out as NaN
+ */
+typedef struct {
+    const void *K, *V;
+    int64_t k_stride_b, k_stride_h, k_stride_n, v_stride_b, v_stride_h, v_stride_n;
+    const int32_t *counts;
+    int32_t N, per_head;
+    const int32_t *base_lens, *new_lens;
+    int32_t *lens;
+    const float *cos_sin;
+    int32_t max_position, rot, interleaved, Hq;
+    const int32_t *positions;
+    const void *Q;
+    void *Q_out;
+    int64_t q_stride_b, q_stride_h, q_stride_n, o_stride_b, o_stride_h, o_stride_n;
+    int32_t q_dtype;           /* sc_dtype */
+} sc_paged_rows;
+sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *rows, void *stream);
+
+/* The workspace of the two calls below: sc_paged_workspace_bytes bytes for a cache of B sequences, Hkv KV heads
+ * and tables of table_len pages, initialised ONCE with sc_paged_init_workspace; calls that share it must be
+ * stream-ordered, and need no more care.  (It starts with one counter per (sequence, KV head): the workgroups that
+ * share a head's rows count themselves off, the last one joins their partial results and leaves the counter at zero.)
+ */
+size_t sc_paged_workspace_bytes(int B, int Hq, int Hkv, int d, int table_len);
+sc_status sc_paged_init_workspace(void *ws, size_t ws_bytes, int B, int Hkv, void *stream);
+
+/* sc_paged_decode_attn — sc_decode_attn over a cache in pages:
+ *     O[b,hq] = softmax_t( Q[b,hq] . K[b,h,t] * scale + ln(counts[b,h,t]) ) V[b,h,t],  t in [0, lens),  h = hq / (Hq / Hkv),
+ * without the logarithm if the cache has no counts.  fp32 (bf16 caches: probabilities in two bf16 parts, queries of fp32 and their probabilities in
+ * three); fp32 accumulation.  Rows of size <= 0 weigh nothing.  A length <= 0 gives O = 0 and
+ * lse = -inf; a length beyond the table's pages counts as the pages' rows.  A page number outside the pool gives NaN for its heads' O and lse.
+ *   Q               device [B, Hq, d] of q_dtype, contiguous, 16-byte aligned; Hq / Hkv <= 16
+ *   lens            device i32 [B], or [B, Hkv] if lens_per_head
+ *   sel, sel_lens   device i32 [B, Hkv, keep] and [B, Hkv], or both NULL (keep is then ignored): only the rows of pages number
+ *                   sel[b,h,0 .. sel_lens[b,h]) of the sequence (places in its table, as sc_paged_select leaves
+ *                   them) attend.  A place outside the table gives NaN like a bad page number
+ *   scale           logit scale; 0 selects 1/sqrt(d)
+ *   O               device [B, Hq, d] of o_dtype, contiguous, 16-byte aligned;  lse  device f32 [B, Hq] or NULL
+ */
+sc_status sc_paged_decode_attn(const sc_paged_cache *cache, const void *Q, sc_dtype q_dtype, int Hq,
+                               const int32_t *lens, int lens_per_head,
+                               const int32_t *sel, const int32_t *sel_lens, int keep, float scale,
+                               void *O, sc_dtype o_dtype, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* sc_paged_select — the pages of every (sequence, KV head) whose keys can come closest to its queries.  With the
+ * bounds of a page, no row of it has a larger logit (before scale > 0) than
+ *     score = max over the Hq / Hkv query heads of  sum_e max(q_e k_min_e, q_e k_max_e).
+ * The first `first` and the last `recent` pages of a sequence are kept in any case, then those of the largest
+ * scores, up to `keep` pages, of equal scores the lowest; a score that is not a number and a page number outside the pool rank
+ * above all others, so that attention over the selection shows them.  Scores are sums in fp64: the choice is
+ * that of exact arithmetic except for scores within some 1e-13 of each other.
+ *   Q, lens         as for sc_paged_decode_attn;  the cache needs k_min and k_max
+ *   keep            1 .. 2^20, at least first + recent (SC_ERR_CAPACITY otherwise)
+ *   sel             device i32 [B, Hkv, keep]: the pages' places in the table, ascending, -1 behind the last
+ *   sel_lens        device i32 [B, Hkv]: how many: min(keep, pages that hold rows)
+ */
+sc_status sc_paged_select(const sc_paged_cache *cache, const void *Q, sc_dtype q_dtype, int Hq,
+                          const int32_t *lens, int lens_per_head, int keep, int first, int recent,
+                          int32_t *sel, int32_t *sel_lens, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
  * sc_stream_read_probe — a measuring aid for benchmarks, not a step of the method: reads the first
  * `bytes` bytes (rounded down to a multiple of 16) of a device buffer once, 16 bytes per lane, fully
  * coalesced, eight non-temporal loads in flight per lane, one workgroup of twelve wavefronts per CU on a

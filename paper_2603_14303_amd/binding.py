@@ -30,6 +30,23 @@ class SemantiCacheError(RuntimeError):
     pass
 
 
+class _PagedCacheStruct(ctypes.Structure):      # sc_paged_cache
+    _fields_ = [(x, ctypes.c_void_p) for x in ("K", "V", "counts", "k_min", "k_max", "table")] + \
+               [(x, ctypes.c_int64) for x in ("stride_page", "stride_head", "stride_row")] + \
+               [(x, ctypes.c_int32) for x in ("dtype", "num_pages", "page_heads", "page_rows", "table_len", "table_per_head", "B", "Hkv", "d")]
+
+
+class _PagedRowsStruct(ctypes.Structure):       # sc_paged_rows
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p)] + \
+               [(x, ctypes.c_int64) for x in ("k_stride_b", "k_stride_h", "k_stride_n", "v_stride_b", "v_stride_h", "v_stride_n")] + \
+               [("counts", ctypes.c_void_p), ("N", ctypes.c_int32), ("per_head", ctypes.c_int32)] + \
+               [(x, ctypes.c_void_p) for x in ("base_lens", "new_lens", "lens", "cos_sin")] + \
+               [(x, ctypes.c_int32) for x in ("max_position", "rot", "interleaved", "Hq")] + \
+               [(x, ctypes.c_void_p) for x in ("positions", "Q", "Q_out")] + \
+               [(x, ctypes.c_int64) for x in ("q_stride_b", "q_stride_h", "q_stride_n", "o_stride_b", "o_stride_h", "o_stride_n")] + \
+               [("q_dtype", ctypes.c_int32)]
+
+
 def load_library() -> ctypes.CDLL:
     """Load libsemanticache.so built in-tree (python -m paper_2603_14303_amd.build)."""
     global _lib, _native
@@ -100,6 +117,17 @@ def load_library() -> ctypes.CDLL:
     lib.sc_gsc_merge_budget.restype = i32
     lib.sc_gsc_merge_budget.argtypes = [vp, vp, i32, i64, i64, i64, vp, vp, i64, vp, i32, i32, i32, i32,
                                         i64, f32, f32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    pc = c.POINTER(_PagedCacheStruct)
+    lib.sc_paged_append.restype = i32
+    lib.sc_paged_append.argtypes = [pc, c.POINTER(_PagedRowsStruct), vp]
+    lib.sc_paged_workspace_bytes.restype = sz
+    lib.sc_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+    lib.sc_paged_init_workspace.restype = i32
+    lib.sc_paged_init_workspace.argtypes = [vp, sz, i32, i32, vp]
+    lib.sc_paged_decode_attn.restype = i32
+    lib.sc_paged_decode_attn.argtypes = [pc, vp, i32, i32, vp, i32, vp, vp, i32, f32, vp, i32, vp, vp, sz, vp]
+    lib.sc_paged_select.restype = i32
+    lib.sc_paged_select.argtypes = [pc, vp, i32, i32, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
     if torch is not None:
         _native = _load_native()
     _lib = lib
@@ -130,6 +158,7 @@ EXPORTED = [
     "sc_multi_attn_workspace_bytes", "sc_multi_attn", "sc_multi_attn_tail",
     "sc_gsc_merge_budget_workspace_bytes", "sc_gsc_merge_budget",
     "sc_gsc_merge_global_workspace_bytes", "sc_gsc_merge_global",
+    "sc_paged_append", "sc_paged_workspace_bytes", "sc_paged_init_workspace", "sc_paged_decode_attn", "sc_paged_select",
 ]
 
 
@@ -469,6 +498,175 @@ def sc_gsc_merge_global(K, V, tau: float, seq_lens=None, cap: Optional[int] = No
                                  _ptr(comp_lens), _ptr(cluster_id), workspace.ptr, workspace.nbytes, _stream())
     _check(st, "sc_gsc_merge_global")
     return Kc, Vc, counts, comp_lens, cluster_id
+
+
+# ------------------------------------------------------------------------------------------------ a cache held in pages
+def _is_i32(t, *shapes) -> bool:
+    return t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) in shapes
+
+
+class PagedCache:
+    """The pools and tables of a cache held in pages (sc_paged_cache); the tensors are the caller's and stay theirs.
+
+    K, V [pages, heads, R, d], any strides with a contiguous last dimension, the same for both; counts i32 [pages, heads, R], k_min and k_max
+    [pages, heads, d] contiguous, if any; table i32 [B, P], or [B, Hkv, P] with pools of one head a page: every KV head then has pages of its own.
+    """
+
+    def __init__(self, K, V, table, counts=None, k_min=None, k_max=None):
+        load_library()
+        if K.dim() != 4 or K.shape != V.shape or K.stride() != V.stride() or K.dtype != V.dtype or (K.shape[3] > 1 and K.stride(3) != 1):
+            raise SemantiCacheError("K and V must be [pages, heads, R, d] with identical strides and dtype and contiguous rows")
+        pages, heads, R, d = K.shape
+        if table.dim() not in (2, 3) or table.dtype != torch.int32 or not table.is_contiguous():
+            raise SemantiCacheError("table must be int32 [B, P] or [B, Hkv, P], contiguous")
+        if table.dim() == 3 and heads != 1:
+            raise SemantiCacheError("a table per KV head needs pools of one head a page")
+        if counts is not None and not _is_i32(counts, (pages, heads, R)):
+            raise SemantiCacheError("counts must be int32 [pages, heads, R], contiguous")
+        for t in (k_min, k_max):
+            if t is not None and (t.dtype != K.dtype or tuple(t.shape) != (pages, heads, d) or not t.is_contiguous()):
+                raise SemantiCacheError("k_min and k_max must be [pages, heads, d] of the pools' dtype, contiguous")
+        if (k_min is None) != (k_max is None):
+            raise SemantiCacheError("k_min and k_max come together")
+        _require_cuda(K, V, table, counts, k_min, k_max)
+        self.K, self.V, self.table, self.counts, self.k_min, self.k_max = K, V, table, counts, k_min, k_max
+        self.B, self.Hkv, self.d = table.shape[0], table.shape[1] if table.dim() == 3 else heads, d
+        self.struct = _PagedCacheStruct(
+            K=_ptr(K), V=_ptr(V), counts=_ptr(counts), k_min=_ptr(k_min), k_max=_ptr(k_max), table=_ptr(table),
+            stride_page=K.stride(0), stride_head=K.stride(1), stride_row=K.stride(2), dtype=_dtype_code(K), num_pages=pages, page_heads=heads,
+            page_rows=R, table_len=table.shape[-1], table_per_head=int(table.dim() == 3), B=self.B, Hkv=self.Hkv, d=d)
+        self.ptr = ctypes.addressof(self.struct)
+
+    def lens_shapes(self):
+        return (self.B,), (self.B, self.Hkv)
+
+
+def sc_paged_append(cache: PagedCache, K, V, base_lens, lens, new_lens=None, counts=None, Q=None, Q_out=None, cos_sin=None, positions=None,
+                    interleaved: bool = False):
+    """K, V [B, Hkv, N, d] go behind the base_lens rows of their sequences, lens receives the new lengths -> (lens, Q_out).
+
+    base_lens, new_lens (None: N everywhere) and lens are int32 [B], or all [B, Hkv] (every head its own number of rows).  With cos_sin f32
+    [max_position, rot] (cosines, then sines) the first rot elements of the keys, and of the queries Q [B, Hq, N, d], are turned by the angles of
+    positions [B] (None: base_lens) + n.  counts [B, Hkv, N]: sizes of the rows, for a cache with counts.
+    """
+    lib = load_library()
+    if _native is not None and K.is_cuda and (Q is None) == (Q_out is None):
+        st = _native.paged_append(cache.ptr, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, _stream())
+        if st >= 0:
+            _check(st, "sc_paged_append")
+            return lens, Q_out
+    _require_cuda(K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions)
+    B, H, d = cache.B, cache.Hkv, cache.d
+    if K.dim() != 4 or K.shape != V.shape or K.shape[0] != B or K.shape[1] != H or K.shape[3] != d or K.dtype != cache.K.dtype or V.dtype != K.dtype:
+        raise SemantiCacheError("K and V must be [B, Hkv, N, d] of the cache's dtype")
+    N = K.shape[2]
+    shapes = cache.lens_shapes()
+    if not _is_i32(base_lens, *shapes) or not _is_i32(lens, tuple(base_lens.shape)) or not (new_lens is None or _is_i32(new_lens, tuple(base_lens.shape))):
+        raise SemantiCacheError("base_lens, lens and new_lens must be int32 [B], or all [B, Hkv], contiguous")
+    if counts is not None and not _is_i32(counts, (B, H, N)):
+        raise SemantiCacheError("counts must be int32 [B, Hkv, N], contiguous")
+    if cos_sin is not None and (cos_sin.dim() != 2 or cos_sin.dtype != torch.float32 or not cos_sin.is_contiguous()):
+        raise SemantiCacheError("cos_sin must be float32 [max_position, rot], contiguous")
+    if positions is not None and not _is_i32(positions, (B,)):
+        raise SemantiCacheError("positions must be int32 [B], contiguous")
+    if Q is not None and Q_out is None:
+        Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if Q is not None and (Q.dim() != 4 or Q.shape != Q_out.shape or Q.dtype != Q_out.dtype or Q.shape[0] != B or Q.shape[2] != N or Q.shape[3] != d):
+        raise SemantiCacheError("Q and Q_out must be [B, Hq, N, d] of one dtype")
+    for t in (K, V, Q, Q_out):
+        if t is not None and t.stride(3) != 1:
+            raise SemantiCacheError("rows must be contiguous")
+    r = _PagedRowsStruct(K=_ptr(K), V=_ptr(V), k_stride_b=K.stride(0), k_stride_h=K.stride(1), k_stride_n=K.stride(2), v_stride_b=V.stride(0),
+                         v_stride_h=V.stride(1), v_stride_n=V.stride(2), counts=_ptr(counts), N=N, per_head=int(base_lens.dim() == 2),
+                         base_lens=_ptr(base_lens), new_lens=_ptr(new_lens), lens=_ptr(lens), cos_sin=_ptr(cos_sin), positions=_ptr(positions),
+                         interleaved=int(bool(interleaved)))
+    if cos_sin is not None:
+        r.max_position, r.rot = cos_sin.shape
+    if Q is not None:
+        r.Q, r.Q_out, r.Hq, r.q_dtype = _ptr(Q), _ptr(Q_out), Q.shape[1], _dtype_code(Q)
+        r.q_stride_b, r.q_stride_h, r.q_stride_n = Q.stride()[:3]
+        r.o_stride_b, r.o_stride_h, r.o_stride_n = Q_out.stride()[:3]
+    _check(lib.sc_paged_append(ctypes.byref(cache.struct), ctypes.byref(r), _stream()), "sc_paged_append")
+    return lens, Q_out
+
+
+def paged_workspace(B: int, Hq: int, Hkv: int, d: int, table_len: int, device) -> Workspace:
+    """Workspace of sc_paged_decode_attn and sc_paged_select, initialised on the current stream."""
+    lib = load_library()
+    nbytes = lib.sc_paged_workspace_bytes(B, Hq, Hkv, d, table_len)
+    if nbytes == 0:
+        raise SemantiCacheError("no workspace for B=%d Hq=%d Hkv=%d d=%d table_len=%d" % (B, Hq, Hkv, d, table_len))
+    ws = Workspace(nbytes, device)
+    _check(lib.sc_paged_init_workspace(ws.ptr, ws.nbytes, B, Hkv, _stream()), "sc_paged_init_workspace")
+    return ws
+
+
+def _paged_query(cache: PagedCache, Q, lens, workspace):
+    _require_cuda(Q, lens)
+    if Q.dim() != 3 or Q.shape[0] != cache.B or Q.shape[2] != cache.d or not Q.is_contiguous():
+        raise SemantiCacheError("Q must be [B, Hq, d], contiguous")
+    if not _is_i32(lens, *cache.lens_shapes()):
+        raise SemantiCacheError("lens must be int32 [B] or [B, Hkv], contiguous")
+    if workspace is None:
+        workspace = paged_workspace(cache.B, Q.shape[1], cache.Hkv, cache.d, cache.table.shape[-1], Q.device)
+    return workspace
+
+
+def sc_paged_decode_attn(cache: PagedCache, Q, lens, scale: float = 0.0, O=None, lse=None, want_lse: bool = False, sel=None, sel_lens=None,
+                         workspace: Optional[Workspace] = None):
+    """Q [B, Hq, d] over the first lens [B] (or [B, Hkv]) rows of a cache in pages -> (O [B, Hq, d], lse [B, Hq] or None).
+
+    With sel [B, Hkv, keep] and sel_lens [B, Hkv] (sc_paged_select) only the rows of those pages attend.
+    """
+    lib = load_library()
+    if _native is not None and Q.is_cuda and O is not None and workspace is not None and not (want_lse and lse is None):
+        st = _native.paged_decode(cache.ptr, Q, lens, scale, O, lse, sel, sel_lens, workspace.ptr, workspace.nbytes, _stream())
+        if st >= 0:
+            _check(st, "sc_paged_decode_attn")
+            return O, lse
+    workspace = _paged_query(cache, Q, lens, workspace)
+    _require_cuda(O, lse, sel, sel_lens)
+    B, Hq, d = Q.shape
+    if O is None:
+        O = torch.empty((B, Hq, d), dtype=Q.dtype, device=Q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=Q.device)
+    if O.shape != Q.shape or not O.is_contiguous() or (lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq) or not lse.is_contiguous())):
+        raise SemantiCacheError("O must be [B, Hq, d] and lse float32 [B, Hq], contiguous")
+    if (sel is None) != (sel_lens is None):
+        raise SemantiCacheError("sel and sel_lens come together")
+    if sel is not None and (sel.dim() != 3 or not _is_i32(sel, (B, cache.Hkv, sel.shape[2])) or not _is_i32(sel_lens, (B, cache.Hkv))):
+        raise SemantiCacheError("sel must be int32 [B, Hkv, keep] and sel_lens int32 [B, Hkv], contiguous")
+    st = lib.sc_paged_decode_attn(ctypes.byref(cache.struct), _ptr(Q), _dtype_code(Q), Hq, _ptr(lens), int(lens.dim() == 2), _ptr(sel), _ptr(sel_lens),
+                                  0 if sel is None else sel.shape[2], float(scale), _ptr(O), _dtype_code(O), _ptr(lse), workspace.ptr,
+                                  workspace.nbytes, _stream())
+    _check(st, "sc_paged_decode_attn")
+    return O, lse
+
+
+def sc_paged_select(cache: PagedCache, Q, lens, keep: int, first: int = 1, recent: int = 1, sel=None, sel_lens=None,
+                    workspace: Optional[Workspace] = None):
+    """The `keep` pages of every (sequence, KV head) with the largest bounds on the logits of Q [B, Hq, d], its first `first` and last `recent`
+    ones in any case -> (sel [B, Hkv, keep] ascending, -1 behind the last, sel_lens [B, Hkv])."""
+    lib = load_library()
+    if _native is not None and Q.is_cuda and sel is not None and sel_lens is not None and workspace is not None:
+        st = _native.paged_select(cache.ptr, Q, lens, keep, first, recent, sel, sel_lens, workspace.ptr, workspace.nbytes, _stream())
+        if st >= 0:
+            _check(st, "sc_paged_select")
+            return sel, sel_lens
+    workspace = _paged_query(cache, Q, lens, workspace)
+    _require_cuda(sel, sel_lens)
+    B, H = cache.B, cache.Hkv
+    if sel is None:
+        sel = torch.empty((B, H, max(1, int(keep))), dtype=torch.int32, device=Q.device)
+    if sel_lens is None:
+        sel_lens = torch.empty((B, H), dtype=torch.int32, device=Q.device)
+    if not _is_i32(sel, (B, H, max(1, int(keep)))) or not _is_i32(sel_lens, (B, H)):
+        raise SemantiCacheError("sel must be int32 [B, Hkv, keep] and sel_lens int32 [B, Hkv], contiguous")
+    st = lib.sc_paged_select(ctypes.byref(cache.struct), _ptr(Q), _dtype_code(Q), Q.shape[1], _ptr(lens), int(lens.dim() == 2), int(keep), int(first),
+                             int(recent), _ptr(sel), _ptr(sel_lens), workspace.ptr, workspace.nbytes, _stream())
+    _check(st, "sc_paged_select")
+    return sel, sel_lens
 
 
 def stream_read_probe(buf, sink) -> None:

@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include "sc_host.h"
+#include "sc_paged.h"
 #include <vector>
 
 namespace sc {
@@ -396,6 +397,157 @@ sc_status sc_multi_attn_tail(const void *Q, sc_dtype q_dtype, int nq, const void
                              float scale, void *O, sc_dtype o_dtype, float *lse, void *ws, size_t ws_bytes, void *stream) {
     return multi_common(Q, q_dtype, nq, Kc, Vc, kv_dtype, cap, counts, comp_lens, Kt, Vt, tail_cap, tail_lens, causal, true,
                         B, Hq, Hkv, d, scale, O, o_dtype, lse, ws, ws_bytes, stream);
+}
+
+
+// ------------------------------------------------------------------------------------------------
+// the cache of the sc_paged_* calls: everything about it that the host can see
+static sc_status paged_check(const sc_paged_cache *c, PagedView &v) {
+    if (!c || !c->K || !c->V || !c->table) return SC_ERR_INVALID_ARG;
+    if (c->B <= 0 || c->Hkv <= 0 || c->num_pages <= 0 || c->table_len <= 0) return SC_ERR_INVALID_ARG;
+    if (!dtype_ok(c->dtype)) return SC_ERR_UNSUPPORTED;
+    if (c->d != 64 && c->d != 128) return SC_ERR_UNSUPPORTED;
+    if (c->B > 65535 || c->Hkv > 65535 || (int64_t)c->B * c->Hkv > (1 << 20)) return SC_ERR_UNSUPPORTED;
+    const int R = c->page_rows;
+    if (R < 16 || R > 1024 || (R & (R - 1))) return SC_ERR_INVALID_ARG;
+    if (c->page_heads != (c->table_per_head ? 1 : c->Hkv)) return SC_ERR_INVALID_ARG;
+    if ((int64_t)c->table_len * R > INT32_MAX) return SC_ERR_UNSUPPORTED;
+    const int64_t es = (int64_t)elem_size(c->dtype);
+    if (c->stride_row < c->d || c->stride_head < 0 || c->stride_page < 0) return SC_ERR_INVALID_ARG;
+    if ((c->stride_row * es) % 16 || (c->stride_head * es) % 16 || (c->stride_page * es) % 16) return SC_ERR_INVALID_ARG;
+    if (c->stride_row > INT32_MAX / (R * es)) return SC_ERR_INVALID_ARG;      // offsets inside the rows of a head are 32-bit
+    // [page, head, row] or [page, row, head]: the heads of a page lie apart, and so do the pages
+    const int64_t rows_span = (R - 1) * c->stride_row + c->d;
+    if (c->page_heads > 1 && c->stride_head < rows_span && !(c->stride_head >= c->d && (c->page_heads - 1) * c->stride_head + c->d <= c->stride_row)) return SC_ERR_INVALID_ARG;
+    if (c->num_pages > 1 && c->stride_page < (c->page_heads - 1) * c->stride_head + rows_span) return SC_ERR_INVALID_ARG;
+    if (!aligned16(c->K) || !aligned16(c->V) || !aligned4(c->table)) return SC_ERR_INVALID_ARG;
+    if (c->counts && !aligned16(c->counts)) return SC_ERR_INVALID_ARG;      // read four at a time
+    if (!c->k_min != !c->k_max) return SC_ERR_INVALID_ARG;
+    if (!aligned16(c->k_min) || !aligned16(c->k_max)) return SC_ERR_INVALID_ARG;
+    v.K = static_cast<char *>(c->K); v.V = static_cast<char *>(c->V);
+    v.counts = c->counts;
+    v.k_min = static_cast<char *>(c->k_min); v.k_max = static_cast<char *>(c->k_max);
+    v.table = c->table;
+    v.page_bytes = c->stride_page * es; v.head_bytes = c->stride_head * es; v.row_bytes = (int)(c->stride_row * es);
+    v.num_pages = c->num_pages; v.page_heads = c->page_heads;
+    v.R = R; v.log2_R = __builtin_ctz((unsigned)R);
+    v.P = c->table_len; v.table_per_head = c->table_per_head != 0;
+    v.B = c->B; v.H = c->Hkv; v.d = c->d; v.dtype = static_cast<DType>(c->dtype);
+    return SC_OK;
+}
+
+// Rows [B, heads, N, d]: aligned, and, where the call writes them, no two the same.  (The stride of a dimension of one means nothing.)
+static bool rows_ok(const void *p, int64_t B, int64_t H, int64_t N, int64_t sb, int64_t sh, int64_t sn, int64_t d, int64_t es, bool written) {
+    const int64_t size[3] = {B, H, N}, stride[3] = {sb, sh, sn};
+    for (int i = 0; i < 3; ++i)
+        if (size[i] > 1 && (stride[i] < 0 || (stride[i] * es) % 16 || (written && stride[i] < d))) return false;
+    return aligned16(p);
+}
+
+sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *r, void *stream) {
+    PagedAppendArgs a;
+    const sc_status st = paged_check(cache, a.c);
+    if (st != SC_OK) return st;
+    if (!r || !r->K || !r->V || !r->base_lens || !r->lens || r->N <= 0) return SC_ERR_INVALID_ARG;
+    if (!aligned4(r->base_lens) || !aligned4(r->lens) || !aligned4(r->new_lens) || !aligned4(r->positions) || !aligned4(r->counts)) return SC_ERR_INVALID_ARG;
+    // every workgroup reads the old lengths while one of them files the new ones
+    if (r->lens == r->base_lens || r->lens == r->new_lens) return SC_ERR_INVALID_ARG;
+    if (!r->counts != !cache->counts) return SC_ERR_INVALID_ARG;
+    const int64_t es = (int64_t)elem_size(cache->dtype);
+    if (!rows_ok(r->K, cache->B, cache->Hkv, r->N, r->k_stride_b, r->k_stride_h, r->k_stride_n, cache->d, es, false)) return SC_ERR_INVALID_ARG;
+    if (!rows_ok(r->V, cache->B, cache->Hkv, r->N, r->v_stride_b, r->v_stride_h, r->v_stride_n, cache->d, es, false)) return SC_ERR_INVALID_ARG;
+    if (r->cos_sin) {
+        if (r->rot <= 0 || r->rot > cache->d || r->rot % 16 || r->max_position <= 0 || !aligned16(r->cos_sin)) return SC_ERR_INVALID_ARG;
+        if (!r->positions && r->per_head) return SC_ERR_INVALID_ARG;      // a token has one position
+    } else if (r->rot != 0 || r->Q) {
+        return SC_ERR_INVALID_ARG;
+    }
+    if (!r->Q != !r->Q_out) return SC_ERR_INVALID_ARG;
+    int64_t qs = 2;
+    if (r->Q) {
+        if (!dtype_ok(r->q_dtype)) return SC_ERR_UNSUPPORTED;
+        if (r->Hq <= 0) return SC_ERR_INVALID_ARG;
+        qs = (int64_t)elem_size(r->q_dtype);
+        if (!rows_ok(r->Q, cache->B, r->Hq, r->N, r->q_stride_b, r->q_stride_h, r->q_stride_n, cache->d, qs, false)) return SC_ERR_INVALID_ARG;
+        if (!rows_ok(r->Q_out, cache->B, r->Hq, r->N, r->o_stride_b, r->o_stride_h, r->o_stride_n, cache->d, qs, true)) return SC_ERR_INVALID_ARG;
+        if (r->Hq > 65535) return SC_ERR_UNSUPPORTED;
+    }
+    if (!paged_append_fits(cache->B, cache->Hkv, cache->page_rows, r->N, r->Q ? r->Hq : 0)) return SC_ERR_UNSUPPORTED;      // grid size
+    a.K = static_cast<const char *>(r->K); a.V = static_cast<const char *>(r->V);
+    a.k_b = r->k_stride_b * es; a.k_h = r->k_stride_h * es; a.k_n = r->k_stride_n * es;
+    a.v_b = r->v_stride_b * es; a.v_h = r->v_stride_h * es; a.v_n = r->v_stride_n * es;
+    a.counts = r->counts;
+    a.N = r->N; a.per_head = r->per_head != 0;
+    a.base_lens = r->base_lens; a.new_lens = r->new_lens; a.lens = r->lens;
+    a.cos_sin = r->cos_sin; a.max_position = r->max_position; a.rot = r->cos_sin ? r->rot : 0; a.interleaved = r->interleaved != 0;
+    a.Hq = r->Hq; a.positions = r->positions;
+    a.Q = static_cast<const char *>(r->Q); a.Q_out = static_cast<char *>(r->Q_out);
+    a.q_b = r->q_stride_b * qs; a.q_h = r->q_stride_h * qs; a.q_n = r->q_stride_n * qs;
+    a.o_b = r->o_stride_b * qs; a.o_h = r->o_stride_h * qs; a.o_n = r->o_stride_n * qs;
+    a.q_dtype = r->Q ? static_cast<DType>(r->q_dtype) : a.c.dtype;
+    return runtime_status(launch_paged_append(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t sc_paged_workspace_bytes(int B, int Hq, int Hkv, int d, int table_len) {
+    if (B <= 0 || Hkv <= 0 || Hq <= 0 || table_len <= 0 || Hq % Hkv || (d != 64 && d != 128)) return 0;
+    const size_t attend = paged_decode_bytes(Hq / Hkv, d), select = paged_select_bytes(B, Hkv, table_len);
+    return paged_state_bytes(B, Hkv) + (attend > select ? attend : select);
+}
+
+sc_status sc_paged_init_workspace(void *ws, size_t ws_bytes, int B, int Hkv, void *stream) {
+    if (B <= 0 || Hkv <= 0) return SC_ERR_INVALID_ARG;
+    const size_t state = paged_state_bytes(B, Hkv);
+    if (!ws || ws_bytes < state || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SC_ERR_WORKSPACE;
+    return runtime_status(launch_decode_init_workspace(ws, state, static_cast<hipStream_t>(stream)));
+}
+
+// what sc_paged_decode_attn and sc_paged_select have in common
+static sc_status paged_query_check(const sc_paged_cache *cache, PagedView &v, const void *Q, sc_dtype q_dtype, int Hq, const int32_t *lens, const void *ws) {
+    const sc_status st = paged_check(cache, v);
+    if (st != SC_OK) return st;
+    if (!Q || !lens || Hq <= 0 || !aligned16(Q) || !aligned4(lens)) return SC_ERR_INVALID_ARG;
+    if (!dtype_ok(q_dtype) || Hq % cache->Hkv || Hq / cache->Hkv > 16) return SC_ERR_UNSUPPORTED;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SC_ERR_WORKSPACE;
+    return SC_OK;
+}
+
+sc_status sc_paged_decode_attn(const sc_paged_cache *cache, const void *Q, sc_dtype q_dtype, int Hq, const int32_t *lens,
+                               int lens_per_head, const int32_t *sel, const int32_t *sel_lens, int keep, float scale, void *O,
+                               sc_dtype o_dtype, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    PagedDecodeArgs a;
+    const sc_status st = paged_query_check(cache, a.c, Q, q_dtype, Hq, lens, ws);
+    if (st != SC_OK) return st;
+    if (!O || !aligned16(O) || !aligned4(lse) || !sel != !sel_lens || !aligned4(sel) || !aligned4(sel_lens)) return SC_ERR_INVALID_ARG;
+    if (!dtype_ok(o_dtype)) return SC_ERR_UNSUPPORTED;
+    if (scale != scale) return SC_ERR_INVALID_ARG;
+    if (sel && keep <= 0) return SC_ERR_CAPACITY;
+    if (sel && keep > (1 << 20)) return SC_ERR_UNSUPPORTED;
+    const int64_t most = (int64_t)(sel ? keep : cache->table_len) * cache->page_rows;
+    if ((most / 64 + 1) * cache->B * cache->Hkv > (1 << 30)) return SC_ERR_UNSUPPORTED;      // the kernel counts stretches of 64 rows and more in 32 bits
+    if (ws_bytes < paged_state_bytes(cache->B, cache->Hkv) + paged_decode_bytes(Hq / cache->Hkv, cache->d)) return SC_ERR_WORKSPACE;
+    a.Q = Q; a.q_dtype = static_cast<DType>(q_dtype); a.Hq = Hq;
+    a.lens = lens; a.lens_per_head = lens_per_head != 0;
+    a.sel = sel; a.sel_lens = sel_lens; a.keep = sel ? keep : 0;
+    a.scale = (scale == 0.f) ? 1.0f / sqrtf((float)cache->d) : scale;
+    a.O = O; a.o_dtype = static_cast<DType>(o_dtype); a.lse = lse; a.ws = ws;
+    return runtime_status(launch_paged_decode(a, static_cast<hipStream_t>(stream)));
+}
+
+sc_status sc_paged_select(const sc_paged_cache *cache, const void *Q, sc_dtype q_dtype, int Hq, const int32_t *lens, int lens_per_head,
+                          int keep, int first, int recent, int32_t *sel, int32_t *sel_lens, void *ws, size_t ws_bytes, void *stream) {
+    PagedSelectArgs a;
+    const sc_status st = paged_query_check(cache, a.c, Q, q_dtype, Hq, lens, ws);
+    if (st != SC_OK) return st;
+    if (!cache->k_min || !sel || !sel_lens || !aligned4(sel) || !aligned4(sel_lens) || first < 0 || recent < 0) return SC_ERR_INVALID_ARG;
+    if (keep <= 0 || (int64_t)first + recent > keep) return SC_ERR_CAPACITY;
+    if (keep > (1 << 20)) return SC_ERR_UNSUPPORTED;
+    if ((int64_t)(cache->table_len / 16 + 1) * cache->B * cache->Hkv > INT32_MAX) return SC_ERR_UNSUPPORTED;      // grid size
+    if (ws_bytes < paged_state_bytes(cache->B, cache->Hkv) + paged_select_bytes(cache->B, cache->Hkv, cache->table_len)) return SC_ERR_WORKSPACE;
+    a.Q = Q; a.q_dtype = static_cast<DType>(q_dtype); a.Hq = Hq;
+    a.lens = lens; a.lens_per_head = lens_per_head != 0;
+    a.keep = keep; a.first = first; a.recent = recent;
+    a.sel = sel; a.sel_lens = sel_lens; a.ws = ws;
+    return runtime_status(launch_paged_select(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -181,11 +181,113 @@ PyObject *multi(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// ---- a cache held in pages: the first argument is the address of its sc_paged_cache, which the wrapper keeps
+inline bool is_i32(const at::Tensor *t) { return t->scalar_type() == at::kInt && t->is_contiguous(); }
+// lengths [B] or [B, Hkv]
+inline bool lengths(const at::Tensor *t, const sc_paged_cache *c, bool &per_head) {
+    if (!is_i32(t) || t->dim() < 1 || t->dim() > 2 || t->size(0) != c->B) return false;
+    per_head = t->dim() == 2;
+    return !per_head || t->size(1) == c->Hkv;
+}
+inline bool is_shape(const at::Tensor *t, int64_t a, int64_t b, int64_t c) { return t->dim() == 3 && t->size(0) == a && t->size(1) == b && t->size(2) == c; }
+
+// (cache, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, stream)
+PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() {
+        const at::Tensor *K, *V, *base, *lens, *fresh, *counts, *Q, *Qo, *angles, *positions;
+        if (n != 13 || !take_some(a[1], K) || !take_some(a[2], V) || !take_some(a[3], base) || !take_some(a[4], lens) || !take(a[5], fresh) || !take(a[6], counts)) return kNotTaken;
+        if (!take(a[7], Q) || !take(a[8], Qo) || !take(a[9], angles) || !take(a[10], positions)) return kNotTaken;
+        const auto *c = static_cast<const sc_paged_cache *>(pointer(a[0]));
+        const int turned = PyObject_IsTrue(a[11]);
+        void *stream = pointer(a[12]);
+        if (PyErr_Occurred() || !c) return kNotTaken;
+        bool per_head, same;
+        if (K->dim() != 4 || K->sizes() != V->sizes() || K->size(0) != c->B || K->size(1) != c->Hkv || K->size(3) != c->d) return kNotTaken;
+        if (code(*K) != c->dtype || code(*V) != c->dtype || K->stride(3) != 1 || V->stride(3) != 1) return kNotTaken;
+        if (!lengths(base, c, per_head) || !lengths(lens, c, same) || same != per_head) return kNotTaken;
+        if (fresh && (!lengths(fresh, c, same) || same != per_head)) return kNotTaken;
+        const int64_t N = K->size(2);
+        if (N != (int)N || (counts && (!is_i32(counts) || !is_shape(counts, c->B, c->Hkv, N)))) return kNotTaken;
+        if (angles && (angles->dim() != 2 || angles->scalar_type() != at::kFloat || !angles->is_contiguous() || angles->size(0) != (int)angles->size(0))) return kNotTaken;
+        if (positions && (!is_i32(positions) || positions->dim() != 1 || positions->size(0) != c->B)) return kNotTaken;
+        sc_paged_rows r = {};
+        r.K = data(K); r.V = data(V);
+        r.k_stride_b = K->stride(0); r.k_stride_h = K->stride(1); r.k_stride_n = K->stride(2);
+        r.v_stride_b = V->stride(0); r.v_stride_h = V->stride(1); r.v_stride_n = V->stride(2);
+        r.counts = data<const int32_t>(counts);
+        r.N = (int)N; r.per_head = per_head;
+        r.base_lens = data<const int32_t>(base); r.new_lens = data<const int32_t>(fresh); r.lens = data<int32_t>(lens);
+        r.cos_sin = data<const float>(angles); r.positions = data<const int32_t>(positions); r.interleaved = turned;
+        if (angles) { r.max_position = (int)angles->size(0); r.rot = (int)angles->size(1); }
+        if (Q) {
+            if (!Qo || Q->dim() != 4 || Q->sizes() != Qo->sizes() || Q->size(0) != c->B || Q->size(2) != N || Q->size(3) != c->d) return kNotTaken;
+            if (code(*Q) < 0 || Q->scalar_type() != Qo->scalar_type() || Q->stride(3) != 1 || Qo->stride(3) != 1) return kNotTaken;
+            r.Q = data(Q); r.Q_out = data(Qo); r.Hq = (int)Q->size(1); r.q_dtype = code(*Q);
+            r.q_stride_b = Q->stride(0); r.q_stride_h = Q->stride(1); r.q_stride_n = Q->stride(2);
+            r.o_stride_b = Qo->stride(0); r.o_stride_h = Qo->stride(1); r.o_stride_n = Qo->stride(2);
+        }
+        return unlocked([&]() { return (int)sc_paged_append(c, &r, stream); });
+    });
+}
+
+// (cache, Q, lens, scale, O, lse, sel, sel_lens, workspace, bytes, stream)
+PyObject *paged_decode(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() {
+        const at::Tensor *Q, *lens, *O, *lse, *sel, *many;
+        if (n != 11 || !take_some(a[1], Q) || !take_some(a[2], lens) || !take_some(a[4], O) || !take(a[5], lse) || !take(a[6], sel) || !take(a[7], many)) return kNotTaken;
+        const auto *c = static_cast<const sc_paged_cache *>(pointer(a[0]));
+        const double scale = PyFloat_AsDouble(a[3]);
+        const size_t bytes = PyLong_AsSize_t(a[9]);
+        void *w = pointer(a[8]), *stream = pointer(a[10]);
+        if (PyErr_Occurred() || !c) return kNotTaken;
+        bool per_head;
+        if (Q->dim() != 3 || Q->size(0) != c->B || Q->size(2) != c->d || !Q->is_contiguous() || Q->sizes() != O->sizes() || !O->is_contiguous()) return kNotTaken;
+        const int qc = code(*Q), oc = code(*O);
+        if (qc < 0 || oc < 0 || !lengths(lens, c, per_head)) return kNotTaken;
+        if (lse && (lse->scalar_type() != at::kFloat || lse->dim() != 2 || lse->size(0) != c->B || lse->size(1) != Q->size(1) || !lse->is_contiguous())) return kNotTaken;
+        if (!sel != !many) return kNotTaken;
+        if (sel && (!is_i32(sel) || sel->dim() != 3 || sel->size(0) != c->B || sel->size(1) != c->Hkv || sel->size(2) != (int)sel->size(2))) return kNotTaken;
+        if (sel && (!is_i32(many) || many->dim() != 2 || many->size(0) != c->B || many->size(1) != c->Hkv)) return kNotTaken;
+        const void *q = data(Q);
+        const auto *l = data<const int32_t>(lens), *s = data<const int32_t>(sel), *m = data<const int32_t>(many);
+        void *o = data(O);
+        auto *e = data<float>(lse);
+        return unlocked([&]() {
+            return (int)sc_paged_decode_attn(c, q, (sc_dtype)qc, (int)Q->size(1), l, per_head, s, m, sel ? (int)sel->size(2) : 0, (float)scale, o, (sc_dtype)oc, e, w, bytes, stream);
+        });
+    });
+}
+
+// (cache, Q, lens, keep, first, recent, sel, sel_lens, workspace, bytes, stream)
+PyObject *paged_select(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() {
+        const at::Tensor *Q, *lens, *sel, *many;
+        if (n != 11 || !take_some(a[1], Q) || !take_some(a[2], lens) || !take_some(a[6], sel) || !take_some(a[7], many)) return kNotTaken;
+        const auto *c = static_cast<const sc_paged_cache *>(pointer(a[0]));
+        const long keep = PyLong_AsLong(a[3]), first = PyLong_AsLong(a[4]), recent = PyLong_AsLong(a[5]);
+        const size_t bytes = PyLong_AsSize_t(a[9]);
+        void *w = pointer(a[8]), *stream = pointer(a[10]);
+        if (PyErr_Occurred() || !c || keep != (int)keep || first != (int)first || recent != (int)recent) return kNotTaken;
+        bool per_head;
+        if (Q->dim() != 3 || Q->size(0) != c->B || Q->size(2) != c->d || !Q->is_contiguous() || code(*Q) < 0 || !lengths(lens, c, per_head)) return kNotTaken;
+        if (!is_i32(sel) || !is_shape(sel, c->B, c->Hkv, keep) || !is_i32(many) || many->dim() != 2 || many->size(0) != c->B || many->size(1) != c->Hkv) return kNotTaken;
+        const void *q = data(Q);
+        const auto *l = data<const int32_t>(lens);
+        auto *s = data<int32_t>(sel), *m = data<int32_t>(many);
+        return unlocked([&]() {
+            return (int)sc_paged_select(c, q, (sc_dtype)code(*Q), (int)Q->size(1), l, per_head, (int)keep, (int)first, (int)recent, s, m, w, bytes, stream);
+        });
+    });
+}
+
 PyMethodDef methods[] = {
     {"segment", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(segment)), METH_FASTCALL, nullptr},
     {"merge", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(merge)), METH_FASTCALL, nullptr},
     {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode)), METH_FASTCALL, nullptr},
     {"multi", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(multi)), METH_FASTCALL, nullptr},
+    {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
+    {"paged_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_decode)), METH_FASTCALL, nullptr},
+    {"paged_select", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_select)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,96 @@
+// A cache held in pages as the kernels see it (internal; the public boundary is include/semanticache.h), and the launchers of its calls.
+#pragma once
+#include "sc_device.h"
+#include "sc_host.h"
+#include "sc_paged_words.h"
+
+namespace sc {
+
+struct PagedView {
+    char *K, *V;
+    int32_t *counts;
+    char *k_min, *k_max;
+    const int32_t *table;
+    int64_t page_bytes, head_bytes;        // strides of the pools
+    int row_bytes;
+    int num_pages, page_heads;
+    int R, log2_R;                         // rows of a page
+    int P;                                 // entries of a table
+    int table_per_head;
+    int B, H, d;
+    DType dtype;
+};
+
+__device__ __forceinline__ const int32_t *paged_table(const PagedView &c, int b, int h) {
+    return c.table + (c.table_per_head ? (int64_t)b * c.H + h : (int64_t)b) * c.P;
+}
+// byte offset of a page's rows for head h, and its number among the pages' heads (counts, summaries)
+__device__ __forceinline__ int64_t paged_offset(const PagedView &c, int page, int h) {
+    return (int64_t)page * c.page_bytes + (c.page_heads == 1 ? 0 : (int64_t)h * c.head_bytes);
+}
+__device__ __forceinline__ int64_t paged_index(const PagedView &c, int page, int h) {
+    return (int64_t)page * c.page_heads + (c.page_heads == 1 ? 0 : h);
+}
+__device__ __forceinline__ bool paged_bad(const PagedView &c, int page) { return (unsigned)page >= (unsigned)c.num_pages; }
+
+// ---- sc_paged_append
+struct PagedAppendArgs {
+    PagedView c;
+    const char *K, *V;
+    int64_t k_b, k_h, k_n, v_b, v_h, v_n;   // bytes
+    const int32_t *counts;
+    int N, per_head;
+    const int32_t *base_lens, *new_lens;
+    int32_t *lens;
+    const float *cos_sin;
+    int max_position, rot, interleaved, Hq;
+    const int32_t *positions;
+    const char *Q;
+    char *Q_out;
+    int64_t q_b, q_h, q_n, o_b, o_h, o_n;   // bytes
+    DType q_dtype;
+};
+// whether the call fits a grid: a workgroup per page and KV head, and per 32 tokens and query head at worst
+inline bool paged_append_fits(int64_t B, int64_t H, int64_t R, int64_t N, int64_t Hq) {
+    return B * H * ((N + R - 2) / R + 1) + B * ((N + 31) / 32) * Hq <= INT32_MAX;
+}
+hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t stream);
+
+// ---- sc_paged_decode_attn
+struct PagedDecodeArgs {
+    PagedView c;
+    const void *Q;
+    DType q_dtype;
+    int Hq;
+    const int32_t *lens;
+    int lens_per_head;
+    const int32_t *sel, *sel_lens;
+    int keep;
+    float scale;
+    void *O;
+    DType o_dtype;
+    float *lse;
+    void *ws;
+};
+hipError_t launch_paged_decode(const PagedDecodeArgs &a, hipStream_t stream);
+
+// ---- sc_paged_select
+struct PagedSelectArgs {
+    PagedView c;
+    const void *Q;
+    DType q_dtype;
+    int Hq;
+    const int32_t *lens;
+    int lens_per_head;
+    int keep, first, recent;
+    int32_t *sel, *sel_lens;
+    void *ws;
+};
+hipError_t launch_paged_select(const PagedSelectArgs &a, hipStream_t stream);
+
+// ---- workspace: counters, then what the two calls need (they follow each other on a stream, so it is the same memory)
+size_t paged_state_bytes(int B, int H);
+size_t paged_decode_bytes(int G, int d);
+size_t paged_select_bytes(int B, int H, int P);
+
+}  // namespace sc

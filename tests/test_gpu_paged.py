@@ -1,0 +1,749 @@
+"""A cache held in pages on the GPU: sc_paged_append, sc_paged_decode_attn and sc_paged_select against plain implementations in fp64.
+
+Tolerances (u = 2^-24, a rounding of fp32; h = half a step of the stored type):
+  * copied rows, sizes, lengths, selections, summaries of the stored keys: equal;
+  * a rotated element a cos - b sin: three roundings of fp32 over |a cos| + |b sin|, then one of the stored type;
+  * attention: a logit is a sum of d products in fp32, scaled, with the logarithm of a size: it is off by at most
+    delta = (d + 16) u (sum_e |q_e k_e| scale + |logit|), so a weight by a factor exp(2 delta).  Weights enter the second product with 16 bits or more:
+    2^-17.  The sums take rows in steps of 16 and join at most some hundred parts: (rows / 16 + 256) u.  All that over sum_t w_t |v_t|, then the rounding of O;
+  * lse: delta, the same error of the sum, and a few roundings of itself.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2603_14303_amd import binding as sc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0**-24
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+class Paged:
+    """A cache in pages on the host: pools full of numbers that nobody may look at (NaN and infinities among them), tables of pages in no order with
+    entries that may not be read behind the last page."""
+
+    def __init__(self, B, Hkv, P, R, d, dtype, per_head_table=False, layout="phrd", counts=False, summary=False, seed=0, spare=3, junk=True):
+        self.B, self.H, self.P, self.R, self.d, self.dtype, self.per_head_table = B, Hkv, P, R, d, dtype, per_head_table
+        self.gen = torch.Generator().manual_seed(seed)
+        heads = 1 if per_head_table else Hkv
+        tables = B * Hkv if per_head_table else B
+        n = tables * P + spare
+        self.n, self.heads = n, heads
+        shape = {"phrd": (n, heads, R, d), "prhd": (n, R, heads, d), "pkv": (n, 2, heads, R, d)}[layout]
+        pools = []
+        for which in range(1 if layout == "pkv" else 2):
+            x = torch.randn(shape, generator=self.gen)
+            if junk:
+                wild = torch.rand(shape, generator=self.gen)
+                x[wild < 0.02] = math.nan
+                x[(wild >= 0.02) & (wild < 0.03)] = math.inf
+            pools.append(x.to(dtype).to(DEV))
+        if layout == "pkv":
+            self.K, self.V = pools[0][:, 0], pools[0][:, 1]
+        else:
+            self.K, self.V = pools
+        if layout == "prhd":
+            self.K, self.V = self.K.permute(0, 2, 1, 3), self.V.permute(0, 2, 1, 3)
+        order = torch.randperm(n, generator=self.gen)[: tables * P].to(torch.int32)
+        self.table = order.reshape((B, Hkv, P) if per_head_table else (B, P))
+        self.counts = torch.randint(1, 50, (n, heads, R), generator=self.gen, dtype=torch.int32).to(DEV) if counts else None
+        self.k_min = self.k_max = None
+        if summary:
+            self.k_min = torch.full((n, heads, d), math.nan, dtype=dtype, device=DEV)
+            self.k_max = torch.full((n, heads, d), math.nan, dtype=dtype, device=DEV)
+
+    def cache(self, table=None):
+        return sc.PagedCache(self.K, self.V, (self.table if table is None else table).to(DEV), counts=self.counts, k_min=self.k_min, k_max=self.k_max)
+
+    def place(self, b, h, t):
+        """Pages, head of a page and rows in them of rows t of (b, h)."""
+        table = self.table[b, h] if self.per_head_table else self.table[b]
+        return table[t // self.R].long(), 0 if self.per_head_table else h, t % self.R
+
+    def fill(self, lens):
+        """Rows of (b, h) below lens[b, h] get numbers; returns them in fp64 by (b, h): keys, values, sizes."""
+        out = {}
+        K, V = self.K.cpu(), self.V.cpu()
+        counts = None if self.counts is None else self.counts.cpu()
+        for b in range(self.B):
+            for h in range(self.H):
+                n = int(lens[b][h])
+                page, head, row = self.place(b, h, torch.arange(n))
+                k = torch.randn((n, self.d), generator=self.gen).to(self.dtype)
+                v = torch.randn((n, self.d), generator=self.gen).to(self.dtype)
+                K[page, head, row], V[page, head, row] = k, v
+                out[b, h] = (k.double(), v.double(), None if counts is None else counts[page, head, row].double())
+        self.K.copy_(K)
+        self.V.copy_(V)
+        return out
+
+
+def attend(q, rows, scale):
+    """q [G, d], rows (k, v, sizes) in fp64 -> O, lse, and how far they may be off before O is rounded."""
+    k, v, counts = rows
+    d = k.shape[1]
+    if k.shape[0] == 0:
+        return torch.zeros_like(q), torch.full((q.shape[0],), -math.inf, dtype=torch.float64), torch.zeros_like(q), torch.zeros(q.shape[0], dtype=torch.float64)
+    z = q @ k.T * scale
+    if counts is not None:
+        z = z + counts.log()
+    delta = (d + 16) * U * ((q.abs() @ k.abs().T * abs(scale)).amax(1) + z.abs().amax(1))
+    w = torch.softmax(z, 1)
+    lse = torch.logsumexp(z, 1)
+    sums = 2.0**-17 + (k.shape[0] / 16 + 256) * U
+    return w @ v, lse, (2 * delta + sums)[:, None] * (w @ v.abs()), delta + sums + 4 * U * lse.abs()
+
+
+def close(got, want, tol):
+    got = got.double().cpu()
+    bad = ~((got - want).abs() <= tol) & ~((got == want) | (got.isnan() & want.isnan()))
+    assert not bad.any(), (int(bad.sum()), float((got - want).abs()[bad].max()), float(tol[bad].min()) if torch.is_tensor(tol) else tol)
+
+
+def check_decode(pc, lens, G, qdt, per_head=True, scale=0.0, sel=None, workspace=None, odt=None, seed=1):
+    """lens [B][H]; sel: {(b, h): list of places} or None."""
+    B, H, d = pc.B, pc.H, pc.d
+    rows = pc.fill(lens)
+    gen = torch.Generator().manual_seed(seed)
+    Q = (1.5 * torch.randn((B, H * G, d), generator=gen)).to(qdt)
+    dl = torch.tensor(lens, dtype=torch.int32)
+    dl = (dl if per_head else dl[:, 0].contiguous()).to(DEV)
+    kw = {}
+    if sel is not None:
+        keep = max(len(x) for x in sel.values()) + 1
+        s = torch.full((B, H, keep), -7, dtype=torch.int32)      # (behind the last: never read)
+        for (b, h), x in sel.items():
+            s[b, h, : len(x)] = torch.tensor(x, dtype=torch.int32)
+        kw = dict(sel=s.to(DEV), sel_lens=torch.tensor([[len(sel[b, h]) for h in range(H)] for b in range(B)], dtype=torch.int32).to(DEV))
+    O = None if odt is None else torch.empty((B, H * G, d), dtype=odt, device=DEV)
+    O, lse = sc.sc_paged_decode_attn(pc.cache(), Q.to(DEV), dl, scale=scale, O=O, want_lse=True, workspace=workspace, **kw)
+    torch.cuda.synchronize()
+    for b in range(B):
+        for h in range(H):
+            k, v, c = rows[b, h]
+            if sel is not None:
+                n = k.shape[0]
+                mine = torch.cat([torch.arange(p * pc.R, max(p * pc.R, min((p + 1) * pc.R, n))) for p in sel[b, h]] + [torch.arange(0)]).long()
+                k, v, c = k[mine], v[mine], None if c is None else c[mine]
+            heads = slice(h * G, (h + 1) * G)
+            wo, wl, to, tl = attend(Q[b, heads].double(), (k, v, c), scale or 1 / math.sqrt(d))
+            close(O[b, heads], wo, to + half_step(O.dtype) * wo.abs() * (1 + 2.0**-6) + 1e-30)
+            close(lse[b, heads], wl, tl)
+    return O, lse
+
+
+# ------------------------------------------------------------------------------------------------ attention
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 33, 95, 96, 97, 170, 191, 193, 300, 700])
+@pytest.mark.parametrize("dtype, d, R", [(BF, 128, 64), (BF, 64, 16), (F32, 128, 32), (F32, 64, 16)])
+def test_decode_lengths(n, dtype, d, R):
+    print("decode lengths", n, dtype, d, R, flush=True)
+    pc = Paged(1, 2, -(-n // R) + 1, R, d, dtype, seed=n)
+    check_decode(pc, [[n, n]], 4, dtype, per_head=False)
+
+
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 7, 8, 13, 16])
+@pytest.mark.parametrize("dtype, qdt, d", [(BF, BF, 128), (BF, F32, 128), (BF, BF, 64), (BF, F32, 64), (F32, F32, 128), (F32, BF, 128), (F32, F32, 64), (F32, BF, 64)])
+def test_decode_groups_and_types(G, dtype, qdt, d):
+    print("decode groups", G, dtype, qdt, d, flush=True)
+    pc = Paged(2, 3, 12, 32, d, dtype, seed=G)
+    check_decode(pc, [[333] * 3, [150] * 3], G, qdt, per_head=False)
+
+
+@pytest.mark.parametrize("layout", ["phrd", "prhd", "pkv"])
+@pytest.mark.parametrize("R", [16, 32, 128, 256, 1024])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_decode_pages_and_layouts(layout, R, dtype):
+    print("decode pages", layout, R, dtype, flush=True)
+    pc = Paged(3, 2, max(2, 1100 // R), R, 128, dtype, layout=layout, counts=layout == "phrd", seed=R)
+    check_decode(pc, [[1000] * 2, [1] * 2, [517] * 2], 5, dtype, per_head=False)
+
+
+@pytest.mark.parametrize("dtype, d", [(BF, 128), (BF, 64), (F32, 128)])
+@pytest.mark.parametrize("own_pages", [False, True])
+def test_decode_every_head_its_own_length(dtype, d, own_pages):
+    """Merged rows with sizes; heads without any row among them, first, last and in between."""
+    print("decode per head", dtype, d, own_pages, flush=True)
+    pc = Paged(3, 4, 40, 32, d, dtype, per_head_table=own_pages, counts=True, seed=3)
+    check_decode(pc, [[0, 900, 1, 0], [33, 0, 0, 1280], [400, 401, 64, 0]], 4, dtype)
+    check_decode(pc, [[0, 0, 0, 0], [0, 0, 0, 0], [0, 0, 0, 0]], 4, dtype)
+
+
+def test_decode_sizes_of_zero_weigh_nothing():
+    print("decode sizes of zero", flush=True)
+    pc = Paged(1, 1, 4, 64, 128, BF, counts=True)
+    pc.counts.copy_(torch.randint(0, 3, pc.counts.shape, generator=pc.gen, dtype=torch.int32) - torch.randint(0, 2, pc.counts.shape, generator=pc.gen, dtype=torch.int32))
+    rows = pc.fill([[200]])[0, 0]
+    some = rows[2] > 0
+    assert some.any() and not some.all()
+    Q = torch.randn((1, 4, 128), generator=pc.gen).to(BF)
+    O, lse = sc.sc_paged_decode_attn(pc.cache(), Q.to(DEV), torch.tensor([200], dtype=torch.int32, device=DEV), want_lse=True)
+    wo, wl, to, tl = attend(Q[0].double(), tuple(x[some] for x in rows), 1 / math.sqrt(128))
+    close(O[0], wo, to + half_step(BF) * wo.abs() * (1 + 2.0**-6))
+    close(lse[0], wl, tl)
+    pc.counts.zero_()
+    O, lse = sc.sc_paged_decode_attn(pc.cache(), Q.to(DEV), torch.tensor([200], dtype=torch.int32, device=DEV), want_lse=True)
+    assert (O == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("B, H, lens", [(1, 1, [9000]), (1, 8, [5400]), (5, 2, [17, 3000, 1, 8000, 900]), (40, 4, list(range(1, 1600, 40))), (130, 2, [31] * 130)])
+def test_decode_work_is_split_and_joined(B, H, lens):
+    """Heads across many workgroups, many heads in one workgroup, ragged; the same answer, bit for bit, on a workspace in use."""
+    print("decode split", B, H, lens[:5], flush=True)
+    pc = Paged(B, H, -(-max(lens) // 64), 64, 128, BF, seed=B, junk=B < 10)
+    ws = sc.paged_workspace(B, 4 * H, H, 128, pc.P, DEV)
+    O, lse = check_decode(pc, [[n] * H for n in lens], 4, BF, per_head=False, workspace=ws)
+    Q = (1.5 * torch.randn((B, H * 4, 128), generator=torch.Generator().manual_seed(1))).to(BF).to(DEV)
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    state = ws.buf[: 4 * B * H].view(torch.int32)
+    for _ in range(4):
+        O2, lse2 = sc.sc_paged_decode_attn(pc.cache(), Q, dl, want_lse=True, workspace=ws)
+        assert torch.equal(O, O2) and torch.equal(lse, lse2) and not state.any()
+
+
+def test_decode_no_row_is_missed():
+    """One row outweighs all others: every row of a cache across pages, steps and workgroups in turn."""
+    print("decode needles", flush=True)
+    n, R = 1333, 32
+    pc = Paged(1, 2, -(-n // R), R, 128, BF, junk=False)
+    pc.fill([[n, n]])
+    q = torch.ones((1, 2, 128), dtype=BF)
+    cache, ws = pc.cache(), sc.paged_workspace(1, 2, 2, 128, pc.P, DEV)
+    dl = torch.tensor([n], dtype=torch.int32, device=DEV)
+    pc.K.mul_(0.1)
+    got = []
+    for t in list(range(0, n, 7)) + [n - 1, n - 2, 15, 16, 95, 96, 31, 32]:
+        page, _, row = pc.place(0, 0, torch.tensor(t))
+        before = pc.K[page, :, row].clone()
+        pc.K[page, :, row] = 4.0
+        O, _ = sc.sc_paged_decode_attn(cache, q.to(DEV), dl, workspace=ws)
+        got.append((t, O.float().cpu(), pc.V[page, :, row].float().cpu()))
+        pc.K[page, :, row] = before
+    for t, O, v in got:      # weight 1 up to e^-40 * n
+        assert torch.equal(O[0], v), t
+
+
+@pytest.mark.parametrize("dtype, d, R", [(BF, 128, 32), (BF, 64, 16), (F32, 128, 64)])
+def test_decode_over_selected_pages(dtype, d, R):
+    print("decode selection", dtype, d, R, flush=True)
+    B, H, P = 2, 3, 30
+    lens = [[R * 30] * 3, [R * 17 + 5] * 3]
+    pc = Paged(B, H, P, R, d, dtype, counts=True, seed=R)
+    sel = {(0, 0): [0, 3, 4, 29], (0, 1): list(range(30)), (0, 2): [7], (1, 0): [17], (1, 1): [0, 16, 17], (1, 2): []}
+    check_decode(pc, lens, 4, dtype, per_head=False, sel=sel)
+    # a selected page that lies behind the length holds no row
+    check_decode(pc, lens, 4, dtype, per_head=False, sel={**sel, (1, 0): [17, 18, 29], (1, 2): [25]})
+
+
+def test_decode_output_type_scale_and_lengths_beyond_the_table():
+    print("decode output type", flush=True)
+    pc = Paged(2, 2, 6, 64, 128, BF)
+    check_decode(pc, [[384] * 2, [100] * 2], 4, BF, per_head=False, scale=0.3, odt=F32)
+    check_decode(pc, [[384] * 2, [100] * 2], 4, F32, per_head=False, scale=-0.05, odt=BF)
+    rows = pc.fill([[384] * 2] * 2)
+    Q = torch.randn((2, 8, 128), generator=pc.gen).to(BF)
+    O, lse = sc.sc_paged_decode_attn(pc.cache(), Q.to(DEV), torch.tensor([2**31 - 1, -1], dtype=torch.int32, device=DEV), want_lse=True)
+    for h in range(2):
+        wo, wl, to, tl = attend(Q[0, 4 * h : 4 * h + 4].double(), rows[0, h], 1 / math.sqrt(128))
+        close(O[0, 4 * h : 4 * h + 4], wo, to + half_step(BF) * wo.abs() * (1 + 2.0**-6))
+        close(lse[0, 4 * h : 4 * h + 4], wl, tl)
+    assert (O[1] == 0).all() and (lse[1] == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_decode_large_logits(dtype):
+    """Logits of some 1e4 to 1e5 apart: the running maximum moves, nothing overflows."""
+    print("decode large logits", dtype, flush=True)
+    pc = Paged(1, 2, 10, 64, 128, dtype, junk=False)
+    rows = pc.fill([[640, 640]])
+    Q = torch.randn((1, 8, 128), generator=pc.gen).mul(1e5).to(dtype)
+    O, lse = sc.sc_paged_decode_attn(pc.cache(), Q.to(DEV), torch.tensor([640], dtype=torch.int32, device=DEV), want_lse=True)
+    assert torch.isfinite(O.float()).all()
+    for h in range(2):
+        z = Q[0, 4 * h : 4 * h + 4].double() @ rows[0, h][0].T / math.sqrt(128)
+        best = z.argmax(1)
+        top = z.sort(1, descending=True)[0]
+        clear = top[:, 0] - top[:, 1] > 1000.0
+        assert clear.any()
+        got = O[0, 4 * h : 4 * h + 4].float().cpu()
+        assert torch.equal(got[clear], rows[0, h][1][best].float()[clear])
+        close(lse[0, 4 * h : 4 * h + 4], torch.logsumexp(z, 1), 200 * U * (Q[0, 4 * h : 4 * h + 4].double().abs() @ rows[0, h][0].abs().T).amax(1))
+
+
+def test_decode_rows_that_are_not_finite_stay_in_their_heads():
+    print("decode not finite", flush=True)
+    pc = Paged(2, 2, 8, 32, 128, BF, junk=False)
+    lens = [[200] * 2, [256] * 2]
+    rows = pc.fill(lens)
+    page, head, row = pc.place(0, 1, torch.tensor(77))
+    pc.K[page, head, row, 5] = math.nan
+    page, head, row = pc.place(1, 0, torch.tensor(13))
+    pc.V[page, head, row, 6] = math.inf
+    Q = torch.randn((2, 8, 128), generator=pc.gen).to(BF)
+    O, lse = sc.sc_paged_decode_attn(pc.cache(), Q.to(DEV), torch.tensor([200, 256], dtype=torch.int32, device=DEV), want_lse=True)
+    assert O[0, 4:].isnan().all() and lse[0, 4:].isnan().all()
+    assert not torch.isfinite(O[1, :4, 6]).any() and torch.isfinite(O[1, :4, :6]).all() and torch.isfinite(O[1, :4, 7:]).all()
+    for b, h in ((0, 0), (1, 1)):
+        wo, wl, to, tl = attend(Q[b, 4 * h : 4 * h + 4].double(), rows[b, h], 1 / math.sqrt(128))
+        close(O[b, 4 * h : 4 * h + 4], wo, to + half_step(BF) * wo.abs() * (1 + 2.0**-6))
+
+
+def test_decode_bad_pages_show_and_are_not_followed():
+    print("decode bad pages", flush=True)
+    pc = Paged(3, 2, 10, 32, 128, BF)
+    lens = [[300] * 2, [300] * 2, [320] * 2]
+    rows = pc.fill(lens)
+    Q = torch.randn((3, 8, 128), generator=pc.gen).to(BF)
+    table = pc.table.clone()
+    table[1, 4], table[2, 9], table[0, 9] = pc.n, -1, pc.table[0, 9]
+    dl = torch.tensor([288, 300, 320], dtype=torch.int32, device=DEV)
+    O, lse = sc.sc_paged_decode_attn(pc.cache(table), Q.to(DEV), dl, want_lse=True)
+    assert O[1:].isnan().all() and lse[1:].isnan().all() and torch.isfinite(O[0].float()).all()
+    table[0, 9] = 2**31 - 1      # behind the length
+    O2, lse2 = sc.sc_paged_decode_attn(pc.cache(table), Q.to(DEV), dl, want_lse=True)
+    assert torch.equal(O2[0], O[0]) and torch.equal(lse2[0], lse[0])
+    # a place outside the table
+    sel = torch.tensor([[[0, 1], [0, 10]], [[2, 3], [-1, 3]], [[0, 8], [9, 0]]], dtype=torch.int32, device=DEV)
+    many = torch.full((3, 2), 2, dtype=torch.int32, device=DEV)
+    O, lse = sc.sc_paged_decode_attn(pc.cache(table), Q.to(DEV), dl, want_lse=True, sel=sel, sel_lens=many)
+    for b, h, bad in ((0, 0, False), (0, 1, True), (1, 0, False), (1, 1, True), (2, 0, False), (2, 1, True)):
+        assert bool(O[b, 4 * h : 4 * h + 4].isnan().all()) == bad and bool(lse[b, 4 * h : 4 * h + 4].isnan().all()) == bad, (b, h)
+
+
+def test_decode_pages_beyond_4_gib():
+    """A pool of more than 2^32 bytes: rows on its last pages."""
+    print("decode far pages", flush=True)
+    R, n = 256, (9 << 30) // (2 * 256 * 128 * 2)
+    K = torch.zeros((n, 2, R, 128), dtype=BF, device=DEV)
+    V = torch.zeros((n, 2, R, 128), dtype=BF, device=DEV)
+    table = torch.tensor([[n - 1, 0, n - 2, n // 2]], dtype=torch.int32, device=DEV)
+    lens = torch.tensor([0], dtype=torch.int32, device=DEV)
+    new = torch.tensor([0], dtype=torch.int32, device=DEV)
+    cache = sc.PagedCache(K, V, table)
+    gen = torch.Generator().manual_seed(5)
+    k, v = (torch.randn((1, 2, 1000, 128), generator=gen).to(BF) for _ in range(2))
+    sc.sc_paged_append(cache, k.to(DEV), v.to(DEV), lens, new)
+    assert int(new) == 1000
+    Q = torch.randn((1, 4, 128), generator=gen).to(BF)
+    O, lse = sc.sc_paged_decode_attn(cache, Q.to(DEV), new, want_lse=True)
+    for h in range(2):
+        wo, wl, to, tl = attend(Q[0, 2 * h : 2 * h + 2].double(), (k[0, h].double(), v[0, h].double(), None), 1 / math.sqrt(128))
+        close(O[0, 2 * h : 2 * h + 2], wo, to + half_step(BF) * wo.abs() * (1 + 2.0**-6))
+
+
+# ------------------------------------------------------------------------------------------------ append
+def angles(rot, most):
+    a = torch.arange(most, dtype=torch.float64)[:, None] * 10000.0 ** (-2.0 * torch.arange(rot // 2, dtype=torch.float64) / rot)
+    return torch.cat((a.cos(), a.sin()), 1).float()
+
+
+def rotated(x, cos_sin, positions, interleaved):
+    """x fp64 [B, heads, N, d] -> turned, and the error of its computation in fp32 (before the type's rounding)."""
+    rot = cos_sin.shape[1]
+    out, tol = x.clone(), torch.zeros_like(x)
+    for b in range(x.shape[0]):
+        t = cos_sin[int(positions[b]) : int(positions[b]) + x.shape[2]].double()
+        c, s = t[:, : rot // 2], t[:, rot // 2 :]
+        i = torch.arange(0, rot, 2) if interleaved else torch.arange(rot // 2)
+        j = i + 1 if interleaved else i + rot // 2
+        a, e = x[b][..., i], x[b][..., j]
+        out[b][..., i], out[b][..., j] = a * c - e * s, e * c + a * s
+        tol[b][..., i], tol[b][..., j] = 3 * U * ((a * c).abs() + (e * s).abs()), 3 * U * ((e * c).abs() + (a * s).abs())
+    return out, tol
+
+
+def check_append(pc, N, base, new, rot=0, interleaved=False, G=0, qdt=None, per_head=False, own_positions=True, fused=False, in_place=False, seed=9):
+    """base, new [B][H]."""
+    B, H, R, d, dt = pc.B, pc.H, pc.R, pc.d, pc.dtype
+    gen = torch.Generator().manual_seed(seed)
+    qdt = qdt or dt
+    if fused:      # [B, N, heads, d], as a projection leaves it
+        x = torch.randn((B, N, (G + 2) * H, d), generator=gen).to(dt)
+        dx = x.to(DEV).permute(0, 2, 1, 3)
+        q, k, v = x.permute(0, 2, 1, 3).split((G * H, H, H), 1)
+        dq, dk, dv = dx.split((G * H, H, H), 1)
+    else:
+        k, v = (torch.randn((B, H, N, d), generator=gen).to(dt) for _ in range(2))
+        q = torch.randn((B, G * H, N, d), generator=gen).to(qdt)
+        dq, dk, dv = q.to(DEV), k.to(DEV), v.to(DEV)
+    sizes = torch.randint(1, 40, (B, H, N), generator=gen, dtype=torch.int32)
+    tb, tn = torch.tensor(base, dtype=torch.int32), torch.tensor(new, dtype=torch.int32)
+    pick = (lambda t: t.contiguous().to(DEV)) if per_head else (lambda t: t[:, 0].contiguous().to(DEV))
+    K0, V0, C0 = pc.K.cpu(), pc.V.cpu(), None if pc.counts is None else pc.counts.cpu()
+    mins0 = None if pc.k_min is None else (pc.k_min.cpu(), pc.k_max.cpu())
+    positions = torch.randint(0, 3000, (B,), generator=gen, dtype=torch.int32) if own_positions else tb[:, 0]
+    cos_sin = angles(rot, 3000 + N + int(tb.max())) if rot else None
+    lens = torch.full_like(pick(tb), -77)
+    kw = {}
+    if rot:
+        kw = dict(cos_sin=cos_sin.to(DEV), positions=positions.to(DEV) if own_positions else None, interleaved=interleaved)
+        if G:
+            kw.update(Q=dq, Q_out=dq if in_place else None)
+    everything = all(n == N for row in new for n in row)
+    _, Qo = sc.sc_paged_append(pc.cache(), dk, dv, pick(tb), lens, new_lens=None if everything else pick(tn), counts=None if pc.counts is None else sizes.to(DEV), **kw)
+    torch.cuda.synchronize()
+    want_k, tol_k = rotated(k.double(), cos_sin, positions, interleaved) if rot else (k.double(), torch.zeros(k.shape, dtype=torch.float64))
+    if rot and G:
+        want_q, tol_q = rotated(q.double(), cos_sin, positions, interleaved)
+        tol_q[..., :rot] += half_step(qdt) * want_q[..., :rot].abs() * (1 + 2.0**-6)
+        close(Qo, want_q, tol_q)
+    tol_k[..., :rot] += half_step(dt) * want_k[..., :rot].abs() * (1 + 2.0**-6)
+    assert torch.equal(lens.cpu(), (tb + tn) if per_head else (tb + tn)[:, 0])
+    K1, V1 = pc.K.cpu(), pc.V.cpu()
+    C1 = None if pc.counts is None else pc.counts.cpu()
+    mins = None if pc.k_min is None else (pc.k_min.cpu(), pc.k_max.cpu())
+    for b in range(B):
+        for h in range(H):
+            at, n = base[b][h], new[b][h]
+            page, head, row = pc.place(b, h, torch.arange(at, at + n))
+            close(K1[page, head, row], want_k[b, h, :n], tol_k[b, h, :n])
+            assert torch.equal(V1[page, head, row], v[b, h, :n])
+            if C1 is not None:
+                assert torch.equal(C1[page, head, row], sizes[b, h, :n])
+                C0[page, head, row] = sizes[b, h, :n]
+            if mins is not None and n:
+                for p in range(at // R, (at + n - 1) // R + 1):
+                    pg, hd, r = pc.place(b, h, torch.arange(p * R, min((p + 1) * R, at + n)))
+                    keys = K1[pg, hd, r].float()
+                    assert torch.equal(mins[0][pg[0], hd].float(), keys.amin(0)) and torch.equal(mins[1][pg[0], hd].float(), keys.amax(0)), (b, h, p)
+                    mins0[0][pg[0], hd], mins0[1][pg[0], hd] = mins[0][pg[0], hd], mins[1][pg[0], hd]
+            K0[page, head, row], V0[page, head, row] = K1[page, head, row], V1[page, head, row]
+    # and nothing else
+    same = lambda x, y: torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
+    assert same(K0, K1) and same(V0, V1)
+    assert C1 is None or same(C0, C1)
+    assert mins is None or (same(mins0[0], mins[0]) and same(mins0[1], mins[1]))
+
+
+@pytest.mark.parametrize("N", [1, 2, 15, 16, 17, 33, 100])
+@pytest.mark.parametrize("base", [0, 1, 15, 16, 31, 63, 64, 100])
+@pytest.mark.parametrize("dtype, d", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
+def test_append_rows(N, base, dtype, d):
+    print("append", N, base, dtype, d, flush=True)
+    pc = Paged(2, 2, 7, 32, d, dtype, summary=True, junk=False, seed=N)
+    pc.fill([[base] * 2] * 2)
+    check_append(pc, N, [[base] * 2] * 2, [[N] * 2] * 2, rot=d, G=2)
+
+
+@pytest.mark.parametrize("R", [16, 64, 256, 1024])
+@pytest.mark.parametrize("rot, interleaved", [(0, False), (16, False), (16, True), (64, False), (64, True), (128, False), (128, True), (48, False), (112, True)])
+@pytest.mark.parametrize("dtype, qdt", [(BF, BF), (BF, F32), (F32, F32), (F32, BF)])
+def test_append_rotations(R, rot, interleaved, dtype, qdt):
+    print("append rotation", R, rot, interleaved, dtype, qdt, flush=True)
+    pc = Paged(2, 3, max(2, 600 // R), R, 128, dtype, layout="prhd" if R == 64 else "phrd", summary=rot != 16)
+    check_append(pc, 70, [[0] * 3, [33 if rot == 16 else 0] * 3], [[70] * 3, [41] * 3], rot=rot, interleaved=interleaved, G=4, qdt=qdt, own_positions=R != 16, in_place=R == 256)
+
+
+@pytest.mark.parametrize("layout", ["phrd", "prhd", "pkv"])
+def test_append_from_a_fused_projection(layout):
+    print("append fused", layout, flush=True)
+    pc = Paged(3, 2, 9, 32, 128, BF, layout=layout, summary=True, junk=False)
+    base = [[0] * 2, [40] * 2, [64] * 2]
+    pc.fill(base)
+    check_append(pc, 99, base, [[99] * 2, [0] * 2, [1] * 2], rot=128, G=4, fused=True)
+    check_append(pc, 99, base, [[99] * 2, [98] * 2, [50] * 2], rot=64, G=4, fused=True, in_place=True, seed=10)
+
+
+@pytest.mark.parametrize("own_pages", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_append_merged_rows(own_pages, dtype):
+    """Every head its own number of rows, with sizes."""
+    print("append merged", own_pages, dtype, flush=True)
+    pc = Paged(2, 3, 12, 16, 128, dtype, per_head_table=own_pages, counts=True, summary=True, junk=False)
+    base = [[0, 17, 100], [64, 5, 0]]
+    pc.fill(base)
+    check_append(pc, 80, base, [[80, 0, 33], [1, 79, 0]], per_head=True)
+    pc2 = Paged(2, 3, 12, 16, 64, dtype, per_head_table=own_pages, counts=True, summary=True, junk=False)
+    check_append(pc2, 80, [[0] * 3] * 2, [[80] * 3, [13] * 3], rot=32, G=2)
+
+
+def test_append_after_going_back():
+    """Rows that are taken back (a shorter length than before) leave no trace in the summaries."""
+    print("append going back", flush=True)
+    pc = Paged(1, 2, 6, 32, 128, BF, summary=True, junk=False)
+    check_append(pc, 90, [[0] * 2], [[90] * 2], rot=128)
+    check_append(pc, 10, [[70] * 2], [[10] * 2], rot=128, seed=4)
+    check_append(pc, 1, [[64] * 2], [[1] * 2], rot=128, seed=5)
+    check_append(pc, 3, [[0] * 2], [[3] * 2], rot=128, seed=6)
+
+
+def test_append_what_does_not_fit_is_reported_and_not_written():
+    print("append refusals on the device", flush=True)
+    pc = Paged(7, 2, 4, 16, 128, BF, summary=True, junk=False)
+    N = 20
+    k = torch.randn((7, 2, N, 128), generator=pc.gen).to(BF).to(DEV)
+    table = pc.table.clone()
+    table[5, 2], table[6, 0] = pc.n, -1
+    base = torch.tensor([44, 45, -1, 2**31 - 1, 10, 25, 16], dtype=torch.int32, device=DEV)
+    new = torch.tensor([20, 20, 3, 20, 21, 20, 20], dtype=torch.int32, device=DEV)
+    lens = torch.zeros(7, dtype=torch.int32, device=DEV)
+    K0 = pc.K.clone()
+    sc.sc_paged_append(pc.cache(table), k, k, base, lens, new_lens=new)
+    assert lens.tolist() == [64, -1, -1, -1, -1, -1, 36]      # page 0 of sequence 6 receives nothing
+    touched = (K0.view(torch.int16) != pc.K.view(torch.int16)).flatten(1).any(1).cpu()
+    allowed = {int(x) for x in table[0, 2:]} | {int(table[5, 1])} | {int(x) for x in table[6, 1:3]}
+    assert {i for i in range(pc.n) if touched[i]} == allowed
+    # positions outside the angles
+    cos_sin = angles(128, 100).to(DEV)
+    base.zero_()
+    new.fill_(5)
+    positions = torch.tensor([0, 95, 96, -1, 100, 80, 2**31 - 1], dtype=torch.int32, device=DEV)
+    K0 = pc.K.clone()
+    q = torch.randn((7, 4, N, 128), generator=pc.gen).to(BF).to(DEV)
+    table[6, 0] = pc.table[6, 0]
+    _, Qo = sc.sc_paged_append(pc.cache(table), k, k, base, lens, new_lens=new, cos_sin=cos_sin, positions=positions, Q=q)
+    assert lens.tolist() == [5, 5, -1, -1, -1, 5, -1]
+    touched = (K0.view(torch.int16) != pc.K.view(torch.int16)).flatten(1).any(1).cpu()
+    assert {i for i in range(pc.n) if touched[i]} == {int(table[b, 0]) for b in (0, 1, 5)}
+    p = positions.cpu().long()[:, None] + torch.arange(N)
+    outside = ((p < 0) | (p >= 100))[:, None, :, None].expand(-1, 4, -1, 128)
+    assert torch.equal(Qo.isnan().cpu(), outside)
+
+
+# ------------------------------------------------------------------------------------------------ selection
+def want_selection(pc, k_min, k_max, Q, lens, G, keep, first, recent):
+    B, H, R = pc.B, pc.H, pc.R
+    sel, many = torch.full((B, H, keep), -1, dtype=torch.int32), torch.zeros((B, H), dtype=torch.int32)
+    for b in range(B):
+        for h in range(H):
+            n = -(-int(lens[b][h]) // R)
+            if n <= 0:
+                continue
+            page, head, _ = pc.place(b, h, torch.arange(n) * R)
+            lo, hi = k_min[page, head].double(), k_max[page, head].double()
+            q = Q[b, h * G : (h + 1) * G].double()
+            score = torch.maximum(q[:, None] * lo, q[:, None] * hi).sum(2)
+            score = torch.where(score.isnan().any(0), math.inf, score.amax(0))
+            place = torch.arange(n)
+            forced = (place < first) | (place >= n - recent)
+            order = sorted(range(n), key=lambda i: (not forced[i], -float(score[i]), i))[:keep]
+            many[b, h] = len(order)
+            sel[b, h, : len(order)] = torch.tensor(sorted(order), dtype=torch.int32)
+    return sel, many
+
+
+@pytest.mark.parametrize("n, keep, first, recent", [(1, 1, 1, 0), (5, 5, 0, 0), (40, 7, 1, 2), (300, 100, 2, 2), (1500, 64, 1, 2), (2600, 1300, 0, 1), (64, 63, 0, 0), (65, 64, 4, 60)])
+@pytest.mark.parametrize("dtype, qdt, d, G", [(BF, BF, 128, 4), (BF, F32, 64, 7), (F32, F32, 128, 1), (F32, BF, 64, 16)])
+def test_select(n, keep, first, recent, dtype, qdt, d, G):
+    print("select", n, keep, first, recent, dtype, qdt, d, G, flush=True)
+    R = 16
+    pc = Paged(2, 2, n + 2, R, d, dtype, junk=False, seed=n)
+    lens = [[n * R] * 2, [max(0, n * R // 2 - 3)] * 2]
+    lo = torch.randn((pc.n, 2, d), generator=pc.gen).to(dtype)
+    hi = (lo.double() + torch.rand((pc.n, 2, d), generator=pc.gen)).to(dtype)
+    pc.k_min, pc.k_max = lo.to(DEV), hi.to(DEV)
+    Q = torch.randn((2, 2 * G, d), generator=pc.gen).to(qdt)
+    sel, many = sc.sc_paged_select(pc.cache(), Q.to(DEV), torch.tensor([x[0] for x in lens], dtype=torch.int32, device=DEV), keep, first=first, recent=recent)
+    want, want_many = want_selection(pc, lo, hi, Q, lens, G, keep, first, recent)
+    assert torch.equal(many.cpu(), want_many) and torch.equal(sel.cpu(), want)
+
+
+def test_select_ties_go_to_the_lowest_page():
+    print("select ties", flush=True)
+    n = 2500
+    pc = Paged(1, 2, n, 16, 128, BF, junk=False)
+    few = torch.randn((3, 128), generator=pc.gen).to(BF)
+    which = torch.randint(0, 3, (pc.n, 2), generator=pc.gen)
+    lo = few[which]
+    pc.k_min = pc.k_max = lo.to(DEV)
+    Q = torch.randn((1, 4, 128), generator=pc.gen).to(BF)
+    dl = torch.tensor([n * 16], dtype=torch.int32, device=DEV)
+    for keep in (1, 10, 800, 1700, 2499):
+        sel, many = sc.sc_paged_select(pc.cache(), Q.to(DEV), dl, keep, first=0, recent=0)
+        want, want_many = want_selection(pc, lo, lo, Q, [[n * 16] * 2], 2, keep, 0, 0)
+        assert torch.equal(many.cpu(), want_many) and torch.equal(sel.cpu(), want), keep
+    # all equal, zeros of both signs
+    zero = torch.where(torch.rand((pc.n, 2, 128), generator=pc.gen) < 0.5, 0.0, -0.0).to(BF)
+    pc.k_min = pc.k_max = zero.to(DEV)
+    sel, _ = sc.sc_paged_select(pc.cache(), Q.to(DEV), dl, 77, first=0, recent=1)
+    assert (sel.cpu() == torch.tensor(list(range(76)) + [n - 1])).all()
+
+
+def test_select_decides_as_exact_arithmetic_does():
+    """Scores that agree to 30 bits and more: sums in fp32 could not tell them apart."""
+    print("select close", flush=True)
+    n = 200
+    pc = Paged(1, 1, n, 16, 128, BF, junk=False)
+    lo = torch.zeros((pc.n, 1, 128))
+    lo[:, 0, 0] = 2.0**20
+    page, _, _ = pc.place(0, 0, torch.arange(n) * 16)
+    rank = torch.randperm(n, generator=pc.gen)
+    lo[page, 0, 1] = 2.0**-14 * (1 + rank // 128)
+    lo[page, 0, 2] = 2.0**-22 * (rank % 128)
+    lo = lo.to(BF)
+    pc.k_min = pc.k_max = lo.to(DEV)
+    Q = torch.ones((1, 1, 128), dtype=BF)
+    for keep in (1, 50, 133):
+        sel, _ = sc.sc_paged_select(pc.cache(), Q.to(DEV), torch.tensor([n * 16], dtype=torch.int32, device=DEV), keep, first=0, recent=0)
+        assert sel.cpu()[0, 0].tolist() == sorted(i for i in range(n) if rank[i] >= n - keep), keep
+
+
+def test_select_what_is_not_a_number_and_bad_pages_are_kept():
+    print("select not a number", flush=True)
+    n = 100
+    pc = Paged(1, 2, n, 16, 128, BF, junk=False)
+    lo = torch.randn((pc.n, 2, 128), generator=pc.gen).to(BF)
+    page, _, _ = pc.place(0, 0, torch.arange(n) * 16)
+    lo[page[33], 0, 7] = math.nan
+    hi = lo + 1
+    lo[page[35], 1, 7], hi[page[36], 1, 3] = -math.inf, math.inf
+    pc.k_min, pc.k_max = lo.to(DEV), hi.to(DEV)
+    table = pc.table.clone()
+    table[0, 71] = pc.n + 5
+    Q = torch.randn((1, 4, 128), generator=pc.gen).to(BF)
+    Q[0, 2:, 3], Q[0, 2:, 7] = 1.0, -1.0
+    sel, many = sc.sc_paged_select(pc.cache(table), Q.to(DEV), torch.tensor([n * 16], dtype=torch.int32, device=DEV), 6, first=1, recent=1)
+    a, b = sel.cpu()[0].tolist()
+    assert {0, 33, 71, 99} <= set(a) and a == sorted(a) and {0, 35, 36, 71, 99} <= set(b) and b == sorted(b)
+
+
+def test_append_select_and_attend_together():
+    """Prompt, then tokens: pages chosen by the summaries that the appends left, attention over them; every length per head too."""
+    print("together", flush=True)
+    B, H, G, R, d = 2, 2, 4, 16, 128
+    pc = Paged(B, H, 40, R, d, BF, summary=True)
+    cache = pc.cache()
+    ws = sc.paged_workspace(B, H * G, H, d, pc.P, DEV)
+    cos_sin = angles(d, 1000).to(DEV)
+    base = torch.zeros(B, dtype=torch.int32, device=DEV)
+    lens = torch.empty_like(base)
+    new = torch.tensor([500, 333], dtype=torch.int32, device=DEV)
+    x = torch.randn((B, 500, (G + 2) * H, d), generator=pc.gen).to(BF).to(DEV).permute(0, 2, 1, 3)
+    q, k, v = x.split((G * H, H, H), 1)
+    sc.sc_paged_append(cache, k, v, base, lens, new_lens=new, Q=q, cos_sin=cos_sin)
+    for step in range(20):
+        x = torch.randn((B, 1, (G + 2) * H, d), generator=pc.gen).to(BF).to(DEV).permute(0, 2, 1, 3)
+        q, k, v = x.split((G * H, H, H), 1)
+        base, lens = lens, torch.empty_like(lens)
+        _, q = sc.sc_paged_append(cache, k, v, base, lens, Q=q, cos_sin=cos_sin)
+        q = q[:, :, 0].contiguous()
+        sel, many = sc.sc_paged_select(cache, q, lens, 9, first=1, recent=2, workspace=ws)
+        O, lse = sc.sc_paged_decode_attn(cache, q, lens, sel=sel, sel_lens=many, want_lse=True, workspace=ws)
+        n = [[500 + step + 1] * H, [333 + step + 1] * H]
+        assert lens.tolist() == [x[0] for x in n]
+        want, want_many = want_selection(pc, pc.k_min.cpu(), pc.k_max.cpu(), q.cpu(), n, G, 9, 1, 2)
+        assert torch.equal(sel.cpu(), want) and torch.equal(many.cpu(), want_many)
+        K, V = pc.K.cpu().double(), pc.V.cpu().double()
+        for b in range(B):
+            for h in range(H):
+                t = torch.cat([torch.arange(p * R, min((p + 1) * R, n[b][h])) for p in want[b, h].tolist()])
+                page, head, row = pc.place(b, h, t)
+                wo, wl, to, tl = attend(q[b, h * G : (h + 1) * G].double().cpu(), (K[page, head, row], V[page, head, row], None), 1 / math.sqrt(d))
+                close(O[b, h * G : (h + 1) * G], wo, to + half_step(BF) * wo.abs() * (1 + 2.0**-6))
+                close(lse[b, h * G : (h + 1) * G], wl, tl)
+
+
+def test_calls_on_another_stream_and_in_a_graph():
+    """A generated token (append, select, attend) captured once and replayed, with the program's own calls in between."""
+    print("graph", flush=True)
+    B, H, G, R, d = 2, 2, 4, 16, 128
+    pc = Paged(B, H, 40, R, d, BF, summary=True)
+    cache = pc.cache()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    cos_sin = angles(d, 1000).to(DEV)
+    with torch.cuda.stream(side):
+        ws = sc.paged_workspace(B, H * G, H, d, pc.P, DEV)
+        base, lens = torch.zeros(B, dtype=torch.int32, device=DEV), torch.zeros(B, dtype=torch.int32, device=DEV)
+        k, v = (torch.randn((B, H, 400, d), generator=pc.gen).to(BF).to(DEV) for _ in range(2))
+        sc.sc_paged_append(cache, k, v, base, lens, cos_sin=cos_sin)
+        base.copy_(lens)
+        x = torch.zeros((B, 1, (G + 2) * H, d), dtype=BF, device=DEV)
+        q, k1, v1 = x.permute(0, 2, 1, 3).split((G * H, H, H), 1)
+        qo = torch.empty((B, G * H, 1, d), dtype=BF, device=DEV)
+        sel, many = torch.empty((B, H, 6), dtype=torch.int32, device=DEV), torch.empty((B, H), dtype=torch.int32, device=DEV)
+        O, lse = torch.empty((B, G * H, d), dtype=BF, device=DEV), torch.empty((B, G * H), dtype=F32, device=DEV)
+
+        def token():
+            sc.sc_paged_append(cache, k1, v1, base, lens, Q=q, Q_out=qo, cos_sin=cos_sin)
+            sc.sc_paged_select(cache, qo[:, :, 0], lens, 6, first=1, recent=2, sel=sel, sel_lens=many, workspace=ws)
+            sc.sc_paged_decode_attn(cache, qo[:, :, 0], lens, O=O, lse=lse, sel=sel, sel_lens=many, workspace=ws)
+            base.copy_(lens)
+        xs = [torch.randn(x.shape, generator=pc.gen).to(BF).to(DEV) for _ in range(12)]
+        x.copy_(xs[0])
+        token()
+        first = (O.clone(), lse.clone(), sel.clone())
+        base.fill_(400)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            token()
+        replayed = []
+        for y in xs:
+            x.copy_(y)
+            graph.replay()
+            replayed.append((O.clone(), lse.clone(), sel.clone()))
+            side.synchronize()
+            sc.sc_paged_decode_attn(cache, qo[:, :, 0], lens, workspace=ws)
+        base.fill_(400)
+        for i, y in enumerate(xs):
+            x.copy_(y)
+            token()
+            if i == 0:
+                assert all(torch.equal(a, e) for a, e in zip(first, (O, lse, sel)))
+            assert all(torch.equal(a, e) for a, e in zip(replayed[i], (O, lse, sel))), i
+    torch.cuda.current_stream().wait_stream(side)
+
+
+def test_wrappers_with_and_without_native_marshalling(monkeypatch):
+    print("marshalling", flush=True)
+    assert sc.load_library() is not None and sc._native is not None
+    B, H, G, R, d = 2, 2, 4, 16, 128
+    outs = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(sc, "_native", None)
+        pc = Paged(B, H, 40, R, d, BF, summary=True, seed=8)
+        cache, ws = pc.cache(), sc.paged_workspace(B, H * G, H, d, pc.P, DEV)
+        base, lens = torch.zeros(B, dtype=torch.int32, device=DEV), torch.zeros(B, dtype=torch.int32, device=DEV)
+        k, v = (torch.randn((B, H, 400, d), generator=pc.gen).to(BF).to(DEV) for _ in range(2))
+        q = torch.randn((B, H * G, 400, d), generator=pc.gen).to(BF).to(DEV)
+        qo = torch.empty_like(q)
+        new = torch.tensor([400, 123], dtype=torch.int32, device=DEV)
+        sc.sc_paged_append(cache, k, v, base, lens, new_lens=new, Q=q, Q_out=qo, cos_sin=angles(d, 500).to(DEV), interleaved=True)
+        sel, many = torch.empty((B, H, 6), dtype=torch.int32, device=DEV), torch.empty((B, H), dtype=torch.int32, device=DEV)
+        q1 = qo[:, :, 50].contiguous()
+        sc.sc_paged_select(cache, q1, lens, 6, first=1, recent=2, sel=sel, sel_lens=many, workspace=ws)
+        O, lse = torch.empty_like(q1), torch.empty((B, G * H), dtype=F32, device=DEV)
+        sc.sc_paged_decode_attn(cache, q1, lens, scale=0.2, O=O, lse=lse, sel=sel, sel_lens=many, workspace=ws)
+        outs.append((pc.K.clone().view(torch.int16), pc.k_max.clone().view(torch.int16), lens, qo, sel, many, O, lse))
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+
+
+def test_wrappers_refuse_what_does_not_fit():
+    print("refusals", flush=True)
+    pc = Paged(2, 2, 4, 16, 128, BF, summary=True)
+    cache = pc.cache()
+    k = torch.zeros((2, 2, 3, 128), dtype=BF, device=DEV)
+    base, lens = torch.zeros(2, dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
+    q = torch.zeros((2, 8, 128), dtype=BF, device=DEV)
+    bad = [
+        lambda: sc.sc_paged_append(cache, k.float(), k.float(), base, lens), lambda: sc.sc_paged_append(cache, k[:1], k[:1], base, lens),
+        lambda: sc.sc_paged_append(cache, k, k, base, base), lambda: sc.sc_paged_append(cache, k, k, base.long(), lens),
+        lambda: sc.sc_paged_append(cache, k, k, base, torch.zeros((2, 2), dtype=torch.int32, device=DEV)),
+        lambda: sc.sc_paged_append(cache, k, k, base, lens, counts=torch.ones((2, 2, 3), dtype=torch.int32, device=DEV)),
+        lambda: sc.sc_paged_append(cache, k, k, base, lens, Q=k), lambda: sc.sc_paged_append(cache, k.cpu(), k.cpu(), base, lens),
+        lambda: sc.sc_paged_append(cache, k.transpose(2, 3).contiguous().transpose(2, 3), k, base, lens),
+        lambda: sc.sc_paged_append(cache, k, k, base, lens, Q=k, cos_sin=torch.zeros((9, 24), device=DEV)),
+        lambda: sc.sc_paged_append(cache, k, k, base, lens, cos_sin=torch.zeros((9, 128), dtype=BF, device=DEV)),
+        lambda: sc.sc_paged_decode_attn(cache, q[:1], base), lambda: sc.sc_paged_decode_attn(cache, q[:, :7].contiguous(), base),
+        lambda: sc.sc_paged_decode_attn(cache, q.half(), base), lambda: sc.sc_paged_decode_attn(cache, q, base.long()),
+        lambda: sc.sc_paged_decode_attn(cache, q, base, O=q.double()), lambda: sc.sc_paged_decode_attn(cache, q, base, lse=base),
+        lambda: sc.sc_paged_decode_attn(cache, q, base, sel=torch.zeros((2, 2, 1), dtype=torch.int32, device=DEV)),
+        lambda: sc.sc_paged_decode_attn(cache, q, base, scale=math.nan), lambda: sc.sc_paged_decode_attn(cache, q, base, workspace=sc.Workspace(256, DEV)),
+        lambda: sc.sc_paged_select(cache, q, base, 1, first=1, recent=1), lambda: sc.sc_paged_select(cache, q, base, 0, first=0, recent=0),
+        lambda: sc.sc_paged_select(cache, q, base, 4, sel=torch.zeros((2, 2, 3), dtype=torch.int32, device=DEV)),
+        lambda: sc.sc_paged_select(sc.PagedCache(pc.K, pc.V, cache.table), q, base, 4),
+        lambda: sc.paged_workspace(2, 7, 2, 128, 4, DEV),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(sc.SemantiCacheError):
+            call()
+            print("not refused:", i, flush=True)
