@@ -438,11 +438,11 @@ sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *rows
 
 /* The workspace of the two calls below: sc_paged_workspace_bytes bytes for a cache of B sequences, Hkv KV heads
  * and tables of table_len pages, initialised ONCE with sc_paged_init_workspace; calls that share it must be
- * stream-ordered, and need no more care.  (It starts with one counter per (sequence, KV head): the workgroups that
- * share a head's rows count themselves off, the last one joins their partial results and leaves the counter at zero.)
+ * stream-ordered, and need no more care.  (It starts with counters: the workgroups that share a head's rows count
+ * themselves off, the last one joins their partial results and leaves the counter at zero.)
  */
 size_t sc_paged_workspace_bytes(int B, int Hq, int Hkv, int d, int table_len);
-sc_status sc_paged_init_workspace(void *ws, size_t ws_bytes, int B, int Hkv, void *stream);
+sc_status sc_paged_init_workspace(void *ws, size_t ws_bytes, void *stream);
 
 /* sc_paged_decode_attn — sc_decode_attn over a cache in pages:
  *     O[b,hq] = softmax_t( Q[b,hq] . K[b,h,t] * scale + ln(counts[b,h,t]) ) V[b,h,t],  t in [0, lens),  h = hq / (Hq / Hkv),

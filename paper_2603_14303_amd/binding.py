@@ -123,7 +123,7 @@ def load_library() -> ctypes.CDLL:
     lib.sc_paged_workspace_bytes.restype = sz
     lib.sc_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
     lib.sc_paged_init_workspace.restype = i32
-    lib.sc_paged_init_workspace.argtypes = [vp, sz, i32, i32, vp]
+    lib.sc_paged_init_workspace.argtypes = [vp, sz, vp]
     lib.sc_paged_decode_attn.restype = i32
     lib.sc_paged_decode_attn.argtypes = [pc, vp, i32, i32, vp, i32, vp, vp, i32, f32, vp, i32, vp, vp, sz, vp]
     lib.sc_paged_select.restype = i32
@@ -597,7 +597,7 @@ def paged_workspace(B: int, Hq: int, Hkv: int, d: int, table_len: int, device) -
     if nbytes == 0:
         raise SemantiCacheError("no workspace for B=%d Hq=%d Hkv=%d d=%d table_len=%d" % (B, Hq, Hkv, d, table_len))
     ws = Workspace(nbytes, device)
-    _check(lib.sc_paged_init_workspace(ws.ptr, ws.nbytes, B, Hkv, _stream()), "sc_paged_init_workspace")
+    _check(lib.sc_paged_init_workspace(ws.ptr, ws.nbytes, _stream()), "sc_paged_init_workspace")
     return ws
 
 

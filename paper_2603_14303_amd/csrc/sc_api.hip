@@ -491,12 +491,11 @@ sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *r, v
 size_t sc_paged_workspace_bytes(int B, int Hq, int Hkv, int d, int table_len) {
     if (B <= 0 || Hkv <= 0 || Hq <= 0 || table_len <= 0 || Hq % Hkv || (d != 64 && d != 128)) return 0;
     const size_t attend = paged_decode_bytes(Hq / Hkv, d), select = paged_select_bytes(B, Hkv, table_len);
-    return paged_state_bytes(B, Hkv) + (attend > select ? attend : select);
+    return paged_state_bytes() + (attend > select ? attend : select);
 }
 
-sc_status sc_paged_init_workspace(void *ws, size_t ws_bytes, int B, int Hkv, void *stream) {
-    if (B <= 0 || Hkv <= 0) return SC_ERR_INVALID_ARG;
-    const size_t state = paged_state_bytes(B, Hkv);
+sc_status sc_paged_init_workspace(void *ws, size_t ws_bytes, void *stream) {
+    const size_t state = paged_state_bytes();
     if (!ws || ws_bytes < state || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SC_ERR_WORKSPACE;
     return runtime_status(launch_decode_init_workspace(ws, state, static_cast<hipStream_t>(stream)));
 }
@@ -524,7 +523,7 @@ sc_status sc_paged_decode_attn(const sc_paged_cache *cache, const void *Q, sc_dt
     if (sel && keep > (1 << 20)) return SC_ERR_UNSUPPORTED;
     const int64_t most = (int64_t)(sel ? keep : cache->table_len) * cache->page_rows;
     if ((most / 64 + 1) * cache->B * cache->Hkv > (1 << 30)) return SC_ERR_UNSUPPORTED;      // the kernel counts stretches of 64 rows and more in 32 bits
-    if (ws_bytes < paged_state_bytes(cache->B, cache->Hkv) + paged_decode_bytes(Hq / cache->Hkv, cache->d)) return SC_ERR_WORKSPACE;
+    if (ws_bytes < paged_state_bytes() + paged_decode_bytes(Hq / cache->Hkv, cache->d)) return SC_ERR_WORKSPACE;
     a.Q = Q; a.q_dtype = static_cast<DType>(q_dtype); a.Hq = Hq;
     a.lens = lens; a.lens_per_head = lens_per_head != 0;
     a.sel = sel; a.sel_lens = sel_lens; a.keep = sel ? keep : 0;
@@ -542,7 +541,7 @@ sc_status sc_paged_select(const sc_paged_cache *cache, const void *Q, sc_dtype q
     if (keep <= 0 || (int64_t)first + recent > keep) return SC_ERR_CAPACITY;
     if (keep > (1 << 20)) return SC_ERR_UNSUPPORTED;
     if ((int64_t)(cache->table_len / 16 + 1) * cache->B * cache->Hkv > INT32_MAX) return SC_ERR_UNSUPPORTED;      // grid size
-    if (ws_bytes < paged_state_bytes(cache->B, cache->Hkv) + paged_select_bytes(cache->B, cache->Hkv, cache->table_len)) return SC_ERR_WORKSPACE;
+    if (ws_bytes < paged_state_bytes() + paged_select_bytes(cache->B, cache->Hkv, cache->table_len)) return SC_ERR_WORKSPACE;
     a.Q = Q; a.q_dtype = static_cast<DType>(q_dtype); a.Hq = Hq;
     a.lens = lens; a.lens_per_head = lens_per_head != 0;
     a.keep = keep; a.first = first; a.recent = recent;

@@ -89,7 +89,7 @@ struct PagedSelectArgs {
 hipError_t launch_paged_select(const PagedSelectArgs &a, hipStream_t stream);
 
 // ---- workspace: counters, then what the two calls need (they follow each other on a stream, so it is the same memory)
-size_t paged_state_bytes(int B, int H);
+size_t paged_state_bytes();
 size_t paged_decode_bytes(int G, int d);
 size_t paged_select_bytes(int B, int H, int P);
 

@@ -1,11 +1,11 @@
 // sc_paged_decode_attn: attention of one new token of every sequence over a cache held in pages.
 //     O = softmax(q K^T scale + ln s) V   per (sequence, query head); the G <= 16 query heads of a KV head together, so that its rows are read once.
 //
-// Work.  Bound by bytes: 4 G operations for every 2 bytes of a row.  The rows of all (sequence, KV head) pairs are cut into units of kUnit rows and
+// Work.  Bound by bytes: 4 G operations for every 2 bytes of a row.  The rows of all (sequence, KV head) pairs are cut into units of a step's rows and
 // laid end to end; every workgroup takes an equal stretch of them, whatever lengths they come from (a ragged batch with a fixed number of splits
 // per head waits for its longest sequence).  The lengths are on the device, so every workgroup adds them up by itself.  A head that lies within one
 // workgroup's stretch is stored directly.  Otherwise every workgroup that holds a part of it leaves a partial result (running maximum, sum, fp32
-// sums) in the workspace and counts itself off at the head's counter; the one that comes last joins the partial results.  Nobody waits.
+// sums) in the workspace and counts itself off; the one that comes last joins the partial results.  Nobody waits.
 //
 // Step.  A wavefront takes 16 rows at a time, always of one page.  Keys are loaded as the first product wants them (lane (g, c) of the wavefront's
 // 4 x 16 lanes: row c, 16 bytes at 64 ks + 16 g), values as the second one does (rows 4 g + i).  The scores leave the first product with lane (g, c)
@@ -18,10 +18,11 @@
 
 namespace sc {
 
-constexpr int kPagWaves = 6;
+constexpr int kPagWaves = 8;
 constexpr int kPagThreads = kPagWaves * kWave;
-constexpr int kUnit = 16 * kPagWaves;        // rows of a unit: one step of every wavefront
-constexpr int kMaxWgs = 512;                 // two workgroups of six wavefronts on each of the 256 compute units
+constexpr int kStep = 16 * kPagWaves;        // rows of a step of all wavefronts; the work's unit, or kAlone of them
+constexpr int kAlone = 2;
+constexpr int kMaxWgs = 256;                 // one on each compute unit
 constexpr int kPagPad = 4;                   // floats behind the sums of a partial result: maximum, sum, two unused
 constexpr int kMaxHeadWgs = 64;              // workgroups per (sequence, KV head) at most, on average: each is a partial result to join
 constexpr float kPagLog2e = 1.4426950408889634f;
@@ -43,24 +44,32 @@ struct PagDecParams {
     void *O;
     int o_is_bf16;
     float *lse;
-    int *counter;        // [B * H] workgroups that have left their part of a head
+    int *counter;        // [2][2 * kMaxWgs] workgroups that have left their part of a head (of a group of parts), groups that have been joined; by the first one's place
     float *part;         // [2 * kMaxWgs][G][D + kPagPad]: a workgroup's first stretch and its last one
     int wgs;             // workgroups of the launch
 };
 
 __device__ __forceinline__ float pag_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// rows of entry e: of sequence e, or of (sequence, KV head) e where lengths or a selection are per head
-__device__ __forceinline__ int pag_rows(const PagDecParams &p, int e) {
-    if (p.sel) return min(max(p.sel_lens[e], 0), p.keep) << p.c.log2_R;      // the rows of whole pages; those behind the length are masked
-    return min(max(p.lens[e], 0), p.c.P << p.c.log2_R);
-}
-__device__ __forceinline__ int pag_units(int rows) { return paged_units(rows, kUnit); }
-
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) x += __shfl_xor(x, off, kWave);
+// Sums over the lanes up to each one (DPP moves inside the rows of 16 lanes, then from row to row), and the maximum over all of them
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_rows(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int x) {
+    x += dpp_rows<0x111, 0xf>(x);      // row_shr 1, 2, 4, 8
+    x += dpp_rows<0x112, 0xf>(x);
+    x += dpp_rows<0x114, 0xf>(x);
+    x += dpp_rows<0x118, 0xf>(x);
+    x += dpp_rows<0x142, 0xa>(x);      // row_bcast 15: lane 15 to the second row, lane 47 to the fourth
+    x += dpp_rows<0x143, 0xc>(x);      // row_bcast 31: lane 31 to the upper half
     return x;
+}
+__device__ __forceinline__ int wave_max(int x) {      // x >= 0
+    x = max(x, dpp_rows<0x111, 0xf>(x));
+    x = max(x, dpp_rows<0x112, 0xf>(x));
+    x = max(x, dpp_rows<0x114, 0xf>(x));
+    x = max(x, dpp_rows<0x118, 0xf>(x));
+    x = max(x, dpp_rows<0x142, 0xa>(x));
+    x = max(x, dpp_rows<0x143, 0xc>(x));
+    return __builtin_amdgcn_readlane(x, kWave - 1);
 }
 
 // x as NP bf16 parts whose sum it is (up to the last one's rounding)
@@ -118,12 +127,127 @@ template <typename T, int D> struct Acc {
     }
 };
 
+__device__ __forceinline__ float row_allreduce_max(float x) {      // over the 16 lanes of a row
+    x = fmaxf(x, dpp<kDppQuadXor1>(x));
+    x = fmaxf(x, dpp<kDppQuadXor2>(x));
+    x = fmaxf(x, dpp<kDppHalfMirror>(x));
+    return fmaxf(x, dpp<kDppMirror>(x));
+}
+
+// ------------------------------------------------------------------------------------------------
+// Partial results: [place][head][D + kPagPad] floats, written through to memory and read from there (the workgroups of a head run on chiplets whose
+// L2s do not see each other's lines within a kernel).
+constexpr int kAuxAgent = 16;      // buffer cache policy: device scope
+typedef unsigned int pag_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int pag_u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ void store_result(const PagDecParams &p, int64_t row, int D, int e, const float4 &o, float m, float l) {
+    const float f = l != 0.f ? 1.0f / l : 0.f;
+    store_row4(p.O, p.o_is_bf16, row * D + e, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
+    if (e == 0 && p.lse) p.lse[row] = l != 0.f ? (m + __log2f(l)) * kPagLn2 : -INFINITY;
+}
+template <int D> __device__ __forceinline__ void store_part(__amdgpu_buffer_rsrc_t rs, int at, int e, const float4 &o, float m, float l) {
+    const pag_u32x4 t = {__float_as_uint(o.x), __float_as_uint(o.y), __float_as_uint(o.z), __float_as_uint(o.w)};
+    __builtin_amdgcn_raw_buffer_store_b128(t, rs, (at + e) * 4, 0, kAuxAgent);
+    if (e == 0) {
+        const pag_u32x2 w = {__float_as_uint(m), __float_as_uint(l)};
+        __builtin_amdgcn_raw_buffer_store_b64(w, rs, (at + D) * 4, 0, kAuxAgent);
+    }
+}
+
+// Joins n partial results, whose places `place_of` gives, and hands each of the G D / 4 pieces to `sink` with its head's maximum and sum.
+// A thread owns one piece of one head and every NS-th part; all its loads of a pass are on their way before the first is used.
+template <int D, typename PlaceOf, typename Sink>
+__device__ __forceinline__ void join_parts(const PagDecParams &p, __amdgpu_buffer_rsrc_t rs, int n, PlaceOf place_of, int tid, float *s_buf, float2 *s_total, Sink sink) {
+    constexpr int QPR = D / 4, kStride = D + kPagPad, PASS = 8;
+    const int G = p.G, lane = tid % kWave, wave = tid / kWave;
+    const int pieces = G * QPR;
+    // thread -> (group of parts, piece); with more pieces than threads, every thread takes several pieces
+    const int NS = pieces < kPagThreads ? kPagThreads / pieces : 1;
+    const int log2_G = G > 1 ? 32 - __clz(G - 1) : 0;      // heads of a part, up to a power of two
+    float *s_m = s_buf, *s_l = s_m + (n << log2_G), *s_red = s_l + ((n << log2_G) + 3) / 4 * 4;
+    for (int piece0 = 0; piece0 < pieces; piece0 += kPagThreads) {
+        const int sg = NS > 1 ? tid / pieces : 0, piece = piece0 + (NS > 1 ? tid - sg * pieces : tid);
+        const bool worker = sg < NS && piece < pieces;
+        const int hh = worker ? piece / QPR : 0, e = worker ? 4 * (piece - hh * QPR) : 0;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k0 = 0; k0 < n; k0 += NS * PASS) {
+            float4 x[PASS];
+#pragma unroll
+            for (int t = 0; t < PASS; ++t) {
+                const int k = k0 + sg + NS * t;
+                const bool there = worker && k < n;
+                const pag_u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(rs, there ? ((place_of(k) * G + hh) * kStride + e) * 4 : 0x7FFFFFF0, 0, kAuxAgent);
+                x[t] = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (piece0 == 0 && k0 == 0) {      // the weights: a wavefront per head
+                for (int i = tid; i < n << log2_G; i += kPagThreads) {
+                    const int k = i >> log2_G, h2 = i & ((1 << log2_G) - 1);
+                    const pag_u32x2 t = __builtin_amdgcn_raw_buffer_load_b64(rs, h2 < G ? ((place_of(k) * G + h2) * kStride + D) * 4 : 0x7FFFFFF0, 0, kAuxAgent);
+                    s_m[i] = __uint_as_float(t.x);
+                    s_l[i] = __uint_as_float(t.y);
+                }
+                __syncthreads();
+                for (int h2 = wave; h2 < G; h2 += kPagWaves) {
+                    float m = -INFINITY;
+                    for (int k = lane; k < n; k += kWave) m = fmaxf(m, s_m[(k << log2_G) + h2]);
+                    m = rows_allreduce_max(row_allreduce_max(m));
+                    const float safe = m == -INFINITY ? 0.f : m;
+                    float l = 0.f;
+                    for (int k = lane; k < n; k += kWave) {
+                        const float f = pag_exp2(s_m[(k << log2_G) + h2] - safe);
+                        s_m[(k << log2_G) + h2] = f;
+                        l = fmaf(s_l[(k << log2_G) + h2], f, l);
+                    }
+                    l = rows_allreduce_sum(row_allreduce_sum<16>(l));
+                    if (lane == 0) s_total[h2] = make_float2(m, l);
+                }
+                __syncthreads();
+            }
+#pragma unroll
+            for (int t = 0; t < PASS; ++t) {
+                const int k = k0 + sg + NS * t;
+                const float f = worker && k < n ? s_m[(k << log2_G) + hh] : 0.f;
+                o.x = fmaf(x[t].x, f, o.x);
+                o.y = fmaf(x[t].y, f, o.y);
+                o.z = fmaf(x[t].z, f, o.z);
+                o.w = fmaf(x[t].w, f, o.w);
+            }
+        }
+        if (NS > 1) {
+            if (worker) *reinterpret_cast<float4 *>(s_red + 4 * (sg * pieces + piece)) = o;
+            __syncthreads();
+            if (worker && sg == 0)
+                for (int r = 1; r < NS; ++r) {
+                    const float4 t = *reinterpret_cast<const float4 *>(s_red + 4 * (r * pieces + piece));
+                    o.x += t.x; o.y += t.y; o.z += t.z; o.w += t.w;
+                }
+        }
+        if (worker && sg == 0) sink(hh, e, o, s_total[hh].x, s_total[hh].y);
+    }
+}
+
+// a workgroup's results are on their way to memory: waits until they are there, counts the workgroup off, and tells the last of `n` (counter clear again)
+__device__ __forceinline__ bool last_of(int *counter, int n, int tid, int *s_last) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // every wavefront: its own stores are acknowledged
+    __syncthreads();
+    if (tid == 0) {
+        const int before = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *s_last = before == n - 1;
+        if (before == n - 1) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return *s_last != 0;
+}
+
 // QP: parts of the queries (bf16 caches)
 template <typename T, int D, int QP>
-__global__ __launch_bounds__(kPagThreads) void paged_decode_kernel(PagDecParams p) {
+__global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecParams p) {
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int KL = Rows<T, D>::KL, VW = Rows<T, D>::VW, NA = Acc<T, D>::N;
     constexpr int PP = QP == 1 ? 2 : 3;       // parts of the probabilities (bf16)
+    constexpr int AHEAD = KL == 8 ? 1 : 2;    // (two would take more than 256 registers with rows of 512 bytes)
     constexpr int kStride = D + kPagPad;
     const PagedView &cv = p.c;
     const int G = p.G;
@@ -135,38 +259,52 @@ __global__ __launch_bounds__(kPagThreads) void paged_decode_kernel(PagDecParams 
     __shared__ __attribute__((aligned(16))) float s_acc[kPagWaves * 16 * D];
     __shared__ float s_m[kPagWaves][16], s_l[kPagWaves][16];
     __shared__ int s_last;
+    __shared__ float2 s_total[16];
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc(p.part, (short)0, 2 * kMaxWgs * G * kStride * 4, 0x00020000);
 
     // ---- my stretch of all units: every wavefront adds up the lengths, 64 at a time
     const bool per_head = p.sel != nullptr || p.lens_per_head != 0;
     const int entries = per_head ? cv.B * cv.H : cv.B, weight = per_head ? 1 : cv.H;
-    int total = 0;
-    for (int e0 = 0; e0 < entries; e0 += kWave) total += (e0 + lane < entries) ? pag_units(pag_rows(p, e0 + lane)) * weight : 0;
-    total = wave_sum(total);
+    int my_rows = 0, my_len = 0;      // of the lane's entry among the 64 at hand
+    auto entry = [&](int e) {
+        my_rows = my_len = 0;
+        if (e < entries) {
+            my_len = min(max(p.lens[p.sel && !p.lens_per_head ? e / cv.H : e], 0), cv.P << cv.log2_R);
+            my_rows = p.sel ? min(max(p.sel_lens[e], 0), p.keep) << cv.log2_R : my_len;      // selected: the rows of whole pages; those behind the length are masked
+        }
+    };
+    int total = 0, longest = 0;
+    for (int e0 = 0; e0 < entries; e0 += kWave) {
+        entry(e0 + lane);
+        total += e0 + lane < entries ? paged_units(my_rows, kStep) * weight : 0;
+        longest = max(longest, my_rows);
+    }
+    total = __builtin_amdgcn_readlane(wave_scan(total), kWave - 1);
+    // A workgroup that has all rows of its heads need not hand them over: worth it for up to three steps
+    int unit = kStep;
+    if (wave_max(longest) <= kAlone * kStep) {
+        unit = kAlone * kStep;
+        total = entries * weight;
+    }
     const int per = (total + p.wgs - 1) / p.wgs;
-    int pos = wg * per;
+    const int pos = wg * per;
     const int stop = min(pos + per, total);
     if (pos >= total) return;
-    int e = 0, cum = 0;      // entry that holds unit `pos`, and the units before it
-    for (int e0 = 0;; e0 += kWave) {
-        const int mine = (e0 + lane < entries) ? pag_units(pag_rows(p, e0 + lane)) * weight : 0;
-        int incl = mine;
-#pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const int t = __shfl_up(incl, off, kWave);
-            incl += lane >= off ? t : 0;
-        }
+    int e0 = 0, e = 0, cum = 0;      // entry that holds unit `pos`, and the units before it
+    for (;; e0 += kWave) {
+        if (entries > kWave) entry(e0 + lane);      // (else the lane has its entry still)
+        const int mine = e0 + lane < entries ? paged_units(my_rows, unit) * weight : 0;
+        const int incl = wave_scan(mine);
         const uint64_t beyond = ballot64(cum + incl > pos);
         if (beyond) {
             const int k = first_bit(beyond);
             e = e0 + k;
-            cum += __shfl(incl - mine, k, kWave);
+            cum += __builtin_amdgcn_readlane(incl - mine, k);
             break;
         }
-        cum += __shfl(incl, kWave - 1, kWave);
+        cum += __builtin_amdgcn_readlane(incl, kWave - 1);
     }
-    e = __builtin_amdgcn_readfirstlane(e);
-    cum = __builtin_amdgcn_readfirstlane(cum);
-    int rows = pag_rows(p, e), units = pag_units(rows);
+    int rows = __builtin_amdgcn_readlane(my_rows, e - e0), len = __builtin_amdgcn_readlane(my_len, e - e0), units = paged_units(rows, unit);
     int b, h;
     if (per_head) {
         b = e / cv.H;
@@ -177,113 +315,151 @@ __global__ __launch_bounds__(kPagThreads) void paged_decode_kernel(PagDecParams 
     }
     int a = per_head ? cum : cum + h * units;       // unit at which the head starts
 
-    while (true) {
-        const int64_t bh = (int64_t)b * cv.H + h;
-        const int end = min(a + units, stop);
-        const int r0 = (pos - a) * kUnit, r1 = min((end - a) * kUnit, rows);
-        const int32_t *table = paged_table(cv, b, h);
-        const int32_t *sel = p.sel ? p.sel + bh * p.keep : nullptr;
-        const int len = min(max(p.lens[p.lens_per_head ? bh : b], 0), cv.P << cv.log2_R);
-
-        // ---- queries: lane (g, c) holds of head c what meets its pieces of a key; heads beyond the group are zero
-        uint4 q[QP][KL];
-        {
-            const int64_t q0 = (((int64_t)b * cv.H + h) * G + c) * D;
+    // ---- a stretch within one head, and the wavefront's steps in it
+    struct Stretch {
+        int b, h, a, units, end;           // units [a, a + units) are the head's, the stretch goes to `end`
+        int len, first, steps;             // rows of the sequence; the wavefront's first row, its steps (every kStep rows)
+        const int32_t *table, *sel;
+    };
+    auto stretch_at = [&](int pos) {
+        Stretch t;
+        t.b = b;
+        t.h = h;
+        t.a = a;
+        t.units = units;
+        t.end = min(a + units, stop);
+        t.len = len;
+        t.first = (pos - a) * unit + 16 * wave;
+        const int r1 = min((t.end - a) * unit, rows);
+        t.steps = t.first < r1 ? (r1 - t.first + kStep - 1) / kStep : 0;
+        t.table = paged_table(cv, b, h);
+        t.sel = p.sel ? p.sel + ((int64_t)b * cv.H + h) * p.keep : nullptr;
+        return t;
+    };
+    // Lane i knows the page of step s0 + i, how many of the step's rows are there, and whether anything is wrong with it
+    struct Pages { int page, left, bad; };
+    auto look_up = [&](const Stretch &t, int s0) {
+        Pages x = {0, 0, 0};
+        if (s0 + lane < t.steps) {
+            const PagedStep y = paged_step(t.first + (s0 + lane) * kStep, cv.log2_R, t.len, cv.P, cv.num_pages, t.table, t.sel != nullptr, t.sel);
+            x = {y.page, y.left, y.bad};
+        }
+        return x;
+    };
+    // Queries: lane (g, c) holds of head c what meets its pieces of a key; heads beyond the group are zero
+    uint4 q[QP][KL];
+    auto load_queries = [&](const Stretch &t) {
+        const int64_t q0 = (((int64_t)t.b * cv.H + t.h) * G + c) * D;
 #pragma unroll
-            for (int ks = 0; ks < KL; ++ks) {
+        for (int ks = 0; ks < KL; ++ks) {
 #pragma unroll
-                for (int k = 0; k < QP; ++k) q[k][ks] = make_uint4(0u, 0u, 0u, 0u);
-                if (c < G) {
-                    if constexpr (kBf16 && QP == 1) {
-                        q[0][ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const bf16_t *>(p.Q) + q0 + 32 * ks + 8 * g);
-                    } else if constexpr (kBf16) {
-                        float x[8];
-                        load8(reinterpret_cast<const float *>(p.Q) + q0 + 32 * ks + 8 * g, x);
-                        uint32_t w[4][QP];
+            for (int k = 0; k < QP; ++k) q[k][ks] = make_uint4(0u, 0u, 0u, 0u);
+            if (c < G) {
+                if constexpr (kBf16 && QP == 1) {
+                    q[0][ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const bf16_t *>(p.Q) + q0 + 32 * ks + 8 * g);
+                } else if constexpr (kBf16) {
+                    float y[8];
+                    load8(reinterpret_cast<const float *>(p.Q) + q0 + 32 * ks + 8 * g, y);
+                    uint32_t w[4][QP];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) split_bf16<QP>(x[2 * i], x[2 * i + 1], w[i]);
+                    for (int i = 0; i < 4; ++i) split_bf16<QP>(y[2 * i], y[2 * i + 1], w[i]);
 #pragma unroll
-                        for (int k = 0; k < QP; ++k) q[k][ks] = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
-                    } else if (p.q_is_bf16) {
-                        const uint2 t = *reinterpret_cast<const uint2 *>(reinterpret_cast<const bf16_t *>(p.Q) + q0 + 16 * ks + 4 * g);
-                        q[0][ks] = make_uint4(t.x << 16, t.x & 0xffff0000u, t.y << 16, t.y & 0xffff0000u);
-                    } else {
-                        q[0][ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const float *>(p.Q) + q0 + 16 * ks + 4 * g);
-                    }
+                    for (int k = 0; k < QP; ++k) q[k][ks] = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
+                } else if (p.q_is_bf16) {
+                    const uint2 y = *reinterpret_cast<const uint2 *>(reinterpret_cast<const bf16_t *>(p.Q) + q0 + 16 * ks + 4 * g);
+                    q[0][ks] = make_uint4(y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u);
+                } else {
+                    q[0][ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const float *>(p.Q) + q0 + 16 * ks + 4 * g);
                 }
             }
+        }
+    };
+    // AHEAD steps are on their way: the registers of a step's keys are requested anew as soon as the first product has used them, those of its values
+    // behind the second.
+    Rows<T, D> x[AHEAD];
+    struct Where { int64_t off; int left; } where[AHEAD];
+    auto request_keys = [&](const Stretch &t, Pages &pages, int s, auto which) {
+        constexpr int W = decltype(which)::value;
+        if (s % kWave == 0 && s != 0) {
+            const Pages y = look_up(t, s);
+            pages = {y.page, y.left, pages.bad | y.bad};
+        }
+        const int page = __builtin_amdgcn_readlane(pages.page, s % kWave), in_page = (t.first + s * kStep) & (cv.R - 1);
+        where[W] = {paged_offset(cv, page, t.h) + (int64_t)in_page * cv.row_bytes, __builtin_amdgcn_readlane(pages.left, s % kWave)};
+        load_keys<T, D>(x[W], cv.K + where[W].off, cv.row_bytes, g, c);
+        if (cv.counts) {
+            const int4 n = *reinterpret_cast<const int4 *>(cv.counts + paged_index(cv, page, t.h) * cv.R + in_page + 4 * g);
+            x[W].n[0] = n.x; x[W].n[1] = n.y; x[W].n[2] = n.z; x[W].n[3] = n.w;
+        }
+    };
+    auto request_values = [&](auto which) {
+        constexpr int W = decltype(which)::value;
+        load_values<T, D>(x[W], cv.V + where[W].off, cv.row_bytes, g, c);
+    };
+    constexpr std::integral_constant<int, 0> kEven{};
+    constexpr std::integral_constant<int, AHEAD - 1> kOdd{};
+    auto request_first = [&](const Stretch &t, Pages &pages) {
+        load_queries(t);
+        if (t.steps > 0) { request_keys(t, pages, 0, kEven); request_values(kEven); }
+        if (AHEAD > 1 && t.steps > 1) { request_keys(t, pages, 1, kOdd); request_values(kOdd); }
+    };
+
+    Stretch cur = stretch_at(pos);
+    Pages pages = look_up(cur, 0);
+    request_first(cur, pages);
+    while (true) {
+        const int64_t bh = (int64_t)cur.b * cv.H + cur.h;
+        // ---- the next head of the workgroup's stretch, if any: its pages are known by the time this one is done
+        const bool more = cur.end < stop;
+        Stretch nxt = cur;
+        Pages nxt_pages = {0, 0, 0};
+        if (more) {
+            a += units;
+            ++h;
+            if (h == cv.H) { h = 0; ++b; }
+            if (per_head || h == 0) {
+                ++e;
+                if (e - e0 == kWave) {
+                    e0 = e;
+                    entry(e0 + lane);
+                }
+                rows = __builtin_amdgcn_readlane(my_rows, e - e0);
+                len = __builtin_amdgcn_readlane(my_len, e - e0);
+                units = paged_units(rows, unit);
+            }
+            nxt = stretch_at(cur.end);
+            nxt_pages = look_up(nxt, 0);
         }
 
         pag_f32x4 acc[NA];
 #pragma unroll
         for (int i = 0; i < NA; ++i) acc[i] = pag_f32x4{0.f, 0.f, 0.f, 0.f};
         float m_run = -INFINITY, l_run = 0.f;
-        bool bad = false;
-
-        // ---- pages: lane i knows the page of the wavefront's step s0 + i and how many of the step's rows are there
-        const int first = r0 + 16 * wave;
-        const int steps = first < r1 ? (r1 - first + kUnit - 1) / kUnit : 0;
-        int my_page = 0, my_left = 0;
-        auto look_up = [&](int s0) {
-            my_page = my_left = 0;
-            if (s0 + lane < steps) {
-                const PagedStep t = paged_step(first + (s0 + lane) * kUnit, cv.log2_R, len, cv.P, cv.num_pages, table, sel != nullptr, sel);
-                my_page = t.page;
-                my_left = t.left;
-                bad |= t.bad;
-            }
-        };
-        Rows<T, D> x;
-        int left = 0, in_page = 0;
-        int64_t off = 0, idx = 0;
-        auto step_at = [&](int s) {
-            if (s % kWave == 0) look_up(s);
-            const int page = __builtin_amdgcn_readlane(my_page, s % kWave);
-            left = __builtin_amdgcn_readlane(my_left, s % kWave);
-            in_page = (first + s * kUnit) & (cv.R - 1);
-            off = paged_offset(cv, page, h) + (int64_t)in_page * cv.row_bytes;
-            idx = paged_index(cv, page, h) * cv.R + in_page;
-        };
-        auto load_sizes = [&]() {
-            if (cv.counts) {
-                const int4 t = *reinterpret_cast<const int4 *>(cv.counts + idx + 4 * g);
-                x.n[0] = t.x; x.n[1] = t.y; x.n[2] = t.z; x.n[3] = t.w;
-            }
-        };
-        if (steps > 0) {
-            step_at(0);
-            load_keys<T, D>(x, cv.K + off, cv.row_bytes, g, c);
-            load_sizes();
-            load_values<T, D>(x, cv.V + off, cv.row_bytes, g, c);
-        }
-        for (int s = 0; s < steps; ++s) {
-            const int here = left;
+        auto step = [&](int s, auto which) {
+            constexpr int W = decltype(which)::value;
+            Rows<T, D> &r = x[W];
+            const int here = where[W].left;
             pag_f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KL; ++ks) {
                 if constexpr (kBf16) {
 #pragma unroll
                     for (int k = QP - 1; k >= 0; --k)      // the smallest part first
-                        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, x.k[ks]), __builtin_bit_cast(pag_bf16x8, q[k][ks]), sc, 0, 0, 0);
+                        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, r.k[ks]), __builtin_bit_cast(pag_bf16x8, q[k][ks]), sc, 0, 0, 0);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(dword_of(x.k[ks], i)), __uint_as_float(dword_of(q[0][ks], i)), sc, 0, 0, 0);
+                        sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(dword_of(r.k[ks], i)), __uint_as_float(dword_of(q[0][ks], i)), sc, 0, 0, 0);
                 }
             }
             float sv[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 sv[i] = sc[i] * p.scale_log2;
-                if (cv.counts) sv[i] = x.n[i] > 0 ? sv[i] + __log2f((float)x.n[i]) : -INFINITY;
+                if (cv.counts) sv[i] = r.n[i] > 0 ? sv[i] + __log2f((float)r.n[i]) : -INFINITY;
                 if (4 * g + i >= here) sv[i] = -INFINITY;
             }
-            const bool more = s + 1 < steps;
-            if (more) {
-                step_at(s + 1);
-                load_keys<T, D>(x, cv.K + off, cv.row_bytes, g, c);
-                load_sizes();
-            }
+            if (s + AHEAD < cur.steps) request_keys(cur, pages, s + AHEAD, which);
             float m_loc = m_run;
 #pragma unroll
             for (int i = 0; i < 4; ++i) m_loc = fmaxf(m_loc, sv[i]);
@@ -308,7 +484,7 @@ __global__ __launch_bounds__(kPagThreads) void paged_decode_kernel(PagDecParams 
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int w = 0; w < VW; ++w) x.v[i][w] = 4 * g + i < here ? x.v[i][w] : 0u;
+                    for (int w = 0; w < VW; ++w) r.v[i][w] = 4 * g + i < here ? r.v[i][w] : 0u;
             }
             if constexpr (kBf16) {
                 uint32_t p01[PP], p23[PP];
@@ -316,8 +492,8 @@ __global__ __launch_bounds__(kPagThreads) void paged_decode_kernel(PagDecParams 
                 split_bf16<PP>(pi[2], pi[3], p23);
 #pragma unroll
                 for (int k = 0; k < NA; ++k) {
-                    const uint32_t lo = (k & 1) ? pack_hi(x.v[0][k / 2], x.v[1][k / 2]) : pack_lo(x.v[0][k / 2], x.v[1][k / 2]);
-                    const uint32_t hi = (k & 1) ? pack_hi(x.v[2][k / 2], x.v[3][k / 2]) : pack_lo(x.v[2][k / 2], x.v[3][k / 2]);
+                    const uint32_t lo = (k & 1) ? pack_hi(r.v[0][k / 2], r.v[1][k / 2]) : pack_lo(r.v[0][k / 2], r.v[1][k / 2]);
+                    const uint32_t hi = (k & 1) ? pack_hi(r.v[2][k / 2], r.v[3][k / 2]) : pack_lo(r.v[2][k / 2], r.v[3][k / 2]);
                     const pag_short4 bb = __builtin_bit_cast(pag_short4, make_uint2(lo, hi));
 #pragma unroll
                     for (int t = PP - 1; t >= 0; --t)
@@ -327,14 +503,20 @@ __global__ __launch_bounds__(kPagThreads) void paged_decode_kernel(PagDecParams 
 #pragma unroll
                 for (int k = 0; k < NA; ++k)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(pi[i], __uint_as_float(x.v[i][k]), acc[k], 0, 0, 0);
+                    for (int i = 0; i < 4; ++i) acc[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(pi[i], __uint_as_float(r.v[i][k]), acc[k], 0, 0, 0);
             }
-            if (more) load_values<T, D>(x, cv.V + off, cv.row_bytes, g, c);
+            if (s + AHEAD < cur.steps) request_values(which);
+        };
+        for (int s = 0; s < cur.steps; s += AHEAD) {
+            step(s, kEven);
+            if (AHEAD > 1 && s + 1 < cur.steps) step(s + 1, kOdd);
         }
+        const bool bad = ballot64(pages.bad != 0) != 0ull;
+        if (more) request_first(nxt, nxt_pages);
 
         // ---- join the wavefronts
         float lw = rows_allreduce_sum(l_run);
-        if (ballot64(bad) != 0ull) lw = __builtin_nanf("");
+        if (bad) lw = __builtin_nanf("");
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int hh = 4 * g + i;
@@ -345,88 +527,61 @@ __global__ __launch_bounds__(kPagThreads) void paged_decode_kernel(PagDecParams 
         }
         if (g == 0) { s_m[wave][c] = m_run; s_l[wave][c] = lw; }
         __syncthreads();
-        const bool whole = pos == a && end == a + units;      // nobody else has a part of the head
-        const int w0 = paged_first_wg(a, per), w1 = paged_last_wg(a, units, per);
-        float *mine = p.part + (int64_t)paged_place(wg, a, per) * G * kStride;
-        for (int i = tid; i < G * D; i += kPagThreads) {
-            const int hh = i / D, el = i - hh * D;
+        const int w0 = paged_first_wg(cur.a, per), w1 = paged_last_wg(cur.a, cur.units, per);
+        const bool whole = w0 == w1;      // nobody else has a part of the head
+        const int at = paged_place(wg, cur.a, per) * G * kStride;
+        for (int i = tid; i < G * (D / 4); i += kPagThreads) {
+            const int hh = i / (D / 4), el = 4 * (i - hh * (D / 4));
             float m = -INFINITY;
 #pragma unroll
             for (int w = 0; w < kPagWaves; ++w) m = fmaxf(m, s_m[w][hh]);
             const float m_safe = (m == -INFINITY) ? 0.f : m;
-            float o = 0.f, l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            float l = 0.f;
 #pragma unroll
             for (int w = 0; w < kPagWaves; ++w) {
                 const float f = pag_exp2(s_m[w][hh] - m_safe);
-                o = fmaf(s_acc[(w * G + hh) * D + el], f, o);
+                const float4 t = *reinterpret_cast<const float4 *>(s_acc + (w * G + hh) * D + el);
+                o.x = fmaf(t.x, f, o.x);
+                o.y = fmaf(t.y, f, o.y);
+                o.z = fmaf(t.z, f, o.z);
+                o.w = fmaf(t.w, f, o.w);
                 l = fmaf(s_l[w][hh], f, l);
             }
-            if (whole) {
-                const int64_t row = bh * G + hh;
-                const float out = o * (l != 0.f ? 1.0f / l : 0.f);
-                if (p.o_is_bf16) reinterpret_cast<uint16_t *>(p.O)[row * D + el] = (uint16_t)pack_bf16x2(out, out);
-                else reinterpret_cast<float *>(p.O)[row * D + el] = out;
-                if (el == 0 && p.lse) p.lse[row] = l != 0.f ? (m + __log2f(l)) * kPagLn2 : -INFINITY;
-            } else {
-                float *dst = mine + hh * kStride;
-                __hip_atomic_store(dst + el, o, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                if (el == 0) {
-                    __hip_atomic_store(dst + D, m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    __hip_atomic_store(dst + D + 1, l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                }
-            }
+            if (whole) store_result(p, bh * G + hh, D, el, o, m, l);
+            else store_part<D>(rs, at + hh * kStride, el, o, m, l);
         }
         if (!whole) {
-            // every wavefront's partial results are acknowledged by memory before the workgroup counts itself off
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            if (tid == 0) {
-                const int before = __hip_atomic_fetch_add(p.counter + bh, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                s_last = before == w1 - w0;
-            }
-            __syncthreads();
-            if (s_last) {
-                if (tid == 0) __hip_atomic_store(p.counter + bh, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                for (int i = tid; i < G * D; i += kPagThreads) {
-                    const int hh = i / D, el = i - hh * D;
-                    float m = -INFINITY, o = 0.f, l = 0.f;
-                    for (int w = w0; w <= w1; ++w) {
-                        const float *src = p.part + ((int64_t)paged_place(w, a, per) * G + hh) * kStride;
-                        const float ow = __hip_atomic_load(src + el, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        const float mw = __hip_atomic_load(src + D, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        const float lw2 = __hip_atomic_load(src + D + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        const float m2 = fmaxf(m, mw);
-                        const float safe = (m2 == -INFINITY) ? 0.f : m2;
-                        const float f0 = pag_exp2(m - safe), f1 = pag_exp2(mw - safe);
-                        o = fmaf(ow, f1, o * f0);
-                        l = fmaf(lw2, f1, l * f0);
-                        m = m2;
-                    }
-                    const int64_t row = bh * G + hh;
-                    const float out = o * (l != 0.f ? 1.0f / l : 0.f);
-                    if (p.o_is_bf16) reinterpret_cast<uint16_t *>(p.O)[row * D + el] = (uint16_t)pack_bf16x2(out, out);
-                    else reinterpret_cast<float *>(p.O)[row * D + el] = out;
-                    if (el == 0 && p.lse) p.lse[row] = l != 0.f ? (m + __log2f(l)) * kPagLn2 : -INFINITY;
-                }
+            // ---- the last of the head's workgroups joins their results; of many, the last of every group first
+            const int n = w1 - w0 + 1, group = paged_group(n, G);
+            const int k0 = (wg - w0) / group * group, in_group = min(group, n - k0), groups = (n + group - 1) / group;
+            auto place_of = [&](int w) { return paged_place(w, cur.a, per); };
+            int *counter = p.counter + place_of(w0 + k0);
+            int parts = in_group, from = w0 + k0, by = 1;
+            bool result = groups == 1;
+            while (last_of(counter, parts, tid, &s_last)) {
+                const int to = place_of(from) * G * kStride;
+                join_parts<D>(p, rs, parts, [&](int k) { return place_of(from + k * by); }, tid, s_acc, s_total, [&](int hh, int el, const float4 &o, float m, float l) {
+                    if (result) store_result(p, bh * G + hh, D, el, o, m, l);
+                    else store_part<D>(rs, to + hh * kStride, el, o, m, l);
+                });
+                if (result) break;
+                counter = p.counter + 2 * kMaxWgs + place_of(w0);
+                parts = groups;
+                from = w0;
+                by = group;
+                result = true;
             }
         }
-        // ---- the next head of the stretch
-        pos = end;
-        if (pos >= stop) return;
+        if (!more) return;
         __syncthreads();      // the wavefronts' sums have been read
-        a += units;
-        ++h;
-        if (h == cv.H) { h = 0; ++b; }
-        if (per_head || h == 0) {
-            ++e;
-            rows = pag_rows(p, e);
-            units = pag_units(rows);
-        }
+        cur = nxt;
+        pages = nxt_pages;
     }
 }
 
 // ------------------------------------------------------------------------------------------------
-size_t paged_state_bytes(int B, int H) { return align_up((size_t)B * H * sizeof(int), 256); }
+size_t paged_state_bytes() { return align_up((size_t)4 * kMaxWgs * sizeof(int), 256); }
 size_t paged_decode_bytes(int G, int d) { return align_up((size_t)2 * kMaxWgs * G * (d + kPagPad) * sizeof(float), 256); }
 
 template <typename T, int D, int QP> static hipError_t launch_k(const PagDecParams &p, hipStream_t stream) {
@@ -446,10 +601,10 @@ hipError_t launch_paged_decode(const PagedDecodeArgs &a, hipStream_t stream) {
     p.scale_log2 = a.scale * kPagLog2e;
     p.O = a.O; p.o_is_bf16 = a.o_dtype == DType::BF16; p.lse = a.lse;
     p.counter = reinterpret_cast<int *>(a.ws);
-    p.part = reinterpret_cast<float *>(reinterpret_cast<char *>(a.ws) + paged_state_bytes(a.c.B, a.c.H));
+    p.part = reinterpret_cast<float *>(reinterpret_cast<char *>(a.ws) + paged_state_bytes());
     // never more workgroups than the tables (the selections) have units for, nor than a head's partial results are worth
     const int64_t heads = (int64_t)a.c.B * a.c.H;
-    const int64_t most = ((int64_t)(a.sel ? a.keep : a.c.P) * a.c.R + kUnit - 1) / kUnit * heads;
+    const int64_t most = ((int64_t)(a.sel ? a.keep : a.c.P) * a.c.R + kStep - 1) / kStep * heads;
     int64_t wgs = kMaxWgs < heads * kMaxHeadWgs ? kMaxWgs : heads * kMaxHeadWgs;
     if (wgs > most) wgs = most;
     p.wgs = (int)wgs;

@@ -199,7 +199,7 @@ hipError_t launch_paged_select(const PagedSelectArgs &a, hipStream_t stream) {
     p.lens = a.lens; p.lens_per_head = a.lens_per_head;
     p.keep = a.keep; p.first = a.first; p.recent = a.recent;
     p.sel = a.sel; p.sel_lens = a.sel_lens;
-    p.keys = reinterpret_cast<unsigned long long *>(reinterpret_cast<char *>(a.ws) + paged_state_bytes(a.c.B, a.c.H));
+    p.keys = reinterpret_cast<unsigned long long *>(reinterpret_cast<char *>(a.ws) + paged_state_bytes());
     p.tiles = (a.c.P + kScorePages - 1) / kScorePages;
     const bool qb = a.q_dtype == DType::BF16;
     if (a.c.dtype == DType::BF16) {

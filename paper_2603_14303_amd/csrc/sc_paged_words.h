@@ -29,6 +29,9 @@ constexpr int paged_first_wg(int a, int per) { return a / per; }
 constexpr int paged_last_wg(int a, int units, int per) { return (a + units - 1) / per; }
 constexpr int paged_place(int w, int a, int per) { return 2 * w + (a > w * per ? 1 : 0); }
 
+// n partial results of G heads are joined at once, or in groups of this many first
+constexpr int paged_group(int n, int G) { return n * G <= 256 || n <= 16 ? n : 16; }
+
 // 16 rows of a head from row `row` (a multiple of 16) on, or from the same row of its selected pages: their page, and how many of them attend
 struct PagedStep {
     int page, left;

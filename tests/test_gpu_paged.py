@@ -201,7 +201,7 @@ def test_decode_work_is_split_and_joined(B, H, lens):
     O, lse = check_decode(pc, [[n] * H for n in lens], 4, BF, per_head=False, workspace=ws)
     Q = (1.5 * torch.randn((B, H * 4, 128), generator=torch.Generator().manual_seed(1))).to(BF).to(DEV)
     dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
-    state = ws.buf[: 4 * B * H].view(torch.int32)
+    state = ws.buf[: sc.load_library().sc_paged_workspace_bytes(1, 1, 1, 64, 1) - 2 * 256 * 68 * 4].view(torch.int32)      # the counters
     for _ in range(4):
         O2, lse2 = sc.sc_paged_decode_attn(pc.cache(), Q, dl, want_lse=True, workspace=ws)
         assert torch.equal(O, O2) and torch.equal(lse, lse2) and not state.any()

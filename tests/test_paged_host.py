@@ -121,8 +121,8 @@ def test_workspace(lib):
     f = lib.sc_paged_workspace_bytes
     assert f(0, 8, 4, 128, 20) == 0 and f(2, 9, 4, 128, 20) == 0 and f(2, 8, 4, 96, 20) == 0 and f(2, 8, 4, 128, 0) == 0
     assert f(2, 8, 4, 128, 20) % 256 == 0 and f(64, 64, 8, 128, 1 << 16) >= 64 * 8 * (1 << 16) * 8
-    assert lib.sc_paged_init_workspace(None, 4096, 2, 4, None) == WORKSPACE and lib.sc_paged_init_workspace(FAKE, 16, 2, 4, None) == WORKSPACE
-    assert lib.sc_paged_init_workspace(FAKE, 4096, 0, 4, None) == ARG
+    assert lib.sc_paged_init_workspace(None, 1 << 20, None) == WORKSPACE and lib.sc_paged_init_workspace(FAKE, 16, None) == WORKSPACE
+    assert lib.sc_paged_init_workspace(FAKE + 8, 1 << 20, None) == WORKSPACE
 
 
 WORDS = r"""
@@ -210,6 +210,12 @@ int main() {
             if (w1 > w0) for (int w = w0; w <= w1; ++w) CHECK(places[paged_place(w, a, per)] == h);
         }
     }
+    // ---- groups of partial results: of one size, few enough to be joined in the shared memory of a workgroup
+    for (int n = 1; n <= 512; ++n)
+        for (int G = 1; G <= 16; ++G) {
+            const int group = paged_group(n, G), groups = (n + group - 1) / group;
+            CHECK(group >= 1 && group <= n && group * G <= 256 && groups <= 32 && (groups == 1 || group == 16));
+        }
     CHECK(paged_units(2147483647, 96) == 22369622 && paged_units(0, 96) == 1 && paged_units(-5, 96) == 1);
     // ---- a step's page: in the pool whatever the arrays hold, its rows those that the length leaves
     for (int t = 0; t < 300000; ++t) {
