@@ -50,9 +50,9 @@ struct PagedAppendArgs {
     int64_t q_b, q_h, q_n, o_b, o_h, o_n;   // bytes
     DType q_dtype;
 };
-// whether the call fits a grid: a workgroup per page and KV head, and per 32 tokens and query head at worst
+// whether the call fits a grid: a workgroup per page and KV head, and per 16 tokens and query head at worst
 inline bool paged_append_fits(int64_t B, int64_t H, int64_t R, int64_t N, int64_t Hq) {
-    return B * H * ((N + R - 2) / R + 1) + B * ((N + 31) / 32) * Hq <= INT32_MAX;
+    return B * H * ((N + R - 2) / R + 1) + B * ((N + 15) / 16) * Hq <= INT32_MAX;
 }
 hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t stream);
 

@@ -3,122 +3,195 @@
 //
 //     a' = a cos - b sin,  b' = b cos + a sin   for the pairs (a, b) of the first `rot` elements of a row, in fp32, rounded once.
 //
-// Bound by bytes: every row is read once and written once, and there are two operations a byte.  A workgroup takes one page of one KV head: all
-// the rows that the call adds to that page, and, where summaries are kept, the keys that the page held before, so that no workgroup depends on
-// another.  A lane holds two 16-byte (bf16) pieces of a row, chosen so that the partners of a rotation are in the same lane; 8 lanes make a row of
-// 128 elements.  The queries are rotated by workgroups of their own, which go over the heads of a group of tokens and read the angles once.
+// Bound by bytes: every row is read once and written once, and there are two operations a byte.  One to four wavefronts take one page of one KV head:
+// all the rows that the call adds to that page, and, where summaries are kept, the keys that the page held before, so that no workgroup depends on
+// another.  A lane holds two pieces of 16 bytes of a row, chosen so that the partners of a rotation are in the same lane.  The queries are rotated by workgroups of their own, which go over the heads of a group of tokens and read the angles once.
 #include "sc_paged.h"
 
 namespace sc {
 
 constexpr int kAppThreads = 256;
 
-// Two pieces of 8 elements of a row, and the angles that turn them.
+// A lane's two pieces of 16 bytes of a row (of E elements each), chosen so that the partners of a rotation are in the same lane
+template <typename T> struct Shape {
+    static constexpr int E = 16 / (int)sizeof(T);
+};
 struct Pieces {
     int ea, eb;       // first elements
     bool turned;
 };
-template <int D> __device__ __forceinline__ Pieces pieces_of(int j, int rot, bool interleaved) {
-    const bool turned = 16 * j < rot;
+template <int E> __device__ __forceinline__ Pieces pieces_of(int j, int rot, bool interleaved) {
+    const bool turned = 2 * E * j < rot;
     const bool halves = turned && !interleaved;      // partners i and i + rot / 2; else neighbours, or elements that stay
-    return {halves ? 8 * j : 16 * j, halves ? 8 * j + rot / 2 : 16 * j + 8, turned};
+    return {halves ? E * j : 2 * E * j, halves ? E * j + rot / 2 : 2 * E * j + E, turned};
 }
-__device__ __forceinline__ void turn(float (&x)[8], float (&y)[8], const float (&c)[8], const float (&s)[8], bool interleaved) {
+// the angles of both are the E from E j on
+template <int E> __device__ __forceinline__ void turn(float (&x)[E], float (&y)[E], const float (&c)[E], const float (&s)[E], bool interleaved) {
     if (interleaved) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < E / 2; ++i) {
             const float a = x[2 * i], b = x[2 * i + 1], e = y[2 * i], f = y[2 * i + 1];
             x[2 * i] = a * c[i] - b * s[i];
             x[2 * i + 1] = b * c[i] + a * s[i];
-            y[2 * i] = e * c[4 + i] - f * s[4 + i];
-            y[2 * i + 1] = f * c[4 + i] + e * s[4 + i];
+            y[2 * i] = e * c[E / 2 + i] - f * s[E / 2 + i];
+            y[2 * i + 1] = f * c[E / 2 + i] + e * s[E / 2 + i];
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < E; ++i) {
             const float a = x[i], b = y[i];
             x[i] = a * c[i] - b * s[i];
             y[i] = b * c[i] + a * s[i];
         }
     }
 }
-// a NaN stays
-__device__ __forceinline__ float lower(float a, float b) { return (b < a || b != b) ? b : a; }
-__device__ __forceinline__ float higher(float a, float b) { return (b > a || b != b) ? b : a; }
-
-template <typename T> __device__ __forceinline__ void rounded(float (&x)[8]) {
-    if constexpr (sizeof(T) == 2) {
+template <int E> __device__ __forceinline__ void load_angles(const float *p, float (&x)[E]) {
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const uint32_t u = pack_bf16x2(x[i], x[i + 1]);
-            x[i] = bf16_lo(u);
-            x[i + 1] = bf16_hi(u);
+    for (int i = 0; i < E; i += 4) {
+        const float4 t = *reinterpret_cast<const float4 *>(p + i);
+        x[i] = t.x; x[i + 1] = t.y; x[i + 2] = t.z; x[i + 3] = t.w;
+    }
+}
+// a NaN stays
+__device__ __forceinline__ float lower(float a, float b) { return __builtin_elementwise_minimum(a, b); }
+__device__ __forceinline__ float higher(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+template <bool LOW> __device__ __forceinline__ float extreme(float a, float b) { return LOW ? lower(a, b) : higher(a, b); }
+
+// 16 bytes as they lie in memory
+typedef unsigned int raw_u32x4 __attribute__((ext_vector_type(4)));      // (HIP's own uint4 would be copied through memory)
+template <typename T> struct Raw {
+    static constexpr int E = Shape<T>::E;
+    raw_u32x4 w;
+    __device__ __forceinline__ void load(const char *p) { w = *reinterpret_cast<const raw_u32x4 *>(p); }
+    __device__ __forceinline__ void store(char *p) const { *reinterpret_cast<raw_u32x4 *>(p) = w; }
+    __device__ __forceinline__ void widen(float (&x)[E]) const {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            if constexpr (sizeof(T) == 2) x[i] = (i & 1) ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+            else x[i] = __uint_as_float(w[i]);
         }
+    }
+    __device__ __forceinline__ void round(const float (&x)[E]) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            if constexpr (sizeof(T) == 2) w[i / 2] = pack_bf16x2(x[i & ~1], x[i | 1]);
+            else w[i] = __float_as_uint(x[i]);
+        }
+    }
+};
+
+// The extremes over the lanes with the same pieces (lane % LPR).  Two values that are exchanged between the halves of the wavefront, and between its
+// rows of 16 lanes, are reduced together, each in one half: lane (row r of 16 lanes, any place in it) ends up with values N / 4 r .. of the N.
+template <int LPR, bool LOW, int N> __device__ __forceinline__ void gather_extremes(const float (&x)[N], float (&z)[N / 4]) {
+    float y[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[i]), __float_as_uint(x[i + N / 2]), false, false);
+        y[i] = extreme<LOW>(__uint_as_float(t[0]), __uint_as_float(t[1]));
+    }
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(y[i]), __float_as_uint(y[i + N / 4]), false, false);
+        z[i] = extreme<LOW>(__uint_as_float(t[0]), __uint_as_float(t[1]));
+        if constexpr (LPR <= 8) z[i] = extreme<LOW>(z[i], dpp<kDppRor8>(z[i]));
+        if constexpr (LPR <= 4) z[i] = extreme<LOW>(z[i], dpp<kDppRor4>(z[i]));
     }
 }
 
+// A number that the whole wavefront reads, and that nobody writes meanwhile: through the scalar cache
+__device__ __forceinline__ int read_scalar(const int32_t *p) { return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p; }
+
 struct AppendGrid {
-    int slots;            // pages that a sequence can touch
-    int kv_blocks;
-    int q_tiles, q_groups, q_heads;      // of tokens, of heads, heads of a group
+    int kv_blocks, page_groups;             // workgroups of the keys and values; of a sequence and head
+    int log2_waves;                         // wavefronts of a page
+    int log2_tokens, q_tiles;               // tokens that a workgroup of the queries holds at a time; tiles of so many
+    int q_heads, q_groups;                  // heads that it goes over; groups of so many
 };
 
-template <typename T, typename TQ, int D>
+// ROT: with angles (without any, there are no queries either)
+template <typename T, typename TQ, int D, bool ROT>
 __global__ __launch_bounds__(kAppThreads) void paged_append_kernel(PagedAppendArgs p, AppendGrid g) {
-    constexpr int LPR = D / 16;
-    constexpr int RPP = kAppThreads / LPR;      // rows of a pass
+    constexpr int WAVES = kAppThreads / kWave;
+    constexpr int U = 2;                        // passes whose loads are on their way together
     const int tid = threadIdx.x;
-    const int j = tid % LPR, r = tid / LPR;
     const PagedView &c = p.c;
-    const Pieces at = pieces_of<D>(j, p.rot, p.interleaved != 0);
     const int half = p.rot / 2;
+    const bool interleaved = p.interleaved != 0;
 
-    if ((int)blockIdx.x >= g.kv_blocks) {
-        // ---- queries: a tile of tokens, the heads of a group
+    if (ROT && (int)blockIdx.x >= g.kv_blocks) {
+        // ---- queries: a tile of tokens, several heads at a time (of few tokens, all heads that there is room for)
+        constexpr int E = Shape<TQ>::E, LPR = D / (2 * E), RPW = kWave / LPR;
+        const int j = tid % LPR;
+        const Pieces at = pieces_of<E>(j, p.rot, interleaved);
         int id = (int)blockIdx.x - g.kv_blocks;
         const int group = id % g.q_groups;
         id /= g.q_groups;
         const int tile = id % g.q_tiles, b = id / g.q_tiles;
-        const int n = tile * RPP + r;
+        const int r = tid / LPR;
+        const int n = (tile << g.log2_tokens) + (r & ((1 << g.log2_tokens) - 1));
         if (n >= p.N) return;
-        const int64_t pos = (int64_t)(p.positions ? p.positions[b] : p.base_lens[b]) + n;
+        const int64_t pos = (int64_t)read_scalar((p.positions ? p.positions : p.base_lens) + b) + n;
         const bool known = pos >= 0 && pos < p.max_position;
-        float co[8], si[8];
+        float co[E], si[E];
         if (at.turned && known) {
-            load8(p.cos_sin + pos * p.rot + 8 * j, co);
-            load8(p.cos_sin + pos * p.rot + half + 8 * j, si);
+            load_angles(p.cos_sin + pos * p.rot + E * j, co);
+            load_angles(p.cos_sin + pos * p.rot + half + E * j, si);
         }
+        const int step = (WAVES * RPW) >> g.log2_tokens;
         const int h1 = min((group + 1) * g.q_heads, p.Hq);
-        for (int h = group * g.q_heads; h < h1; ++h) {
-            const TQ *src = reinterpret_cast<const TQ *>(p.Q + b * p.q_b + h * p.q_h + n * p.q_n);
-            TQ *dst = reinterpret_cast<TQ *>(p.Q_out + b * p.o_b + h * p.o_h + n * p.o_n);
-            float x[8], y[8];
-            load8(src + at.ea, x);
-            load8(src + at.eb, y);
-            if (!known) {
+        const char *src = p.Q + b * p.q_b + n * p.q_n;
+        char *dst = p.Q_out + b * p.o_b + n * p.o_n;
+        for (int h = group * g.q_heads + (r >> g.log2_tokens); h < h1; h += U * step) {
+            Raw<TQ> a[U], e[U];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = y[i] = __builtin_nanf("");
-            } else if (at.turned) {
-                turn(x, y, co, si, p.interleaved != 0);
-            }
-            store8(dst + at.ea, x);
-            store8(dst + at.eb, y);
+            for (int u = 0; u < U; ++u)
+                if (h + u * step < h1) {
+                    a[u].load(src + (h + u * step) * p.q_h + at.ea * (int)sizeof(TQ));
+                    e[u].load(src + (h + u * step) * p.q_h + at.eb * (int)sizeof(TQ));
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (h + u * step < h1) {
+                    if (!known || at.turned) {
+                        float x[E], y[E];
+                        a[u].widen(x);
+                        e[u].widen(y);
+                        if (known) turn(x, y, co, si, interleaved);
+#pragma unroll
+                        for (int i = 0; i < E; ++i) {
+                            x[i] = known ? x[i] : __builtin_nanf("");
+                            y[i] = known ? y[i] : __builtin_nanf("");
+                        }
+                        a[u].round(x);
+                        e[u].round(y);
+                    }
+                    a[u].store(dst + (h + u * step) * p.o_h + at.ea * (int)sizeof(TQ));
+                    e[u].store(dst + (h + u * step) * p.o_h + at.eb * (int)sizeof(TQ));
+                }
         }
         return;
     }
 
-    // ---- keys and values: one page of one KV head
+    // ---- keys and values: the wavefronts of the workgroup have one page of one KV head together, or several pages
+    constexpr int E = Shape<T>::E, LPR = D / (2 * E);
+    constexpr int RPW = kWave / LPR;            // rows of a wavefront's pass
+    const int lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int j = lane % LPR;
+    const Pieces at = pieces_of<E>(j, p.rot, interleaved);
     int id = (int)blockIdx.x;
     const int h = id % c.H;
     id /= c.H;
-    const int slot = id % g.slots, b = id / g.slots;
+    const int group = id % g.page_groups, b = id / g.page_groups;
+    const int wpp = 1 << g.log2_waves, part = wave & (wpp - 1);
     const int li = p.per_head ? b * c.H + h : b;
-    const int base = p.base_lens[li];
-    const int fresh = p.new_lens ? p.new_lens[li] : p.N;
-    const int64_t pos0 = p.positions ? p.positions[b] : base;
+    const int base = read_scalar(p.base_lens + li), new_len = read_scalar((p.new_lens ? p.new_lens : p.base_lens) + li);
+    const int position = read_scalar(p.positions ? p.positions + b : p.base_lens + li);
+    const int fresh = p.new_lens ? new_len : p.N;
+    const int64_t pos0 = position;
     const PagedAppendPlan plan = paged_append_plan(base, fresh, p.N, c.P, c.log2_R, p.cos_sin != nullptr, pos0, p.max_position);
     const int32_t *table = paged_table(c, b, h);
-    if (slot == 0 && (p.per_head || h == 0)) {
+    const int place = plan.first + group * (WAVES >> g.log2_waves) + (wave >> g.log2_waves);
+    if (group == 0 && (p.per_head || h == 0)) {
         // the length of the sequence (and head): -1 if any page that it needs is not there
         int bad = 0;
         const int heads = (c.table_per_head && !p.per_head) ? c.H : 1;      // pages of their own, one length
@@ -127,120 +200,146 @@ __global__ __launch_bounds__(kAppThreads) void paged_append_kernel(PagedAppendAr
         bad = __syncthreads_or(bad);
         if (tid == 0) p.lens[li] = (plan.ok && !bad) ? base + fresh : -1;
     }
-    const int place = plan.first + slot;
-    if (place > plan.last) return;
-    const int page = table[place];
-    if (paged_bad(c, page)) return;
-    const int64_t row0 = (int64_t)place << c.log2_R;       // row of the sequence at the page's start
-    const int r0 = (int)max((int64_t)base - row0, (int64_t)0), r1 = (int)min((int64_t)base + fresh - row0, (int64_t)c.R);
-    char *kp = c.K + paged_offset(c, page, h), *vp = c.V + paged_offset(c, page, h);
+    const int page = place <= plan.last ? read_scalar(table + place) : -1;
+    const bool there = !paged_bad(c, page);
     const bool summary = c.k_min != nullptr;
-    float lo[16], hi[16];
+    const int64_t row0 = (int64_t)place << c.log2_R;       // row of the sequence at the page's start
+    const int r0 = (int)max((int64_t)base - row0, (int64_t)0), r1 = there ? (int)min((int64_t)base + fresh - row0, (int64_t)c.R) : 0;
+    char *kp = c.K + (there ? paged_offset(c, page, h) : 0), *vp = c.V + (there ? paged_offset(c, page, h) : 0);
+    const char *ks = p.K + b * p.k_b + h * p.k_h, *vs = p.V + b * p.v_b + h * p.v_h;
+    const int32_t *sizes = p.counts + ((int64_t)b * c.H + h) * p.N;
+    int32_t *counts = c.counts + (there ? paged_index(c, page, h) * c.R : 0);
+    const int oa = at.ea * (int)sizeof(T), ob = at.eb * (int)sizeof(T);
+    const int pass = RPW << g.log2_waves, from = summary ? 0 : r0;
+    float lo[2 * E], hi[2 * E];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) { lo[i] = INFINITY; hi[i] = -INFINITY; }
-    for (int row = (summary ? 0 : r0 / RPP * RPP) + r; row < r1; row += RPP) {
-        T *kd = reinterpret_cast<T *>(kp + (int64_t)row * c.row_bytes);
-        float x[8], y[8];
-        if (row < r0) {
-            if (!summary) continue;
-            load8(kd + at.ea, x);
-            load8(kd + at.eb, y);
-        } else {
-            const int64_t n = row0 + row - base;
-            const T *ks = reinterpret_cast<const T *>(p.K + b * p.k_b + h * p.k_h + n * p.k_n);
-            const T *vs = reinterpret_cast<const T *>(p.V + b * p.v_b + h * p.v_h + n * p.v_n);
-            T *vd = reinterpret_cast<T *>(vp + (int64_t)row * c.row_bytes);
-            float u[8], w[8];
-            load8(ks + at.ea, x);
-            load8(ks + at.eb, y);
-            load8(vs + at.ea, u);
-            load8(vs + at.eb, w);
-            if (at.turned) {
-                float co[8], si[8];
-                load8(p.cos_sin + (pos0 + n) * p.rot + 8 * j, co);
-                load8(p.cos_sin + (pos0 + n) * p.rot + half + 8 * j, si);
-                turn(x, y, co, si, p.interleaved != 0);
+    for (int i = 0; i < 2 * E; ++i) { lo[i] = INFINITY; hi[i] = -INFINITY; }
+    // rows t of the page: those below r0 are there already (and count in the summary), r0 .. r1 are new.  Lanes behind the last row read it again, so
+    // that all loads of a pass are on their way at once.
+    for (int t0 = from / pass * pass + part * RPW; t0 < r1; t0 += U * pass) {
+        Raw<T> ka[U], kb[U], va[U], vb[U];
+        float co[U][E], si[U][E];
+        int size[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int t = min(max(t0 + u * pass + lane / LPR, from), r1 - 1);
+            const int64_t n = row0 + max(t, r0) - base;      // row of the call
+            const char *k = t < r0 ? kp + (int64_t)t * c.row_bytes : ks + n * p.k_n, *v = vs + n * p.v_n;
+            ka[u].load(k + oa);
+            kb[u].load(k + ob);
+            va[u].load(v + oa);
+            vb[u].load(v + ob);
+            if constexpr (ROT) {
+                const float *angles = p.cos_sin + (pos0 + n) * p.rot + (at.turned ? E * j : 0);
+                load_angles(angles, co[u]);
+                load_angles(angles + half, si[u]);
             }
-            store8(kd + at.ea, x);
-            store8(kd + at.eb, y);
-            store8(vd + at.ea, u);
-            store8(vd + at.eb, w);
-            if (c.counts && j == 0) c.counts[paged_index(c, page, h) * c.R + row] = p.counts[((int64_t)b * c.H + h) * p.N + n];
-            if (summary) {      // of the keys as stored
-                rounded<T>(x);
-                rounded<T>(y);
-            }
+            if (c.counts) size[u] = sizes[n];
         }
-        if (summary) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                lo[i] = lower(lo[i], x[i]);
-                hi[i] = higher(hi[i], x[i]);
-                lo[8 + i] = lower(lo[8 + i], y[i]);
-                hi[8 + i] = higher(hi[8 + i], y[i]);
+        for (int u = 0; u < U; ++u) {
+            const int t = t0 + u * pass + lane / LPR;
+            const bool is_new = t >= r0 && t < r1;
+            if constexpr (ROT) {
+                if (is_new && at.turned) {
+                    float x[E], y[E];
+                    ka[u].widen(x);
+                    kb[u].widen(y);
+                    turn(x, y, co[u], si[u], interleaved);
+                    ka[u].round(x);
+                    kb[u].round(y);
+                }
+            }
+            if (is_new) {
+                ka[u].store(kp + (int64_t)t * c.row_bytes + oa);
+                kb[u].store(kp + (int64_t)t * c.row_bytes + ob);
+                va[u].store(vp + (int64_t)t * c.row_bytes + oa);
+                vb[u].store(vp + (int64_t)t * c.row_bytes + ob);
+                if (c.counts && j == 0) counts[t] = size[u];
+            }
+            if (summary && t < r1) {      // of the keys as stored
+                float x[E], y[E];
+                ka[u].widen(x);
+                kb[u].widen(y);
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    lo[i] = lower(lo[i], x[i]);
+                    hi[i] = higher(hi[i], x[i]);
+                    lo[E + i] = lower(lo[E + i], y[i]);
+                    hi[E + i] = higher(hi[E + i], y[i]);
+                }
             }
         }
     }
     if (!summary) return;
-    // ---- the lanes with the same pieces, then the wavefronts
-    __shared__ float s_lo[kAppThreads / kWave][D], s_hi[kAppThreads / kWave][D];
+    // ---- the lanes with the same pieces, then the page's wavefronts
+    constexpr int M = E / 2;                // elements that a lane ends up with
+    __shared__ __attribute__((aligned(16))) float s_lo[WAVES][D], s_hi[WAVES][D];
+    float l[M], u[M];
+    gather_extremes<LPR, true>(lo, l);
+    gather_extremes<LPR, false>(hi, u);
+    const int first = M * (lane / 16);
+    const int el = first < E ? at.ea + first : at.eb + first - E;
+    const bool writes = lane % 16 < LPR;
+    if (wpp > 1) {
+        if (writes) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-#pragma unroll
-        for (int off = LPR; off < kWave; off <<= 1) {
-            lo[i] = lower(lo[i], __shfl_xor(lo[i], off, kWave));
-            hi[i] = higher(hi[i], __shfl_xor(hi[i], off, kWave));
+            for (int i = 0; i < M; ++i) {
+                s_lo[wave][el + i] = l[i];
+                s_hi[wave][el + i] = u[i];
+            }
         }
+        __syncthreads();
+        if (part != 0) return;
+        if (writes)
+            for (int w = 1; w < wpp; ++w)
+#pragma unroll
+                for (int i = 0; i < M; ++i) {
+                    l[i] = lower(l[i], s_lo[wave + w][el + i]);
+                    u[i] = higher(u[i], s_hi[wave + w][el + i]);
+                }
     }
-    if (tid % kWave < LPR) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int e = i < 8 ? at.ea + i : at.eb + i - 8;
-            s_lo[tid / kWave][e] = lo[i];
-            s_hi[tid / kWave][e] = hi[i];
-        }
-    }
-    __syncthreads();
-    if (tid < D) {
-        float a = s_lo[0][tid], e = s_hi[0][tid];
-#pragma unroll
-        for (int w = 1; w < kAppThreads / kWave; ++w) {
-            a = lower(a, s_lo[w][tid]);
-            e = higher(e, s_hi[w][tid]);
-        }
-        const int64_t off = paged_index(c, page, h) * D + tid;
-        if constexpr (sizeof(T) == 2) {      // exact: the values are bf16
-            reinterpret_cast<uint16_t *>(c.k_min)[off] = (uint16_t)(__float_as_uint(a) >> 16);
-            reinterpret_cast<uint16_t *>(c.k_max)[off] = (uint16_t)(__float_as_uint(e) >> 16);
+    if (writes && there) {
+        const int64_t off = paged_index(c, page, h) * D + el;      // (exact: the values are of the type)
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<uint2 *>(c.k_min + 2 * off) = make_uint2(pack_bf16x2(l[0], l[1]), pack_bf16x2(l[2], l[3]));
+            *reinterpret_cast<uint2 *>(c.k_max + 2 * off) = make_uint2(pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3]));
         } else {
-            reinterpret_cast<float *>(c.k_min)[off] = a;
-            reinterpret_cast<float *>(c.k_max)[off] = e;
+            *reinterpret_cast<float2 *>(c.k_min + 4 * off) = make_float2(l[0], l[1]);
+            *reinterpret_cast<float2 *>(c.k_max + 4 * off) = make_float2(u[0], u[1]);
         }
     }
 }
 
-template <typename T, typename TQ, int D>
+template <typename T, typename TQ, int D, bool ROT>
 static hipError_t launch_append(const PagedAppendArgs &a, hipStream_t stream) {
-    constexpr int RPP = kAppThreads / (D / 16);
+    constexpr int WAVES = kAppThreads / kWave;
+    constexpr int RPW = kWave / (D / (2 * Shape<T>::E)), QRPW = kWave / (D / (2 * Shape<TQ>::E));      // rows of a wavefront's pass
     AppendGrid g;
-    g.slots = paged_append_slots(a.N, a.c.R, a.c.P);
-    g.kv_blocks = a.c.B * a.c.H * g.slots;
-    g.q_tiles = (a.N + RPP - 1) / RPP;
-    g.q_heads = 4;
+    // wavefronts of a page: two passes each, up to all four
+    g.log2_waves = 0;
+    while (g.log2_waves < 2 && (2 * RPW << g.log2_waves) < a.c.R) ++g.log2_waves;
+    const int pages = WAVES >> g.log2_waves, slots = paged_append_slots(a.N, a.c.R, a.c.P);
+    g.page_groups = (slots + pages - 1) / pages;
+    g.kv_blocks = a.c.B * a.c.H * g.page_groups;
+    g.log2_tokens = 0;
+    while ((1 << g.log2_tokens) < a.N && (1 << g.log2_tokens) < WAVES * QRPW) ++g.log2_tokens;
+    g.q_tiles = (a.N + (1 << g.log2_tokens) - 1) >> g.log2_tokens;
+    g.q_heads = max(2, (WAVES * QRPW) >> g.log2_tokens);      // (32768 tokens, 8 + 32 heads: 2 heads 159 us, 4 161, 8 163, 16 169)
     g.q_groups = a.Q ? (a.Hq + g.q_heads - 1) / g.q_heads : 0;
     const unsigned blocks = (unsigned)g.kv_blocks + (unsigned)(a.c.B * g.q_tiles * g.q_groups);      // (paged_append_fits)
-    hipLaunchKernelGGL((paged_append_kernel<T, TQ, D>), dim3(blocks), dim3(kAppThreads), 0, stream, a, g);
+    hipLaunchKernelGGL((paged_append_kernel<T, TQ, D, ROT>), dim3(blocks), dim3(kAppThreads), 0, stream, a, g);
     return hipGetLastError();
 }
 
-template <typename T, typename TQ> static hipError_t launch_append_d(const PagedAppendArgs &a, hipStream_t stream) {
-    return a.c.d == 128 ? launch_append<T, TQ, 128>(a, stream) : launch_append<T, TQ, 64>(a, stream);
+template <typename T, int D> static hipError_t launch_append_q(const PagedAppendArgs &a, hipStream_t stream) {
+    if (!a.cos_sin) return launch_append<T, T, D, false>(a, stream);
+    return a.q_dtype == DType::BF16 ? launch_append<T, bf16_t, D, true>(a, stream) : launch_append<T, float, D, true>(a, stream);
 }
 
 hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t stream) {
-    if (a.c.dtype == DType::BF16)
-        return a.q_dtype == DType::BF16 ? launch_append_d<bf16_t, bf16_t>(a, stream) : launch_append_d<bf16_t, float>(a, stream);
-    return a.q_dtype == DType::BF16 ? launch_append_d<float, bf16_t>(a, stream) : launch_append_d<float, float>(a, stream);
+    if (a.c.dtype == DType::BF16) return a.c.d == 128 ? launch_append_q<bf16_t, 128>(a, stream) : launch_append_q<bf16_t, 64>(a, stream);
+    return a.c.d == 128 ? launch_append_q<float, 128>(a, stream) : launch_append_q<float, 64>(a, stream);
 }
 
 }  // namespace sc
