@@ -399,12 +399,12 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     constexpr std::integral_constant<int, 0> kEven{};
     constexpr std::integral_constant<int, AHEAD - 1> kOdd{};
     auto request_first = [&](const Stretch &t, Pages &pages) {
-        load_queries(t);
         if (t.steps > 0) { request_keys(t, pages, 0, kEven); request_values(kEven); }
         if (AHEAD > 1 && t.steps > 1) { request_keys(t, pages, 1, kOdd); request_values(kOdd); }
     };
 
     Stretch cur = stretch_at(pos);
+    load_queries(cur);
     Pages pages = look_up(cur, 0);
     request_first(cur, pages);
     while (true) {
@@ -512,7 +512,10 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
             if (AHEAD > 1 && s + 1 < cur.steps) step(s + 1, kOdd);
         }
         const bool bad = ballot64(pages.bad != 0) != 0ull;
-        if (more) request_first(nxt, nxt_pages);
+        if (more) {
+            load_queries(nxt);
+            request_first(nxt, nxt_pages);
+        }
 
         // ---- join the wavefronts
         float lw = rows_allreduce_sum(l_run);

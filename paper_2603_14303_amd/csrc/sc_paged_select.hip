@@ -2,16 +2,13 @@
 //     score(page) = max over the G heads of  sum_e max(q_e k_min_e, q_e k_max_e) = max over heads of (q+ . k_max + q- . k_min),  q+ = max(q, 0), q- = min(q, 0):
 // no key between the page's bounds has a larger product with any of the queries.
 //
-// Two kernels.  The scores, bound by the summaries' bytes (2 d elements a page and head), are two products on the fp64 matrix cores (16 pages x 16 heads,
-// v_mfma_f64_16x16x4_f64): the products of two bf16 numbers are exact in fp64 and their sums very nearly so, and the choice between two pages is
-// that of exact arithmetic unless they are some 1e-13 apart.  (Sums in fp32 would choose another page than an exact evaluation in a few calls of a
-// hundred, and which one would depend on the order of the sum.)  Then one workgroup per (sequence, KV head) finds the key of the last page to keep, eight bits at a time, and
-// writes the places in order.
+// Two kernels.  The scores are two products on the fp64 matrix cores: the products of two bf16 numbers are exact in fp64 and their sums very nearly so,
+// and the choice between two pages is that of exact arithmetic unless they are some 1e-13 apart.  (Sums in fp32 would choose another page than an
+// exact evaluation in a few calls of a hundred, and which one would depend on the order of the sum.)  Then one workgroup per (sequence, KV head) finds
+// the last page to keep and writes the places in order.
 #include "sc_paged.h"
 
 namespace sc {
-
-typedef double sel_f64x4 __attribute__((ext_vector_type(4)));
 
 struct PagSelParams {
     PagedView c;
@@ -78,36 +75,54 @@ __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams
         lo[ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(cv.k_min) + row + E * (4 * ks + g));
         hi[ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(cv.k_max) + row + E * (4 * ks + g));
     }
-    // rows of the products: query heads; those behind the group are its last one again and do not change the maximum
-    const TQ *q = reinterpret_cast<const TQ *>(p.Q) + (bh * p.G + min(c, p.G - 1)) * D;
-    sel_f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+    // v_mfma_f64_4x4x4_4b: four products of 4 heads x 4 pages, the lanes' pages being the columns of all four; heads behind the group are its last one
+    // again and do not change the maximum
+    double best = 0.0;
+    for (int h0 = 0; h0 < p.G; h0 += 4) {
+        const TQ *q = reinterpret_cast<const TQ *>(p.Q) + (bh * p.G + min(h0 + lane % 4, p.G - 1)) * D;
+        double acc = 0.0;
 #pragma unroll
-    for (int ks = 0; ks < KL; ++ks) {
-        float x[E], l[E], u[E];
-        query_piece<E>(q + E * (4 * ks + g), x);
-        widen(lo[ks], l);
-        widen(hi[ks], u);
+        for (int ks = 0; ks < KL; ++ks) {
+            float x[E], l[E], u[E];
+            query_piece<E>(q + E * (4 * ks + g), x);
+            widen(lo[ks], l);
+            widen(hi[ks], u);
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            // (a NaN in a query goes through either product)
-            acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(x[i] < 0.f ? 0.f : x[i]), (double)u[i], acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(x[i] > 0.f ? 0.f : x[i]), (double)l[i], acc, 0, 0, 0);
+            for (int i = 0; i < E; ++i) {
+                // (a NaN in a query goes through either product)
+                acc = __builtin_amdgcn_mfma_f64_4x4x4f64((double)(x[i] < 0.f ? 0.f : x[i]), (double)u[i], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f64_4x4x4f64((double)(x[i] > 0.f ? 0.f : x[i]), (double)l[i], acc, 0, 0, 0);
+            }
         }
-    }
-    // the maximum over the heads: over the registers, and over the lanes that share the page (whatever row is where)
-    double best = acc[0];
+        // the maximum over the heads: over the lanes that share the page (whatever head is where)
 #pragma unroll
-    for (int i = 1; i < 4; ++i) best = (acc[i] > best || acc[i] != acc[i]) ? acc[i] : best;
-#pragma unroll
-    for (int off = 16; off < kWave; off <<= 1) {
-        const double other = __shfl_xor(best, off, kWave);
-        best = (other > best || other != other) ? other : best;
+        for (int off = 16; off < kWave; off <<= 1) {
+            const double other = __shfl_xor(acc, off, kWave);
+            acc = (other > acc || other != other) ? other : acc;
+        }
+        best = (h0 == 0 || acc > best || acc != acc) ? acc : best;
     }
     if (g == 0 && place < pages) {
         unsigned long long key = there ? score_key(best) : kKeyNaN;
         if (place < p.first || place >= pages - p.recent) key = kKeyForced;
         p.keys[bh * cv.P + place] = key;
     }
+}
+
+// One workgroup per (sequence, KV head).  The keys are spread over kBuckets buckets, evenly between the smallest and the largest number, by one pass; the
+// bucket that the last page to keep falls into holds a few of them, which are ranked against each other.  If they are more than fit (scores that are
+// equal, or lie together far from a few others), the key is found eight bits at a time.
+constexpr int kBuckets = 2048, kRanked = 256, kSelWaves = kSelThreads / kWave;
+
+__device__ __forceinline__ double key_score(unsigned long long k) { return __builtin_bit_cast(double, (k >> 63) ? k & ~(1ull << 63) : ~k); }
+
+__device__ __forceinline__ int scan_add(int x) {      // over the lanes up to each one
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+        const int t = __shfl_up(x, off, kWave);
+        x += (int)(threadIdx.x % kWave) >= off ? t : 0;
+    }
+    return x;
 }
 
 __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams p) {
@@ -122,53 +137,136 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
         return;
     }
     const unsigned long long *keys = p.keys + bh * p.c.P;
-    // ---- the key of rank keep, from the top eight bits down
-    __shared__ int hist[256];
-    __shared__ int s_digit, s_need;
-    unsigned long long prefix = 0, mask = 0;
-    int need = keep;      // of the keys that agree with the prefix
-    for (int shift = 56; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += kSelThreads) {
-            const unsigned long long k = keys[i];
-            if ((k & mask) == prefix) atomicAdd(&hist[(int)(k >> shift) & 255], 1);
+    constexpr int K = 4;                                // keys that a thread keeps in registers; those behind them are read again
+    __shared__ int s_hist[kBuckets];
+    __shared__ float s_low[kSelWaves], s_high[kSelWaves];
+    __shared__ int s_above[kSelWaves], s_equal[kSelWaves];
+    __shared__ int s_bucket, s_need, s_ranked;
+    __shared__ unsigned long long s_key[kRanked], s_border;
+    __shared__ int s_place[kRanked], s_border_place;
+    unsigned long long mine[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) mine[k] = tid + k * kSelThreads < n ? keys[tid + k * kSelThreads] : 0ull;
+    auto each = [&](auto f) {      // every key and its place
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (tid + k * kSelThreads < n) f(mine[k], tid + k * kSelThreads);
+        for (int i = tid + K * kSelThreads; i < n; i += kSelThreads) f(keys[i], i);
+    };
+    // ---- the smallest and the largest finite score (as fp32: the buckets only need an order)
+    float low = INFINITY, high = -INFINITY;
+    each([&](unsigned long long k, int) {
+        const float x = k < kKeyNaN ? (float)key_score(k) : INFINITY;
+        if (fabsf(x) < INFINITY) {
+            low = fminf(low, x);
+            high = fmaxf(high, x);
         }
-        __syncthreads();
-        if (wave == 0) {      // lane i: digits 255 - 4 i .. 252 - 4 i
-            int v[4], sum = 0;
+    });
 #pragma unroll
-            for (int t = 0; t < 4; ++t) { v[t] = hist[255 - 4 * lane - t]; sum += v[t]; }
-            int before = sum;
-#pragma unroll
-            for (int off = 1; off < kWave; off <<= 1) {
-                const int t = __shfl_up(before, off, kWave);
-                before += lane >= off ? t : 0;
-            }
-            before -= sum;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                if (before < need && before + v[t] >= need) { s_digit = 255 - 4 * lane - t; s_need = need - before; }
-                before += v[t];
-            }
-        }
-        __syncthreads();
-        prefix |= (unsigned long long)s_digit << shift;
-        mask |= 255ull << shift;
-        need = s_need;
-        __syncthreads();
+    for (int off = 1; off < kWave; off <<= 1) {
+        low = fminf(low, __shfl_xor(low, off, kWave));
+        high = fmaxf(high, __shfl_xor(high, off, kWave));
     }
-    // ---- the places, ascending: keys above it, and the first `need` of those equal to it
-    __shared__ int s_above[kSelThreads / kWave], s_equal[kSelThreads / kWave];
+    if (lane == 0) { s_low[wave] = low; s_high[wave] = high; }
+    for (int i = tid; i < kBuckets; i += kSelThreads) s_hist[i] = 0;
+    if (tid == 0) s_ranked = 0;
+    __syncthreads();
+    for (int w = 0; w < kSelWaves; ++w) {
+        low = fminf(low, s_low[w]);
+        high = fmaxf(high, s_high[w]);
+    }
+    const float spread = high > low ? (float)(kBuckets - 5) / (high - low) : 0.f;      // (0 too where high - low is not finite)
+    auto bucket = [&](unsigned long long k) {      // never falls where the key grows
+        if (k >= kKeyNaN) return kBuckets - 1 - (int)(k == kKeyNaN);
+        const float x = (float)key_score(k);
+        return x >= INFINITY ? kBuckets - 3 : x <= -INFINITY ? 0 : 1 + min((int)((x - low) * spread), kBuckets - 5);
+    };
+    each([&](unsigned long long k, int) { atomicAdd(&s_hist[bucket(k)], 1); });
+    __syncthreads();
+    // ---- the bucket of rank keep: thread t has buckets kBuckets - 1 - 2 t and the one below
+    {
+        const int v0 = s_hist[kBuckets - 1 - 2 * tid], v1 = s_hist[kBuckets - 2 - 2 * tid];
+        const int upto = scan_add(v0 + v1);
+        if (lane == kWave - 1) s_above[wave] = upto;
+        __syncthreads();
+        int before = upto - v0 - v1;
+        for (int w = 0; w < wave; ++w) before += s_above[w];
+        if (before < keep && before + v0 >= keep) { s_bucket = kBuckets - 1 - 2 * tid; s_need = keep - before; }
+        before += v0;
+        if (before < keep && before + v1 >= keep) { s_bucket = kBuckets - 2 - 2 * tid; s_need = keep - before; }
+    }
+    __syncthreads();
+    const int at = s_bucket;
+    int need = s_need;      // of the keys that count as equal to the border's
+    unsigned long long border = 0;
+    int border_place = n;   // keys equal to the border's are kept up to this place
+    if (s_hist[at] <= kRanked) {
+        each([&](unsigned long long k, int i) {
+            if (bucket(k) == at) {
+                const int r = atomicAdd(&s_ranked, 1);
+                s_key[r] = k;
+                s_place[r] = i;
+            }
+        });
+        __syncthreads();
+        const int m = s_ranked;
+        if (tid < m) {
+            const unsigned long long k = s_key[tid];
+            const int i = s_place[tid];
+            int rank = 0;
+            for (int r = 0; r < m; ++r) rank += s_key[r] > k || (s_key[r] == k && s_place[r] < i);
+            if (rank == need - 1) { s_border = k; s_border_place = i; }
+        }
+        __syncthreads();
+        border = s_border;
+        border_place = s_border_place;
+    } else {
+        unsigned long long mask = 0;
+        for (int shift = 56; shift >= 0; shift -= 8) {
+            __syncthreads();
+            if (tid < 256) s_hist[tid] = 0;
+            __syncthreads();
+            each([&](unsigned long long k, int) {
+                if (bucket(k) == at && (k & mask) == border) atomicAdd(&s_hist[(int)(k >> shift) & 255], 1);
+            });
+            __syncthreads();
+            if (wave == 0) {      // lane i: digits 255 - 4 i .. 252 - 4 i
+                int v[4], sum = 0;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) { v[t] = s_hist[255 - 4 * lane - t]; sum += v[t]; }
+                int before = scan_add(sum) - sum;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    if (before < need && before + v[t] >= need) { s_bucket = 255 - 4 * lane - t; s_need = need - before; }
+                    before += v[t];
+                }
+            }
+            __syncthreads();
+            border |= (unsigned long long)s_bucket << shift;
+            mask |= 255ull << shift;
+            need = s_need;
+        }
+    }
+    // ---- the places, ascending: keys above the border's, and of those equal to it the first ones (up to a place, or `need` of them)
+    const bool by_place = border_place < n;
     int above0 = 0, equal0 = 0;      // before this stretch of kSelThreads pages
-    for (int i0 = 0; i0 < n; i0 += kSelThreads) {
-        const unsigned long long k = i0 + tid < n ? keys[i0 + tid] : 0ull;
-        const bool is_above = i0 + tid < n && k > prefix, is_equal = i0 + tid < n && k == prefix;
+    for (int k = 0, i0 = 0; i0 < n; ++k, i0 += kSelThreads) {
+        const int i = i0 + tid;
+        unsigned long long x = 0ull;
+        if (k < K) {
+#pragma unroll
+            for (int t = 0; t < K; ++t) x = t == k ? mine[t] : x;
+        } else if (i < n) {
+            x = keys[i];
+        }
+        const bool is_equal = !by_place && i < n && x == border, is_above = i < n && (x > border || (by_place && x == border && i <= border_place));
         const uint64_t ba = ballot64(is_above), be = ballot64(is_equal);
+        __syncthreads();
         if (lane == 0) { s_above[wave] = __popcll(ba); s_equal[wave] = __popcll(be); }
         __syncthreads();
         int above = above0, equal = equal0;
-        for (int w = 0; w < kSelThreads / kWave; ++w) {
+#pragma unroll
+        for (int w = 0; w < kSelWaves; ++w) {
             above += w < wave ? s_above[w] : 0;
             equal += w < wave ? s_equal[w] : 0;
             above0 += s_above[w];
@@ -177,8 +275,7 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
         const uint64_t below = (1ull << lane) - 1;
         above += __popcll(ba & below);
         equal += __popcll(be & below);
-        if (is_above || (is_equal && equal < need)) sel[above + min(equal, need)] = i0 + tid;
-        __syncthreads();
+        if (is_above || (is_equal && equal < need)) sel[above + min(equal, need)] = i;
     }
 }
 
