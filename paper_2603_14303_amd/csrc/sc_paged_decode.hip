@@ -20,8 +20,9 @@ namespace sc {
 
 constexpr int kPagWaves = 8;
 constexpr int kPagThreads = kPagWaves * kWave;
-constexpr int kStep = 16 * kPagWaves;        // rows of a step of all wavefronts; the work's unit, or kAlone of them
-constexpr int kAlone = 2;
+constexpr int kStep = 16 * kPagWaves;        // rows of a step of all wavefronts: the unit of work
+constexpr int kAlone = 2;                    // steps up to which a head goes to one workgroup, if there is one for every head
+constexpr int kMore = 2;                     // steps beyond an equal share for which workgroups have parts of one head only
 constexpr int kMaxWgs = 256;                 // one on each compute unit
 constexpr int kPagPad = 4;                   // floats behind the sums of a partial result: maximum, sum, two unused
 constexpr int kMaxHeadWgs = 64;              // workgroups per (sequence, KV head) at most, on average: each is a partial result to join
@@ -29,6 +30,8 @@ constexpr float kPagLog2e = 1.4426950408889634f;
 constexpr float kPagLn2 = 0.6931471805599453f;
 
 typedef float pag_f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int pag_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int pag_u32x2 __attribute__((ext_vector_type(2)));
 typedef short pag_short4 __attribute__((ext_vector_type(4)));
 typedef __bf16 pag_bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -49,6 +52,10 @@ struct PagDecParams {
     int wgs;             // workgroups of the launch
 };
 
+// a value that all lanes agree on, kept in a scalar register (what a division or a conversion gives is in a vector register otherwise, and every
+// branch on it is one on lanes)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float inverse_of(int y) { return __builtin_amdgcn_rcpf((float)y); }
 __device__ __forceinline__ float pag_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Sums over the lanes up to each one (DPP moves inside the rows of 16 lanes, then from row to row), and the maximum over all of them
@@ -91,24 +98,31 @@ template <typename T, int D> struct Rows {
     int32_t n[4];
 };
 
-template <typename T, int D> __device__ __forceinline__ void load_keys(Rows<T, D> &x, const char *k, int row_bytes, int g, int c) {
-    const char *at = k + (uint32_t)(c * row_bytes + 16 * g);
+// Rows come through buffer descriptors that begin at the step's first row and end behind the last one that attends: what lies behind reads as zeros
+// (it may be anything in memory, and 0 times a NaN is one), a step without rows asks nothing of memory, and the lane's offsets are 32-bit and the same
+// for every step.
+typedef __amdgpu_buffer_rsrc_t pag_rsrc;
+__device__ __forceinline__ pag_rsrc rows_at(const char *p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p), (short)0, bytes, 0x00020000); }
+constexpr int kAuxNt = 2;          // buffer cache policy: read once by this launch
+template <typename T, int D> __device__ __forceinline__ void load_keys(Rows<T, D> &x, pag_rsrc k, int lane_offset) {
 #pragma unroll
-    for (int ks = 0; ks < Rows<T, D>::KL; ++ks) x.k[ks] = load16_stream(at + 64 * ks);
+    for (int ks = 0; ks < Rows<T, D>::KL; ++ks) {
+        const pag_u32x4 t = __builtin_amdgcn_raw_buffer_load_b128(k, lane_offset + 64 * ks, 0, kAuxNt);
+        x.k[ks] = make_uint4(t.x, t.y, t.z, t.w);
+    }
 }
-template <typename T, int D> __device__ __forceinline__ void load_values(Rows<T, D> &x, const char *v, int row_bytes, int g, int c) {
+template <typename T, int D> __device__ __forceinline__ void load_values(Rows<T, D> &x, pag_rsrc v, int lane_offset, int row_bytes) {
     constexpr int VW = Rows<T, D>::VW;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const char *at = v + (uint32_t)((4 * g + i) * row_bytes);
         if constexpr (VW == 2) {
-            const uint2 t = *reinterpret_cast<const uint2 *>(at + 8 * c);
+            const pag_u32x2 t = __builtin_amdgcn_raw_buffer_load_b64(v, lane_offset + i * row_bytes, 0, kAuxNt);
             x.v[i][0] = t.x;
             x.v[i][1] = t.y;
         } else {
 #pragma unroll
             for (int q = 0; q < VW / 4; ++q) {
-                const uint4 t = load16_stream(at + 256 * q + 16 * c);
+                const pag_u32x4 t = __builtin_amdgcn_raw_buffer_load_b128(v, lane_offset + i * row_bytes + 256 * q, 0, kAuxNt);
                 x.v[i][4 * q] = t.x;
                 x.v[i][4 * q + 1] = t.y;
                 x.v[i][4 * q + 2] = t.z;
@@ -138,8 +152,6 @@ __device__ __forceinline__ float row_allreduce_max(float x) {      // over the 1
 // Partial results: [place][head][D + kPagPad] floats, written through to memory and read from there (the workgroups of a head run on chiplets whose
 // L2s do not see each other's lines within a kernel).
 constexpr int kAuxAgent = 16;      // buffer cache policy: device scope
-typedef unsigned int pag_u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int pag_u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ void store_result(const PagDecParams &p, int64_t row, int D, int e, const float4 &o, float m, float l) {
     const float f = l != 0.f ? 1.0f / l : 0.f;
@@ -158,7 +170,7 @@ template <int D> __device__ __forceinline__ void store_part(__amdgpu_buffer_rsrc
 // Joins n partial results, whose places `place_of` gives, and hands each of the G D / 4 pieces to `sink` with its head's maximum and sum.
 // A thread owns one piece of one head and every NS-th part; all its loads of a pass are on their way before the first is used.
 template <int D, typename PlaceOf, typename Sink>
-__device__ __forceinline__ void join_parts(const PagDecParams &p, __amdgpu_buffer_rsrc_t rs, int n, PlaceOf place_of, int tid, float *s_buf, float2 *s_total, Sink sink) {
+__device__ __forceinline__ void join_parts(const PagDecParams &p, __amdgpu_buffer_rsrc_t rs, int n, PlaceOf place_of, int tid, float *s_buf, float *s_total, Sink sink) {
     constexpr int QPR = D / 4, kStride = D + kPagPad, PASS = 8;
     const int G = p.G, lane = tid % kWave, wave = tid / kWave;
     const int pieces = G * QPR;
@@ -201,7 +213,10 @@ __device__ __forceinline__ void join_parts(const PagDecParams &p, __amdgpu_buffe
                         l = fmaf(s_l[(k << log2_G) + h2], f, l);
                     }
                     l = rows_allreduce_sum(row_allreduce_sum<16>(l));
-                    if (lane == 0) s_total[h2] = make_float2(m, l);
+                    if (lane == 0) {
+                        s_total[h2] = m;
+                        s_total[16 + h2] = l;
+                    }
                 }
                 __syncthreads();
             }
@@ -224,7 +239,7 @@ __device__ __forceinline__ void join_parts(const PagDecParams &p, __amdgpu_buffe
                     o.x += t.x; o.y += t.y; o.z += t.z; o.w += t.w;
                 }
         }
-        if (worker && sg == 0) sink(hh, e, o, s_total[hh].x, s_total[hh].y);
+        if (worker && sg == 0) sink(hh, e, o, s_total[hh], s_total[16 + hh]);
     }
 }
 
@@ -247,7 +262,6 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int KL = Rows<T, D>::KL, VW = Rows<T, D>::VW, NA = Acc<T, D>::N;
     constexpr int PP = QP == 1 ? 2 : 3;       // parts of the probabilities (bf16)
-    constexpr int AHEAD = KL == 8 ? 1 : 2;    // (two would take more than 256 registers with rows of 512 bytes)
     constexpr int kStride = D + kPagPad;
     const PagedView &cv = p.c;
     const int G = p.G;
@@ -259,7 +273,7 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     __shared__ __attribute__((aligned(16))) float s_acc[kPagWaves * 16 * D];
     __shared__ float s_m[kPagWaves][16], s_l[kPagWaves][16];
     __shared__ int s_last;
-    __shared__ float2 s_total[16];
+    __shared__ float s_total[32];
     const auto rs = __builtin_amdgcn_make_buffer_rsrc(p.part, (short)0, 2 * kMaxWgs * G * kStride * 4, 0x00020000);
 
     // ---- my stretch of all units: every wavefront adds up the lengths, 64 at a time
@@ -273,27 +287,49 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
             my_rows = p.sel ? min(max(p.sel_lens[e], 0), p.keep) << cv.log2_R : my_len;      // selected: the rows of whole pages; those behind the length are masked
         }
     };
+    // Units of a head: its steps, rounded up to what a workgroup takes, so that no workgroup has parts of two heads (each costs it a start and a store,
+    // as long as some two steps of a chip at work), if that gives no workgroup more than kMore steps beyond an equal share, or if all heads are short.
+    // Otherwise every workgroup has its equal share, wherever heads begin in it.
     int total = 0, longest = 0;
     for (int e0 = 0; e0 < entries; e0 += kWave) {
         entry(e0 + lane);
         total += e0 + lane < entries ? paged_units(my_rows, kStep) * weight : 0;
         longest = max(longest, my_rows);
     }
-    total = __builtin_amdgcn_readlane(wave_scan(total), kWave - 1);
-    // A workgroup that has all rows of its heads need not hand them over: worth it for up to three steps
-    int unit = kStep;
-    if (wave_max(longest) <= kAlone * kStep) {
-        unit = kAlone * kStep;
-        total = entries * weight;
+    const int most = paged_units(wave_max(longest), kStep);
+    int per, multiple;
+    if (most <= kAlone && cv.B * cv.H <= p.wgs) {
+        per = multiple = most;
+        total = cv.B * cv.H * most;
+    } else {
+        total = __builtin_amdgcn_readlane(wave_scan(total), kWave - 1);
+        const int share = total <= p.wgs ? 1 : uniform((total + p.wgs - 1) / p.wgs);
+        per = share;
+        multiple = 1;
+        for (int t = share; share > 1 && t <= share + kMore; ++t) {
+            const float inverse = inverse_of(t);
+            int parts = 0;
+            for (int e0 = 0; e0 < entries; e0 += kWave) {
+                if (entries > kWave) entry(e0 + lane);
+                parts += e0 + lane < entries ? paged_parts(paged_units(my_rows, kStep), t, inverse) * weight : 0;
+            }
+            parts = __builtin_amdgcn_readlane(wave_scan(parts), kWave - 1);
+            if (parts <= p.wgs) {
+                per = multiple = t;
+                total = parts * t;
+                break;
+            }
+        }
     }
-    const int per = (total + p.wgs - 1) / p.wgs;
+    const float per_inverse = inverse_of(per), multiple_inverse = inverse_of(multiple);
+    auto units_of = [&](int rows) { return multiple > 1 ? paged_parts(paged_units(rows, kStep), multiple, multiple_inverse) * multiple : paged_units(rows, kStep); };
     const int pos = wg * per;
     const int stop = min(pos + per, total);
     if (pos >= total) return;
     int e0 = 0, e = 0, cum = 0;      // entry that holds unit `pos`, and the units before it
     for (;; e0 += kWave) {
         if (entries > kWave) entry(e0 + lane);      // (else the lane has its entry still)
-        const int mine = e0 + lane < entries ? paged_units(my_rows, unit) * weight : 0;
+        const int mine = e0 + lane < entries ? units_of(my_rows) * weight : 0;
         const int incl = wave_scan(mine);
         const uint64_t beyond = ballot64(cum + incl > pos);
         if (beyond) {
@@ -304,15 +340,9 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
         }
         cum += __builtin_amdgcn_readlane(incl, kWave - 1);
     }
-    int rows = __builtin_amdgcn_readlane(my_rows, e - e0), len = __builtin_amdgcn_readlane(my_len, e - e0), units = paged_units(rows, unit);
-    int b, h;
-    if (per_head) {
-        b = e / cv.H;
-        h = e - b * cv.H;
-    } else {
-        b = e;
-        h = (pos - cum) / units;
-    }
+    int rows = __builtin_amdgcn_readlane(my_rows, e - e0), len = __builtin_amdgcn_readlane(my_len, e - e0), units = uniform(units_of(rows));
+    const int b0 = per_head ? uniform(paged_quotient(e, cv.H, inverse_of(cv.H))) : e;
+    int b = b0, h = per_head ? e - b0 * cv.H : uniform(paged_quotient(pos - cum, units, inverse_of(units)));
     int a = per_head ? cum : cum + h * units;       // unit at which the head starts
 
     // ---- a stretch within one head, and the wavefront's steps in it
@@ -323,15 +353,15 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     };
     auto stretch_at = [&](int pos) {
         Stretch t;
-        t.b = b;
-        t.h = h;
-        t.a = a;
-        t.units = units;
-        t.end = min(a + units, stop);
-        t.len = len;
-        t.first = (pos - a) * unit + 16 * wave;
-        const int r1 = min((t.end - a) * unit, rows);
-        t.steps = t.first < r1 ? (r1 - t.first + kStep - 1) / kStep : 0;
+        t.b = uniform(b);
+        t.h = uniform(h);
+        t.a = uniform(a);
+        t.units = uniform(units);
+        t.end = uniform(min(a + units, stop));
+        t.len = uniform(len);
+        t.first = uniform((pos - a) * kStep + 16 * wave);
+        const int r1 = min((t.end - a) * kStep, rows);
+        t.steps = uniform(t.first < r1 ? (r1 - t.first + kStep - 1) / kStep : 0);
         t.table = paged_table(cv, b, h);
         t.sel = p.sel ? p.sel + ((int64_t)b * cv.H + h) * p.keep : nullptr;
         return t;
@@ -374,92 +404,64 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
             }
         }
     };
-    // AHEAD steps are on their way: the registers of a step's keys are requested anew as soon as the first product has used them, those of its values
-    // behind the second.
-    Rows<T, D> x[AHEAD];
-    struct Where { int64_t off; int left; } where[AHEAD];
-    auto request_keys = [&](const Stretch &t, Pages &pages, int s, auto which) {
-        constexpr int W = decltype(which)::value;
+    // The next step is on its way while one is worked on: the registers of the keys are requested anew as soon as the first product has used them, those of
+    // the values behind the second, without asking whether there is another step (with a load that is issued or not, the compiler has the next step wait
+    // for everything under way).  Two steps ahead were no faster anywhere, and 0.8 us slower with one or two steps (the requests beyond the last).
+    Rows<T, D> x;
+    const char *values = nullptr;
+    int left = 0;
+    const int k_lane = c * cv.row_bytes + 16 * g, v_lane = 4 * g * cv.row_bytes + (VW == 2 ? 8 : 16) * c;
+    const int size_bytes = cv.counts ? 64 : 0;
+    auto request_keys = [&](const Stretch &t, Pages &pages, int s) {
         if (s % kWave == 0 && s != 0) {
             const Pages y = look_up(t, s);
             pages = {y.page, y.left, pages.bad | y.bad};
         }
         const int page = __builtin_amdgcn_readlane(pages.page, s % kWave), in_page = (t.first + s * kStep) & (cv.R - 1);
-        where[W] = {paged_offset(cv, page, t.h) + (int64_t)in_page * cv.row_bytes, __builtin_amdgcn_readlane(pages.left, s % kWave)};
-        load_keys<T, D>(x[W], cv.K + where[W].off, cv.row_bytes, g, c);
-        if (cv.counts) {
-            const int4 n = *reinterpret_cast<const int4 *>(cv.counts + paged_index(cv, page, t.h) * cv.R + in_page + 4 * g);
-            x[W].n[0] = n.x; x[W].n[1] = n.y; x[W].n[2] = n.z; x[W].n[3] = n.w;
-        }
+        const int64_t off = paged_offset(cv, page, t.h) + (int64_t)in_page * cv.row_bytes;
+        left = __builtin_amdgcn_readlane(pages.left, s % kWave);
+        values = cv.V + off;
+        load_keys<T, D>(x, rows_at(cv.K + off, left * cv.row_bytes), k_lane);
+        const char *sizes = reinterpret_cast<const char *>(cv.counts) + (paged_index(cv, page, t.h) * cv.R + in_page) * (int64_t)sizeof(int32_t);
+        const pag_u32x4 n = __builtin_amdgcn_raw_buffer_load_b128(rows_at(sizes, left > 0 ? size_bytes : 0), 16 * g, 0, 0);
+        x.n[0] = (int)n.x; x.n[1] = (int)n.y; x.n[2] = (int)n.z; x.n[3] = (int)n.w;
     };
-    auto request_values = [&](auto which) {
-        constexpr int W = decltype(which)::value;
-        load_values<T, D>(x[W], cv.V + where[W].off, cv.row_bytes, g, c);
-    };
-    constexpr std::integral_constant<int, 0> kEven{};
-    constexpr std::integral_constant<int, AHEAD - 1> kOdd{};
-    auto request_first = [&](const Stretch &t, Pages &pages) {
-        if (t.steps > 0) { request_keys(t, pages, 0, kEven); request_values(kEven); }
-        if (AHEAD > 1 && t.steps > 1) { request_keys(t, pages, 1, kOdd); request_values(kOdd); }
-    };
+    auto request_values = [&]() { load_values<T, D>(x, rows_at(values, left * cv.row_bytes), v_lane, cv.row_bytes); };
 
     Stretch cur = stretch_at(pos);
     load_queries(cur);
     Pages pages = look_up(cur, 0);
-    request_first(cur, pages);
+    request_keys(cur, pages, 0);
+    request_values();
     while (true) {
         const int64_t bh = (int64_t)cur.b * cv.H + cur.h;
-        // ---- the next head of the workgroup's stretch, if any: its pages are known by the time this one is done
-        const bool more = cur.end < stop;
-        Stretch nxt = cur;
-        Pages nxt_pages = {0, 0, 0};
-        if (more) {
-            a += units;
-            ++h;
-            if (h == cv.H) { h = 0; ++b; }
-            if (per_head || h == 0) {
-                ++e;
-                if (e - e0 == kWave) {
-                    e0 = e;
-                    entry(e0 + lane);
-                }
-                rows = __builtin_amdgcn_readlane(my_rows, e - e0);
-                len = __builtin_amdgcn_readlane(my_len, e - e0);
-                units = paged_units(rows, unit);
-            }
-            nxt = stretch_at(cur.end);
-            nxt_pages = look_up(nxt, 0);
-        }
-
         pag_f32x4 acc[NA];
 #pragma unroll
         for (int i = 0; i < NA; ++i) acc[i] = pag_f32x4{0.f, 0.f, 0.f, 0.f};
         float m_run = -INFINITY, l_run = 0.f;
-        auto step = [&](int s, auto which) {
-            constexpr int W = decltype(which)::value;
-            Rows<T, D> &r = x[W];
-            const int here = where[W].left;
+        for (int s = 0; s < cur.steps; ++s) {
+            const int here = left;
             pag_f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KL; ++ks) {
                 if constexpr (kBf16) {
 #pragma unroll
                     for (int k = QP - 1; k >= 0; --k)      // the smallest part first
-                        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, r.k[ks]), __builtin_bit_cast(pag_bf16x8, q[k][ks]), sc, 0, 0, 0);
+                        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, x.k[ks]), __builtin_bit_cast(pag_bf16x8, q[k][ks]), sc, 0, 0, 0);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(dword_of(r.k[ks], i)), __uint_as_float(dword_of(q[0][ks], i)), sc, 0, 0, 0);
+                        sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(dword_of(x.k[ks], i)), __uint_as_float(dword_of(q[0][ks], i)), sc, 0, 0, 0);
                 }
             }
             float sv[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 sv[i] = sc[i] * p.scale_log2;
-                if (cv.counts) sv[i] = r.n[i] > 0 ? sv[i] + __log2f((float)r.n[i]) : -INFINITY;
+                if (cv.counts) sv[i] = x.n[i] > 0 ? sv[i] + __log2f((float)x.n[i]) : -INFINITY;
                 if (4 * g + i >= here) sv[i] = -INFINITY;
             }
-            if (s + AHEAD < cur.steps) request_keys(cur, pages, s + AHEAD, which);
+            request_keys(cur, pages, s + 1);
             float m_loc = m_run;
 #pragma unroll
             for (int i = 0; i < 4; ++i) m_loc = fmaxf(m_loc, sv[i]);
@@ -480,20 +482,14 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[k][i] *= al[i];
             }
-            if (here < 16) {      // what lies behind the last row is not looked at (it may be anything, and 0 times a NaN is one)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int w = 0; w < VW; ++w) r.v[i][w] = 4 * g + i < here ? r.v[i][w] : 0u;
-            }
             if constexpr (kBf16) {
                 uint32_t p01[PP], p23[PP];
                 split_bf16<PP>(pi[0], pi[1], p01);
                 split_bf16<PP>(pi[2], pi[3], p23);
 #pragma unroll
                 for (int k = 0; k < NA; ++k) {
-                    const uint32_t lo = (k & 1) ? pack_hi(r.v[0][k / 2], r.v[1][k / 2]) : pack_lo(r.v[0][k / 2], r.v[1][k / 2]);
-                    const uint32_t hi = (k & 1) ? pack_hi(r.v[2][k / 2], r.v[3][k / 2]) : pack_lo(r.v[2][k / 2], r.v[3][k / 2]);
+                    const uint32_t lo = (k & 1) ? pack_hi(x.v[0][k / 2], x.v[1][k / 2]) : pack_lo(x.v[0][k / 2], x.v[1][k / 2]);
+                    const uint32_t hi = (k & 1) ? pack_hi(x.v[2][k / 2], x.v[3][k / 2]) : pack_lo(x.v[2][k / 2], x.v[3][k / 2]);
                     const pag_short4 bb = __builtin_bit_cast(pag_short4, make_uint2(lo, hi));
 #pragma unroll
                     for (int t = PP - 1; t >= 0; --t)
@@ -503,18 +499,37 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
 #pragma unroll
                 for (int k = 0; k < NA; ++k)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(pi[i], __uint_as_float(r.v[i][k]), acc[k], 0, 0, 0);
+                    for (int i = 0; i < 4; ++i) acc[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(pi[i], __uint_as_float(x.v[i][k]), acc[k], 0, 0, 0);
             }
-            if (s + AHEAD < cur.steps) request_values(which);
-        };
-        for (int s = 0; s < cur.steps; s += AHEAD) {
-            step(s, kEven);
-            if (AHEAD > 1 && s + 1 < cur.steps) step(s + 1, kOdd);
+            request_values();
         }
+        // ---- the next head of the workgroup's stretch, if any: its first rows are on their way while the results of this one are stored
+        const bool more = cur.end < stop;
+        Stretch nxt = cur;
+        Pages nxt_pages = {0, 0, 0};
+        if (more) {
+            a += units;
+            ++h;
+            if (h == cv.H) { h = 0; ++b; }
+            if (per_head || h == 0) {
+                ++e;
+                if (e - e0 == kWave) {
+                    e0 = e;
+                    entry(e0 + lane);
+                }
+                rows = __builtin_amdgcn_readlane(my_rows, e - e0);
+                len = __builtin_amdgcn_readlane(my_len, e - e0);
+                units = uniform(units_of(rows));
+            }
+            nxt = stretch_at(cur.end);
+            nxt_pages = look_up(nxt, 0);
+        }
+
         const bool bad = ballot64(pages.bad != 0) != 0ull;
         if (more) {
             load_queries(nxt);
-            request_first(nxt, nxt_pages);
+            request_keys(nxt, nxt_pages, 0);
+            request_values();
         }
 
         // ---- join the wavefronts
@@ -530,7 +545,7 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
         }
         if (g == 0) { s_m[wave][c] = m_run; s_l[wave][c] = lw; }
         __syncthreads();
-        const int w0 = paged_first_wg(cur.a, per), w1 = paged_last_wg(cur.a, cur.units, per);
+        const int w0 = uniform(paged_first_wg(cur.a, per, per_inverse)), w1 = uniform(paged_last_wg(cur.a, cur.units, per, per_inverse));
         const bool whole = w0 == w1;      // nobody else has a part of the head
         const int at = paged_place(wg, cur.a, per) * G * kStride;
         for (int i = tid; i < G * (D / 4); i += kPagThreads) {

@@ -21,12 +21,24 @@ constexpr int paged_append_slots(int N, int R, int P) {
     return most < P ? (int)most : P;
 }
 
-// ---- sc_paged_decode_attn: units of rows, laid end to end over all heads, in equal stretches of `per`
+// ---- sc_paged_decode_attn
+// x / y for x >= 0, y > 0 and quotients up to 2^20, given 1 / y up to a few roundings (the kernel's lengths are on the device, and a division there costs
+// as much as a trip to the cache)
+constexpr int paged_quotient(int x, int y, float inverse) {
+    int q = (int)((float)x * inverse);
+    const int rest = x - q * y;
+    q += rest >= y ? 1 : 0;
+    return rest < 0 ? q - 1 : q;
+}
+// Units of rows, laid end to end over all heads.  A head's units are rounded up to a multiple of what a workgroup takes (`multiple`; 1: not at all).
 constexpr int paged_units(int rows, int unit) { return rows > unit ? (int)(((int64_t)rows + unit - 1) / unit) : 1; }
-// The head of units [a, a + units): the workgroups that hold a part of it, and where workgroup w leaves its partial result.  Every workgroup has two
-// places: for the stretch at its start, and for one that begins later in it (only a head's first workgroup can have begun with another head).
-constexpr int paged_first_wg(int a, int per) { return a / per; }
-constexpr int paged_last_wg(int a, int units, int per) { return (a + units - 1) / per; }
+// workgroups of a head that take up to `per` units each and nothing of another head
+constexpr int paged_parts(int units, int per, float inverse) { return paged_quotient(units + per - 1, per, inverse); }
+// The head of units [a, a + units), in stretches of `per`: the workgroups that hold a part of it, and where workgroup w leaves its partial result.
+// Every workgroup has two places: for the stretch at its start, and for one that begins later in it (only a head's first workgroup can have begun with
+// another head).
+constexpr int paged_first_wg(int a, int per, float inverse) { return paged_quotient(a, per, inverse); }
+constexpr int paged_last_wg(int a, int units, int per, float inverse) { return paged_quotient(a + units - 1, per, inverse); }
 constexpr int paged_place(int w, int a, int per) { return 2 * w + (a > w * per ? 1 : 0); }
 
 // n partial results of G heads are joined at once, or in groups of this many first

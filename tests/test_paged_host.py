@@ -126,6 +126,7 @@ def test_workspace(lib):
 
 
 WORDS = r"""
+#include <math.h>
 #include <stdio.h>
 #include <stdlib.h>
 #include <algorithm>
@@ -145,6 +146,13 @@ static int weird(int most) {
         case 3: return 2147483647;
         default: return any(0, most - 1);
     }
+}
+
+// 1 / y with an error of up to three roundings
+static float inverse_of(int y) {
+    float f = 1.0f / (float)y;
+    for (int k = any(-3, 3); k; k += k > 0 ? -1 : 1) f = nextafterf(f, k > 0 ? 2.0f * f : 0.0f);
+    return f;
 }
 
 // a table (a selection) that knows which of its entries may be read
@@ -180,7 +188,26 @@ int main() {
             CHECK((long long)units.back() * unit >= rows && units.back() >= 1 && (units.back() == 1 || (units.back() - 1) * unit < rows));
             total += units.back();
         }
-        const int per = (total + wgs - 1) / wgs;
+        // equal shares, or heads rounded up to a multiple of a workgroup's units
+        int per = (total + wgs - 1) / wgs, multiple = 1;
+        if (any(0, 1)) {
+            for (multiple = per;; ++multiple) {
+                int parts = 0;
+                for (int u : units) parts += paged_parts(u, multiple, inverse_of(multiple));
+                if (parts <= wgs || multiple > 4 * per + 400) break;
+            }
+            int parts = 0;
+            for (int &u : units) {
+                const int n = paged_parts(u, multiple, inverse_of(multiple));
+                CHECK(n * multiple >= u && (n - 1) * multiple < u);
+                parts += n;
+                u = n * multiple;
+            }
+            if (parts > wgs) continue;
+            per = multiple;
+            total = parts * multiple;
+        }
+        const float inverse = inverse_of(per);
         std::vector<int> covered(total, 0), places(2 * wgs, -1), left(heads, 0);
         for (int w = 0; w < wgs; ++w) {
             int pos = w * per;
@@ -190,11 +217,11 @@ int main() {
             for (; pos < stop; a += units[h++]) {
                 const int end = std::min(a + units[h], stop);
                 for (int u = pos; u < end; ++u) covered[u]++;
-                const int w0 = paged_first_wg(a, per), w1 = paged_last_wg(a, units[h], per);
-                CHECK(w0 <= w && w <= w1);
-                if (pos == a && end == a + units[h]) CHECK(w0 == w1);
+                const int w0 = paged_first_wg(a, per, inverse), w1 = paged_last_wg(a, units[h], per, inverse);
+                CHECK(w0 == a / per && w1 == (a + units[h] - 1) / per && w0 <= w && w <= w1);
+                if (multiple > 1) CHECK(pos == w * per && end == stop);      // parts of one head only
+                if (w0 == w1) CHECK(pos == a && end == a + units[h]);
                 else {
-                    CHECK(w0 < w1);
                     const int place = paged_place(w, a, per);
                     CHECK(place >= 0 && place < 2 * wgs && places[place] == -1);
                     places[place] = h;
@@ -205,10 +232,19 @@ int main() {
         }
         for (int u = 0; u < total; ++u) CHECK(covered[u] == 1);
         for (int h = 0, a = 0; h < heads; a += units[h++]) {
-            const int w0 = paged_first_wg(a, per), w1 = paged_last_wg(a, units[h], per);
+            const int w0 = paged_first_wg(a, per, inverse), w1 = paged_last_wg(a, units[h], per, inverse);
             CHECK(left[h] == (w1 > w0 ? w1 - w0 + 1 : 0));
             if (w1 > w0) for (int w = w0; w <= w1; ++w) CHECK(places[paged_place(w, a, per)] == h);
         }
+    }
+    // ---- quotients, from inverses that are off by some roundings
+    for (int t = 0; t < 2000000; ++t) {
+        const int y = any(0, 1) ? any(1, 300) : 1 + (int)((long long)rand() * rand() % (1 << 30)), most = (int)std::min<long long>(2147483647ll - 2 * y, (1ll << 20) * y);
+        if (most <= 0) continue;
+        int x = (int)(((long long)rand() << 20 ^ rand()) % most);
+        if (any(0, 2) == 0) x = x / y * y;
+        if (any(0, 2) == 0 && x >= y) x = x / y * y - 1;
+        CHECK(paged_quotient(x, y, inverse_of(y)) == x / y);
     }
     // ---- groups of partial results: of one size, few enough to be joined in the shared memory of a workgroup
     for (int n = 1; n <= 512; ++n)
