@@ -33,6 +33,35 @@ __device__ __forceinline__ int64_t paged_index(const PagedView &c, int page, int
 }
 __device__ __forceinline__ bool paged_bad(const PagedView &c, int page) { return (unsigned)page >= (unsigned)c.num_pages; }
 
+// ---- across the lanes
+// Sums over the lanes up to each one (DPP moves inside the rows of 16 lanes, then from row to row), and the maximum over all of them
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_rows(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int x) {
+    x += dpp_rows<0x111, 0xf>(x);      // row_shr 1, 2, 4, 8
+    x += dpp_rows<0x112, 0xf>(x);
+    x += dpp_rows<0x114, 0xf>(x);
+    x += dpp_rows<0x118, 0xf>(x);
+    x += dpp_rows<0x142, 0xa>(x);      // row_bcast 15: lane 15 to the second row, lane 47 to the fourth
+    x += dpp_rows<0x143, 0xc>(x);      // row_bcast 31: lane 31 to the upper half
+    return x;
+}
+__device__ __forceinline__ int wave_max(int x) {      // x >= 0
+    x = max(x, dpp_rows<0x111, 0xf>(x));
+    x = max(x, dpp_rows<0x112, 0xf>(x));
+    x = max(x, dpp_rows<0x114, 0xf>(x));
+    x = max(x, dpp_rows<0x118, 0xf>(x));
+    x = max(x, dpp_rows<0x142, 0xa>(x));
+    x = max(x, dpp_rows<0x143, 0xc>(x));
+    return __builtin_amdgcn_readlane(x, kWave - 1);
+}
+
+__device__ __forceinline__ float row_allreduce_max(float x) {      // over the 16 lanes of a row
+    x = fmaxf(x, dpp<kDppQuadXor1>(x));
+    x = fmaxf(x, dpp<kDppQuadXor2>(x));
+    x = fmaxf(x, dpp<kDppHalfMirror>(x));
+    return fmaxf(x, dpp<kDppMirror>(x));
+}
+
 // ---- sc_paged_append
 struct PagedAppendArgs {
     PagedView c;

@@ -24,6 +24,7 @@ constexpr int kStep = 16 * kPagWaves;        // rows of a step of all wavefronts
 constexpr int kAlone = 2;                    // steps up to which a head goes to one workgroup, if there is one for every head
 constexpr int kMore = 2;                     // steps beyond an equal share for which workgroups have parts of one head only
 constexpr int kMaxWgs = 256;                 // one on each compute unit
+constexpr int kMaxPairs = 512;              // (part, head) pairs that are joined at once, heads up to a power of two (paged_group)
 constexpr int kPagPad = 4;                   // floats behind the sums of a partial result: maximum, sum, two unused
 constexpr int kMaxHeadWgs = 64;              // workgroups per (sequence, KV head) at most, on average: each is a partial result to join
 constexpr float kPagLog2e = 1.4426950408889634f;
@@ -57,27 +58,6 @@ struct PagDecParams {
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ float inverse_of(int y) { return __builtin_amdgcn_rcpf((float)y); }
 __device__ __forceinline__ float pag_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Sums over the lanes up to each one (DPP moves inside the rows of 16 lanes, then from row to row), and the maximum over all of them
-template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_rows(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
-__device__ __forceinline__ int wave_scan(int x) {
-    x += dpp_rows<0x111, 0xf>(x);      // row_shr 1, 2, 4, 8
-    x += dpp_rows<0x112, 0xf>(x);
-    x += dpp_rows<0x114, 0xf>(x);
-    x += dpp_rows<0x118, 0xf>(x);
-    x += dpp_rows<0x142, 0xa>(x);      // row_bcast 15: lane 15 to the second row, lane 47 to the fourth
-    x += dpp_rows<0x143, 0xc>(x);      // row_bcast 31: lane 31 to the upper half
-    return x;
-}
-__device__ __forceinline__ int wave_max(int x) {      // x >= 0
-    x = max(x, dpp_rows<0x111, 0xf>(x));
-    x = max(x, dpp_rows<0x112, 0xf>(x));
-    x = max(x, dpp_rows<0x114, 0xf>(x));
-    x = max(x, dpp_rows<0x118, 0xf>(x));
-    x = max(x, dpp_rows<0x142, 0xa>(x));
-    x = max(x, dpp_rows<0x143, 0xc>(x));
-    return __builtin_amdgcn_readlane(x, kWave - 1);
-}
 
 // x as NP bf16 parts whose sum it is (up to the last one's rounding)
 template <int NP> __device__ __forceinline__ void split_bf16(float x0, float x1, uint32_t (&part)[NP]) {
@@ -141,13 +121,6 @@ template <typename T, int D> struct Acc {
     }
 };
 
-__device__ __forceinline__ float row_allreduce_max(float x) {      // over the 16 lanes of a row
-    x = fmaxf(x, dpp<kDppQuadXor1>(x));
-    x = fmaxf(x, dpp<kDppQuadXor2>(x));
-    x = fmaxf(x, dpp<kDppHalfMirror>(x));
-    return fmaxf(x, dpp<kDppMirror>(x));
-}
-
 // ------------------------------------------------------------------------------------------------
 // Partial results: [place][head][D + kPagPad] floats, written through to memory and read from there (the workgroups of a head run on chiplets whose
 // L2s do not see each other's lines within a kernel).
@@ -167,80 +140,82 @@ template <int D> __device__ __forceinline__ void store_part(__amdgpu_buffer_rsrc
     }
 }
 
-// Joins n partial results, whose places `place_of` gives, and hands each of the G D / 4 pieces to `sink` with its head's maximum and sum.
+// Joins n partial results, whose places `place_of` gives, and hands each of the G D / 4 pieces of 16 bytes to `sink` with its head's maximum and sum.
 // A thread owns one piece of one head and every NS-th part; all its loads of a pass are on their way before the first is used.
 template <int D, typename PlaceOf, typename Sink>
-__device__ __forceinline__ void join_parts(const PagDecParams &p, __amdgpu_buffer_rsrc_t rs, int n, PlaceOf place_of, int tid, float *s_buf, float *s_total, Sink sink) {
+__device__ __forceinline__ void join_parts(const PagDecParams &p, __amdgpu_buffer_rsrc_t rs, int n, PlaceOf place_of, int tid, float *s_red, float (*s_weight)[kMaxPairs],
+                                           float *s_total, Sink sink) {
     constexpr int QPR = D / 4, kStride = D + kPagPad, PASS = 8;
-    const int G = p.G, lane = tid % kWave, wave = tid / kWave;
-    const int pieces = G * QPR;
-    // thread -> (group of parts, piece); with more pieces than threads, every thread takes several pieces
-    const int NS = pieces < kPagThreads ? kPagThreads / pieces : 1;
+    constexpr int kNowhere = 0x7FFFFFF0;      // beyond the descriptor: zeros, and no memory traffic
+    static_assert(16 * QPR <= kPagThreads, "a thread for every piece");
+    const int G = p.G, lane = tid % kWave, wave = uniform(tid / kWave);
     const int log2_G = G > 1 ? 32 - __clz(G - 1) : 0;      // heads of a part, up to a power of two
-    float *s_m = s_buf, *s_l = s_m + (n << log2_G), *s_red = s_l + ((n << log2_G) + 3) / 4 * 4;
-    for (int piece0 = 0; piece0 < pieces; piece0 += kPagThreads) {
-        const int sg = NS > 1 ? tid / pieces : 0, piece = piece0 + (NS > 1 ? tid - sg * pieces : tid);
-        const bool worker = sg < NS && piece < pieces;
-        const int hh = worker ? piece / QPR : 0, e = worker ? 4 * (piece - hh * QPR) : 0;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k0 = 0; k0 < n; k0 += NS * PASS) {
-            float4 x[PASS];
+    const int pieces = G * QPR;
+    const float pieces_inverse = inverse_of(pieces);
+    const int NS = min(uniform(paged_quotient(kPagThreads, pieces, pieces_inverse)), n);
+    const int sg = paged_quotient(tid, pieces, pieces_inverse), piece = tid - sg * pieces;
+    const bool worker = sg < NS;
+    const int hh = piece / QPR, e = 4 * (piece - hh * QPR);
+    float *s_m = s_weight[0], *s_l = s_weight[1];
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = 0; k0 < n; k0 += NS * PASS) {
+        pag_u32x4 x[PASS];
 #pragma unroll
-            for (int t = 0; t < PASS; ++t) {
+        for (int t = 0; t < PASS; ++t)
+            if (k0 + NS * t < n) {
                 const int k = k0 + sg + NS * t;
-                const bool there = worker && k < n;
-                const pag_u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(rs, there ? ((place_of(k) * G + hh) * kStride + e) * 4 : 0x7FFFFFF0, 0, kAuxAgent);
-                x[t] = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
+                x[t] = __builtin_amdgcn_raw_buffer_load_b128(rs, worker && k < n ? ((place_of(k) * G + hh) * kStride + e) * 4 : kNowhere, 0, kAuxAgent);
             }
-            __builtin_amdgcn_sched_barrier(0);
-            if (piece0 == 0 && k0 == 0) {      // the weights: a wavefront per head
-                for (int i = tid; i < n << log2_G; i += kPagThreads) {
-                    const int k = i >> log2_G, h2 = i & ((1 << log2_G) - 1);
-                    const pag_u32x2 t = __builtin_amdgcn_raw_buffer_load_b64(rs, h2 < G ? ((place_of(k) * G + h2) * kStride + D) * 4 : 0x7FFFFFF0, 0, kAuxAgent);
-                    s_m[i] = __uint_as_float(t.x);
-                    s_l[i] = __uint_as_float(t.y);
-                }
-                __syncthreads();
-                for (int h2 = wave; h2 < G; h2 += kPagWaves) {
-                    float m = -INFINITY;
-                    for (int k = lane; k < n; k += kWave) m = fmaxf(m, s_m[(k << log2_G) + h2]);
-                    m = rows_allreduce_max(row_allreduce_max(m));
-                    const float safe = m == -INFINITY ? 0.f : m;
-                    float l = 0.f;
-                    for (int k = lane; k < n; k += kWave) {
-                        const float f = pag_exp2(s_m[(k << log2_G) + h2] - safe);
-                        s_m[(k << log2_G) + h2] = f;
-                        l = fmaf(s_l[(k << log2_G) + h2], f, l);
-                    }
-                    l = rows_allreduce_sum(row_allreduce_sum<16>(l));
-                    if (lane == 0) {
-                        s_total[h2] = m;
-                        s_total[16 + h2] = l;
-                    }
-                }
-                __syncthreads();
+        if (k0 == 0) {      // the weights: a wavefront per head
+            for (int i = tid; i < n << log2_G; i += kPagThreads) {
+                const int k = i >> log2_G, h2 = i & ((1 << log2_G) - 1);
+                const pag_u32x2 t = __builtin_amdgcn_raw_buffer_load_b64(rs, h2 < G ? ((place_of(k) * G + h2) * kStride + D) * 4 : kNowhere, 0, kAuxAgent);
+                s_m[i] = __uint_as_float(t.x);
+                s_l[i] = __uint_as_float(t.y);
             }
+            __syncthreads();
+            for (int h2 = wave; h2 < G; h2 += kPagWaves) {
+                float m = -INFINITY;
+                for (int k = lane; k < n; k += kWave) m = fmaxf(m, s_m[(k << log2_G) + h2]);
+                m = rows_allreduce_max(row_allreduce_max(m));
+                const float safe = m == -INFINITY ? 0.f : m;
+                float l = 0.f;
+                for (int k = lane; k < n; k += kWave) {
+                    const float f = pag_exp2(s_m[(k << log2_G) + h2] - safe);
+                    s_m[(k << log2_G) + h2] = f;
+                    l = fmaf(s_l[(k << log2_G) + h2], f, l);
+                }
+                l = rows_allreduce_sum(row_allreduce_sum<16>(l));
+                if (lane == 0) {
+                    s_total[h2] = m;
+                    s_total[16 + h2] = l;
+                }
+            }
+            __syncthreads();
+        }
 #pragma unroll
-            for (int t = 0; t < PASS; ++t) {
+        for (int t = 0; t < PASS; ++t)
+            if (k0 + NS * t < n) {
                 const int k = k0 + sg + NS * t;
                 const float f = worker && k < n ? s_m[(k << log2_G) + hh] : 0.f;
-                o.x = fmaf(x[t].x, f, o.x);
-                o.y = fmaf(x[t].y, f, o.y);
-                o.z = fmaf(x[t].z, f, o.z);
-                o.w = fmaf(x[t].w, f, o.w);
+                o.x = fmaf(__uint_as_float(x[t].x), f, o.x);
+                o.y = fmaf(__uint_as_float(x[t].y), f, o.y);
+                o.z = fmaf(__uint_as_float(x[t].z), f, o.z);
+                o.w = fmaf(__uint_as_float(x[t].w), f, o.w);
+            }
+    }
+    if (NS > 1) {
+        if (worker && sg > 0) *reinterpret_cast<float4 *>(s_red + 4 * tid) = o;
+        __syncthreads();
+        if (sg == 0) {
+#pragma unroll 4
+            for (int r = 1; r < NS; ++r) {
+                const float4 t = *reinterpret_cast<const float4 *>(s_red + 4 * (r * pieces + piece));
+                o.x += t.x; o.y += t.y; o.z += t.z; o.w += t.w;
             }
         }
-        if (NS > 1) {
-            if (worker) *reinterpret_cast<float4 *>(s_red + 4 * (sg * pieces + piece)) = o;
-            __syncthreads();
-            if (worker && sg == 0)
-                for (int r = 1; r < NS; ++r) {
-                    const float4 t = *reinterpret_cast<const float4 *>(s_red + 4 * (r * pieces + piece));
-                    o.x += t.x; o.y += t.y; o.z += t.z; o.w += t.w;
-                }
-        }
-        if (worker && sg == 0) sink(hh, e, o, s_total[hh], s_total[16 + hh]);
     }
+    if (sg == 0) sink(hh, e, o, s_total[hh], s_total[16 + hh]);
 }
 
 // a workgroup's results are on their way to memory: waits until they are there, counts the workgroup off, and tells the last of `n` (counter clear again)
@@ -273,7 +248,7 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     __shared__ __attribute__((aligned(16))) float s_acc[kPagWaves * 16 * D];
     __shared__ float s_m[kPagWaves][16], s_l[kPagWaves][16];
     __shared__ int s_last;
-    __shared__ float s_total[32];
+    __shared__ float s_weight[2][kMaxPairs], s_total[32];
     const auto rs = __builtin_amdgcn_make_buffer_rsrc(p.part, (short)0, 2 * kMaxWgs * G * kStride * 4, 0x00020000);
 
     // ---- my stretch of all units: every wavefront adds up the lengths, 64 at a time
@@ -579,7 +554,7 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
             bool result = groups == 1;
             while (last_of(counter, parts, tid, &s_last)) {
                 const int to = place_of(from) * G * kStride;
-                join_parts<D>(p, rs, parts, [&](int k) { return place_of(from + k * by); }, tid, s_acc, s_total, [&](int hh, int el, const float4 &o, float m, float l) {
+                join_parts<D>(p, rs, parts, [&](int k) { return place_of(from + k * by); }, tid, s_acc, s_weight, s_total, [&](int hh, int el, const float4 &o, float m, float l) {
                     if (result) store_result(p, bh * G + hh, D, el, o, m, l);
                     else store_part<D>(rs, to + hh * kStride, el, o, m, l);
                 });

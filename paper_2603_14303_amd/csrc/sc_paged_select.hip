@@ -10,10 +10,12 @@
 
 namespace sc {
 
+typedef double sel_f64x4 __attribute__((ext_vector_type(4)));
+
 struct PagSelParams {
     PagedView c;
     const void *Q;
-    int G;
+    int q_is_bf16, G;
     const int32_t *lens;
     int lens_per_head;
     int keep, first, recent;
@@ -37,37 +39,44 @@ __device__ __forceinline__ int held_pages(const PagSelParams &p, int64_t bh, int
     const int len = min(max(p.lens[p.lens_per_head ? bh : b], 0), p.c.P << p.c.log2_R);
     return (len + p.c.R - 1) >> p.c.log2_R;
 }
-// 16 bytes as 8 (bf16) or 4 (fp32) numbers
-__device__ __forceinline__ void widen(const uint4 &v, float (&x)[8]) {
-    x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
-    x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
-}
-__device__ __forceinline__ void widen(const uint4 &v, float (&x)[4]) {
-    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
-}
-template <int N> __device__ __forceinline__ void query_piece(const bf16_t *q, float (&x)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = __uint_as_float((uint32_t)q[i].bits << 16);
-}
-template <int N> __device__ __forceinline__ void query_piece(const float *q, float (&x)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = q[i];
+// element i of 16 bytes of the type
+template <typename T> __device__ __forceinline__ double element(const uint4 &v, int i) {
+    if constexpr (sizeof(T) == 2) return (double)((i & 1) ? bf16_hi(dword_of(v, i / 2)) : bf16_lo(dword_of(v, i / 2)));
+    else return (double)__uint_as_float(dword_of(v, i));
 }
 
-template <typename T, typename TQ, int D>
+// A wavefront has 16 pages, the columns of its products; a lane holds of its page (lane % 16) every fourth piece of 16 bytes.  The heads are the rows, in
+// fp64 in shared memory, their positive and their negative parts side by side.  NT: groups of four heads (v_mfma_f64_4x4x4_4b: four products of 4 heads x
+// 4 pages), or 0: 16 heads (v_mfma_f64_16x16x4).  Bound by the matrix cores with several heads: us for 2048 pages x 8 heads, G = 4, and for 1100 to 2048
+// pages x 32 heads, G = 7, both d = 128, bf16: groups of four 4.9 and 11.1, 16 heads 5.3 and 13.8, vector instructions 7.0 and 31.8.
+template <typename T, int D, int NT>
 __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams p) {
     constexpr int E = 16 / (int)sizeof(T);            // elements of 16 bytes
     constexpr int KL = D / (4 * E);                   // pieces of a row per lane: 4 lanes share a row
+    constexpr int HEADS = NT ? 4 * NT : 16, STRIDE = HEADS + 1;
+    __shared__ double2 s_q[D * STRIDE];
     const PagedView &cv = p.c;
     const int64_t bh = blockIdx.x / p.tiles;
     const int tile = (int)(blockIdx.x - bh * p.tiles);
     const int b = (int)(bh / cv.H), h = (int)(bh - (int64_t)b * cv.H);
     const int lane = threadIdx.x % kWave, g = lane / 16, c = lane % 16;
-    const int place = tile * kScorePages + 16 * (int)(threadIdx.x / kWave) + c;      // the lane's page: column c of the products
     const int pages = held_pages(p, bh, b);
-    if (place - c >= pages) return;
+    if (tile * kScorePages >= pages) return;
+    const int place = tile * kScorePages + 16 * (int)(threadIdx.x / kWave) + c;      // the lane's page: column c of the products
     const int page = place < pages ? paged_table(cv, b, h)[place] : 0;
     const bool there = place < pages && !paged_bad(cv, page);
+    // heads behind the group are its last one again and do not change the maximum; a thread has PER neighbouring elements of a head
+    constexpr int PER = D * HEADS / kScoreThreads, TPH = kScoreThreads / HEADS;
+    const int head = threadIdx.x / TPH, e0 = threadIdx.x % TPH * PER;
+    const int64_t q_at = (bh * p.G + min(head, p.G - 1)) * D + e0;
+    double x[PER];
+    if (p.q_is_bf16) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) x[i] = load1_f64(reinterpret_cast<const bf16_t *>(p.Q) + q_at + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) x[i] = load1_f64(reinterpret_cast<const float *>(p.Q) + q_at + i);
+    }
     const int64_t row = paged_index(cv, there ? page : 0, h) * D;
     uint4 lo[KL], hi[KL];
 #pragma unroll
@@ -75,32 +84,47 @@ __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams
         lo[ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(cv.k_min) + row + E * (4 * ks + g));
         hi[ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(cv.k_max) + row + E * (4 * ks + g));
     }
-    // v_mfma_f64_4x4x4_4b: four products of 4 heads x 4 pages, the lanes' pages being the columns of all four; heads behind the group are its last one
-    // again and do not change the maximum
-    double best = 0.0;
-    for (int h0 = 0; h0 < p.G; h0 += 4) {
-        const TQ *q = reinterpret_cast<const TQ *>(p.Q) + (bh * p.G + min(h0 + lane % 4, p.G - 1)) * D;
-        double acc = 0.0;
 #pragma unroll
-        for (int ks = 0; ks < KL; ++ks) {
-            float x[E], l[E], u[E];
-            query_piece<E>(q + E * (4 * ks + g), x);
-            widen(lo[ks], l);
-            widen(hi[ks], u);
+    for (int i = 0; i < PER; ++i) s_q[(e0 + i) * STRIDE + head] = make_double2(x[i] < 0.0 ? 0.0 : x[i], x[i] > 0.0 ? 0.0 : x[i]);      // (a NaN is in both)
+    __syncthreads();
+    double best;
+    if constexpr (NT > 0) {
+        double acc[NT] = {};
+#pragma unroll
+        for (int ks = 0; ks < KL; ++ks)
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                // (a NaN in a query goes through either product)
-                acc = __builtin_amdgcn_mfma_f64_4x4x4f64((double)(x[i] < 0.f ? 0.f : x[i]), (double)u[i], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f64_4x4x4f64((double)(x[i] > 0.f ? 0.f : x[i]), (double)l[i], acc, 0, 0, 0);
-            }
-        }
-        // the maximum over the heads: over the lanes that share the page (whatever head is where)
+                const double u = element<T>(hi[ks], i), l = element<T>(lo[ks], i);
+                const double2 *q = s_q + (E * (4 * ks + g) + i) * STRIDE + lane % 4;
 #pragma unroll
-        for (int off = 16; off < kWave; off <<= 1) {
-            const double other = __shfl_xor(acc, off, kWave);
-            acc = (other > acc || other != other) ? other : acc;
-        }
-        best = (h0 == 0 || acc > best || acc != acc) ? acc : best;
+                for (int t = 0; t < NT; ++t) {
+                    const double2 y = q[4 * t];
+                    acc[t] = __builtin_amdgcn_mfma_f64_4x4x4f64(y.x, u, acc[t], 0, 0, 0);
+                    acc[t] = __builtin_amdgcn_mfma_f64_4x4x4f64(y.y, l, acc[t], 0, 0, 0);
+                }
+            }
+        best = acc[0];
+#pragma unroll
+        for (int t = 1; t < NT; ++t) best = (acc[t] > best || acc[t] != acc[t]) ? acc[t] : best;
+    } else {
+        sel_f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+        for (int ks = 0; ks < KL; ++ks)
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const double2 y = s_q[(E * (4 * ks + g) + i) * STRIDE + c];
+                acc = __builtin_amdgcn_mfma_f64_16x16x4f64(y.x, element<T>(hi[ks], i), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f64_16x16x4f64(y.y, element<T>(lo[ks], i), acc, 0, 0, 0);
+            }
+        best = acc[0];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) best = (acc[i] > best || acc[i] != acc[i]) ? acc[i] : best;
+    }
+    // the maximum over the heads: over the lanes that share the page (whatever head is where)
+#pragma unroll
+    for (int off = 16; off < kWave; off <<= 1) {
+        const double other = __shfl_xor(best, off, kWave);
+        best = (other > best || other != other) ? other : best;
     }
     if (g == 0 && place < pages) {
         unsigned long long key = there ? score_key(best) : kKeyNaN;
@@ -116,15 +140,6 @@ constexpr int kBuckets = 2048, kRanked = 256, kSelWaves = kSelThreads / kWave;
 
 __device__ __forceinline__ double key_score(unsigned long long k) { return __builtin_bit_cast(double, (k >> 63) ? k & ~(1ull << 63) : ~k); }
 
-__device__ __forceinline__ int scan_add(int x) {      // over the lanes up to each one
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const int t = __shfl_up(x, off, kWave);
-        x += (int)(threadIdx.x % kWave) >= off ? t : 0;
-    }
-    return x;
-}
-
 __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams p) {
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / p.c.H);
@@ -137,10 +152,10 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
         return;
     }
     const unsigned long long *keys = p.keys + bh * p.c.P;
-    constexpr int K = 4;                                // keys that a thread keeps in registers; those behind them are read again
+    constexpr int K = kWave / kSelWaves;                // keys that a thread keeps in registers; those behind them are read again
     __shared__ int s_hist[kBuckets];
     __shared__ float s_low[kSelWaves], s_high[kSelWaves];
-    __shared__ int s_above[kSelWaves], s_equal[kSelWaves];
+    __shared__ int s_above[kSelWaves], s_count[kWave];
     __shared__ int s_bucket, s_need, s_ranked;
     __shared__ unsigned long long s_key[kRanked], s_border;
     __shared__ int s_place[kRanked], s_border_place;
@@ -162,19 +177,14 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
             high = fmaxf(high, x);
         }
     });
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        low = fminf(low, __shfl_xor(low, off, kWave));
-        high = fmaxf(high, __shfl_xor(high, off, kWave));
-    }
+    low = -rows_allreduce_max(row_allreduce_max(-low));
+    high = rows_allreduce_max(row_allreduce_max(high));
     if (lane == 0) { s_low[wave] = low; s_high[wave] = high; }
     for (int i = tid; i < kBuckets; i += kSelThreads) s_hist[i] = 0;
     if (tid == 0) s_ranked = 0;
     __syncthreads();
-    for (int w = 0; w < kSelWaves; ++w) {
-        low = fminf(low, s_low[w]);
-        high = fmaxf(high, s_high[w]);
-    }
+    low = -row_allreduce_max(-s_low[lane % kSelWaves]);
+    high = row_allreduce_max(s_high[lane % kSelWaves]);
     const float spread = high > low ? (float)(kBuckets - 5) / (high - low) : 0.f;      // (0 too where high - low is not finite)
     auto bucket = [&](unsigned long long k) {      // never falls where the key grows
         if (k >= kKeyNaN) return kBuckets - 1 - (int)(k == kKeyNaN);
@@ -186,7 +196,7 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
     // ---- the bucket of rank keep: thread t has buckets kBuckets - 1 - 2 t and the one below
     {
         const int v0 = s_hist[kBuckets - 1 - 2 * tid], v1 = s_hist[kBuckets - 2 - 2 * tid];
-        const int upto = scan_add(v0 + v1);
+        const int upto = wave_scan(v0 + v1);
         if (lane == kWave - 1) s_above[wave] = upto;
         __syncthreads();
         int before = upto - v0 - v1;
@@ -234,7 +244,7 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
                 int v[4], sum = 0;
 #pragma unroll
                 for (int t = 0; t < 4; ++t) { v[t] = s_hist[255 - 4 * lane - t]; sum += v[t]; }
-                int before = scan_add(sum) - sum;
+                int before = wave_scan(sum) - sum;
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     if (before < need && before + v[t] >= need) { s_bucket = 255 - 4 * lane - t; s_need = need - before; }
@@ -247,46 +257,51 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
             need = s_need;
         }
     }
-    // ---- the places, ascending: keys above the border's, and of those equal to it the first ones (up to a place, or `need` of them)
+    // ---- the places, ascending: keys above the border's, and of those equal to it the first ones (up to a place, or `need` of them); K stretches of
+    // kSelThreads pages at a time, lane 16 k + w of every wavefront counting for stretch k and wavefront w
     const bool by_place = border_place < n;
-    int above0 = 0, equal0 = 0;      // before this stretch of kSelThreads pages
-    for (int k = 0, i0 = 0; i0 < n; ++k, i0 += kSelThreads) {
-        const int i = i0 + tid;
-        unsigned long long x = 0ull;
-        if (k < K) {
+    int above0 = 0, equal0 = 0;
+    for (int i0 = 0; i0 < n; i0 += K * kSelThreads) {
+        uint64_t ba[K], be[K];
 #pragma unroll
-            for (int t = 0; t < K; ++t) x = t == k ? mine[t] : x;
-        } else if (i < n) {
-            x = keys[i];
+        for (int k = 0; k < K; ++k) {
+            const int i = i0 + k * kSelThreads + tid;
+            const unsigned long long x = i0 == 0 ? mine[k] : i < n ? keys[i] : 0ull;
+            ba[k] = ballot64(i < n && (x > border || (by_place && x == border && i <= border_place)));
+            be[k] = ballot64(!by_place && i < n && x == border);
         }
-        const bool is_equal = !by_place && i < n && x == border, is_above = i < n && (x > border || (by_place && x == border && i <= border_place));
-        const uint64_t ba = ballot64(is_above), be = ballot64(is_equal);
-        __syncthreads();
-        if (lane == 0) { s_above[wave] = __popcll(ba); s_equal[wave] = __popcll(be); }
-        __syncthreads();
-        int above = above0, equal = equal0;
+        if (i0 > 0) __syncthreads();
+        if (lane < K) {
+            uint64_t a = 0, e = 0;
 #pragma unroll
-        for (int w = 0; w < kSelWaves; ++w) {
-            above += w < wave ? s_above[w] : 0;
-            equal += w < wave ? s_equal[w] : 0;
-            above0 += s_above[w];
-            equal0 += s_equal[w];
+            for (int k = 0; k < K; ++k) {
+                a = lane == k ? ba[k] : a;
+                e = lane == k ? be[k] : e;
+            }
+            s_count[lane * kSelWaves + wave] = __popcll(a) | __popcll(e) << 16;
         }
-        const uint64_t below = (1ull << lane) - 1;
-        above += __popcll(ba & below);
-        equal += __popcll(be & below);
-        if (is_above || (is_equal && equal < need)) sel[above + min(equal, need)] = i;
+        __syncthreads();
+        const int counts = s_count[lane], upto = wave_scan(counts);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int before = __builtin_amdgcn_readlane(upto - counts, k * kSelWaves + wave);
+            const uint64_t below = (1ull << lane) - 1;
+            const int above = above0 + (before & 0xffff) + __popcll(ba[k] & below), equal = equal0 + (before >> 16) + __popcll(be[k] & below);
+            if (ba[k] >> lane & 1 || (be[k] >> lane & 1 && equal < need)) sel[above + min(equal, need)] = i0 + k * kSelThreads + tid;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
+        above0 += all & 0xffff;
+        equal0 += all >> 16;
     }
 }
 
 size_t paged_select_bytes(int B, int H, int P) { return align_up((size_t)B * H * P * sizeof(unsigned long long), 256); }
 
-template <typename T, typename TQ, int D> static void launch_score(const PagSelParams &p, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_score_kernel<T, TQ, D>), dim3((unsigned)((int64_t)p.tiles * p.c.B * p.c.H)), dim3(kScoreThreads), 0, stream, p);
-}
-template <typename T, typename TQ> static void launch_score_d(const PagSelParams &p, hipStream_t stream) {
-    if (p.c.d == 128) launch_score<T, TQ, 128>(p, stream);
-    else launch_score<T, TQ, 64>(p, stream);
+template <typename T, int D> static void launch_score(const PagSelParams &p, hipStream_t stream) {
+    const dim3 grid((unsigned)((int64_t)p.tiles * p.c.B * p.c.H)), threads(kScoreThreads);
+    if (p.G <= 4) hipLaunchKernelGGL((paged_score_kernel<T, D, 1>), grid, threads, 0, stream, p);
+    else if (p.G <= 8) hipLaunchKernelGGL((paged_score_kernel<T, D, 2>), grid, threads, 0, stream, p);
+    else hipLaunchKernelGGL((paged_score_kernel<T, D, 0>), grid, threads, 0, stream, p);
 }
 
 hipError_t launch_paged_select(const PagedSelectArgs &a, hipStream_t stream) {
@@ -298,13 +313,13 @@ hipError_t launch_paged_select(const PagedSelectArgs &a, hipStream_t stream) {
     p.sel = a.sel; p.sel_lens = a.sel_lens;
     p.keys = reinterpret_cast<unsigned long long *>(reinterpret_cast<char *>(a.ws) + paged_state_bytes());
     p.tiles = (a.c.P + kScorePages - 1) / kScorePages;
-    const bool qb = a.q_dtype == DType::BF16;
+    p.q_is_bf16 = a.q_dtype == DType::BF16;
     if (a.c.dtype == DType::BF16) {
-        if (qb) launch_score_d<bf16_t, bf16_t>(p, stream);
-        else launch_score_d<bf16_t, float>(p, stream);
+        if (a.c.d == 128) launch_score<bf16_t, 128>(p, stream);
+        else launch_score<bf16_t, 64>(p, stream);
     } else {
-        if (qb) launch_score_d<float, bf16_t>(p, stream);
-        else launch_score_d<float, float>(p, stream);
+        if (a.c.d == 128) launch_score<float, 128>(p, stream);
+        else launch_score<float, 64>(p, stream);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
