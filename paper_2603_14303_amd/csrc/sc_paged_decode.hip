@@ -258,7 +258,7 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     auto entry = [&](int e) {
         my_rows = my_len = 0;
         if (e < entries) {
-            my_len = min(max(p.lens[p.sel && !p.lens_per_head ? e / cv.H : e], 0), cv.P << cv.log2_R);
+            my_len = min(max(p.lens[p.sel && !p.lens_per_head ? paged_quotient(e, cv.H, inverse_of(cv.H)) : e], 0), cv.P << cv.log2_R);
             my_rows = p.sel ? min(max(p.sel_lens[e], 0), p.keep) << cv.log2_R : my_len;      // selected: the rows of whole pages; those behind the length are masked
         }
     };

@@ -5,7 +5,8 @@
 // Two kernels.  The scores are two products on the fp64 matrix cores: the products of two bf16 numbers are exact in fp64 and their sums very nearly so,
 // and the choice between two pages is that of exact arithmetic unless they are some 1e-13 apart.  (Sums in fp32 would choose another page than an
 // exact evaluation in a few calls of a hundred, and which one would depend on the order of the sum.)  Then one workgroup per (sequence, KV head) finds
-// the last page to keep and writes the places in order.
+// the last page to keep and writes the places in order.  (As one kernel, in which the last workgroup of a head to have written its scores selects:
+// 13.7 us with 256 threads and 15.0 with 1024 instead of 4.9 + 6.5 for 2048 pages x 8 heads.)
 #include "sc_paged.h"
 
 namespace sc {
@@ -61,7 +62,7 @@ __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams
     const int b = (int)(bh / cv.H), h = (int)(bh - (int64_t)b * cv.H);
     const int lane = threadIdx.x % kWave, g = lane / 16, c = lane % 16;
     const int pages = held_pages(p, bh, b);
-    if (tile * kScorePages >= pages) return;
+    if (pages <= p.keep || tile * kScorePages >= pages) return;
     const int place = tile * kScorePages + 16 * (int)(threadIdx.x / kWave) + c;      // the lane's page: column c of the products
     const int page = place < pages ? paged_table(cv, b, h)[place] : 0;
     const bool there = place < pages && !paged_bad(cv, page);
