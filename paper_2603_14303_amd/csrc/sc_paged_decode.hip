@@ -126,7 +126,12 @@ template <typename T, int D> struct Acc {
 // L2s do not see each other's lines within a kernel).
 constexpr int kAuxAgent = 16;      // buffer cache policy: device scope
 
-__device__ __forceinline__ void store_result(const PagDecParams &p, int64_t row, int D, int e, const float4 &o, float m, float l) {
+struct Output {
+    void *O;
+    int o_is_bf16;
+    float *lse;
+};
+__device__ __forceinline__ void store_result(const Output &p, int64_t row, int D, int e, const float4 &o, float m, float l) {
     const float f = l != 0.f ? 1.0f / l : 0.f;
     store_row4(p.O, p.o_is_bf16, row * D + e, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
     if (e == 0 && p.lse) p.lse[row] = l != 0.f ? (m + __log2f(l)) * kPagLn2 : -INFINITY;
@@ -143,12 +148,12 @@ template <int D> __device__ __forceinline__ void store_part(__amdgpu_buffer_rsrc
 // Joins n partial results, whose places `place_of` gives, and hands each of the G D / 4 pieces of 16 bytes to `sink` with its head's maximum and sum.
 // A thread owns one piece of one head and every NS-th part; all its loads of a pass are on their way before the first is used.
 template <int D, typename PlaceOf, typename Sink>
-__device__ __forceinline__ void join_parts(const PagDecParams &p, __amdgpu_buffer_rsrc_t rs, int n, PlaceOf place_of, int tid, float *s_red, float (*s_weight)[kMaxPairs],
+__device__ __forceinline__ void join_parts(int G, __amdgpu_buffer_rsrc_t rs, int n, PlaceOf place_of, int tid, float *s_red, float (*s_weight)[kMaxPairs],
                                            float *s_total, Sink sink) {
     constexpr int QPR = D / 4, kStride = D + kPagPad, PASS = 8;
     constexpr int kNowhere = 0x7FFFFFF0;      // beyond the descriptor: zeros, and no memory traffic
     static_assert(16 * QPR <= kPagThreads, "a thread for every piece");
-    const int G = p.G, lane = tid % kWave, wave = uniform(tid / kWave);
+    const int lane = tid % kWave, wave = uniform(tid / kWave);
     const int log2_G = G > 1 ? 32 - __clz(G - 1) : 0;      // heads of a part, up to a power of two
     const int pieces = G * QPR;
     const float pieces_inverse = inverse_of(pieces);
@@ -249,7 +254,6 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     __shared__ float s_m[kPagWaves][16], s_l[kPagWaves][16];
     __shared__ int s_last;
     __shared__ float s_weight[2][kMaxPairs], s_total[32];
-    const auto rs = __builtin_amdgcn_make_buffer_rsrc(p.part, (short)0, 2 * kMaxWgs * G * kStride * 4, 0x00020000);
 
     // ---- my stretch of all units: every wavefront adds up the lengths, 64 at a time
     const bool per_head = p.sel != nullptr || p.lens_per_head != 0;
@@ -351,31 +355,29 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
         }
         return x;
     };
-    // Queries: lane (g, c) holds of head c what meets its pieces of a key; heads beyond the group are zero
+    // Queries: lane (g, c) holds of head c what meets its pieces of a key; heads beyond the group read as zeros
     uint4 q[QP][KL];
     auto load_queries = [&](const Stretch &t) {
-        const int64_t q0 = (((int64_t)t.b * cv.H + t.h) * G + c) * D;
+        const int qs = p.q_is_bf16 ? 2 : 4;
+        const pag_rsrc rows = rows_at(static_cast<const char *>(p.Q) + ((int64_t)t.b * cv.H + t.h) * G * D * qs, G * D * qs);
 #pragma unroll
         for (int ks = 0; ks < KL; ++ks) {
+            if constexpr (kBf16 && QP > 1) {
+                const int at = (c * D + 32 * ks + 8 * g) * 4;
+                const pag_u32x4 y0 = __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, 0), y1 = __builtin_amdgcn_raw_buffer_load_b128(rows, at + 16, 0, 0);
+                uint32_t w[4][QP];
+                split_bf16<QP>(__uint_as_float(y0.x), __uint_as_float(y0.y), w[0]);
+                split_bf16<QP>(__uint_as_float(y0.z), __uint_as_float(y0.w), w[1]);
+                split_bf16<QP>(__uint_as_float(y1.x), __uint_as_float(y1.y), w[2]);
+                split_bf16<QP>(__uint_as_float(y1.z), __uint_as_float(y1.w), w[3]);
 #pragma unroll
-            for (int k = 0; k < QP; ++k) q[k][ks] = make_uint4(0u, 0u, 0u, 0u);
-            if (c < G) {
-                if constexpr (kBf16 && QP == 1) {
-                    q[0][ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const bf16_t *>(p.Q) + q0 + 32 * ks + 8 * g);
-                } else if constexpr (kBf16) {
-                    float y[8];
-                    load8(reinterpret_cast<const float *>(p.Q) + q0 + 32 * ks + 8 * g, y);
-                    uint32_t w[4][QP];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) split_bf16<QP>(y[2 * i], y[2 * i + 1], w[i]);
-#pragma unroll
-                    for (int k = 0; k < QP; ++k) q[k][ks] = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
-                } else if (p.q_is_bf16) {
-                    const uint2 y = *reinterpret_cast<const uint2 *>(reinterpret_cast<const bf16_t *>(p.Q) + q0 + 16 * ks + 4 * g);
-                    q[0][ks] = make_uint4(y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u);
-                } else {
-                    q[0][ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const float *>(p.Q) + q0 + 16 * ks + 4 * g);
-                }
+                for (int k = 0; k < QP; ++k) q[k][ks] = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
+            } else if (!kBf16 && p.q_is_bf16) {
+                const pag_u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(rows, (c * D + 16 * ks + 4 * g) * 2, 0, 0);
+                q[0][ks] = make_uint4(y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u);
+            } else {
+                const pag_u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(rows, c * D * (int)sizeof(T) + 64 * ks + 16 * g, 0, 0);
+                q[0][ks] = make_uint4(y.x, y.y, y.z, y.w);
             }
         }
     };
@@ -507,6 +509,11 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
             request_values();
         }
 
+        // What only follows is read from the kernel's arguments here, not kept in scalar registers (of which there are too few) from the start
+        const auto *tail = (const __attribute__((address_space(4))) PagDecParams *)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(tail));
+        const Output out = {tail->O, tail->o_is_bf16, tail->lse};
+        const auto rs = __builtin_amdgcn_make_buffer_rsrc(tail->part, (short)0, 2 * kMaxWgs * G * kStride * 4, 0x00020000);
         // ---- join the wavefronts
         float lw = rows_allreduce_sum(l_run);
         if (bad) lw = __builtin_nanf("");
@@ -541,7 +548,7 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
                 o.w = fmaf(t.w, f, o.w);
                 l = fmaf(s_l[w][hh], f, l);
             }
-            if (whole) store_result(p, bh * G + hh, D, el, o, m, l);
+            if (whole) store_result(out, bh * G + hh, D, el, o, m, l);
             else store_part<D>(rs, at + hh * kStride, el, o, m, l);
         }
         if (!whole) {
@@ -549,17 +556,17 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
             const int n = w1 - w0 + 1, group = paged_group(n, G);
             const int k0 = (wg - w0) / group * group, in_group = min(group, n - k0), groups = (n + group - 1) / group;
             auto place_of = [&](int w) { return paged_place(w, cur.a, per); };
-            int *counter = p.counter + place_of(w0 + k0);
+            int *counter = tail->counter + place_of(w0 + k0);
             int parts = in_group, from = w0 + k0, by = 1;
             bool result = groups == 1;
             while (last_of(counter, parts, tid, &s_last)) {
                 const int to = place_of(from) * G * kStride;
-                join_parts<D>(p, rs, parts, [&](int k) { return place_of(from + k * by); }, tid, s_acc, s_weight, s_total, [&](int hh, int el, const float4 &o, float m, float l) {
-                    if (result) store_result(p, bh * G + hh, D, el, o, m, l);
+                join_parts<D>(G, rs, parts, [&](int k) { return place_of(from + k * by); }, tid, s_acc, s_weight, s_total, [&](int hh, int el, const float4 &o, float m, float l) {
+                    if (result) store_result(out, bh * G + hh, D, el, o, m, l);
                     else store_part<D>(rs, to + hh * kStride, el, o, m, l);
                 });
                 if (result) break;
-                counter = p.counter + 2 * kMaxWgs + place_of(w0);
+                counter = tail->counter + 2 * kMaxWgs + place_of(w0);
                 parts = groups;
                 from = w0;
                 by = group;
