@@ -81,7 +81,7 @@ struct PagedAppendArgs {
 };
 // whether the call fits a grid: a workgroup per page and KV head, and per 16 tokens and query head at worst
 inline bool paged_append_fits(int64_t B, int64_t H, int64_t R, int64_t N, int64_t Hq) {
-    return B * H * ((N + R - 2) / R + 1) + B * ((N + 15) / 16) * Hq <= INT32_MAX;
+    return (B * ((N + R - 2) / R + 1) + 7) * H + B * ((N + 15) / 16) * Hq <= INT32_MAX;
 }
 hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t stream);
 

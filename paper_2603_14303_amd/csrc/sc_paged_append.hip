@@ -11,6 +11,7 @@
 namespace sc {
 
 constexpr int kAppThreads = 256;
+constexpr int kNearItems = 64;         // pages from which the heads of one are kept on a chiplet: eight for each of them
 
 // A lane's two pieces of 16 bytes of a row (of E elements each), chosen so that the partners of a rotation are in the same lane
 template <typename T> struct Shape {
@@ -104,6 +105,7 @@ __device__ __forceinline__ int read_scalar(const int32_t *p) { return *(const __
 struct AppendGrid {
     int kv_blocks, page_groups;             // workgroups of the keys and values; of a sequence and head
     int log2_waves;                         // wavefronts of a page
+    int kv_near;                            // the heads of a page on one chiplet (paged_share)
     int log2_tokens, q_tiles;               // tokens that a workgroup of the queries holds at a time; tiles of so many
     int q_heads, q_groups;                  // heads that it goes over; groups of so many
 };
@@ -178,10 +180,9 @@ __global__ __launch_bounds__(kAppThreads) void paged_append_kernel(PagedAppendAr
     const int lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int j = lane % LPR;
     const Pieces at = pieces_of<E>(j, p.rot, interleaved);
-    int id = (int)blockIdx.x;
-    const int h = id % c.H;
-    id /= c.H;
-    const int group = id % g.page_groups, b = id / g.page_groups;
+    const PagedShare at_work = paged_share((int)blockIdx.x, c.H, g.kv_near != 0);
+    const int h = at_work.share, group = at_work.item % g.page_groups, b = at_work.item / g.page_groups;
+    if (b >= c.B) return;
     const int wpp = 1 << g.log2_waves, part = wave & (wpp - 1);
     const int li = p.per_head ? b * c.H + h : b;
     const int base = read_scalar(p.base_lens + li), new_len = read_scalar((p.new_lens ? p.new_lens : p.base_lens) + li);
@@ -321,7 +322,11 @@ static hipError_t launch_append(const PagedAppendArgs &a, hipStream_t stream) {
     while (g.log2_waves < 2 && (2 * RPW << g.log2_waves) < a.c.R) ++g.log2_waves;
     const int pages = WAVES >> g.log2_waves, slots = paged_append_slots(a.N, a.c.R, a.c.P);
     g.page_groups = (slots + pages - 1) / pages;
-    g.kv_blocks = a.c.B * a.c.H * g.page_groups;
+    // Near: 32768 tokens 158 -> 152 us, merged rows 37.3 -> 35.8 (angles from one chiplet's cache, neighbouring rows of a projection read together); with
+    // few pages there would be chiplets without work.  (The queries' workgroups too: 157.)
+    const int64_t kv_items = (int64_t)a.c.B * g.page_groups;
+    g.kv_near = kv_items >= kNearItems;
+    g.kv_blocks = (int)paged_share_ids(kv_items, a.c.H, g.kv_near != 0);
     g.log2_tokens = 0;
     while ((1 << g.log2_tokens) < a.N && (1 << g.log2_tokens) < WAVES * QRPW) ++g.log2_tokens;
     g.q_tiles = (a.N + (1 << g.log2_tokens) - 1) >> g.log2_tokens;

@@ -21,6 +21,18 @@ constexpr int paged_append_slots(int N, int R, int P) {
     return most < P ? (int)most : P;
 }
 
+// `shares` workgroups (KV heads) for each of `items` (pages): workgroup id -> item and share.  The hardware hands ids to the 8 chiplets in turn; with `near`,
+// all shares of an item are on one chiplet, whose cache then has the angles for them.
+struct PagedShare {
+    int item, share;
+};
+constexpr PagedShare paged_share(int id, int shares, bool near) {
+    if (!near) return {id / shares, id % shares};
+    const int k = id / 8;
+    return {k / shares * 8 + id % 8, k % shares};
+}
+constexpr int64_t paged_share_ids(int64_t items, int shares, bool near) { return near ? (items + 7) / 8 * 8 * shares : items * shares; }
+
 // ---- sc_paged_decode_attn
 // x / y for x >= 0, y > 0 and quotients up to 2^20, given 1 / y up to a few roundings (the kernel's lengths are on the device, and a division there costs
 // as much as a trip to the cache)

@@ -177,6 +177,21 @@ int main() {
     CHECK(!paged_append_plan(2147483647, 2147483647, 2147483647, 1 << 20, 10, false, 0, 0).ok);
     CHECK(paged_append_slots(2147483647, 16, 1 << 20) == 1 << 20 && paged_append_slots(1, 16, 9) == 1 && paged_append_slots(2, 16, 9) == 2 && paged_append_slots(17, 16, 9) == 2);
     CHECK(paged_append_slots(18, 16, 9) == 3);
+    // ---- shares of items: every one has an id, those behind the last item are known by it; near shares are eight ids apart
+    for (int t = 0; t < 2000; ++t) {
+        const int items = any(1, 100), shares = any(1, 40), near = any(0, 1);
+        std::vector<int> seen(items * shares, 0), chiplet(items, -1);
+        const long long ids = paged_share_ids(items, shares, near);
+        CHECK(ids < (long long)(items + 8) * shares);
+        for (int id = 0; id < ids; ++id) {
+            const PagedShare s = paged_share(id, shares, near);
+            CHECK(s.share >= 0 && s.share < shares && s.item >= 0 && s.item < items + 8);
+            if (s.item >= items) { CHECK(near); continue; }
+            seen[s.item * shares + s.share]++;
+            if (near) { CHECK(chiplet[s.item] < 0 || chiplet[s.item] == id % 8); chiplet[s.item] = id % 8; }
+        }
+        for (int x : seen) CHECK(x == 1);
+    }
     // ---- stretches: every unit of every head belongs to one workgroup, its parts have places of their own, and the workgroups count themselves off
     for (int t = 0; t < 20000; ++t) {
         const int heads = any(1, 40), wgs = any(1, 64), unit = 16 * any(1, 12);
