@@ -6,7 +6,7 @@
 // and the choice between two pages is that of exact arithmetic unless they are some 1e-13 apart.  (Sums in fp32 would choose another page than an
 // exact evaluation in a few calls of a hundred, and which one would depend on the order of the sum.)  Then one workgroup per (sequence, KV head) finds
 // the last page to keep and writes the places in order.  (As one kernel, in which the last workgroup of a head to have written its scores selects:
-// 13.7 us with 256 threads and 15.0 with 1024 instead of 4.9 + 6.5 for 2048 pages x 8 heads.)
+// 13.7 us with 256 threads and 15.0 with 1024 when these two took 4.9 + 6.5 for 2048 pages x 8 heads.)
 #include "sc_paged.h"
 
 namespace sc {
@@ -137,14 +137,18 @@ __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams
 // One workgroup per (sequence, KV head).  The keys are spread over kBuckets buckets, evenly between the smallest and the largest number, by one pass; the
 // bucket that the last page to keep falls into holds a few of them, which are ranked against each other.  If they are more than fit (scores that are
 // equal, or lie together far from a few others), the key is found eight bits at a time.
+// One workgroup's 16 wavefronts share four SIMDs, so the instructions per key are what bounds it: keys, numbers and buckets stay in registers, stretches
+// without keys are passed by.  2048 pages: 5.9 us (6.8 with the bucket found anew in every pass and four stretches counted whatever n is), of which loads
+// 0.6, the range 0.8, the buckets 0.7, the rank's bucket 0.5, its keys 0.8, the places 0.9; 8192 pages: 9.6 us (13.7 with half of the keys in registers).
 constexpr int kBuckets = 2048, kRanked = 256, kSelWaves = kSelThreads / kWave;
 
+__device__ __forceinline__ int lanes_below(uint64_t m) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0)); }
 __device__ __forceinline__ double key_score(unsigned long long k) { return __builtin_bit_cast(double, (k >> 63) ? k & ~(1ull << 63) : ~k); }
 
 __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams p) {
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / p.c.H);
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int n = held_pages(p, bh, b), keep = p.keep;
     int32_t *sel = p.sel + bh * keep;
     if (tid == 0) p.sel_lens[bh] = min(n, keep);
@@ -153,31 +157,33 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
         return;
     }
     const unsigned long long *keys = p.keys + bh * p.c.P;
-    constexpr int K = kWave / kSelWaves;                // keys that a thread keeps in registers; those behind them are read again
+    constexpr int K = kWave / kSelWaves, HELD = 2 * K;  // HELD: keys that a thread keeps in registers; those behind them are read again
     __shared__ int s_hist[kBuckets];
     __shared__ float s_low[kSelWaves], s_high[kSelWaves];
     __shared__ int s_above[kSelWaves], s_count[kWave];
     __shared__ int s_bucket, s_need, s_ranked;
     __shared__ unsigned long long s_key[kRanked], s_border;
     __shared__ int s_place[kRanked], s_border_place;
-    unsigned long long mine[K];
+    unsigned long long mine[HELD];
+    float number[HELD];      // the scores in fp32 (the buckets only need an order), then, as integers, their buckets
 #pragma unroll
-    for (int k = 0; k < K; ++k) mine[k] = tid + k * kSelThreads < n ? keys[tid + k * kSelThreads] : 0ull;
-    auto each = [&](auto f) {      // every key and its place
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (tid + k * kSelThreads < n) f(mine[k], tid + k * kSelThreads);
-        for (int i = tid + K * kSelThreads; i < n; i += kSelThreads) f(keys[i], i);
-    };
-    // ---- the smallest and the largest finite score (as fp32: the buckets only need an order)
+    for (int k = 0; k < HELD; ++k) mine[k] = tid + k * kSelThreads < n ? keys[tid + k * kSelThreads] : 0ull;
+    const auto number_of = [&](unsigned long long k) { return k < kKeyNaN ? (float)key_score(k) : INFINITY; };
+    // ---- the smallest and the largest finite score
     float low = INFINITY, high = -INFINITY;
-    each([&](unsigned long long k, int) {
-        const float x = k < kKeyNaN ? (float)key_score(k) : INFINITY;
+    const auto widen = [&](float x) {
         if (fabsf(x) < INFINITY) {
             low = fminf(low, x);
             high = fmaxf(high, x);
         }
-    });
+    };
+#pragma unroll
+    for (int k = 0; k < HELD; ++k)
+        if (k * kSelThreads < n && tid + k * kSelThreads < n) {
+            number[k] = number_of(mine[k]);
+            widen(number[k]);
+        }
+    for (int i = tid + HELD * kSelThreads; i < n; i += kSelThreads) widen(number_of(keys[i]));
     low = -rows_allreduce_max(row_allreduce_max(-low));
     high = rows_allreduce_max(row_allreduce_max(high));
     if (lane == 0) { s_low[wave] = low; s_high[wave] = high; }
@@ -187,12 +193,27 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
     low = -row_allreduce_max(-s_low[lane % kSelWaves]);
     high = row_allreduce_max(s_high[lane % kSelWaves]);
     const float spread = high > low ? (float)(kBuckets - 5) / (high - low) : 0.f;      // (0 too where high - low is not finite)
-    auto bucket = [&](unsigned long long k) {      // never falls where the key grows
-        if (k >= kKeyNaN) return kBuckets - 1 - (int)(k == kKeyNaN);
-        const float x = (float)key_score(k);
-        return x >= INFINITY ? kBuckets - 3 : x <= -INFINITY ? 0 : 1 + min((int)((x - low) * spread), kBuckets - 5);
+    const auto bucket_of = [&](unsigned long long k, float x) {      // never falls where the key grows
+        const float at = fminf(fmaxf((x - low) * spread, 0.f), (float)(kBuckets - 5));      // (no number where infinity is multiplied by zero: 0)
+        return k >= kKeyNaN ? kBuckets - 1 - (int)(k == kKeyNaN) : x >= INFINITY ? kBuckets - 3 : x <= -INFINITY ? 0 : 1 + (int)at;
     };
-    each([&](unsigned long long k, int) { atomicAdd(&s_hist[bucket(k)], 1); });
+#pragma unroll
+    for (int k = 0; k < HELD; ++k)
+        if (k * kSelThreads < n && tid + k * kSelThreads < n) {
+            const int to = bucket_of(mine[k], number[k]);
+            number[k] = __int_as_float(to);
+            atomicAdd(&s_hist[to], 1);
+        }
+    for (int i = tid + HELD * kSelThreads; i < n; i += kSelThreads) atomicAdd(&s_hist[bucket_of(keys[i], number_of(keys[i]))], 1);
+    const auto each_of = [&](int bucket, auto f) {      // every key of a bucket, and its place
+#pragma unroll
+        for (int k = 0; k < HELD; ++k)
+            if (k * kSelThreads < n && tid + k * kSelThreads < n && __float_as_int(number[k]) == bucket) f(mine[k], tid + k * kSelThreads);
+        for (int i = tid + HELD * kSelThreads; i < n; i += kSelThreads) {
+            const unsigned long long k = keys[i];
+            if (bucket_of(k, number_of(k)) == bucket) f(k, i);
+        }
+    };
     __syncthreads();
     // ---- the bucket of rank keep: thread t has buckets kBuckets - 1 - 2 t and the one below
     {
@@ -200,8 +221,8 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
         const int upto = wave_scan(v0 + v1);
         if (lane == kWave - 1) s_above[wave] = upto;
         __syncthreads();
-        int before = upto - v0 - v1;
-        for (int w = 0; w < wave; ++w) before += s_above[w];
+        const int others = wave_scan(lane < kSelWaves ? s_above[lane % kSelWaves] : 0);
+        int before = upto - v0 - v1 + (wave ? __builtin_amdgcn_readlane(others, wave - 1) : 0);
         if (before < keep && before + v0 >= keep) { s_bucket = kBuckets - 1 - 2 * tid; s_need = keep - before; }
         before += v0;
         if (before < keep && before + v1 >= keep) { s_bucket = kBuckets - 2 - 2 * tid; s_need = keep - before; }
@@ -212,12 +233,10 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
     unsigned long long border = 0;
     int border_place = n;   // keys equal to the border's are kept up to this place
     if (s_hist[at] <= kRanked) {
-        each([&](unsigned long long k, int i) {
-            if (bucket(k) == at) {
-                const int r = atomicAdd(&s_ranked, 1);
-                s_key[r] = k;
-                s_place[r] = i;
-            }
+        each_of(at, [&](unsigned long long k, int i) {
+            const int r = atomicAdd(&s_ranked, 1);
+            s_key[r] = k;
+            s_place[r] = i;
         });
         __syncthreads();
         const int m = s_ranked;
@@ -237,8 +256,8 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
             __syncthreads();
             if (tid < 256) s_hist[tid] = 0;
             __syncthreads();
-            each([&](unsigned long long k, int) {
-                if (bucket(k) == at && (k & mask) == border) atomicAdd(&s_hist[(int)(k >> shift) & 255], 1);
+            each_of(at, [&](unsigned long long k, int) {
+                if ((k & mask) == border) atomicAdd(&s_hist[(int)(k >> shift) & 255], 1);
             });
             __syncthreads();
             if (wave == 0) {      // lane i: digits 255 - 4 i .. 252 - 4 i
@@ -262,38 +281,38 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
     // kSelThreads pages at a time, lane 16 k + w of every wavefront counting for stretch k and wavefront w
     const bool by_place = border_place < n;
     int above0 = 0, equal0 = 0;
-    for (int i0 = 0; i0 < n; i0 += K * kSelThreads) {
+    const auto put = [&](int i0, auto key_of) {
         uint64_t ba[K], be[K];
+        int mine_of = 0;      // lane k: of stretch k
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int i = i0 + k * kSelThreads + tid;
-            const unsigned long long x = i0 == 0 ? mine[k] : i < n ? keys[i] : 0ull;
-            ba[k] = ballot64(i < n && (x > border || (by_place && x == border && i <= border_place)));
-            be[k] = ballot64(!by_place && i < n && x == border);
+            ba[k] = be[k] = 0;
+            if (i0 + k * kSelThreads < n) {
+                const int i = i0 + k * kSelThreads + tid;
+                const unsigned long long x = key_of(k, i);      // (0 behind the last one)
+                ba[k] = ballot64(x > border || (i <= border_place && x == border && by_place));
+                if (!by_place) be[k] = ballot64(i < n && x == border);
+                mine_of = lane == k ? __popcll(ba[k]) | __popcll(be[k]) << 16 : mine_of;
+            }
         }
         if (i0 > 0) __syncthreads();
-        if (lane < K) {
-            uint64_t a = 0, e = 0;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                a = lane == k ? ba[k] : a;
-                e = lane == k ? be[k] : e;
-            }
-            s_count[lane * kSelWaves + wave] = __popcll(a) | __popcll(e) << 16;
-        }
+        if (lane < K) s_count[lane * kSelWaves + wave] = mine_of;
         __syncthreads();
         const int counts = s_count[lane], upto = wave_scan(counts);
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int before = __builtin_amdgcn_readlane(upto - counts, k * kSelWaves + wave);
-            const uint64_t below = (1ull << lane) - 1;
-            const int above = above0 + (before & 0xffff) + __popcll(ba[k] & below), equal = equal0 + (before >> 16) + __popcll(be[k] & below);
-            if (ba[k] >> lane & 1 || (be[k] >> lane & 1 && equal < need)) sel[above + min(equal, need)] = i0 + k * kSelThreads + tid;
-        }
+        for (int k = 0; k < K; ++k)
+            if (ba[k] | be[k]) {
+                const int before = __builtin_amdgcn_readlane(upto - counts, k * kSelWaves + wave);
+                const int above = above0 + (before & 0xffff) + lanes_below(ba[k]), equal = equal0 + (before >> 16) + lanes_below(be[k]);
+                if (ba[k] >> lane & 1 || (be[k] >> lane & 1 && equal < need)) sel[above + min(equal, need)] = i0 + k * kSelThreads + tid;
+            }
         const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
         above0 += all & 0xffff;
         equal0 += all >> 16;
-    }
+    };
+    put(0, [&](int k, int) { return mine[k]; });
+    if (n > K * kSelThreads) put(K * kSelThreads, [&](int k, int) { return mine[K + k]; });
+    for (int i0 = HELD * kSelThreads; i0 < n; i0 += K * kSelThreads) put(i0, [&](int, int i) { return i < n ? keys[i] : 0ull; });
 }
 
 size_t paged_select_bytes(int B, int H, int P) { return align_up((size_t)B * H * P * sizeof(unsigned long long), 256); }

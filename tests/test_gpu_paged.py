@@ -584,6 +584,53 @@ def test_select_decides_as_exact_arithmetic_does():
         assert sel.cpu()[0, 0].tolist() == sorted(i for i in range(n) if rank[i] >= n - keep), keep
 
 
+@pytest.mark.parametrize("dtype, qdt", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("k_exp, q_exp", [(-126, -3), (-130, 90), (-120, -90), (120, 20), (124, 0), (125, -128)])
+def test_select_scores_beyond_the_range_of_fp32(dtype, qdt, k_exp, q_exp):
+    """Summaries and queries at the ends of their range, denormal ones among them: products and sums that fp32 does not hold decide all the same."""
+    print("select range", dtype, qdt, k_exp, q_exp, flush=True)
+    n, G = 700, 3
+    pc = Paged(1, 2, n, 16, 64, dtype, junk=False, seed=k_exp + 200)
+    lo = torch.ldexp(torch.randn((pc.n, 2, 64), generator=pc.gen), torch.tensor(k_exp)).to(dtype)
+    hi = torch.ldexp(torch.randn((pc.n, 2, 64), generator=pc.gen), torch.tensor(k_exp)).to(dtype)
+    lo, hi = torch.minimum(lo, hi), torch.maximum(lo, hi)
+    assert lo.isfinite().all() and hi.isfinite().all()
+    pc.k_min, pc.k_max = lo.to(DEV), hi.to(DEV)
+    Q = torch.ldexp(torch.randn((1, 2 * G, 64), generator=pc.gen).double(), torch.tensor(q_exp)).to(qdt)
+    dl = torch.tensor([n * 16], dtype=torch.int32, device=DEV)
+    for keep in (3, 400):
+        sel, many = sc.sc_paged_select(pc.cache(), Q.to(DEV), dl, keep, first=0, recent=0)
+        want, want_many = want_selection(pc, lo, hi, Q, [[n * 16] * 2], G, keep, 0, 0)
+        assert torch.equal(many.cpu(), want_many) and torch.equal(sel.cpu(), want), keep
+
+
+@pytest.mark.parametrize("n, G", [(900, 4), (9000, 1), (9000, 5)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_select_among_many_scores_that_lie_together(n, G, dtype):
+    """Hundreds or thousands of scores within a few parts in 2^30 of each other, some of them equal, and a few far above and below."""
+    print("select together", n, G, dtype, flush=True)
+    pc = Paged(1, 2, n, 16, 128, dtype, junk=False, seed=n + G)
+    lo = torch.zeros((pc.n, 2, 128))
+    lo[:, :, 0] = 2.0**20
+    lo[:, :, 1] = 2.0**-10 * torch.randint(0, 64, (pc.n, 2), generator=pc.gen)
+    lo[:, :, 2] = 2.0**-16 * torch.randint(0, 64, (pc.n, 2), generator=pc.gen)
+    far = torch.rand((pc.n, 2), generator=pc.gen)
+    lo[:, :, 0] = torch.where(far < 0.02, 2.0**30 * (1 + torch.randint(0, 4, far.shape, generator=pc.gen)), torch.where(far > 0.9, -(2.0**25), lo[:, :, 0]))
+    lo = lo.to(dtype)
+    pc.k_min = pc.k_max = lo.to(DEV)
+    Q = torch.rand((1, 2 * G, 128), generator=pc.gen).mul(0.5)
+    Q[:, ::G, :3] = 1.0
+    Q = Q.to(dtype)
+    dl = torch.tensor([n * 16], dtype=torch.int32, device=DEV)
+    for keep, first, recent in ((1, 0, 0), (130, 1, 2), (n // 2, 0, 0), (n - n // 20, 3, 300)):
+        sel, many = sc.sc_paged_select(pc.cache(), Q.to(DEV), dl, keep, first=first, recent=recent)
+        want, want_many = want_selection(pc, lo, lo, Q, [[n * 16] * 2], G, keep, first, recent)
+        assert torch.equal(many.cpu(), want_many) and torch.equal(sel.cpu(), want), keep
+    # queries of zeros: every score is the same
+    sel, _ = sc.sc_paged_select(pc.cache(), torch.zeros_like(Q).to(DEV), dl, 40, first=2, recent=3)
+    assert (sel.cpu() == torch.tensor(list(range(37)) + [n - 3, n - 2, n - 1])).all()
+
+
 def test_select_what_is_not_a_number_and_bad_pages_are_kept():
     print("select not a number", flush=True)
     n = 100
