@@ -57,9 +57,9 @@ __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams
     constexpr int HEADS = NT ? 4 * NT : 16, STRIDE = HEADS + 1;
     __shared__ double2 s_q[D * STRIDE];
     const PagedView &cv = p.c;
-    const int64_t bh = blockIdx.x / p.tiles;
-    const int tile = (int)(blockIdx.x - bh * p.tiles);
-    const int b = (int)(bh / cv.H), h = (int)(bh - (int64_t)b * cv.H);
+    const unsigned head_of = blockIdx.x / (unsigned)p.tiles;
+    const int64_t bh = head_of;
+    const int tile = (int)(blockIdx.x - head_of * (unsigned)p.tiles), b = (int)(head_of / (unsigned)cv.H), h = (int)(head_of - (unsigned)b * (unsigned)cv.H);
     const int lane = threadIdx.x % kWave, g = lane / 16, c = lane % 16;
     const int pages = held_pages(p, bh, b);
     if (pages <= p.keep || tile * kScorePages >= pages) return;
@@ -147,7 +147,7 @@ __device__ __forceinline__ double key_score(unsigned long long k) { return __bui
 
 __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams p) {
     const int64_t bh = blockIdx.x;
-    const int b = (int)(bh / p.c.H);
+    const int b = (int)(blockIdx.x / (unsigned)p.c.H);
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int n = held_pages(p, bh, b), keep = p.keep;
     int32_t *sel = p.sel + bh * keep;
