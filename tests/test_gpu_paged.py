@@ -586,10 +586,11 @@ def test_select_decides_as_exact_arithmetic_does():
 
 @pytest.mark.parametrize("dtype, qdt", [(BF, BF), (BF, F32), (F32, F32)])
 @pytest.mark.parametrize("k_exp, q_exp", [(-126, -3), (-130, 90), (-120, -90), (120, 20), (124, 0), (125, -128)])
-def test_select_scores_beyond_the_range_of_fp32(dtype, qdt, k_exp, q_exp):
+@pytest.mark.parametrize("G", [3, 11])
+def test_select_scores_beyond_the_range_of_fp32(dtype, qdt, k_exp, q_exp, G):
     """Summaries and queries at the ends of their range, denormal ones among them: products and sums that fp32 does not hold decide all the same."""
-    print("select range", dtype, qdt, k_exp, q_exp, flush=True)
-    n, G = 700, 3
+    print("select range", dtype, qdt, k_exp, q_exp, G, flush=True)
+    n = 700
     pc = Paged(1, 2, n, 16, 64, dtype, junk=False, seed=k_exp + 200)
     lo = torch.ldexp(torch.randn((pc.n, 2, 64), generator=pc.gen), torch.tensor(k_exp)).to(dtype)
     hi = torch.ldexp(torch.randn((pc.n, 2, 64), generator=pc.gen), torch.tensor(k_exp)).to(dtype)
@@ -604,7 +605,7 @@ def test_select_scores_beyond_the_range_of_fp32(dtype, qdt, k_exp, q_exp):
         assert torch.equal(many.cpu(), want_many) and torch.equal(sel.cpu(), want), keep
 
 
-@pytest.mark.parametrize("n, G", [(900, 4), (9000, 1), (9000, 5)])
+@pytest.mark.parametrize("n, G", [(900, 4), (900, 8), (9000, 1), (9000, 5)])
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_select_among_many_scores_that_lie_together(n, G, dtype):
     """Hundreds or thousands of scores within a few parts in 2^30 of each other, some of them equal, and a few far above and below."""
@@ -648,6 +649,35 @@ def test_select_what_is_not_a_number_and_bad_pages_are_kept():
     sel, many = sc.sc_paged_select(pc.cache(table), Q.to(DEV), torch.tensor([n * 16], dtype=torch.int32, device=DEV), 6, first=1, recent=1)
     a, b = sel.cpu()[0].tolist()
     assert {0, 33, 71, 99} <= set(a) and a == sorted(a) and {0, 35, 36, 71, 99} <= set(b) and b == sorted(b)
+
+
+@pytest.mark.parametrize("dtype, d, G", [(BF, 128, 6), (F32, 64, 16)])
+def test_select_with_many_heads_ties_and_what_is_not_a_number(dtype, d, G):
+    print("select many heads", dtype, d, G, flush=True)
+    n = 2500
+    pc = Paged(1, 2, n, 16, d, dtype, junk=False, seed=G)
+    few = torch.randn((3, d), generator=pc.gen).to(dtype)
+    lo = few[torch.randint(0, 3, (pc.n, 2), generator=pc.gen)]
+    dl = torch.tensor([n * 16], dtype=torch.int32, device=DEV)
+    Q = torch.randn((1, 2 * G, d), generator=pc.gen).to(dtype)
+    pc.k_min = pc.k_max = lo.to(DEV)
+    for keep, first, recent in ((1, 0, 0), (10, 4, 6), (800, 1, 1), (1700, 300, 300), (2499, 0, 0)):
+        sel, many = sc.sc_paged_select(pc.cache(), Q.to(DEV), dl, keep, first=first, recent=recent)
+        want, want_many = want_selection(pc, lo, lo, Q, [[n * 16] * 2], G, keep, first, recent)
+        assert torch.equal(many.cpu(), want_many) and torch.equal(sel.cpu(), want), keep
+    # pages of no number and infinite ones in one head's summaries, and in the other head's a query of no number: its pages are all alike
+    lo = torch.randn((pc.n, 2, d), generator=pc.gen).to(dtype)
+    hi = lo + 1
+    page, _, _ = pc.place(0, 0, torch.arange(n) * 16)
+    lo[page[33], 0, 7] = math.nan
+    lo[page[1035], 0, 7], hi[page[2036], 0, 3] = -math.inf, math.inf
+    pc.k_min, pc.k_max = lo.to(DEV), hi.to(DEV)
+    Q[0, :G, 3], Q[0, :G, 7] = 1.0, -1.0
+    Q[0, G + 2, 5] = math.nan
+    for keep in (6, 300, 2000):
+        sel, many = sc.sc_paged_select(pc.cache(), Q.to(DEV), dl, keep, first=1, recent=1)
+        want, want_many = want_selection(pc, lo, hi, Q, [[n * 16] * 2], G, keep, 1, 1)
+        assert torch.equal(many.cpu(), want_many) and torch.equal(sel.cpu(), want), keep
 
 
 def test_append_select_and_attend_together():
