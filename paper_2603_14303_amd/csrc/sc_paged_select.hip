@@ -55,7 +55,9 @@ __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams
     constexpr int E = 16 / (int)sizeof(T);            // elements of 16 bytes
     constexpr int KL = D / (4 * E);                   // pieces of a row per lane: 4 lanes share a row
     constexpr int HEADS = NT ? 4 * NT : 16, STRIDE = HEADS + 1;
-    __shared__ double2 s_q[D * STRIDE];
+    __shared__ double2 s_q[D * STRIDE + 4 * (D / E)];
+    // element e of a head: four places more for every piece, so that the pieces that four rows of lanes read at a time lie in banks of their own
+    const auto q_place = [](int e, int head) { return e * STRIDE + 4 * (e / E) + head; };
     const PagedView &cv = p.c;
     const unsigned head_of = blockIdx.x / (unsigned)p.tiles;
     const int64_t bh = head_of;
@@ -86,40 +88,45 @@ __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams
         hi[ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(cv.k_max) + row + E * (4 * ks + g));
     }
 #pragma unroll
-    for (int i = 0; i < PER; ++i) s_q[(e0 + i) * STRIDE + head] = make_double2(x[i] < 0.0 ? 0.0 : x[i], x[i] > 0.0 ? 0.0 : x[i]);      // (a NaN is in both)
+    for (int i = 0; i < PER; ++i) s_q[q_place(e0 + i, head)] = make_double2(x[i] < 0.0 ? 0.0 : x[i], x[i] > 0.0 ? 0.0 : x[i]);      // (a NaN is in both)
     __syncthreads();
     double best;
+    // several sums side by side: a product takes four times as long as the next one that does not wait for it
     if constexpr (NT > 0) {
-        double acc[NT] = {};
+        double acc[NT][4] = {};
 #pragma unroll
         for (int ks = 0; ks < KL; ++ks)
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 const double u = element<T>(hi[ks], i), l = element<T>(lo[ks], i);
-                const double2 *q = s_q + (E * (4 * ks + g) + i) * STRIDE + lane % 4;
+                const double2 *q = s_q + q_place(E * (4 * ks + g) + i, lane % 4);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     const double2 y = q[4 * t];
-                    acc[t] = __builtin_amdgcn_mfma_f64_4x4x4f64(y.x, u, acc[t], 0, 0, 0);
-                    acc[t] = __builtin_amdgcn_mfma_f64_4x4x4f64(y.y, l, acc[t], 0, 0, 0);
+                    acc[t][2 * (i % 2)] = __builtin_amdgcn_mfma_f64_4x4x4f64(y.x, u, acc[t][2 * (i % 2)], 0, 0, 0);
+                    acc[t][2 * (i % 2) + 1] = __builtin_amdgcn_mfma_f64_4x4x4f64(y.y, l, acc[t][2 * (i % 2) + 1], 0, 0, 0);
                 }
             }
-        best = acc[0];
+        best = (acc[0][0] + acc[0][1]) + (acc[0][2] + acc[0][3]);
 #pragma unroll
-        for (int t = 1; t < NT; ++t) best = (acc[t] > best || acc[t] != acc[t]) ? acc[t] : best;
+        for (int t = 1; t < NT; ++t) {
+            const double sum = (acc[t][0] + acc[t][1]) + (acc[t][2] + acc[t][3]);
+            best = (sum > best || sum != sum) ? sum : best;
+        }
     } else {
-        sel_f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+        sel_f64x4 acc[2] = {{0.0, 0.0, 0.0, 0.0}, {0.0, 0.0, 0.0, 0.0}};
 #pragma unroll
         for (int ks = 0; ks < KL; ++ks)
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const double2 y = s_q[(E * (4 * ks + g) + i) * STRIDE + c];
-                acc = __builtin_amdgcn_mfma_f64_16x16x4f64(y.x, element<T>(hi[ks], i), acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f64_16x16x4f64(y.y, element<T>(lo[ks], i), acc, 0, 0, 0);
+                const double2 y = s_q[q_place(E * (4 * ks + g) + i, c)];
+                acc[0] = __builtin_amdgcn_mfma_f64_16x16x4f64(y.x, element<T>(hi[ks], i), acc[0], 0, 0, 0);
+                acc[1] = __builtin_amdgcn_mfma_f64_16x16x4f64(y.y, element<T>(lo[ks], i), acc[1], 0, 0, 0);
             }
-        best = acc[0];
+        acc[0] += acc[1];
+        best = acc[0][0];
 #pragma unroll
-        for (int i = 1; i < 4; ++i) best = (acc[i] > best || acc[i] != acc[i]) ? acc[i] : best;
+        for (int i = 1; i < 4; ++i) best = (acc[0][i] > best || acc[0][i] != acc[0][i]) ? acc[0][i] : best;
     }
     // the maximum over the heads: over the lanes that share the page (whatever head is where)
 #pragma unroll
