@@ -6,7 +6,7 @@
 // and the choice between two pages is that of exact arithmetic unless they are some 1e-13 apart.  (Sums in fp32 would choose another page than an
 // exact evaluation in a few calls of a hundred, and which one would depend on the order of the sum.)  Then one workgroup per (sequence, KV head) finds
 // the last page to keep and writes the places in order.  (As one kernel, in which the last workgroup of a head to have written its scores selects:
-// 13.7 us with 256 threads and 15.0 with 1024 when these two took 4.9 + 6.5 for 2048 pages x 8 heads.)
+// 13.7 us with 256 threads and 15.0 with 1024 when these two took 4.9 + 6.5 for 2048 pages x 8 heads; now 4.4 + 5.8.)
 #include "sc_paged.h"
 
 namespace sc {
@@ -48,8 +48,12 @@ template <typename T> __device__ __forceinline__ double element(const uint4 &v, 
 
 // A wavefront has 16 pages, the columns of its products; a lane holds of its page (lane % 16) every fourth piece of 16 bytes.  The heads are the rows, in
 // fp64 in shared memory, their positive and their negative parts side by side.  NT: groups of four heads (v_mfma_f64_4x4x4_4b: four products of 4 heads x
-// 4 pages), or 0: 16 heads (v_mfma_f64_16x16x4).  Bound by the matrix cores with several heads: us for 2048 pages x 8 heads, G = 4, and for 1100 to 2048
-// pages x 32 heads, G = 7, both d = 128, bf16: groups of four 4.9 and 11.1, 16 heads 5.3 and 13.8, vector instructions 7.0 and 31.8.
+// 4 pages), or 0: 16 heads (v_mfma_f64_16x16x4).  us for 2048 pages x 8 heads, G = 4; 1500 pages x 32 heads, G = 7; 2048 pages x 64 heads, G = 16 (d = 128,
+// bf16): NT = 1 4.4; NT = 2 5.0 and 8.7; 16 heads 6.4, 12.1 and 24.7; NT = 4 27.0 for the last.  Vector instructions take two to three times as long, also
+// with a query's element broadcast over a row of lanes on its way into the multiplication (51 for the last).  The first is a chain of trips to memory, the
+// second lies between the bytes (4 us) and the matrix cores, the third is bound by the matrix cores.  With one query head a KV head it is the bytes: 131 MB of
+// summaries in 24.6 us.  Products in fp32 with a bound on their error, and an evaluation in fp64 of the pages near the border by the second kernel,
+// took 3.9, 6.2 and 14.3 here and 3 to 5 us more there, for one way or the other only with more than eight query heads a KV head and many sequences.
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams p) {
     constexpr int E = 16 / (int)sizeof(T);            // elements of 16 bytes
