@@ -53,15 +53,17 @@ template <typename T> __device__ __forceinline__ double element(const uint4 &v, 
 // with a query's element broadcast over a row of lanes on its way into the multiplication (51 for the last).  The first is a chain of trips to memory, the
 // second lies between the bytes (4 us) and the matrix cores, the third is bound by the matrix cores.  With one query head a KV head it is the bytes: 131 MB of
 // summaries in 24.6 us.  Products in fp32 with a bound on their error, and an evaluation in fp64 of the pages near the border by the second kernel,
-// took 3.9, 6.2 and 14.3 here and 3 to 5 us more there, for one way or the other only with more than eight query heads a KV head and many sequences.
+// took 3.9, 6.2 and 14.3 us here and 3 to 5 more there: less in all only with more than eight query heads a KV head and many sequences.
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams p) {
     constexpr int E = 16 / (int)sizeof(T);            // elements of 16 bytes
     constexpr int KL = D / (4 * E);                   // pieces of a row per lane: 4 lanes share a row
     constexpr int HEADS = NT ? 4 * NT : 16, STRIDE = HEADS + 1;
-    __shared__ double2 s_q[D * STRIDE + 4 * (D / E)];
-    // element e of a head: four places more for every piece, so that the pieces that four rows of lanes read at a time lie in banks of their own
-    const auto q_place = [](int e, int head) { return e * STRIDE + 4 * (e / E) + head; };
+    // element e of a head: four rows of lanes read four neighbouring pieces at a time, and those lie in banks of their own if a piece is 16 banks more than a
+    // multiple of 32 (pieces of four elements are: STRIDE is odd)
+    constexpr int PAD = E == 8 ? 4 : 0;
+    __shared__ double2 s_q[D * STRIDE + PAD * (D / E)];
+    const auto q_place = [](int e, int head) { return e * STRIDE + PAD * (e / E) + head; };
     const PagedView &cv = p.c;
     const unsigned head_of = blockIdx.x / (unsigned)p.tiles;
     const int64_t bh = head_of;
