@@ -27,7 +27,6 @@ struct PagSelParams {
 
 constexpr int kScoreThreads = 256;
 constexpr int kScorePages = 16 * (kScoreThreads / kWave);
-constexpr int kSelThreads = 1024;
 // keys in the order of the scores: forced pages above what is not a number, above every number
 constexpr unsigned long long kKeyForced = ~0ull, kKeyNaN = ~0ull - 1;
 
@@ -147,18 +146,20 @@ __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams
     }
 }
 
-// One workgroup per (sequence, KV head).  The keys are spread over kBuckets buckets, evenly between the smallest and the largest number, by one pass; the
+// One workgroup per (sequence, KV head).  The keys are spread over two buckets a thread, evenly between the smallest and the largest number, by one pass; the
 // bucket that the last page to keep falls into holds a few of them, which are ranked against each other.  If they are more than fit (scores that are
 // equal, or lie together far from a few others), the key is found eight bits at a time.
-// One workgroup's 16 wavefronts share four SIMDs, so the instructions per key are what bounds it: keys, numbers and buckets stay in registers, stretches
-// without keys are passed by.  2048 pages: 5.9 us (6.8 with the bucket found anew in every pass and four stretches counted whatever n is), of which loads
-// 0.6, the range 0.8, the buckets 0.7, the rank's bucket 0.5, its keys 0.8, the places 0.9; 8192 pages: 9.6 us (13.7 with half of the keys in registers).
-constexpr int kBuckets = 2048, kRanked = 256, kSelWaves = kSelThreads / kWave;
+// One workgroup's wavefronts share four SIMDs, so the instructions, per key and per wavefront, are what bounds it: keys, numbers and buckets stay in registers
+// (HELD a thread; MORE: those behind them are read again), stretches without keys are passed by, and few pages have few wavefronts.  2048 pages with 1024
+// threads: 5.9 us (6.8 with the bucket found anew in every pass and four stretches counted whatever n is), of which loads 0.6, the range 0.8, the buckets 0.7,
+// the rank's bucket 0.5, its keys 0.8, the places 0.9; 8192 pages: 9.6 us (13.7 with half of the keys in registers).
+constexpr int kRanked = 256;
 
 __device__ __forceinline__ int lanes_below(uint64_t m) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0)); }
 __device__ __forceinline__ double key_score(unsigned long long k) { return __builtin_bit_cast(double, (k >> 63) ? k & ~(1ull << 63) : ~k); }
 
-__global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams p) {
+template <int THREADS, int HELD, bool MORE>
+__global__ __launch_bounds__(THREADS) void paged_select_kernel(PagSelParams p) {
     const int64_t bh = blockIdx.x;
     const int b = (int)(blockIdx.x / (unsigned)p.c.H);
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -166,21 +167,23 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
     int32_t *sel = p.sel + bh * keep;
     if (tid == 0) p.sel_lens[bh] = min(n, keep);
     if (n <= keep) {
-        for (int i = tid; i < keep; i += kSelThreads) sel[i] = i < n ? i : -1;
+        for (int i = tid; i < keep; i += THREADS) sel[i] = i < n ? i : -1;
         return;
     }
     const unsigned long long *keys = p.keys + bh * p.c.P;
-    constexpr int K = kWave / kSelWaves, HELD = 2 * K;  // HELD: keys that a thread keeps in registers; those behind them are read again
-    __shared__ int s_hist[kBuckets];
-    __shared__ float s_low[kSelWaves], s_high[kSelWaves];
-    __shared__ int s_above[kSelWaves], s_count[kWave];
+    constexpr int WAVES = THREADS / kWave, BUCKETS = 2 * THREADS;
+    constexpr int LANES = kWave / WAVES, K = LANES < HELD ? LANES : HELD;      // stretches that a wavefront can count at a time, that it does
+    static_assert(kRanked <= THREADS && HELD == (MORE ? 2 * K : K), "a thread for every ranked key, one or two rounds of counting");
+    __shared__ int s_hist[BUCKETS];
+    __shared__ float s_low[WAVES], s_high[WAVES];
+    __shared__ int s_above[WAVES], s_count[kWave];
     __shared__ int s_bucket, s_need, s_ranked;
     __shared__ unsigned long long s_key[kRanked], s_border;
     __shared__ int s_place[kRanked], s_border_place;
     unsigned long long mine[HELD];
     float number[HELD];      // the scores in fp32 (the buckets only need an order), then, as integers, their buckets
 #pragma unroll
-    for (int k = 0; k < HELD; ++k) mine[k] = tid + k * kSelThreads < n ? keys[tid + k * kSelThreads] : 0ull;
+    for (int k = 0; k < HELD; ++k) mine[k] = tid + k * THREADS < n ? keys[tid + k * THREADS] : 0ull;
     const auto number_of = [&](unsigned long long k) { return k < kKeyNaN ? (float)key_score(k) : INFINITY; };
     // ---- the smallest and the largest finite score
     float low = INFINITY, high = -INFINITY;
@@ -192,53 +195,53 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
     };
 #pragma unroll
     for (int k = 0; k < HELD; ++k)
-        if (k * kSelThreads < n && tid + k * kSelThreads < n) {
+        if (k * THREADS < n && tid + k * THREADS < n) {
             number[k] = number_of(mine[k]);
             widen(number[k]);
         }
-    for (int i = tid + HELD * kSelThreads; i < n; i += kSelThreads) widen(number_of(keys[i]));
+    for (int i = tid + HELD * THREADS; MORE && i < n; i += THREADS) widen(number_of(keys[i]));
     low = -rows_allreduce_max(row_allreduce_max(-low));
     high = rows_allreduce_max(row_allreduce_max(high));
     if (lane == 0) { s_low[wave] = low; s_high[wave] = high; }
-    for (int i = tid; i < kBuckets; i += kSelThreads) s_hist[i] = 0;
+    for (int i = tid; i < BUCKETS; i += THREADS) s_hist[i] = 0;
     if (tid == 0) s_ranked = 0;
     __syncthreads();
-    low = -row_allreduce_max(-s_low[lane % kSelWaves]);
-    high = row_allreduce_max(s_high[lane % kSelWaves]);
-    const float spread = high > low ? (float)(kBuckets - 5) / (high - low) : 0.f;      // (0 too where high - low is not finite)
+    low = -row_allreduce_max(-s_low[lane % WAVES]);
+    high = row_allreduce_max(s_high[lane % WAVES]);
+    const float spread = high > low ? (float)(BUCKETS - 5) / (high - low) : 0.f;      // (0 too where high - low is not finite)
     const auto bucket_of = [&](unsigned long long k, float x) {      // never falls where the key grows
-        const float at = fminf(fmaxf((x - low) * spread, 0.f), (float)(kBuckets - 5));      // (no number where infinity is multiplied by zero: 0)
-        return k >= kKeyNaN ? kBuckets - 1 - (int)(k == kKeyNaN) : x >= INFINITY ? kBuckets - 3 : x <= -INFINITY ? 0 : 1 + (int)at;
+        const float at = fminf(fmaxf((x - low) * spread, 0.f), (float)(BUCKETS - 5));      // (no number where infinity is multiplied by zero: 0)
+        return k >= kKeyNaN ? BUCKETS - 1 - (int)(k == kKeyNaN) : x >= INFINITY ? BUCKETS - 3 : x <= -INFINITY ? 0 : 1 + (int)at;
     };
 #pragma unroll
     for (int k = 0; k < HELD; ++k)
-        if (k * kSelThreads < n && tid + k * kSelThreads < n) {
+        if (k * THREADS < n && tid + k * THREADS < n) {
             const int to = bucket_of(mine[k], number[k]);
             number[k] = __int_as_float(to);
             atomicAdd(&s_hist[to], 1);
         }
-    for (int i = tid + HELD * kSelThreads; i < n; i += kSelThreads) atomicAdd(&s_hist[bucket_of(keys[i], number_of(keys[i]))], 1);
+    for (int i = tid + HELD * THREADS; MORE && i < n; i += THREADS) atomicAdd(&s_hist[bucket_of(keys[i], number_of(keys[i]))], 1);
     const auto each_of = [&](int bucket, auto f) {      // every key of a bucket, and its place
 #pragma unroll
         for (int k = 0; k < HELD; ++k)
-            if (k * kSelThreads < n && tid + k * kSelThreads < n && __float_as_int(number[k]) == bucket) f(mine[k], tid + k * kSelThreads);
-        for (int i = tid + HELD * kSelThreads; i < n; i += kSelThreads) {
+            if (k * THREADS < n && tid + k * THREADS < n && __float_as_int(number[k]) == bucket) f(mine[k], tid + k * THREADS);
+        for (int i = tid + HELD * THREADS; MORE && i < n; i += THREADS) {
             const unsigned long long k = keys[i];
             if (bucket_of(k, number_of(k)) == bucket) f(k, i);
         }
     };
     __syncthreads();
-    // ---- the bucket of rank keep: thread t has buckets kBuckets - 1 - 2 t and the one below
+    // ---- the bucket of rank keep: thread t has buckets BUCKETS - 1 - 2 t and the one below
     {
-        const int v0 = s_hist[kBuckets - 1 - 2 * tid], v1 = s_hist[kBuckets - 2 - 2 * tid];
+        const int v0 = s_hist[BUCKETS - 1 - 2 * tid], v1 = s_hist[BUCKETS - 2 - 2 * tid];
         const int upto = wave_scan(v0 + v1);
         if (lane == kWave - 1) s_above[wave] = upto;
         __syncthreads();
-        const int others = wave_scan(lane < kSelWaves ? s_above[lane % kSelWaves] : 0);
+        const int others = wave_scan(lane < WAVES ? s_above[lane % WAVES] : 0);
         int before = upto - v0 - v1 + (wave ? __builtin_amdgcn_readlane(others, wave - 1) : 0);
-        if (before < keep && before + v0 >= keep) { s_bucket = kBuckets - 1 - 2 * tid; s_need = keep - before; }
+        if (before < keep && before + v0 >= keep) { s_bucket = BUCKETS - 1 - 2 * tid; s_need = keep - before; }
         before += v0;
-        if (before < keep && before + v1 >= keep) { s_bucket = kBuckets - 2 - 2 * tid; s_need = keep - before; }
+        if (before < keep && before + v1 >= keep) { s_bucket = BUCKETS - 2 - 2 * tid; s_need = keep - before; }
     }
     __syncthreads();
     const int at = s_bucket;
@@ -291,7 +294,7 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
         }
     }
     // ---- the places, ascending: keys above the border's, and of those equal to it the first ones (up to a place, or `need` of them); K stretches of
-    // kSelThreads pages at a time, lane 16 k + w of every wavefront counting for stretch k and wavefront w
+    // THREADS pages at a time, lane 16 k + w of every wavefront counting for stretch k and wavefront w
     const bool by_place = border_place < n;
     int above0 = 0, equal0 = 0;
     const auto put = [&](int i0, auto key_of) {
@@ -300,8 +303,8 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             ba[k] = be[k] = 0;
-            if (i0 + k * kSelThreads < n) {
-                const int i = i0 + k * kSelThreads + tid;
+            if (i0 + k * THREADS < n) {
+                const int i = i0 + k * THREADS + tid;
                 const unsigned long long x = key_of(k, i);      // (0 behind the last one)
                 ba[k] = ballot64(x > border || (i <= border_place && x == border && by_place));
                 if (!by_place) be[k] = ballot64(i < n && x == border);
@@ -309,23 +312,25 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(PagSelParams 
             }
         }
         if (i0 > 0) __syncthreads();
-        if (lane < K) s_count[lane * kSelWaves + wave] = mine_of;
+        if (lane < LANES) s_count[lane * WAVES + wave] = mine_of;
         __syncthreads();
         const int counts = s_count[lane], upto = wave_scan(counts);
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (ba[k] | be[k]) {
-                const int before = __builtin_amdgcn_readlane(upto - counts, k * kSelWaves + wave);
+                const int before = __builtin_amdgcn_readlane(upto - counts, k * WAVES + wave);
                 const int above = above0 + (before & 0xffff) + lanes_below(ba[k]), equal = equal0 + (before >> 16) + lanes_below(be[k]);
-                if (ba[k] >> lane & 1 || (be[k] >> lane & 1 && equal < need)) sel[above + min(equal, need)] = i0 + k * kSelThreads + tid;
+                if (ba[k] >> lane & 1 || (be[k] >> lane & 1 && equal < need)) sel[above + min(equal, need)] = i0 + k * THREADS + tid;
             }
         const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
         above0 += all & 0xffff;
         equal0 += all >> 16;
     };
     put(0, [&](int k, int) { return mine[k]; });
-    if (n > K * kSelThreads) put(K * kSelThreads, [&](int k, int) { return mine[K + k]; });
-    for (int i0 = HELD * kSelThreads; i0 < n; i0 += K * kSelThreads) put(i0, [&](int, int i) { return i < n ? keys[i] : 0ull; });
+    if constexpr (MORE) {
+        if (n > K * THREADS) put(K * THREADS, [&](int k, int) { return mine[K + k]; });
+        for (int i0 = HELD * THREADS; i0 < n; i0 += K * THREADS) put(i0, [&](int, int i) { return i < n ? keys[i] : 0ull; });
+    }
 }
 
 size_t paged_select_bytes(int B, int H, int P) { return align_up((size_t)B * H * P * sizeof(unsigned long long), 256); }
@@ -335,6 +340,10 @@ template <typename T, int D> static void launch_score(const PagSelParams &p, hip
     if (p.G <= 4) hipLaunchKernelGGL((paged_score_kernel<T, D, 1>), grid, threads, 0, stream, p);
     else if (p.G <= 8) hipLaunchKernelGGL((paged_score_kernel<T, D, 2>), grid, threads, 0, stream, p);
     else hipLaunchKernelGGL((paged_score_kernel<T, D, 0>), grid, threads, 0, stream, p);
+}
+
+template <int THREADS, int HELD, bool MORE> static void launch_choice(const PagSelParams &p, hipStream_t stream) {
+    hipLaunchKernelGGL((paged_select_kernel<THREADS, HELD, MORE>), dim3((unsigned)(p.c.B * p.c.H)), dim3(THREADS), 0, stream, p);
 }
 
 hipError_t launch_paged_select(const PagedSelectArgs &a, hipStream_t stream) {
@@ -356,7 +365,10 @@ hipError_t launch_paged_select(const PagedSelectArgs &a, hipStream_t stream) {
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(paged_select_kernel, dim3((unsigned)(a.c.B * a.c.H)), dim3(kSelThreads), 0, stream, p);
+    // both kernels, 64, 500, 1000, 1500, 2040 pages of 8 heads: 7.1, 7.8, 8.3, 8.8, 9.4 us with 512 threads, 8.2, 8.6, 8.8, 9.1, 9.5 with 1024; 256 threads take 7.0,
+    // 8.1 and 9.2 for the first three; without the keys behind four stretches 1024 take 10.8 and 11.6 for 3000 and 4000, with them 10.9 and 11.7
+    if (a.c.P <= 2048) launch_choice<512, 4, false>(p, stream);
+    else launch_choice<1024, 8, true>(p, stream);
     return hipGetLastError();
 }
 

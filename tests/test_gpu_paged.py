@@ -544,6 +544,23 @@ def test_select(n, keep, first, recent, dtype, qdt, d, G):
     assert torch.equal(many.cpu(), want_many) and torch.equal(sel.cpu(), want)
 
 
+@pytest.mark.parametrize("P", [511, 512, 513, 2047, 2048, 2049, 4096, 4097, 8191, 8192, 8193, 12290])
+def test_select_tables_of_many_lengths(P):
+    """Tables and lengths around whole stretches of pages; equal scores among the others."""
+    print("select tables", P, flush=True)
+    pc = Paged(5, 1, P, 16, 64, BF, junk=False, seed=P)
+    lens = [[P * 16], [P * 16 - 15], [P * 8], [min(P, 520) * 16 - 8], [max(0, P - 4095) * 16]]
+    lo = torch.randn((pc.n, 1, 64), generator=pc.gen).to(BF)
+    lo[torch.rand((pc.n,), generator=pc.gen) < 0.2] = 0.5
+    hi = (lo.double() + 0.25).to(BF)
+    pc.k_min, pc.k_max = lo.to(DEV), hi.to(DEV)
+    Q = torch.randn((5, 2, 64), generator=pc.gen).to(BF)
+    for keep, first, recent in ((33, 1, 2), (P // 3, 0, 0), (P - 1, 5, 7)):
+        sel, many = sc.sc_paged_select(pc.cache(), Q.to(DEV), torch.tensor([x[0] for x in lens], dtype=torch.int32, device=DEV), keep, first=first, recent=recent)
+        want, want_many = want_selection(pc, lo, hi, Q, lens, 2, keep, first, recent)
+        assert torch.equal(many.cpu(), want_many) and torch.equal(sel.cpu(), want), keep
+
+
 def test_select_ties_go_to_the_lowest_page():
     print("select ties", flush=True)
     n = 2500
