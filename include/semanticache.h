@@ -467,7 +467,8 @@ sc_status sc_paged_decode_attn(const sc_paged_cache *cache, const void *Q, sc_dt
  *     score = max over the Hq / Hkv query heads of  sum_e max(q_e k_min_e, q_e k_max_e).
  * The first `first` and the last `recent` pages of a sequence are kept in any case, then those of the largest
  * scores, up to `keep` pages, of equal scores the lowest; a score that is not a number and a page number outside the pool rank
- * above all others, so that attention over the selection shows them.  Scores are sums in fp64: the choice is
+ * above all others, so that attention over the selection shows them.  (0 times infinity is no number; an infinite
+ * bound on the side that the larger product does not need changes nothing.)  Scores are sums in fp64: the choice is
  * that of exact arithmetic except for scores within some 1e-13 of each other.
  *   Q, lens         as for sc_paged_decode_attn;  the cache needs k_min and k_max
  *   keep            1 .. 2^20, at least first + recent (SC_ERR_CAPACITY otherwise)

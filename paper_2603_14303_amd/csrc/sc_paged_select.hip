@@ -93,7 +93,7 @@ __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams
         hi[ks] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(cv.k_max) + row + E * (4 * ks + g));
     }
 #pragma unroll
-    for (int i = 0; i < PER; ++i) s_q[q_place(e0 + i, head)] = make_double2(x[i] < 0.0 ? 0.0 : x[i], x[i] > 0.0 ? 0.0 : x[i]);      // (a NaN is in both)
+    for (int i = 0; i < PER; ++i) s_q[q_place(e0 + i, head)] = make_double2(x[i] < 0.0 ? 0.0 * x[i] : x[i], x[i] > 0.0 ? 0.0 * x[i] : x[i]);      // (a NaN is in both, and beside infinity)
     __syncthreads();
     double best;
     // several sums side by side: a product takes four times as long as the next one that does not wait for it
@@ -138,6 +138,32 @@ __global__ __launch_bounds__(kScoreThreads) void paged_score_kernel(PagSelParams
     for (int off = 16; off < kWave; off <<= 1) {
         const double other = __shfl_xor(best, off, kWave);
         best = (other > best || other != other) ? other : best;
+    }
+    // Where a bound or a query's element is infinite, the products above hold 0 x infinity, and their sum is no number; the larger product is one all the same
+    // (unless an infinity meets a zero in it).  Pages without a number are worked out anew by the maximum, the four lanes of a page a piece of the row each.
+    // (All lanes of the wavefront take part in the exchange, and the four of a page have the same sum and maximum.)
+    if (ballot64(there && best != best) != 0ull) {
+        double by_max = -INFINITY;
+        for (int hh = 0; hh < p.G; ++hh) {
+            double sum = 0.0;
+            int64_t again = row;
+            asm volatile("" : "+v"(again));      // (the bounds are read anew for every head: kept over the loop, in fp64, they would halve the workgroups of a compute unit)
+#pragma unroll 1
+            for (int ks = 0; ks < KL; ++ks) {
+                const uint4 l = *reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(cv.k_min) + again + E * (4 * ks + g));
+                const uint4 u = *reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(cv.k_max) + again + E * (4 * ks + g));
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const double2 y = s_q[q_place(E * (4 * ks + g) + i, hh)];
+                    const double q = y.y != y.y ? y.x : y.x != y.x ? y.y : y.x + y.y, x = q * element<T>(l, i), z = q * element<T>(u, i);
+                    sum += (x > z || x != x) ? x : z;      // (a NaN in either is the maximum)
+                }
+            }
+#pragma unroll
+            for (int off = 16; off < kWave; off <<= 1) sum += __shfl_xor(sum, off, kWave);
+            by_max = (sum > by_max || sum != sum) ? sum : by_max;
+        }
+        if (best != best) best = by_max;
     }
     if (g == 0 && place < pages) {
         unsigned long long key = there ? score_key(best) : kKeyNaN;

@@ -697,6 +697,57 @@ def test_select_with_many_heads_ties_and_what_is_not_a_number(dtype, d, G):
         assert torch.equal(many.cpu(), want_many) and torch.equal(sel.cpu(), want), keep
 
 
+@pytest.mark.parametrize("dtype, qdt, d, G, n", [(BF, BF, 128, 3, 300), (BF, F32, 64, 7, 300), (F32, F32, 128, 16, 300), (F32, BF, 64, 1, 300), (BF, BF, 128, 8, 2500)])
+def test_select_infinite_bounds_and_queries(dtype, qdt, d, G, n):
+    """The score is the sum of the larger products: a bound that is infinite on the side that a query does not look at changes nothing, on the other side it
+    puts the page first or last; an infinite element of a query likewise.  0 x infinity is no number, and those pages come before all others."""
+    print("select infinite", dtype, qdt, d, G, n, flush=True)
+    pc = Paged(1, 3, n, 16, d, dtype, junk=False, seed=G)
+    lo = torch.randn((pc.n, 3, d), generator=pc.gen).to(dtype)
+    hi = (lo.double() + torch.rand((pc.n, 3, d), generator=pc.gen)).to(dtype)
+    Q = torch.randn((1, 3, G, d), generator=pc.gen)
+    Q[..., :8], Q[..., 8:16] = Q[..., :8].abs() + 0.1, -Q[..., 8:16].abs() - 0.1      # (of one sign in all heads)
+    Q[0, 2, G - 1, 20], Q[0, 2, 0, 21] = math.inf, -math.inf
+    Q[0, 2, :, 22] = 0.0
+    kind = torch.randint(0, 40, (pc.n, 3), generator=pc.gen)
+    for h in range(3):
+        for page in range(pc.n):
+            k, e = int(kind[page, h]), int(torch.randint(0, 8, (1,), generator=pc.gen))
+            if k < 6:      # nothing changes
+                lo[page, h, e] = -math.inf
+            elif k < 12:
+                hi[page, h, 8 + e] = math.inf
+            elif k == 12:      # first, last
+                hi[page, h, e] = math.inf
+            elif k == 13:
+                lo[page, h, e] = hi[page, h, e] = -math.inf
+            elif k == 14:
+                lo[page, h, 8 + e] = hi[page, h, 8 + e] = math.inf
+            elif k == 15 and h == 1:      # +inf and -inf in one sum, or no number to begin with
+                lo[page, h, e], hi[page, h, e], lo[page, h, 8 + e] = -math.inf, -math.inf, -math.inf
+            elif k == 16 and h == 1:
+                lo[page, h, e] = math.nan
+            elif k < 20 and h == 2:      # for the infinite elements of the queries: products with zero, of both signs, of one
+                lo[page, h, 20 + k % 2] = 0.0
+            elif k < 24 and h == 2:
+                hi[page, h, 22] = math.inf
+            elif k < 38 and h == 2:      # products of -inf, which the other heads outdo
+                lo[page, h, 20], hi[page, h, 20], lo[page, h, 21], hi[page, h, 21] = -2.0, -1.0, 1.0, 2.0
+    pc.k_min, pc.k_max = lo.to(DEV), hi.to(DEV)
+    Q = Q.reshape(1, 3 * G, d).to(qdt)
+    dl = torch.tensor([n * 16], dtype=torch.int32, device=DEV)
+    for keep, first, recent in ((1, 0, 0), (n // 8, 1, 2), (n // 2, 0, 0), (n - 5, 0, 1)):
+        sel, many = sc.sc_paged_select(pc.cache(), Q.to(DEV), dl, keep, first=first, recent=recent)
+        assert (many.cpu() == keep).all()
+        for h in range(3):
+            page, head, _ = pc.place(0, h, torch.arange(n) * 16)
+            q = Q[0, h * G : (h + 1) * G].double()
+            score = torch.maximum(q[:, None] * lo[page, head].double(), q[:, None] * hi[page, head].double()).sum(2)
+            odd, score = score.isnan().any(0).tolist(), score.amax(0).tolist()
+            order = sorted(range(n), key=lambda i: (not (i < first or i >= n - recent), not odd[i], 0.0 if odd[i] else -score[i], i))
+            assert sel[0, h].tolist() == sorted(order[:keep]), (h, keep)
+
+
 def test_append_select_and_attend_together():
     """Prompt, then tokens: pages chosen by the summaries that the appends left, attention over them; every length per head too."""
     print("together", flush=True)
