@@ -409,7 +409,8 @@ typedef struct {
  *   counts          device i32 [B, Hkv, N], contiguous; required if and only if the cache has counts
  *   base_lens       device i32: rows that the cache holds
  *   new_lens        device i32 or NULL (= N for all): rows to append, 0 .. N
- *   lens            device i32: the new lengths; not the same array as base_lens or new_lens.  Set to -1, with nothing
+ *   lens            device i32: the new lengths; no element in common with base_lens, new_lens or positions (they are
+ *                   read while it is written: SC_ERR_INVALID_ARG).  Set to -1, with nothing
  *                   written to the cache for it, if base_lens is negative, new_lens outside [0, N], the sum
  *                   beyond table_len * page_rows, or a position of a row outside the angles; set to -1
  *                   if a page it needs has a number outside the pool (rows of its other pages are written)

@@ -444,14 +444,18 @@ static bool rows_ok(const void *p, int64_t B, int64_t H, int64_t N, int64_t sb, 
     return aligned16(p);
 }
 
+// whether two arrays have no element in common (b may be NULL)
+static bool apart(const int32_t *a, int64_t na, const int32_t *b, int64_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return !b || x + na * sizeof(int32_t) <= y || y + nb * sizeof(int32_t) <= x;
+}
+
 sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *r, void *stream) {
     PagedAppendArgs a;
     const sc_status st = paged_check(cache, a.c);
     if (st != SC_OK) return st;
     if (!r || !r->K || !r->V || !r->base_lens || !r->lens || r->N <= 0) return SC_ERR_INVALID_ARG;
     if (!aligned4(r->base_lens) || !aligned4(r->lens) || !aligned4(r->new_lens) || !aligned4(r->positions) || !aligned4(r->counts)) return SC_ERR_INVALID_ARG;
-    // every workgroup reads the old lengths while one of them files the new ones
-    if (r->lens == r->base_lens || r->lens == r->new_lens) return SC_ERR_INVALID_ARG;
     if (!r->counts != !cache->counts) return SC_ERR_INVALID_ARG;
     const int64_t es = (int64_t)elem_size(cache->dtype);
     if (!rows_ok(r->K, cache->B, cache->Hkv, r->N, r->k_stride_b, r->k_stride_h, r->k_stride_n, cache->d, es, false)) return SC_ERR_INVALID_ARG;
@@ -473,6 +477,9 @@ sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *r, v
         if (r->Hq > 65535) return SC_ERR_UNSUPPORTED;
     }
     if (!paged_append_fits(cache->B, cache->Hkv, cache->page_rows, r->N, r->Q ? r->Hq : 0)) return SC_ERR_UNSUPPORTED;      // grid size
+    // every workgroup reads the old lengths and the positions while one of them files the new lengths
+    const int64_t n = (int64_t)cache->B * (r->per_head ? cache->Hkv : 1);
+    if (!apart(r->lens, n, r->base_lens, n) || !apart(r->lens, n, r->new_lens, n) || !apart(r->lens, n, r->positions, cache->B)) return SC_ERR_INVALID_ARG;
     a.K = static_cast<const char *>(r->K); a.V = static_cast<const char *>(r->V);
     a.k_b = r->k_stride_b * es; a.k_h = r->k_stride_h * es; a.k_n = r->k_stride_n * es;
     a.v_b = r->v_stride_b * es; a.v_h = r->v_stride_h * es; a.v_n = r->v_stride_n * es;

@@ -463,6 +463,19 @@ def test_append_merged_rows(own_pages, dtype):
     check_append(pc2, 80, [[0] * 3] * 2, [[80] * 3, [13] * 3], rot=32, G=2)
 
 
+def test_append_lengths_side_by_side():
+    """Old lengths, new ones and positions as neighbours in one array."""
+    print("append neighbours", flush=True)
+    pc = Paged(3, 2, 4, 16, 128, BF, junk=False)
+    k = torch.randn((3, 2, 5, 128), generator=pc.gen).to(BF).to(DEV)
+    x = torch.tensor([7, 16, 30, -9, -9, -9, 0, 50, 9], dtype=torch.int32, device=DEV)
+    sc.sc_paged_append(pc.cache(), k, k, x[:3], x[3:6], cos_sin=angles(128, 60).to(DEV), positions=x[6:])
+    assert x.tolist() == [7, 16, 30, 12, 21, 35, 0, 50, 9]
+    for lens in (x[2:5], x[4:7], x[6:]):
+        with pytest.raises(sc.SemantiCacheError):
+            sc.sc_paged_append(pc.cache(), k, k, x[:3], lens, cos_sin=angles(128, 60).to(DEV), positions=x[6:])
+
+
 def test_append_after_going_back():
     """Rows that are taken back (a shorter length than before) leave no trace in the summaries."""
     print("append going back", flush=True)

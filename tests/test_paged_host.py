@@ -74,6 +74,19 @@ def test_append_rejects_bad_arguments(lib):
     assert _status(call, dict(B=60000, Hkv=16, page_heads=16, page_rows=16, table_len=2**27 - 1, stride_page=16 * 32 * 128), N=2**31 - 1) == UNSUPPORTED      # grid
 
 
+def test_append_refuses_lengths_that_are_read_while_they_are_written(lib):
+    """positions, base_lens and new_lens are read by every workgroup; one of them writes lens.  B = 2 sequences, 4 heads."""
+    arrays = dict(base_lens=FAKE + 1024, new_lens=FAKE + 3072, positions=FAKE + 4096)
+
+    def status(lens, per_head=0):
+        r = sc._PagedRowsStruct(**{**ROWS, **arrays, "lens": lens, "per_head": per_head})
+        return lib.sc_paged_append(ctypes.byref(sc._PagedCacheStruct(**CACHE)), ctypes.byref(r), None)
+    for name, at in arrays.items():
+        assert status(at) == ARG and status(at + 4) == ARG and status(at - 4) == ARG, name
+        # every head its own length: eight of them, and positions of the two sequences
+        assert status(at, 1) == ARG and status(at + (4 if name == "positions" else 28), 1) == ARG and status(at - 28, 1) == ARG, name
+
+
 def test_decode_rejects_bad_arguments(lib):
     need = lib.sc_paged_workspace_bytes(2, 8, 4, 128, 20)
     ok = dict(Q=FAKE, qdt=1, Hq=8, lens=FAKE, per_head=0, sel=FAKE, sel_lens=FAKE, keep=5, scale=0.0, O=FAKE, odt=1, lse=FAKE, ws=FAKE, wsb=need)
