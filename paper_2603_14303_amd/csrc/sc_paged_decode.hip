@@ -441,6 +441,12 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
                 if (cv.counts) sv[i] = x.n[i] > 0 ? sv[i] + __log2f((float)x.n[i]) : -INFINITY;
                 if (4 * g + i >= here) sv[i] = -INFINITY;
             }
+            // rows without weight: their values may be anything, and 0 times a NaN is one
+            int nothing = 0;
+            if (cv.counts) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) nothing |= x.n[i] > 0 ? 0 : 1 << i;
+            }
             request_keys(cur, pages, s + 1);
             float m_loc = m_run;
 #pragma unroll
@@ -461,6 +467,12 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
                 for (int k = 0; k < NA; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[k][i] *= al[i];
+            }
+            if (ballot64(nothing != 0) != 0ull) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int k = 0; k < VW; ++k) x.v[i][k] = nothing >> i & 1 ? 0u : x.v[i][k];
             }
             if constexpr (kBf16) {
                 uint32_t p01[PP], p23[PP];

@@ -192,6 +192,31 @@ def test_decode_sizes_of_zero_weigh_nothing():
     assert (O == 0).all() and (lse == -math.inf).all()
 
 
+@pytest.mark.parametrize("dtype, qdt, d, n", [(BF, BF, 128, 200), (BF, F32, 128, 4000), (BF, BF, 64, 77), (F32, F32, 128, 500), (F32, BF, 64, 3000)])
+def test_decode_rows_of_size_zero_may_hold_anything(dtype, qdt, d, n):
+    """Neither a key nor a value of a row without weight shows, whatever it is."""
+    print("decode size zero holds anything", dtype, qdt, d, n, flush=True)
+    pc = Paged(1, 2, -(-n // 32), 32, d, dtype, counts=True, seed=n)
+    pc.counts.copy_(torch.randint(-1, 4, pc.counts.shape, generator=pc.gen, dtype=torch.int32))
+    rows = pc.fill([[n, n]])
+    wild = torch.tensor([math.nan, math.inf, -math.inf], dtype=dtype)
+    K, V = pc.K.cpu(), pc.V.cpu()
+    for h in range(2):
+        page, head, row = pc.place(0, h, torch.arange(n))
+        none = rows[0, h][2] <= 0
+        for X in (K, V):
+            X[page[none], head, row[none]] = wild[torch.randint(0, 3, (int(none.sum()), d), generator=pc.gen)]
+    pc.K.copy_(K)
+    pc.V.copy_(V)
+    Q = torch.randn((1, 10, d), generator=pc.gen).to(qdt)
+    O, lse = sc.sc_paged_decode_attn(pc.cache(), Q.to(DEV), torch.tensor([n], dtype=torch.int32, device=DEV), want_lse=True)
+    for h in range(2):
+        some = rows[0, h][2] > 0
+        wo, wl, to, tl = attend(Q[0, 5 * h : 5 * h + 5].double(), tuple(x[some] for x in rows[0, h]), 1 / math.sqrt(d))
+        close(O[0, 5 * h : 5 * h + 5], wo, to + half_step(qdt) * wo.abs() * (1 + 2.0**-6))
+        close(lse[0, 5 * h : 5 * h + 5], wl, tl)
+
+
 @pytest.mark.parametrize("B, H, lens", [(1, 1, [9000]), (1, 8, [5400]), (5, 2, [17, 3000, 1, 8000, 900]), (40, 4, list(range(1, 1600, 40))), (130, 2, [31] * 130)])
 def test_decode_work_is_split_and_joined(B, H, lens):
     """Heads across many workgroups, many heads in one workgroup, ragged; the same answer, bit for bit, on a workspace in use."""
