@@ -217,6 +217,23 @@ def test_decode_rows_of_size_zero_may_hold_anything(dtype, qdt, d, n):
         close(lse[0, 5 * h : 5 * h + 5], wl, tl)
 
 
+@pytest.mark.parametrize("qdt", [F32, BF])
+def test_decode_logits_of_an_fp32_cache_are_summed_in_parts(qdt):
+    """Logits that are zero exactly, sums of d = 128 products whose second half takes the first one back, as the lse of single rows.  With four sums of d / 4 the k-th
+    partial one has the variance k up to its middle and ends at zero; every rounding is off by at most u times it, evenly spread: a mean square of at most
+    4 (d / 4)^2 / 4 u^2 / 3, in products of one (one sum over all d would have up to four times that)."""
+    print("decode sums in parts", qdt, flush=True)
+    B, H, G, d = 64, 8, 8, 128
+    pc = Paged(B, H, 1, 16, d, F32, junk=False)
+    q, k = torch.randn((B, H * G, d // 2), generator=pc.gen).to(qdt), torch.randn((B, H, d // 2), generator=pc.gen)
+    K = pc.K.cpu()
+    K[pc.table[:, 0].long(), :, 0] = torch.cat((k, -k), 2)
+    pc.K.copy_(K)
+    _, lse = sc.sc_paged_decode_attn(pc.cache(), torch.cat((q, q), 2).to(DEV), torch.ones(B, dtype=torch.int32, device=DEV), scale=1.0, want_lse=True)
+    off = float(lse.double().square().mean().sqrt())
+    assert 0 < off <= math.sqrt(d * d / 16 / 3) * U, off / U
+
+
 @pytest.mark.parametrize("B, H, lens", [(1, 1, [9000]), (1, 8, [5400]), (5, 2, [17, 3000, 1, 8000, 900]), (40, 4, list(range(1, 1600, 40))), (130, 2, [31] * 130)])
 def test_decode_work_is_split_and_joined(B, H, lens):
     """Heads across many workgroups, many heads in one workgroup, ragged; the same answer, bit for bit, on a workspace in use."""
