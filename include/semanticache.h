@@ -447,8 +447,8 @@ sc_status sc_paged_init_workspace(void *ws, size_t ws_bytes, void *stream);
 
 /* sc_paged_decode_attn — sc_decode_attn over a cache in pages:
  *     O[b,hq] = softmax_t( Q[b,hq] . K[b,h,t] * scale + ln(counts[b,h,t]) ) V[b,h,t],  t in [0, lens),  h = hq / (Hq / Hkv),
- * without the logarithm if the cache has no counts.  fp32 (bf16 caches: probabilities in two bf16 parts, queries of fp32 and their probabilities in
- * three); fp32 accumulation.  Rows of size <= 0 weigh nothing.  A length <= 0 gives O = 0 and
+ * without the logarithm if the cache has no counts.  fp32 (bf16 caches: probabilities, and queries of fp32, as sums of
+ * three bf16 parts); fp32 accumulation.  Rows of size <= 0 weigh nothing.  A length <= 0 gives O = 0 and
  * lse = -inf; a length beyond the table's pages counts as the pages' rows.  A page number outside the pool gives NaN for its heads' O and lse.
  *   Q               device [B, Hq, d] of q_dtype, contiguous, 16-byte aligned; Hq / Hkv <= 16
  *   lens            device i32 [B], or [B, Hkv] if lens_per_head

@@ -10,8 +10,8 @@
 // Step.  A wavefront takes 16 rows at a time, always of one page.  Keys are loaded as the first product wants them (lane (g, c) of the wavefront's
 // 4 x 16 lanes: row c, 16 bytes at 64 ks + 16 g), values as the second one does (rows 4 g + i).  The scores leave the first product with lane (g, c)
 // holding head c, rows 4 g + i: the second product's own layout, so the probabilities never move.  Softmax is online, in the exp2 domain.  bf16:
-// v_mfma_f32_16x16x32_bf16 and v_mfma_f32_16x16x16_bf16, probabilities as two bf16 parts (a rounding of 2^-18; one part would put 2^-9 of each weight
-// into the result, as much as its own rounding); fp32 queries over a bf16 cache as three parts, as are their probabilities; fp32 caches: v_mfma_f32_16x16x4_f32.
+// v_mfma_f32_16x16x32_bf16 and v_mfma_f32_16x16x16_bf16, probabilities as three bf16 parts, which hold all bits of fp32 (two parts, a rounding of 2^-18, are not
+// faster: 8 heads x 32768 rows 27.9 us with either, 170 rows 6.6 and 6.5); fp32 queries over a bf16 cache as three parts, too; fp32 caches: v_mfma_f32_16x16x4_f32.
 //
 // Measured (d = 128, bf16): 8 heads x 32768 rows, G = 4: 27.4 us (4.9 TB/s; 18 us of it the rows, 7.4 TB/s); 128 heads of 8192 to 16384 rows, G = 7: 127 us
 // (6.3 TB/s); 8 heads x 170 rows: 6.6 us, x 1 row 5.5, of which the launch is 1.8: arguments, lengths, page numbers, rows and the results' store follow each other.
@@ -244,7 +244,7 @@ template <typename T, int D, int QP>
 __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecParams p) {
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int KL = Rows<T, D>::KL, VW = Rows<T, D>::VW, NA = Acc<T, D>::N;
-    constexpr int PP = QP == 1 ? 2 : 3;       // parts of the probabilities (bf16)
+    constexpr int PP = 3;                     // parts of the probabilities (bf16)
     constexpr int kStride = D + kPagPad;
     const PagedView &cv = p.c;
     const int G = p.G;

@@ -217,6 +217,30 @@ def test_decode_rows_of_size_zero_may_hold_anything(dtype, qdt, d, n):
         close(lse[0, 5 * h : 5 * h + 5], wl, tl)
 
 
+@pytest.mark.parametrize("d, G", [(128, 16), (64, 7)])
+def test_decode_weights_of_a_bf16_cache_have_the_bits_of_fp32(d, G):
+    """Values that are unit vectors show the weights of 16 rows; O in fp32, logits within 1.5 of each other from single exact products.  In roundings u of fp32: a logit
+    in the exp2 domain is off by 2 of its at most 2.2 (the factor's and the product's), so is the largest one, their difference by one more, exp2 by 2, the sum of 16 by
+    16 additions' at most half of that (pairs, then rows of lanes: 6) and its terms', the quotient by 3, a weight's three parts and the product by 2: below 30 in all.
+    (Weights in 16 bits would be off by up to 64.)"""
+    print("decode weights", d, G, flush=True)
+    B, H = 8, 2
+    pc = Paged(B, H, 1, 16, d, BF, junk=False)
+    K, V, Q = torch.zeros(pc.K.shape, dtype=BF), torch.zeros(pc.V.shape, dtype=BF), torch.zeros((B, H * G, d), dtype=BF)
+    K[..., 3] = (torch.rand(K.shape[:3], generator=pc.gen) * 0.75).to(BF)
+    Q[..., 3] = (torch.rand(Q.shape[:2], generator=pc.gen) * 2 - 1).to(BF)
+    V[:, :, range(16), range(16)] = 1.0
+    pc.K.copy_(K)
+    pc.V.copy_(V)
+    O = torch.empty((B, H * G, d), dtype=F32, device=DEV)
+    sc.sc_paged_decode_attn(pc.cache(), Q.to(DEV), torch.full((B,), 16, dtype=torch.int32, device=DEV), scale=2.0, O=O)
+    for b in range(B):
+        for h in range(H):
+            z = 2.0 * Q[b, h * G : (h + 1) * G, 3:4].double() * K[int(pc.table[b, 0]), h, :, 3].double()
+            close(O[b, h * G : (h + 1) * G, :16], torch.softmax(z, 1), 30 * U * torch.softmax(z, 1))
+    assert not O[..., 16:].any()
+
+
 @pytest.mark.parametrize("qdt", [F32, BF])
 def test_decode_logits_of_an_fp32_cache_are_summed_in_parts(qdt):
     """Logits that are zero exactly, sums of d = 128 products whose second half takes the first one back, as the lse of single rows.  With four sums of d / 4 the k-th
