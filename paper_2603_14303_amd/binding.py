@@ -510,6 +510,7 @@ class PagedCache:
 
     K, V [pages, heads, R, d], any strides with a contiguous last dimension, the same for both; counts i32 [pages, heads, R], k_min and k_max
     [pages, heads, d] contiguous, if any; table i32 [B, P], or [B, Hkv, P] with pools of one head a page: every KV head then has pages of its own.
+    The tensors' contents may change between calls; another tensor (a longer table, say) takes a new PagedCache: the calls go by the addresses.
     """
 
     def __init__(self, K, V, table, counts=None, k_min=None, k_max=None):
@@ -536,6 +537,15 @@ class PagedCache:
             stride_page=K.stride(0), stride_head=K.stride(1), stride_row=K.stride(2), dtype=_dtype_code(K), num_pages=pages, page_heads=heads,
             page_rows=R, table_len=table.shape[-1], table_per_head=int(table.dim() == 3), B=self.B, Hkv=self.Hkv, d=d)
         self.ptr = ctypes.addressof(self.struct)
+        self._made = True
+
+    def _fixed(self, name, *value):
+        # (the calls read the addresses in `struct`: they would go on with memory that the old tensor has given back)
+        if "_made" in self.__dict__:
+            raise SemantiCacheError("the tensors of a PagedCache stay the same ones: make a new PagedCache for another %s" % name)
+        object.__setattr__(self, name, *value)
+
+    __setattr__ = __delattr__ = _fixed
 
     def lens_shapes(self):
         return (self.B,), (self.B, self.Hkv)

@@ -335,3 +335,18 @@ def test_the_wrappers_refuse_what_does_not_fit():
         sc.PagedCache(K, K.clone(), table, k_min=torch.zeros((3, 2, 64)))
     with pytest.raises(sc.SemantiCacheError, match="dtype"):
         sc.PagedCache(K, K.clone(), table, k_min=torch.zeros((3, 2, 64)), k_max=torch.zeros((3, 2, 64), dtype=torch.bfloat16))
+
+
+def test_the_tensors_of_a_cache_stay_the_same_ones(monkeypatch):
+    """The library is given addresses: a tensor put in the place of another would not be seen, and the old one's memory would be used after it was freed."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(sc, "_require_cuda", lambda *a: None)
+    K, table = torch.zeros((3, 2, 16, 64)), torch.zeros((1, 2), dtype=torch.int32)
+    cache = sc.PagedCache(K, K.clone(), table)
+    assert cache.struct.table == table.data_ptr() and cache.ptr == ctypes.addressof(cache.struct)
+    for name, value in (("table", torch.zeros((1, 9), dtype=torch.int32)), ("K", K.clone()), ("counts", None), ("struct", None), ("ptr", 0), ("B", 2), ("other", 1)):
+        with pytest.raises(sc.SemantiCacheError, match="new PagedCache"):
+            setattr(cache, name, value)
+    with pytest.raises(sc.SemantiCacheError, match="new PagedCache"):
+        del cache.V
+    assert cache.table is table and cache.struct.table == table.data_ptr()
