@@ -418,7 +418,7 @@ typedef struct {
  *   rot             0 without cos_sin, else a multiple of 16 up to d
  *   positions       device i32 [B]: position of row 0 of the call, or NULL: base_lens (not with per_head)
  *   Q, Q_out        device [B, Hq, N, d] of q_dtype (strides as for K and V), or both NULL; only with cos_sin.  Q_out may
- *                   be Q itself.  A query whose position lies outside the angles comes out as NaN
+ *                   be Q itself, and shares nothing with it otherwise; its rows do not overlap.  A query whose position lies outside the angles comes out as NaN
  */
 typedef struct {
     const void *K, *V;

@@ -6,6 +6,7 @@
 
 #include "sc_host.h"
 #include "sc_paged.h"
+#include <algorithm>
 #include <vector>
 
 namespace sc {
@@ -436,7 +437,21 @@ static sc_status paged_check(const sc_paged_cache *c, PagedView &v) {
     return SC_OK;
 }
 
-// Rows [B, heads, N, d]: aligned, and, where the call writes them, no two the same.  (The stride of a dimension of one means nothing.)
+// Whether the rows of d elements of a three-dimensional array have no element in common: from the smallest stride on, each has to reach beyond what lies within it.
+// (The stride of a dimension of one means nothing.)
+static bool rows_apart(const int64_t (&size)[3], const int64_t (&stride)[3], int64_t d) {
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+    int64_t span = d;
+    for (int i : order) {
+        if (size[i] <= 1) continue;
+        if (stride[i] < span || stride[i] > INT64_MAX / 4 / size[i]) return false;
+        span += (size[i] - 1) * stride[i];
+    }
+    return true;
+}
+
+// Rows [B, heads, N, d]: aligned, and, where the call writes them, none with a stride of less than a row.
 static bool rows_ok(const void *p, int64_t B, int64_t H, int64_t N, int64_t sb, int64_t sh, int64_t sn, int64_t d, int64_t es, bool written) {
     const int64_t size[3] = {B, H, N}, stride[3] = {sb, sh, sn};
     for (int i = 0; i < 3; ++i)
@@ -477,6 +492,8 @@ sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *r, v
         if (r->Hq > 65535) return SC_ERR_UNSUPPORTED;
     }
     if (!paged_append_fits(cache->B, cache->Hkv, cache->page_rows, r->N, r->Q ? r->Hq : 0)) return SC_ERR_UNSUPPORTED;      // grid size
+    const int64_t q_size[3] = {cache->B, r->Hq, r->N}, o_stride[3] = {r->o_stride_b, r->o_stride_h, r->o_stride_n};
+    if (r->Q && !rows_apart(q_size, o_stride, cache->d)) return SC_ERR_INVALID_ARG;
     // every workgroup reads the old lengths and the positions while one of them files the new lengths
     const int64_t n = (int64_t)cache->B * (r->per_head ? cache->Hkv : 1);
     if (!apart(r->lens, n, r->base_lens, n) || !apart(r->lens, n, r->new_lens, n) || !apart(r->lens, n, r->positions, cache->B)) return SC_ERR_INVALID_ARG;

@@ -87,6 +87,16 @@ def test_append_refuses_lengths_that_are_read_while_they_are_written(lib):
         assert status(at, 1) == ARG and status(at + (4 if name == "positions" else 28), 1) == ARG and status(at - 28, 1) == ARG, name
 
 
+def test_append_refuses_queries_that_are_written_over_each_other(lib):
+    """Q_out's rows [2, 8, 8, 128]: strides that are each as long as a row and still meet."""
+    def status(b, h, n):
+        r = sc._PagedRowsStruct(**{**ROWS, "new_lens": FAKE + 512, "o_stride_b": b, "o_stride_h": h, "o_stride_n": n})
+        return lib.sc_paged_append(ctypes.byref(sc._PagedCacheStruct(**CACHE)), ctypes.byref(r), None)
+    for strides in ((8192, 128, 128), (128, 1024, 128), (1024, 1024, 128), (8192, 1024, 136), (8184, 1024, 128), (8192 - 128, 128, 1024), (120, 128, 1024),
+                    (2**62, 1024, 128)):
+        assert status(*strides) == ARG, strides
+
+
 def test_decode_rejects_bad_arguments(lib):
     need = lib.sc_paged_workspace_bytes(2, 8, 4, 128, 20)
     ok = dict(Q=FAKE, qdt=1, Hq=8, lens=FAKE, per_head=0, sel=FAKE, sel_lens=FAKE, keep=5, scale=0.0, O=FAKE, odt=1, lse=FAKE, ws=FAKE, wsb=need)
