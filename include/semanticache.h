@@ -363,7 +363,7 @@ sc_status sc_multi_attn(const void *Q, sc_dtype q_dtype, int nq,
  *
  *   pools       K, V     [num_pages, page_heads, page_rows, d] of dtype, addressed as
  *                        base + page*stride_page + head*stride_head + row*stride_row (+ e), strides in
- *                        ELEMENTS, the same for K and V, multiples of 16 bytes; 16-byte aligned
+ *                        ELEMENTS, the same for K and V, in any order of size, multiples of 16 bytes; 16-byte aligned
  *               counts   i32 [num_pages, page_heads, page_rows], contiguous, or NULL: sizes of the rows
  *               k_min, k_max   [num_pages, page_heads, d] of dtype, contiguous, 16-byte aligned, or both
  *                        NULL: per page the minimum and maximum of the keys that it holds
@@ -379,7 +379,7 @@ sc_status sc_multi_attn(const void *Q, sc_dtype q_dtype, int nq,
  * name the same page (a common prefix), but rows are appended only to pages that one of them names.
  *
  * Common host errors: NULL or misaligned pointers, sizes <= 0, page_rows not a power of two or out of
- * range, page_heads neither Hkv nor 1, strides that let rows overlap or reach 2 GiB inside a page
+ * range, page_heads neither Hkv nor 1, strides that let rows overlap, rows of a page 2 GiB apart
  * (SC_ERR_INVALID_ARG); d not in {64, 128}, bad dtype, B or Hkv > 65535, B * Hkv > 2^20, table_len *
  * page_rows >= 2^31 (SC_ERR_UNSUPPORTED).
  */

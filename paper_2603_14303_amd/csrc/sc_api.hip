@@ -402,6 +402,20 @@ sc_status sc_multi_attn_tail(const void *Q, sc_dtype q_dtype, int nq, const void
 
 
 // ------------------------------------------------------------------------------------------------
+// Whether the rows of d elements of a three-dimensional array have no element in common: from the smallest stride on, each has to reach beyond what lies within it.
+// (The stride of a dimension of one means nothing.)
+static bool rows_apart(const int64_t (&size)[3], const int64_t (&stride)[3], int64_t d) {
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+    int64_t span = d;
+    for (int i : order) {
+        if (size[i] <= 1) continue;
+        if (stride[i] < span || stride[i] > INT64_MAX / 4 / size[i]) return false;
+        span += (size[i] - 1) * stride[i];
+    }
+    return true;
+}
+
 // the cache of the sc_paged_* calls: everything about it that the host can see
 static sc_status paged_check(const sc_paged_cache *c, PagedView &v) {
     if (!c || !c->K || !c->V || !c->table) return SC_ERR_INVALID_ARG;
@@ -414,13 +428,12 @@ static sc_status paged_check(const sc_paged_cache *c, PagedView &v) {
     if (c->page_heads != (c->table_per_head ? 1 : c->Hkv)) return SC_ERR_INVALID_ARG;
     if ((int64_t)c->table_len * R > INT32_MAX) return SC_ERR_UNSUPPORTED;
     const int64_t es = (int64_t)elem_size(c->dtype);
-    if (c->stride_row < c->d || c->stride_head < 0 || c->stride_page < 0) return SC_ERR_INVALID_ARG;
-    if ((c->stride_row * es) % 16 || (c->stride_head * es) % 16 || (c->stride_page * es) % 16) return SC_ERR_INVALID_ARG;
-    if (c->stride_row > INT32_MAX / (R * es)) return SC_ERR_INVALID_ARG;      // offsets inside the rows of a head are 32-bit
-    // [page, head, row] or [page, row, head]: the heads of a page lie apart, and so do the pages
-    const int64_t rows_span = (R - 1) * c->stride_row + c->d;
-    if (c->page_heads > 1 && c->stride_head < rows_span && !(c->stride_head >= c->d && (c->page_heads - 1) * c->stride_head + c->d <= c->stride_row)) return SC_ERR_INVALID_ARG;
-    if (c->num_pages > 1 && c->stride_page < (c->page_heads - 1) * c->stride_head + rows_span) return SC_ERR_INVALID_ARG;
+    // in any order of pages, heads and rows
+    const int64_t size[3] = {c->num_pages, c->page_heads, R}, stride[3] = {c->stride_page, c->stride_head, c->stride_row};
+    for (int i = 0; i < 3; ++i)
+        if (size[i] > 1 && (stride[i] < 0 || (stride[i] * es) % 16)) return SC_ERR_INVALID_ARG;
+    if (c->stride_row < c->d || c->stride_row > INT32_MAX / (R * es)) return SC_ERR_INVALID_ARG;      // offsets inside the rows of a head are 32-bit
+    if (!rows_apart(size, stride, c->d)) return SC_ERR_INVALID_ARG;
     if (!aligned16(c->K) || !aligned16(c->V) || !aligned4(c->table)) return SC_ERR_INVALID_ARG;
     if (c->counts && !aligned16(c->counts)) return SC_ERR_INVALID_ARG;      // read four at a time
     if (!c->k_min != !c->k_max) return SC_ERR_INVALID_ARG;
@@ -435,20 +448,6 @@ static sc_status paged_check(const sc_paged_cache *c, PagedView &v) {
     v.P = c->table_len; v.table_per_head = c->table_per_head != 0;
     v.B = c->B; v.H = c->Hkv; v.d = c->d; v.dtype = static_cast<DType>(c->dtype);
     return SC_OK;
-}
-
-// Whether the rows of d elements of a three-dimensional array have no element in common: from the smallest stride on, each has to reach beyond what lies within it.
-// (The stride of a dimension of one means nothing.)
-static bool rows_apart(const int64_t (&size)[3], const int64_t (&stride)[3], int64_t d) {
-    int order[3] = {0, 1, 2};
-    std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
-    int64_t span = d;
-    for (int i : order) {
-        if (size[i] <= 1) continue;
-        if (stride[i] < span || stride[i] > INT64_MAX / 4 / size[i]) return false;
-        span += (size[i] - 1) * stride[i];
-    }
-    return true;
 }
 
 // Rows [B, heads, N, d]: aligned, and, where the call writes them, none with a stride of less than a row.

@@ -542,6 +542,21 @@ def test_append_lengths_side_by_side():
             sc.sc_paged_append(pc.cache(), k, k, x[:3], lens, cos_sin=angles(128, 60).to(DEV), positions=x[6:])
 
 
+@pytest.mark.parametrize("order", [(1, 0, 2), (2, 0, 1), (1, 2, 0), (2, 1, 0)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_pools_in_any_order(order, dtype):
+    """Pools whose heads, or rows, are the outermost dimension in memory: appended to and attended to as the others."""
+    print("pools in any order", order, dtype, flush=True)
+    pc = Paged(2, 3, 5, 32, 128, dtype, summary=True, junk=False)
+    size = (pc.n, 3, 32)
+    back = [order.index(i) for i in range(3)]
+    pc.K, pc.V = (torch.randn([size[i] for i in order] + [128], generator=pc.gen).to(dtype).to(DEV).permute(*back, 3) for _ in range(2))
+    assert pc.K.shape == (pc.n, 3, 32, 128)
+    check_append(pc, 40, [[0] * 3, [33] * 3], [[40] * 3, [31] * 3], rot=64, G=2)
+    check_append(pc, 1, [[40] * 3, [64] * 3], [[1] * 3] * 2, rot=128, G=2)
+    check_decode(pc, [[160] * 3, [77] * 3], 4, dtype, per_head=False)
+
+
 def test_append_after_going_back():
     """Rows that are taken back (a shorter length than before) leave no trace in the summaries."""
     print("append going back", flush=True)

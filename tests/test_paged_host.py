@@ -87,6 +87,20 @@ def test_append_refuses_lengths_that_are_read_while_they_are_written(lib):
         assert status(at, 1) == ARG and status(at + (4 if name == "positions" else 28), 1) == ARG and status(at - 28, 1) == ARG, name
 
 
+def test_pools_of_any_order_and_none_that_overlap(lib):
+    """Strides of pages, heads and rows (100 pages of 4 heads and 32 rows).  What passes is refused for its workspace."""
+    def status(page, head, row, **kw):
+        c = sc._PagedCacheStruct(**{**CACHE, "stride_page": page, "stride_head": head, "stride_row": row, **kw})
+        return lib.sc_paged_decode_attn(ctypes.byref(c), FAKE, 1, 8, FAKE, 0, None, None, 0, 0.0, FAKE, 1, None, FAKE, 0, None)
+    for s in ((16384, 4096, 128), (16384, 128, 512), (4096, 409600, 128), (128, 409600, 12800), (128, 12800, 51200), (512, 128, 51200), (20000, 4096, 128)):
+        assert status(*s) == WORKSPACE, s
+    for s in ((4088, 409600, 128), (4096, 409600 - 4096, 128), (128, 409600, 12792), (128, 128, 51200), (512, 128, 51192), (16384, 4096, 120), (2**61, 4096, 128), (16384, 0, 128), (16384, 4104, 128)):
+        assert status(*s) == ARG, s
+    # the stride of a dimension of one means nothing
+    assert status(3, 4096, 128, num_pages=1) == WORKSPACE
+    assert status(4096, 3, 128, page_heads=1, Hkv=8, table_per_head=1) == WORKSPACE
+
+
 def test_append_refuses_queries_that_are_written_over_each_other(lib):
     """Q_out's rows [2, 8, 8, 128]: strides that are each as long as a row and still meet."""
     def status(b, h, n):
