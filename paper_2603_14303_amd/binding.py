@@ -505,6 +505,13 @@ def _is_i32(t, *shapes) -> bool:
     return t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) in shapes
 
 
+def _c_ints(**values):
+    # (ctypes keeps the lower 32 bits of what it is given)
+    for name, x in values.items():
+        if not -2**31 <= int(x) < 2**31:
+            raise SemantiCacheError("%s = %d does not fit a 32-bit integer" % (name, x))
+
+
 class PagedCache:
     """The pools and tables of a cache held in pages (sc_paged_cache); the tensors are the caller's and stay theirs.
 
@@ -566,6 +573,9 @@ def sc_paged_append(cache: PagedCache, K, V, base_lens, lens, new_lens=None, cou
             _check(st, "sc_paged_append")
             return lens, Q_out
     _require_cuda(K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions)
+    for t in (K, Q, cos_sin):
+        if t is not None:
+            _c_ints(**{"dimension %d" % i: n for i, n in enumerate(t.shape)})
     B, H, d = cache.B, cache.Hkv, cache.d
     if K.dim() != 4 or K.shape != V.shape or K.shape[0] != B or K.shape[1] != H or K.shape[3] != d or K.dtype != cache.K.dtype or V.dtype != K.dtype:
         raise SemantiCacheError("K and V must be [B, Hkv, N, d] of the cache's dtype")
@@ -664,6 +674,7 @@ def sc_paged_select(cache: PagedCache, Q, lens, keep: int, first: int = 1, recen
         if st >= 0:
             _check(st, "sc_paged_select")
             return sel, sel_lens
+    _c_ints(keep=keep, first=first, recent=recent)
     workspace = _paged_query(cache, Q, lens, workspace)
     _require_cuda(sel, sel_lens)
     B, H = cache.B, cache.Hkv

@@ -374,3 +374,18 @@ def test_the_tensors_of_a_cache_stay_the_same_ones(monkeypatch):
     with pytest.raises(sc.SemantiCacheError, match="new PagedCache"):
         del cache.V
     assert cache.table is table and cache.struct.table == table.data_ptr()
+
+
+def test_numbers_beyond_32_bits_are_refused(monkeypatch):
+    """2^32 + 5 pages to keep are not five, and 2^32 + 3 rows (of stride zero) not three."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(sc, "_require_cuda", lambda *a: None)
+    K, table, lens = torch.zeros((3, 2, 16, 64)), torch.zeros((1, 2), dtype=torch.int32), torch.zeros((1,), dtype=torch.int32)
+    cache = sc.PagedCache(K, K.clone(), table)
+    Q = torch.zeros((1, 2, 64))
+    for kw in (dict(keep=2**32 + 5), dict(keep=5, first=2**32), dict(keep=5, recent=2**32 + 1)):
+        with pytest.raises(sc.SemantiCacheError, match="32-bit"):
+            sc.sc_paged_select(cache, Q, lens, **kw, sel=torch.zeros((1, 2, 5), dtype=torch.int32), workspace=object())
+    rows = torch.zeros((1, 2, 1, 64)).expand(1, 2, 2**32 + 3, 64)
+    with pytest.raises(sc.SemantiCacheError, match="32-bit"):
+        sc.sc_paged_append(cache, rows, rows, lens, lens.clone())
