@@ -273,6 +273,99 @@ def test_decode_work_is_split_and_joined(B, H, lens):
         assert torch.equal(O, O2) and torch.equal(lse, lse2) and not state.any()
 
 
+def work_plan(pc, lens, G, per_head):
+    """How sc_paged_decode_attn splits a call (its kernel's rules): (parts of every head, heads that are split and begin inside a workgroup's stretch, whether a
+    workgroup goes on from one group of 64 lengths to the next, units of a workgroup)."""
+    heads = [lens[b][h] for b in range(pc.B) for h in range(pc.H)]
+    units = [max(1, -(-n // 128)) for n in heads]
+    wgs = min(256, 64 * len(heads), -(-pc.P * pc.R // 128) * len(heads))
+    per = multiple = max(units)
+    if per > 2 or len(heads) > wgs:
+        per, multiple = -(-sum(units) // wgs), 1
+        for t in range(per, per + 3) if per > 1 else []:
+            if sum(-(-u // t) for u in units) <= wgs:
+                per = multiple = t
+                break
+    units = [-(-u // multiple) * multiple for u in units]
+    starts = [sum(units[:i]) for i in range(len(units))]
+    parts = [(a + u - 1) // per - a // per + 1 for a, u in zip(starts, units)]
+    inside = sum(n > 1 and a % per != 0 for n, a in zip(parts, starts))
+    step = 64 if per_head else 64 * pc.H
+    return parts, inside, any(starts[i] % per for i in range(step, len(units), step)), per
+
+
+@pytest.mark.parametrize("B, H, G, n, dtype, d", [(1, 1, 16, 9000, BF, 128), (1, 1, 8, 8800, BF, 64), (1, 4, 7, 32768, BF, 128), (2, 1, 13, 16000, F32, 128), (1, 1, 16, 4000, F32, 64)])
+def test_decode_many_parts_are_joined_in_groups(B, H, G, n, dtype, d):
+    """More (part, head) pairs than are joined at once: groups of 16 parts first, the last one not full; the same, bit for bit, on a workspace in use."""
+    print("decode groups of parts", B, H, G, n, dtype, d, flush=True)
+    pc = Paged(B, H, -(-n // 64), 64, d, dtype, seed=G, junk=False)
+    lens = [[n - 700 * b] * H for b in range(B)]
+    parts, _, _, _ = work_plan(pc, lens, G, False)
+    assert min(parts) > 16 and min(parts) * G > 256, parts
+    ws = sc.paged_workspace(B, H * G, H, d, pc.P, DEV)
+    O, lse = check_decode(pc, lens, G, dtype, per_head=False, workspace=ws)
+    Q = (1.5 * torch.randn((B, H * G, d), generator=torch.Generator().manual_seed(1))).to(dtype).to(DEV)
+    dl = torch.tensor([x[0] for x in lens], dtype=torch.int32, device=DEV)
+    for _ in range(4):
+        O2, lse2 = sc.sc_paged_decode_attn(pc.cache(), Q, dl, want_lse=True, workspace=ws)
+        assert torch.equal(O, O2) and torch.equal(lse, lse2) and not ws.buf[: 4 * 256 * 4].any()      # (the counters)
+
+
+@pytest.mark.parametrize("per_head", [False, True])
+@pytest.mark.parametrize("G, dtype, d", [(4, BF, 128), (3, F32, 64)])
+def test_decode_heads_that_begin_inside_a_stretch(per_head, G, dtype, d):
+    """More heads than workgroups: equal shares, wherever heads begin, and more lengths than a wavefront holds at a time."""
+    print("decode inside a stretch", per_head, G, dtype, d, flush=True)
+    B, H = 70, 4
+    pc = Paged(B, H, 24, 64, d, dtype, seed=G, counts=per_head, junk=False)
+    n = torch.randint(0, 1500, (B, H), generator=pc.gen).tolist()
+    if not per_head:
+        n = [[x[0]] * H for x in n]
+    n[5], n[64], n[69] = [0] * H, [1] * H, [1500] * H
+    parts, inside, across, per = work_plan(pc, n, G, per_head)
+    assert inside > 20 and across and per > 2 and max(parts) > 2, (inside, across, per)
+    ws = sc.paged_workspace(B, H * G, H, d, pc.P, DEV)
+    O, lse = check_decode(pc, n, G, dtype, per_head=per_head, workspace=ws)
+    Q = (1.5 * torch.randn((B, H * G, d), generator=torch.Generator().manual_seed(1))).to(dtype).to(DEV)
+    dl = torch.tensor(n if per_head else [x[0] for x in n], dtype=torch.int32, device=DEV)
+    for _ in range(3):
+        O2, lse2 = sc.sc_paged_decode_attn(pc.cache(), Q, dl, want_lse=True, workspace=ws)
+        assert torch.equal(O, O2) and torch.equal(lse, lse2) and not ws.buf[: 4 * 256 * 4].any()
+
+
+def test_decode_more_steps_than_lanes():
+    """A workgroup with more than 64 steps of one head looks pages up twice; a bad page that only the second look finds shows."""
+    print("decode many steps", flush=True)
+    R, per = 128, 66
+    n = 64 * per * R - 50
+    pc = Paged(1, 1, -(-n // R), R, 64, BF, junk=False)
+    assert work_plan(pc, [[n]], 2, False) == ([64], 0, False, per)
+    check_decode(pc, [[n]], 2, BF, per_head=False)
+    Q = torch.randn((1, 2, 64), generator=pc.gen).to(BF).to(DEV)
+    dl = torch.tensor([n], dtype=torch.int32, device=DEV)
+    for place in (3 * per + 65, 63 * per + 64):
+        table = pc.table.clone()
+        table[0, place] = pc.n
+        O, lse = sc.sc_paged_decode_attn(pc.cache(table), Q, dl, want_lse=True)
+        assert O.isnan().all() and lse.isnan().all()
+
+
+@pytest.mark.parametrize("dtype, d", [(BF, 128), (F32, 64)])
+def test_decode_over_selections_of_many_heads(dtype, d):
+    """More (sequence, head) pairs with a selection than a wavefront holds lengths of; fewer and more than workgroups."""
+    print("decode many selections", dtype, d, flush=True)
+    for B, H in ((20, 4), (66, 4)):
+        pc = Paged(B, H, 30, 32, d, dtype, seed=B, junk=False)
+        lens = [[int(x)] * H for x in torch.randint(1, 960, (B,), generator=pc.gen)]
+        sel = {}
+        for b in range(B):
+            for h in range(H):
+                pages = -(-lens[b][h] // 32)
+                some = torch.randperm(pages, generator=pc.gen)[: int(torch.randint(0, pages + 1, (1,), generator=pc.gen))]
+                sel[b, h] = sorted(some.tolist())
+        check_decode(pc, lens, 3, dtype, per_head=False, sel=sel)
+
+
 def test_decode_no_row_is_missed():
     """One row outweighs all others: every row of a cache across pages, steps and workgroups in turn."""
     print("decode needles", flush=True)
@@ -540,6 +633,54 @@ def test_append_lengths_side_by_side():
     for lens in (x[2:5], x[4:7], x[6:]):
         with pytest.raises(sc.SemantiCacheError):
             sc.sc_paged_append(pc.cache(), k, k, x[:3], lens, cos_sin=angles(128, 60).to(DEV), positions=x[6:])
+
+
+@pytest.mark.parametrize("B, H, N, R, dtype, own_pages", [(9, 3, 500, 16, BF, False), (35, 2, 20, 256, BF, False), (9, 2, 300, 16, F32, True), (17, 3, 200, 32, BF, True)])
+def test_append_to_many_pages(B, H, N, R, dtype, own_pages):
+    """So many pages that all heads of one go to one chiplet; groups of pages that are no multiple of eight; ragged."""
+    print("append many pages", B, H, N, R, dtype, own_pages, flush=True)
+    most = max(R, N // 3)
+    pc = Paged(B, H, -(-(N + most) // R), R, 128, dtype, per_head_table=own_pages, counts=own_pages, summary=True, junk=False)
+    waves = min(4, max(1, R // (16 if dtype == BF else 8)))      # of a page
+    groups = B * -(-min(pc.P, (N + R - 2) // R + 1) // (4 // waves))
+    assert groups >= 64 and groups % 8, groups
+    base, new = (torch.randint(0, x + 1, (B, H), generator=pc.gen).tolist() for x in (most, N))
+    new[1] = [N] * H
+    if not own_pages:
+        base, new = [[x[0]] * H for x in base], [[x[0]] * H for x in new]
+    pc.fill(base)
+    if own_pages:
+        check_append(pc, N, base, new, per_head=True)
+    else:
+        check_append(pc, N, base, new, rot=128, G=2)
+
+
+def test_append_keys_that_are_not_numbers_show_in_the_summaries():
+    print("append not a number", flush=True)
+    for dtype, d, R in ((BF, 128, 32), (BF, 64, 256), (F32, 128, 16)):
+        pc = Paged(1, 2, 8, R, d, dtype, summary=True, junk=False)
+        N = 5 * R // 2
+        k = torch.randn((1, 2, N, d), generator=pc.gen).to(dtype)
+        k[0, 0, R // 2, 7], k[0, 1, N - 1, d - 1], k[0, 0, 3, 0], k[0, 1, R, 9] = math.nan, math.nan, -math.inf, math.inf
+        lens = torch.zeros(1, dtype=torch.int32, device=DEV)
+
+        def check(n):
+            K, k_min, k_max = pc.K.cpu().float(), pc.k_min.cpu().float(), pc.k_max.cpu().float()
+            for h in range(2):
+                for p in range(-(-n // R)):
+                    page, head, row = pc.place(0, h, torch.arange(p * R, min((p + 1) * R, n)))
+                    keys = K[page, head, row]      # (amin and amax hand a NaN on)
+                    assert torch.equal(k_min[page[0], head].nan_to_num(9e9, 1e9, -1e9), keys.amin(0).nan_to_num(9e9, 1e9, -1e9)), (dtype, h, p)
+                    assert torch.equal(k_max[page[0], head].nan_to_num(9e9, 1e9, -1e9), keys.amax(0).nan_to_num(9e9, 1e9, -1e9)), (dtype, h, p)
+        sc.sc_paged_append(pc.cache(), k.to(DEV), k.to(DEV), lens, torch.empty_like(lens))
+        check(N)
+        assert int(pc.k_min.isnan().sum()) >= 2 and pc.k_min.isinf().any() and pc.k_max.isinf().any()
+        # a token behind them, and one in the place of the last of them
+        for base in (N, N - 1):
+            lens.fill_(base)
+            one = torch.randn((1, 2, 1, d), generator=pc.gen).to(dtype).to(DEV)
+            sc.sc_paged_append(pc.cache(), one, one, lens, torch.empty_like(lens))
+            check(base + 1)
 
 
 @pytest.mark.parametrize("order", [(1, 0, 2), (2, 0, 1), (1, 2, 0), (2, 1, 0)])
