@@ -62,11 +62,12 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 __device__ __forceinline__ float inverse_of(int y) { return __builtin_amdgcn_rcpf((float)y); }
 __device__ __forceinline__ float pag_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// x as NP bf16 parts whose sum it is (up to the last one's rounding)
+// x as NP bf16 parts, the upper 8 bits of what is left each time: three hold all bits of fp32.  (Rounded parts would, too, but the first one of a number beyond
+// bf16's largest is infinity.)
 template <int NP> __device__ __forceinline__ void split_bf16(float x0, float x1, uint32_t (&part)[NP]) {
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-        part[k] = pack_bf16x2(x0, x1);
+        part[k] = pack_hi(__float_as_uint(x0), __float_as_uint(x1));
         x0 -= bf16_lo(part[k]);
         x1 -= bf16_hi(part[k]);
     }

@@ -241,6 +241,23 @@ def test_decode_weights_of_a_bf16_cache_have_the_bits_of_fp32(d, G):
     assert not O[..., 16:].any()
 
 
+def test_decode_queries_beyond_the_largest_bf16():
+    """fp32 queries between bf16's largest number and fp32's, over a bf16 cache of small keys: logits of a few units."""
+    print("decode large queries", flush=True)
+    n, d = 100, 64
+    pc = Paged(1, 1, 4, 32, d, BF, junk=False)
+    rows = pc.fill([[n]])[0, 0]
+    k = (rows[0].sign() * (1 + rows[0].abs()) * 2.0**-125).to(BF).double()
+    page, head, row = pc.place(0, 0, torch.arange(n))
+    pc.K[page.to(DEV), head, row.to(DEV)] = k.to(BF).to(DEV)
+    Q = torch.where(torch.rand((1, 3, d), generator=pc.gen) < 0.5, -1.0, 1.0) * (3.397e38 + 0.004e38 * torch.rand((1, 3, d), generator=pc.gen))
+    assert torch.isfinite(Q).all() and (Q.abs() > torch.finfo(BF).max).all()
+    O, lse = sc.sc_paged_decode_attn(pc.cache(), Q.to(DEV), torch.tensor([n], dtype=torch.int32, device=DEV), want_lse=True)
+    wo, wl, to, tl = attend(Q[0].double(), (k, rows[1], None), 1 / math.sqrt(d))
+    close(O[0], wo, to + half_step(F32) * wo.abs() * (1 + 2.0**-6))
+    close(lse[0], wl, tl)
+
+
 @pytest.mark.parametrize("qdt", [F32, BF])
 def test_decode_logits_of_an_fp32_cache_are_summed_in_parts(qdt):
     """Logits that are zero exactly, sums of d = 128 products whose second half takes the first one back, as the lse of single rows.  With four sums of d / 4 the k-th
