@@ -424,11 +424,18 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
             const int here = left;
             pag_f32x4 sc = {0.f, 0.f, 0.f, 0.f};
             if constexpr (kBf16) {
+                pag_f32x4 rest = sc;      // of the queries' lower parts
 #pragma unroll
-                for (int ks = 0; ks < KL; ++ks)
+                for (int ks = 0; ks < KL; ++ks) {
+                    sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, x.k[ks]), __builtin_bit_cast(pag_bf16x8, q[0][ks]), sc, 0, 0, 0);
 #pragma unroll
-                    for (int k = QP - 1; k >= 0; --k)      // the smallest part first
-                        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, x.k[ks]), __builtin_bit_cast(pag_bf16x8, q[k][ks]), sc, 0, 0, 0);
+                    for (int k = QP - 1; k > 0; --k)
+                        rest = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, x.k[ks]), __builtin_bit_cast(pag_bf16x8, q[k][ks]), rest, 0, 0, 0);
+                }
+                if constexpr (QP > 1) {      // a lower part that is zero meets an infinite key: the upper parts' sum is infinite, or no number, by itself then
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sc[i] += fabsf(rest[i]) < INFINITY ? rest[i] : 0.f;
+                }
             } else {
                 // four sums side by side: one over all d has twice the error (3 x 2 heads of 500 to 1000 rows take 9.0 us with either)
                 pag_f32x4 part[4] = {sc, sc, sc, sc};

@@ -258,6 +258,33 @@ def test_decode_queries_beyond_the_largest_bf16():
     close(lse[0], wl, tl)
 
 
+@pytest.mark.parametrize("dtype, qdt, d", [(BF, F32, 128), (BF, F32, 64), (BF, BF, 128), (F32, F32, 64), (F32, BF, 128)])
+def test_decode_infinite_keys_that_weigh_nothing(dtype, qdt, d):
+    """Keys with an infinite element on the far side of all queries of the group: logits of -inf, and the result is that of the other rows."""
+    print("decode infinite keys", dtype, qdt, d, flush=True)
+    n, G = 333, 4
+    pc = Paged(1, 2, 11, 32, d, dtype, junk=False)
+    rows = pc.fill([[n, n]])
+    gone = torch.rand(n, generator=pc.gen) < 0.3
+    K = pc.K.cpu()
+    for h in range(2):
+        page, head, row = pc.place(0, h, torch.arange(n))
+        for t in gone.nonzero()[:, 0].tolist():
+            e = int(torch.randint(0, 8, (1,), generator=pc.gen))
+            K[page[t], head, row[t], e] = -math.inf if e < 4 else math.inf
+    pc.K.copy_(K)
+    Q = torch.randn((1, 2 * G, d), generator=pc.gen)
+    Q[..., :4], Q[..., 4:8] = Q[..., :4].abs() + 0.25, -Q[..., 4:8].abs() - 0.25
+    Q[..., 0] = 2.0      # (in one part)
+    Q = Q.to(qdt)
+    O, lse = sc.sc_paged_decode_attn(pc.cache(), Q.to(DEV), torch.tensor([n], dtype=torch.int32, device=DEV), want_lse=True)
+    for h in range(2):
+        k, v, _ = rows[0, h]
+        wo, wl, to, tl = attend(Q[0, h * G : (h + 1) * G].double(), (k[~gone], v[~gone], None), 1 / math.sqrt(d))
+        close(O[0, h * G : (h + 1) * G], wo, to + half_step(qdt) * wo.abs() * (1 + 2.0**-6))
+        close(lse[0, h * G : (h + 1) * G], wl, tl)
+
+
 @pytest.mark.parametrize("qdt", [F32, BF])
 def test_decode_logits_of_an_fp32_cache_are_summed_in_parts(qdt):
     """Logits that are zero exactly, sums of d = 128 products whose second half takes the first one back, as the lse of single rows.  With four sums of d / 4 the k-th
