@@ -364,7 +364,7 @@ sc_status sc_multi_attn(const void *Q, sc_dtype q_dtype, int nq,
  *   pools       K, V     [num_pages, page_heads, page_rows, d] of dtype, addressed as
  *                        base + page*stride_page + head*stride_head + row*stride_row (+ e), strides in
  *                        ELEMENTS, the same for K and V, in any order of size, multiples of 16 bytes; 16-byte aligned
- *               counts   i32 [num_pages, page_heads, page_rows], contiguous, or NULL: sizes of the rows
+ *               counts   i32 [num_pages, page_heads, page_rows], contiguous, 16-byte aligned, or NULL: sizes of the rows
  *               k_min, k_max   [num_pages, page_heads, d] of dtype, contiguous, 16-byte aligned, or both
  *                        NULL: per page the minimum and maximum of the keys that it holds
  *   page_heads           Hkv: a page holds its rows for all KV heads, table [B, table_len];
@@ -448,7 +448,8 @@ sc_status sc_paged_init_workspace(void *ws, size_t ws_bytes, void *stream);
 /* sc_paged_decode_attn — sc_decode_attn over a cache in pages:
  *     O[b,hq] = softmax_t( Q[b,hq] . K[b,h,t] * scale + ln(counts[b,h,t]) ) V[b,h,t],  t in [0, lens),  h = hq / (Hq / Hkv),
  * without the logarithm if the cache has no counts.  fp32 (bf16 caches: probabilities, and queries of fp32, as sums of
- * three bf16 parts); fp32 accumulation.  Rows of size <= 0 weigh nothing.  A length <= 0 gives O = 0 and
+ * three bf16 parts); fp32 accumulation.  Rows of size <= 0 weigh nothing, whatever they hold.
+ * An infinite element of V makes that element of O infinite or NaN.  A length <= 0 gives O = 0 and
  * lse = -inf; a length beyond the table's pages counts as the pages' rows.  A page number outside the pool gives NaN for its heads' O and lse.
  *   Q               device [B, Hq, d] of q_dtype, contiguous, 16-byte aligned; Hq / Hkv <= 16
  *   lens            device i32 [B], or [B, Hkv] if lens_per_head

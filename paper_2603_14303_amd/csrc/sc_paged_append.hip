@@ -14,7 +14,9 @@
 namespace sc {
 
 constexpr int kAppThreads = 256;
-constexpr int kNearItems = 64;         // pages from which the heads of one are kept on a chiplet: eight for each of them
+// groups of pages from which the heads of one are kept on a chiplet: eight for each of them.  Prompts of 4096 and 8192 tokens (64 and 128 groups) 23.9 and 44.2 us, 24.2
+// and 45.4 otherwise; below, chiplets would be left without work: 256 tokens (four groups) 4.8 us, 5.1 near; a token each of 16 and 32 sequences 4.4 and 4.5, 4.6 near
+constexpr int kNearItems = 64;
 
 // A lane's two pieces of 16 bytes of a row (of E elements each), chosen so that the partners of a rotation are in the same lane
 template <typename T> struct Shape {
@@ -320,7 +322,8 @@ static hipError_t launch_append(const PagedAppendArgs &a, hipStream_t stream) {
     constexpr int WAVES = kAppThreads / kWave;
     constexpr int RPW = kWave / (D / (2 * Shape<T>::E)), QRPW = kWave / (D / (2 * Shape<TQ>::E));      // rows of a wavefront's pass
     AppendGrid g;
-    // wavefronts of a page: two passes each, up to all four
+    // wavefronts of a page: two passes each, up to all four (32768 tokens in pages of 16 rows 153 us, with one pass each 160; merged rows in pages of 64 36.1 us, with four
+    // 39.1; a token of 64 sequences in pages of 32 4.75 us, with four 4.5)
     g.log2_waves = 0;
     while (g.log2_waves < 2 && (2 * RPW << g.log2_waves) < a.c.R) ++g.log2_waves;
     const int pages = WAVES >> g.log2_waves, slots = paged_append_slots(a.N, a.c.R, a.c.P);

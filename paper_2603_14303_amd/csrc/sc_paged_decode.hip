@@ -13,8 +13,8 @@
 // v_mfma_f32_16x16x32_bf16 and v_mfma_f32_16x16x16_bf16, probabilities as three bf16 parts, which hold all bits of fp32 (two parts, a rounding of 2^-18, are not
 // faster: 8 heads x 32768 rows 27.9 us with either, 170 rows 6.6 and 6.5); fp32 queries over a bf16 cache as three parts, too; fp32 caches: v_mfma_f32_16x16x4_f32.
 //
-// Measured (d = 128, bf16): 8 heads x 32768 rows, G = 4: 27.4 us (4.9 TB/s; 18 us of it the rows, 7.4 TB/s); 128 heads of 8192 to 16384 rows, G = 7: 127 us
-// (6.3 TB/s); 8 heads x 170 rows: 6.6 us, x 1 row 5.5, of which the launch is 1.8: arguments, lengths, page numbers, rows and the results' store follow each other.
+// Measured (d = 128, bf16): 8 heads x 32768 rows, G = 4: 27.4 us (4.9 TB/s; 18 us of it the rows, 7.4 TB/s); 128 heads of 8192 to 16384 rows, G = 7: 128 us
+// from a graph (6.3 TB/s), 131 called one after another; 8 heads x 170 rows: 6.6 us, x 1 row 5.5, of which the launch is 1.8: arguments, lengths, page numbers, rows and the results' store follow each other.
 #include <type_traits>
 
 #include "sc_paged.h"
@@ -24,12 +24,18 @@ namespace sc {
 constexpr int kPagWaves = 8;
 constexpr int kPagThreads = kPagWaves * kWave;
 constexpr int kStep = 16 * kPagWaves;        // rows of a step of all wavefronts: the unit of work
-constexpr int kAlone = 2;                    // steps up to which a head goes to one workgroup, if there is one for every head
-constexpr int kMore = 2;                     // steps beyond an equal share for which workgroups have parts of one head only
+// steps up to which a head goes to one workgroup, if there is one for every head: 8 heads of 170 and 250 rows (two steps) 6.6 and 7.4 us, 8.2 and 8.3 split; of 400
+// and 512 rows (four) 8.8 and 10.5 alone, 8.4 and 8.7 split
+constexpr int kAlone = 2;
+// steps beyond an equal share for which workgroups have parts of one head only: 64 heads of 3000 to 6000 rows 32.4 us, 33.0 with 0; but 24 of 9000 27.0 and 26.4, 128 of
+// 1500 to 3000 33.6 and 32.9 (with 4 36.1)
+constexpr int kMore = 2;
 constexpr int kMaxWgs = 256;                 // one on each compute unit
 constexpr int kMaxPairs = 512;              // (part, head) pairs that are joined at once, heads up to a power of two (paged_group)
 constexpr int kPagPad = 4;                   // floats behind the sums of a partial result: maximum, sum, two unused
-constexpr int kMaxHeadWgs = 64;              // workgroups per (sequence, KV head) at most, on average: each is a partial result to join
+// workgroups per (sequence, KV head) at most, on average.  It only says something for up to three heads in all.  One head of 9000, 32768 and 131072 rows, G = 4: 11.5,
+// 17.4 and 39 us; with 32 12.0, 22.6 and 64.  More workgroups would be faster yet (256: 11.0, 12.6 and 20), although each leaves a partial result to join.
+constexpr int kMaxHeadWgs = 64;
 constexpr float kPagLog2e = 1.4426950408889634f;
 constexpr float kPagLn2 = 0.6931471805599453f;
 

@@ -49,8 +49,9 @@ template <typename T> __device__ __forceinline__ double element(const uint4 &v, 
 // fp64 in shared memory, their positive and their negative parts side by side.  NT: groups of four heads (v_mfma_f64_4x4x4_4b: four products of 4 heads x
 // 4 pages), or 0: 16 heads (v_mfma_f64_16x16x4).  us for 2048 pages x 8 heads, G = 4; 1500 pages x 32 heads, G = 7; 2048 pages x 64 heads, G = 16 (d = 128,
 // bf16): NT = 1 4.4; NT = 2 5.0 and 8.7; 16 heads 6.4, 12.1 and 24.7; NT = 4 27.0 for the last.  Vector instructions take two to three times as long, also
-// with a query's element broadcast over a row of lanes on its way into the multiplication (51 for the last).  The first is a chain of trips to memory, the
-// second lies between the bytes (4 us) and the matrix cores, the third is bound by the matrix cores.  With one query head a KV head it is the bytes: 131 MB of
+// with a query's element broadcast over a row of lanes on its way into the multiplication (51 for the last).  The first is a chain of trips to memory.
+// The second has the matrix cores busy 30 % of its time and would take 4 us for the bytes, the third 60 %: every workgroup prepares all queries in fp64 for 64 pages,
+// and a wavefront reads all of them from shared memory for 16.  With one query head a KV head it is the bytes: 131 MB of
 // summaries in 24.6 us.  Products in fp32 with a bound on their error, and an evaluation in fp64 of the pages near the border by the second kernel,
 // took 3.9, 6.2 and 14.3 us here and 3 to 5 more there: less in all only with more than eight query heads a KV head and many sequences.
 template <typename T, int D, int NT>

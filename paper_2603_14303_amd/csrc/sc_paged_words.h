@@ -53,7 +53,8 @@ constexpr int paged_first_wg(int a, int per, float inverse) { return paged_quoti
 constexpr int paged_last_wg(int a, int units, int per, float inverse) { return paged_quotient(a + units - 1, per, inverse); }
 constexpr int paged_place(int w, int a, int per) { return 2 * w + (a > w * per ? 1 : 0); }
 
-// n partial results of G heads are joined at once, or in groups of this many first
+// n partial results of G heads are joined at once, or in groups of this many first (64 of 8 heads, on four KV heads of 32768 rows: 20.5 us in groups, 22.6 at once; 32 of
+// 16: 13.9 and 14.3; with 128 in place of 256 no difference)
 constexpr int paged_group(int n, int G) { return n * G <= 256 || n <= 16 ? n : 16; }
 
 // 16 rows of a head from row `row` (a multiple of 16) on, or from the same row of its selected pages: their page, and how many of them attend
