@@ -76,7 +76,7 @@ def test_append_rejects_bad_arguments(lib):
 
 def test_append_refuses_lengths_that_are_read_while_they_are_written(lib):
     """positions, base_lens and new_lens are read by every workgroup; one of them writes lens.  B = 2 sequences, 4 heads."""
-    arrays = dict(base_lens=FAKE + 1024, new_lens=FAKE + 3072, positions=FAKE + 4096)
+    arrays = dict(base_lens=FAKE + 1024, new_lens=FAKE + 5120, positions=FAKE + 4096)
 
     def status(lens, per_head=0):
         r = sc._PagedRowsStruct(**{**ROWS, **arrays, "lens": lens, "per_head": per_head})
