@@ -481,6 +481,89 @@ sc_status sc_paged_select(const sc_paged_cache *cache, const void *Q, sc_dtype q
                           const int32_t *lens, int lens_per_head, int keep, int first, int recent,
                           int32_t *sel, int32_t *sel_lens, void *ws, size_t ws_bytes, void *stream);
 
+/* sc_paged_window_attn — sc_paged_decode_attn where only a window of a sequence and its first rows attend: rows t of
+ *     [0, lens) with t >= lens - window or t < sinks.
+ * Pages without such rows are not looked up: their entries in the table may be anything (sc_paged_reserve takes such
+ * pages back).  Rows that do not attend may hold anything.
+ *   window          rows, the newest among them; 0: all rows attend (then sinks says nothing).  window or sinks < 0: SC_ERR_INVALID_ARG
+ */
+sc_status sc_paged_window_attn(const sc_paged_cache *cache, const void *Q, sc_dtype q_dtype, int Hq,
+                               const int32_t *lens, int lens_per_head, int window, int sinks, float scale,
+                               void *O, sc_dtype o_dtype, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * A cache held in pages of 8-bit codes: a row's element is code * scale, with a scale for every block of rows and head.
+ *
+ *   pools       K, V     codes [num_pages, page_heads, page_rows, d], addressed as those of sc_paged_cache (an element is a byte):
+ *                        SC_E4M3: floating point of 4 bits of exponent and 3 behind the point (up to 448, 0x7f and 0xff are
+ *                        no number); SC_I8: signed whole numbers
+ *               k_scale, v_scale   f32 [num_pages, page_heads, page_rows / block_rows], contiguous
+ *               counts   as in sc_paged_cache
+ *   block_rows           a power of two, 16 .. 128, page_rows at most
+ * Everything else as in sc_paged_cache (there are no k_min and k_max).  Host errors as there, code unknown: SC_ERR_UNSUPPORTED,
+ * block_rows out of range: SC_ERR_INVALID_ARG.
+ */
+typedef enum { SC_E4M3 = 0, SC_I8 = 1 } sc_code;
+typedef struct {
+    void *K, *V;
+    float *k_scale, *v_scale;
+    int32_t *counts;
+    const int32_t *table;
+    int64_t stride_page, stride_head, stride_row;
+    int32_t code;              /* sc_code */
+    int32_t block_rows, num_pages, page_heads, page_rows;
+    int32_t table_len, table_per_head;
+    int32_t B, Hkv, d;
+} sc_paged8_cache;
+
+/* sc_paged8_append — sc_paged_append for such a cache.  Rows of kv_dtype are rotated in fp32 (three roundings: a cos - b sin is not fused) and
+ * rounded once, to codes.  For every block that receives rows, for keys and values each,
+ *     need  = the smallest power of two, at least 2^-126, with  max |x| <= Q need  over the new rows of the block  (Q = 448, or 127)
+ *     scale = max(old scale, need) if the block holds rows below base_lens, else need
+ *     codes of new rows  = x * (1 / scale), rounded to nearest, ties to even
+ *     codes that it held = code * (old scale / scale), rounded the same, where the scale has grown
+ * so scales are powers of two unless the caller has put others there (positive ones).  A new number that is not finite makes its block's scale
+ * NaN, and attention over the block shows it; the scale stays so until the block's first row is written again.
+ * rows->K and V are of kv_dtype; everything else in rows, and lens, as for sc_paged_append.
+ */
+sc_status sc_paged8_append(const sc_paged8_cache *cache, const sc_paged_rows *rows, sc_dtype kv_dtype, void *stream);
+
+/* sc_paged8_decode_attn — sc_paged_window_attn over such a cache (window 0: all rows attend).  Codes and their products with bf16 are exact; queries of
+ * fp32 and probabilities enter as three bf16 parts, scales and sums are fp32.  Workspace as for sc_paged_decode_attn.
+ */
+sc_status sc_paged8_decode_attn(const sc_paged8_cache *cache, const void *Q, sc_dtype q_dtype, int Hq,
+                                const int32_t *lens, int lens_per_head, int window, int sinks, float scale,
+                                void *O, sc_dtype o_dtype, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* sc_paged_reserve — page tables and slots from the sequences' lengths, on the device.  Every sequence (every KV head of it, where heads have pages of
+ * their own) has a row of the table; its entries hold a page number, or anything outside [0, num_pages) for "no page" (-1 at the start).  The call makes
+ * the table hold what the sequence needs to receive new_lens rows behind its base_lens, and takes back what it does not need:
+ *     needed     places p with p R < base + new  and, with a window,  p R < sinks  or  (p + 1) R > base + 1 - window   (R = page_rows):
+ *                those that hold rows that a token at position base, or behind it, can see
+ *     given back pages of places that are not needed; their entries become -1.  (new_lens 0 takes back what was reserved ahead, base_lens 0 with it everything.)
+ *     taken      pages for needed places without one: first those that the call itself takes back, the first one first, in order of (sequence, place), then
+ *                from the top of the stack, free_pages[num_free - 1] first.  What is given back and not taken goes on the stack, the last one first.
+ * A call that is followed by its opposite leaves the stack as it was.  Nothing depends on the order in which the device runs.
+ * A sequence gets all pages that it lacks or none: where the pages do not suffice, those that lack some are served in order as long as their sum fits.
+ *   table           device i32 [sequences, table_len], contiguous.  A page is in one place of one row only (a shared prefix is not for this call)
+ *   base_lens       device i32 [sequences]: rows that the cache holds
+ *   new_lens        device i32 [sequences] or NULL (= N for all): rows to come, 0 .. N
+ *   window, sinks   as for sc_paged_window_attn; window 0: everything is kept
+ *   free_pages      device i32 [num_pages]: the stack;   num_free  device i32 [1]: how many it holds (taken as 0 .. num_pages)
+ *   lens            device i32 [sequences]: base_lens + new_lens, or -1: not served (its rows get no pages; what it does not need has gone back), or lengths that are not possible, or a needed page
+ *                   with rows below base_lens that the table does not have (a sequence that is taken back behind its window): nothing is changed for these two.
+ *                   No element in common with base_lens or new_lens (SC_ERR_INVALID_ARG)
+ *   slots           device i32 [sequences, N] or NULL: page * page_rows + row of every new row, -1 behind new_lens and for sequences of length -1
+ *   ws              sc_paged_reserve_workspace_bytes bytes, initialised ONCE with sc_paged_init_workspace
+ * Host errors: NULL or misaligned pointers, sizes <= 0 (N < 0), window or sinks < 0, page_rows no power of two or out of range (SC_ERR_INVALID_ARG); sequences > 2^20, sequences * table_len > 2^28,
+ * table_len * page_rows or num_pages * page_rows >= 2^31 (SC_ERR_UNSUPPORTED).
+ */
+size_t sc_paged_reserve_workspace_bytes(int sequences, int table_len);
+sc_status sc_paged_reserve(int32_t *table, int sequences, int table_len, int num_pages, int page_rows,
+                           const int32_t *base_lens, const int32_t *new_lens, int N, int window, int sinks,
+                           int32_t *free_pages, int32_t *num_free, int32_t *lens, int32_t *slots,
+                           void *ws, size_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------------------------------------------------
  * sc_stream_read_probe — a measuring aid for benchmarks, not a step of the method: reads the first
  * `bytes` bytes (rounded down to a multiple of 16) of a device buffer once, 16 bytes per lane, fully

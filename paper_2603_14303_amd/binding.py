@@ -21,6 +21,7 @@ LIB_PATH = os.path.join(_HERE, "libsemanticache.so")
 
 SC_OK = 0
 SC_F32, SC_BF16 = 0, 1
+SC_E4M3, SC_I8 = 0, 1
 
 _lib = None
 _native = None      # csrc/sc_binding.cpp: the wrappers' marshalling in C++, loaded with the library if it can be
@@ -34,6 +35,12 @@ class _PagedCacheStruct(ctypes.Structure):      # sc_paged_cache
     _fields_ = [(x, ctypes.c_void_p) for x in ("K", "V", "counts", "k_min", "k_max", "table")] + \
                [(x, ctypes.c_int64) for x in ("stride_page", "stride_head", "stride_row")] + \
                [(x, ctypes.c_int32) for x in ("dtype", "num_pages", "page_heads", "page_rows", "table_len", "table_per_head", "B", "Hkv", "d")]
+
+
+class _Paged8CacheStruct(ctypes.Structure):     # sc_paged8_cache
+    _fields_ = [(x, ctypes.c_void_p) for x in ("K", "V", "k_scale", "v_scale", "counts", "table")] + \
+               [(x, ctypes.c_int64) for x in ("stride_page", "stride_head", "stride_row")] + \
+               [(x, ctypes.c_int32) for x in ("code", "block_rows", "num_pages", "page_heads", "page_rows", "table_len", "table_per_head", "B", "Hkv", "d")]
 
 
 class _PagedRowsStruct(ctypes.Structure):       # sc_paged_rows
@@ -128,6 +135,17 @@ def load_library() -> ctypes.CDLL:
     lib.sc_paged_decode_attn.argtypes = [pc, vp, i32, i32, vp, i32, vp, vp, i32, f32, vp, i32, vp, vp, sz, vp]
     lib.sc_paged_select.restype = i32
     lib.sc_paged_select.argtypes = [pc, vp, i32, i32, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+    lib.sc_paged_window_attn.restype = i32
+    lib.sc_paged_window_attn.argtypes = [pc, vp, i32, i32, vp, i32, i32, i32, f32, vp, i32, vp, vp, sz, vp]
+    pc8 = c.POINTER(_Paged8CacheStruct)
+    lib.sc_paged8_append.restype = i32
+    lib.sc_paged8_append.argtypes = [pc8, c.POINTER(_PagedRowsStruct), i32, vp]
+    lib.sc_paged8_decode_attn.restype = i32
+    lib.sc_paged8_decode_attn.argtypes = [pc8, vp, i32, i32, vp, i32, i32, i32, f32, vp, i32, vp, vp, sz, vp]
+    lib.sc_paged_reserve_workspace_bytes.restype = sz
+    lib.sc_paged_reserve_workspace_bytes.argtypes = [i32, i32]
+    lib.sc_paged_reserve.restype = i32
+    lib.sc_paged_reserve.argtypes = [vp, i32, i32, i32, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
     if torch is not None:
         _native = _load_native()
     _lib = lib
@@ -159,6 +177,7 @@ EXPORTED = [
     "sc_gsc_merge_budget_workspace_bytes", "sc_gsc_merge_budget",
     "sc_gsc_merge_global_workspace_bytes", "sc_gsc_merge_global",
     "sc_paged_append", "sc_paged_workspace_bytes", "sc_paged_init_workspace", "sc_paged_decode_attn", "sc_paged_select",
+    "sc_paged_window_attn", "sc_paged8_append", "sc_paged8_decode_attn", "sc_paged_reserve_workspace_bytes", "sc_paged_reserve",
 ]
 
 
@@ -558,27 +577,15 @@ class PagedCache:
         return (self.B,), (self.B, self.Hkv)
 
 
-def sc_paged_append(cache: PagedCache, K, V, base_lens, lens, new_lens=None, counts=None, Q=None, Q_out=None, cos_sin=None, positions=None,
-                    interleaved: bool = False):
-    """K, V [B, Hkv, N, d] go behind the base_lens rows of their sequences, lens receives the new lengths -> (lens, Q_out).
-
-    base_lens, new_lens (None: N everywhere) and lens are int32 [B], or all [B, Hkv] (every head its own number of rows).  With cos_sin f32
-    [max_position, rot] (cosines, then sines) the first rot elements of the keys, and of the queries Q [B, Hq, N, d], are turned by the angles of
-    positions [B] (None: base_lens) + n.  counts [B, Hkv, N]: sizes of the rows, for a cache with counts.
-    """
-    lib = load_library()
-    if _native is not None and K.is_cuda and (Q is None) == (Q_out is None):
-        st = _native.paged_append(cache.ptr, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, _stream())
-        if st >= 0:
-            _check(st, "sc_paged_append")
-            return lens, Q_out
+def _paged_rows(cache, dtype, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved):
+    """The rows of a call that appends, checked -> (their sc_paged_rows, Q_out)."""
     _require_cuda(K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions)
     for t in (K, Q, cos_sin):
         if t is not None:
             _c_ints(**{"dimension %d" % i: n for i, n in enumerate(t.shape)})
     B, H, d = cache.B, cache.Hkv, cache.d
-    if K.dim() != 4 or K.shape != V.shape or K.shape[0] != B or K.shape[1] != H or K.shape[3] != d or K.dtype != cache.K.dtype or V.dtype != K.dtype:
-        raise SemantiCacheError("K and V must be [B, Hkv, N, d] of the cache's dtype")
+    if K.dim() != 4 or K.shape != V.shape or K.shape[0] != B or K.shape[1] != H or K.shape[3] != d or V.dtype != K.dtype or (dtype is not None and K.dtype != dtype):
+        raise SemantiCacheError("K and V must be [B, Hkv, N, d] of one dtype, the cache's if it keeps its numbers")
     N = K.shape[2]
     shapes = cache.lens_shapes()
     if not _is_i32(base_lens, *shapes) or not _is_i32(lens, tuple(base_lens.shape)) or not (new_lens is None or _is_i32(new_lens, tuple(base_lens.shape))):
@@ -606,6 +613,24 @@ def sc_paged_append(cache: PagedCache, K, V, base_lens, lens, new_lens=None, cou
         r.Q, r.Q_out, r.Hq, r.q_dtype = _ptr(Q), _ptr(Q_out), Q.shape[1], _dtype_code(Q)
         r.q_stride_b, r.q_stride_h, r.q_stride_n = Q.stride()[:3]
         r.o_stride_b, r.o_stride_h, r.o_stride_n = Q_out.stride()[:3]
+    return r, Q_out
+
+
+def sc_paged_append(cache: PagedCache, K, V, base_lens, lens, new_lens=None, counts=None, Q=None, Q_out=None, cos_sin=None, positions=None,
+                    interleaved: bool = False):
+    """K, V [B, Hkv, N, d] go behind the base_lens rows of their sequences, lens receives the new lengths -> (lens, Q_out).
+
+    base_lens, new_lens (None: N everywhere) and lens are int32 [B], or all [B, Hkv] (every head its own number of rows).  With cos_sin f32
+    [max_position, rot] (cosines, then sines) the first rot elements of the keys, and of the queries Q [B, Hq, N, d], are turned by the angles of
+    positions [B] (None: base_lens) + n.  counts [B, Hkv, N]: sizes of the rows, for a cache with counts.
+    """
+    lib = load_library()
+    if _native is not None and K.is_cuda and (Q is None) == (Q_out is None):
+        st = _native.paged_append(cache.ptr, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, _stream())
+        if st >= 0:
+            _check(st, "sc_paged_append")
+            return lens, Q_out
+    r, Q_out = _paged_rows(cache, cache.K.dtype, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved)
     _check(lib.sc_paged_append(ctypes.byref(cache.struct), ctypes.byref(r), _stream()), "sc_paged_append")
     return lens, Q_out
 
@@ -632,6 +657,18 @@ def _paged_query(cache: PagedCache, Q, lens, workspace):
     return workspace
 
 
+def _paged_outputs(Q, O, lse, want_lse):
+    _require_cuda(O, lse)
+    B, Hq, d = Q.shape
+    if O is None:
+        O = torch.empty((B, Hq, d), dtype=Q.dtype, device=Q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=Q.device)
+    if O.shape != Q.shape or not O.is_contiguous() or (lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq) or not lse.is_contiguous())):
+        raise SemantiCacheError("O must be [B, Hq, d] and lse float32 [B, Hq], contiguous")
+    return O, lse
+
+
 def sc_paged_decode_attn(cache: PagedCache, Q, lens, scale: float = 0.0, O=None, lse=None, want_lse: bool = False, sel=None, sel_lens=None,
                          workspace: Optional[Workspace] = None):
     """Q [B, Hq, d] over the first lens [B] (or [B, Hkv]) rows of a cache in pages -> (O [B, Hq, d], lse [B, Hq] or None).
@@ -645,14 +682,9 @@ def sc_paged_decode_attn(cache: PagedCache, Q, lens, scale: float = 0.0, O=None,
             _check(st, "sc_paged_decode_attn")
             return O, lse
     workspace = _paged_query(cache, Q, lens, workspace)
-    _require_cuda(O, lse, sel, sel_lens)
+    _require_cuda(sel, sel_lens)
+    O, lse = _paged_outputs(Q, O, lse, want_lse)
     B, Hq, d = Q.shape
-    if O is None:
-        O = torch.empty((B, Hq, d), dtype=Q.dtype, device=Q.device)
-    if lse is None and want_lse:
-        lse = torch.empty((B, Hq), dtype=torch.float32, device=Q.device)
-    if O.shape != Q.shape or not O.is_contiguous() or (lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq) or not lse.is_contiguous())):
-        raise SemantiCacheError("O must be [B, Hq, d] and lse float32 [B, Hq], contiguous")
     if (sel is None) != (sel_lens is None):
         raise SemantiCacheError("sel and sel_lens come together")
     if sel is not None and (sel.dim() != 3 or not _is_i32(sel, (B, cache.Hkv, sel.shape[2])) or not _is_i32(sel_lens, (B, cache.Hkv))):
@@ -688,6 +720,138 @@ def sc_paged_select(cache: PagedCache, Q, lens, keep: int, first: int = 1, recen
                              int(recent), _ptr(sel), _ptr(sel_lens), workspace.ptr, workspace.nbytes, _stream())
     _check(st, "sc_paged_select")
     return sel, sel_lens
+
+
+def sc_paged_window_attn(cache: PagedCache, Q, lens, window: int, sinks: int = 0, scale: float = 0.0, O=None, lse=None, want_lse: bool = False,
+                         workspace: Optional[Workspace] = None):
+    """sc_paged_decode_attn where only the newest `window` rows (0: all) and the first `sinks` rows of a sequence attend -> (O, lse or None)."""
+    return _windowed("sc_paged_window_attn", PagedCache, cache, Q, lens, window, sinks, scale, O, lse, want_lse, workspace)
+
+
+def _windowed(name, kind, cache, Q, lens, window, sinks, scale, O, lse, want_lse, workspace):
+    lib = load_library()
+    if not isinstance(cache, kind):
+        raise SemantiCacheError("%s takes a %s" % (name, kind.__name__))
+    _c_ints(window=window, sinks=sinks)
+    workspace = _paged_query(cache, Q, lens, workspace)
+    O, lse = _paged_outputs(Q, O, lse, want_lse)
+    st = getattr(lib, name)(ctypes.byref(cache.struct), _ptr(Q), _dtype_code(Q), Q.shape[1], _ptr(lens), int(lens.dim() == 2), int(window), int(sinks),
+                            float(scale), _ptr(O), _dtype_code(O), _ptr(lse), workspace.ptr, workspace.nbytes, _stream())
+    _check(st, name)
+    return O, lse
+
+
+# ------------------------------------------------------------------------------------------------ a cache in pages of 8-bit codes
+class PagedCache8:
+    """The pools and tables of a cache held in pages of 8-bit codes (sc_paged8_cache); the tensors are the caller's and stay theirs.
+
+    K, V torch.float8_e4m3fn or torch.int8 [pages, heads, R, d], any strides with a contiguous last dimension, the same for both; k_scale, v_scale
+    float32 [pages, heads, R / block] contiguous: an element is code * scale of its row's block; counts and table as in a PagedCache.
+    """
+
+    def __init__(self, K, V, k_scale, v_scale, table, counts=None):
+        load_library()
+        if K.dim() != 4 or K.shape != V.shape or K.stride() != V.stride() or K.dtype != V.dtype or (K.shape[3] > 1 and K.stride(3) != 1):
+            raise SemantiCacheError("K and V must be [pages, heads, R, d] with identical strides and dtype and contiguous rows")
+        codes = {torch.float8_e4m3fn: SC_E4M3, torch.int8: SC_I8}
+        if K.dtype not in codes:
+            raise SemantiCacheError("K and V must be float8_e4m3fn or int8")
+        pages, heads, R, d = K.shape
+        if table.dim() not in (2, 3) or table.dtype != torch.int32 or not table.is_contiguous():
+            raise SemantiCacheError("table must be int32 [B, P] or [B, Hkv, P], contiguous")
+        if table.dim() == 3 and heads != 1:
+            raise SemantiCacheError("a table per KV head needs pools of one head a page")
+        if counts is not None and not _is_i32(counts, (pages, heads, R)):
+            raise SemantiCacheError("counts must be int32 [pages, heads, R], contiguous")
+        blocks = k_scale.shape[2] if k_scale.dim() == 3 else 0
+        if blocks <= 0 or R % blocks or tuple(k_scale.shape) != (pages, heads, blocks) or k_scale.shape != v_scale.shape or \
+                k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or not k_scale.is_contiguous() or not v_scale.is_contiguous():
+            raise SemantiCacheError("k_scale and v_scale must be float32 [pages, heads, R / block], contiguous")
+        _require_cuda(K, V, k_scale, v_scale, table, counts)
+        self.K, self.V, self.k_scale, self.v_scale, self.table, self.counts = K, V, k_scale, v_scale, table, counts
+        self.B, self.Hkv, self.d = table.shape[0], table.shape[1] if table.dim() == 3 else heads, d
+        self.struct = _Paged8CacheStruct(
+            K=_ptr(K), V=_ptr(V), k_scale=_ptr(k_scale), v_scale=_ptr(v_scale), counts=_ptr(counts), table=_ptr(table),
+            stride_page=K.stride(0), stride_head=K.stride(1), stride_row=K.stride(2), code=codes[K.dtype], block_rows=R // blocks, num_pages=pages,
+            page_heads=heads, page_rows=R, table_len=table.shape[-1], table_per_head=int(table.dim() == 3), B=self.B, Hkv=self.Hkv, d=d)
+        self.ptr = ctypes.addressof(self.struct)
+        self._made = True
+
+    _fixed = PagedCache._fixed
+    __setattr__ = __delattr__ = _fixed
+    lens_shapes = PagedCache.lens_shapes
+
+
+def sc_paged8_append(cache: PagedCache8, K, V, base_lens, lens, new_lens=None, counts=None, Q=None, Q_out=None, cos_sin=None, positions=None,
+                     interleaved: bool = False):
+    """sc_paged_append for a cache of 8-bit codes: K, V float32 or bfloat16 [B, Hkv, N, d] -> (lens, Q_out).
+
+    The scale of a block that receives rows becomes the smallest power of two that its largest number fits (and stays at least what it was while
+    the block holds rows, whose codes follow it).
+    """
+    lib = load_library()
+    if not isinstance(cache, PagedCache8):
+        raise SemantiCacheError("sc_paged8_append takes a PagedCache8")
+    r, Q_out = _paged_rows(cache, None, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved)
+    _check(lib.sc_paged8_append(ctypes.byref(cache.struct), ctypes.byref(r), _dtype_code(K), _stream()), "sc_paged8_append")
+    return lens, Q_out
+
+
+def sc_paged8_decode_attn(cache: PagedCache8, Q, lens, window: int = 0, sinks: int = 0, scale: float = 0.0, O=None, lse=None, want_lse: bool = False,
+                          workspace: Optional[Workspace] = None):
+    """Q [B, Hq, d] over the first lens [B] (or [B, Hkv]) rows of a cache of 8-bit codes, or over the newest `window` and the first `sinks` of them
+    -> (O [B, Hq, d], lse [B, Hq] or None).  Workspace: paged_workspace."""
+    return _windowed("sc_paged8_decode_attn", PagedCache8, cache, Q, lens, window, sinks, scale, O, lse, want_lse, workspace)
+
+
+# ------------------------------------------------------------------------------------------------ pages handed out on the GPU
+def paged_reserve_workspace(sequences: int, table_len: int, device) -> Workspace:
+    """Workspace of sc_paged_reserve for tables of `sequences` rows, initialised on the current stream."""
+    lib = load_library()
+    _c_ints(sequences=sequences, table_len=table_len)
+    nbytes = lib.sc_paged_reserve_workspace_bytes(int(sequences), int(table_len))
+    if nbytes == 0:
+        raise SemantiCacheError("no workspace for sequences=%d table_len=%d" % (sequences, table_len))
+    ws = Workspace(nbytes, device)
+    _check(lib.sc_paged_init_workspace(ws.ptr, ws.nbytes, _stream()), "sc_paged_init_workspace")
+    return ws
+
+
+def sc_paged_reserve(table, page_rows: int, base_lens, lens, free_pages, num_free, new_lens=None, N: Optional[int] = None, window: int = 0, sinks: int = 0,
+                     slots=None, want_slots: bool = False, workspace: Optional[Workspace] = None):
+    """Pages for the rows that arrive, and back with those that nobody needs -> (lens, slots or None).
+
+    table int32 [..., P] (-1: no page) and the stack free_pages int32 [pages] with num_free int32 [1] are changed; base_lens, lens and new_lens (None: N
+    everywhere) are int32 [...] like the table's rows.  slots int32 [..., N]: page * page_rows + row of every new row, -1 for none.  N is the
+    slots' last dimension, else the argument (default 1; with new_lens and no slots it says nothing: any number goes).  lens: base_lens + new_lens, or -1.
+    """
+    lib = load_library()
+    if table.dim() < 2 or table.dtype != torch.int32 or not table.is_contiguous():
+        raise SemantiCacheError("table must be int32 [..., P], contiguous")
+    rows = tuple(table.shape[:-1])
+    if slots is not None:
+        if slots.dim() != table.dim() or (N is not None and N != slots.shape[-1]):
+            raise SemantiCacheError("slots must be int32 [..., N], contiguous")
+        N = slots.shape[-1]
+    elif N is None:
+        N = 1 if new_lens is None or want_slots else 2**31 - 1
+    _c_ints(page_rows=page_rows, N=N, window=window, sinks=sinks, **{"dimension %d" % i: n for i, n in enumerate(table.shape)})
+    if not _is_i32(base_lens, rows) or not _is_i32(lens, rows) or not (new_lens is None or _is_i32(new_lens, rows)):
+        raise SemantiCacheError("base_lens, lens and new_lens must be int32 like the table's rows, contiguous")
+    if free_pages.dim() != 1 or not _is_i32(free_pages, tuple(free_pages.shape)) or not _is_i32(num_free, (1,)):
+        raise SemantiCacheError("free_pages must be int32 [pages] and num_free int32 [1], contiguous")
+    if slots is None and want_slots:
+        slots = torch.empty((*rows, N), dtype=torch.int32, device=table.device)
+    if slots is not None and not _is_i32(slots, (*rows, N)):
+        raise SemantiCacheError("slots must be int32 [..., N], contiguous")
+    _require_cuda(table, base_lens, lens, new_lens, free_pages, num_free, slots)
+    S, P = base_lens.numel(), table.shape[-1]
+    if workspace is None:
+        workspace = paged_reserve_workspace(S, P, table.device)
+    st = lib.sc_paged_reserve(_ptr(table), S, P, free_pages.numel(), int(page_rows), _ptr(base_lens), _ptr(new_lens), int(N), int(window), int(sinks),
+                              _ptr(free_pages), _ptr(num_free), _ptr(lens), _ptr(slots), workspace.ptr, workspace.nbytes, _stream())
+    _check(st, "sc_paged_reserve")
+    return lens, slots
 
 
 def stream_read_probe(buf, sink) -> None:

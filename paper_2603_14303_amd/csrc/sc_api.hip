@@ -417,17 +417,17 @@ static bool rows_apart(const int64_t (&size)[3], const int64_t (&stride)[3], int
 }
 
 // the cache of the sc_paged_* calls: everything about it that the host can see
-static sc_status paged_check(const sc_paged_cache *c, PagedView &v) {
+static sc_status paged_check(const sc_paged_cache *c, PagedView &v, int64_t code_bytes = 0) {
     if (!c || !c->K || !c->V || !c->table) return SC_ERR_INVALID_ARG;
     if (c->B <= 0 || c->Hkv <= 0 || c->num_pages <= 0 || c->table_len <= 0) return SC_ERR_INVALID_ARG;
-    if (!dtype_ok(c->dtype)) return SC_ERR_UNSUPPORTED;
+    if (!code_bytes && !dtype_ok(c->dtype)) return SC_ERR_UNSUPPORTED;
     if (c->d != 64 && c->d != 128) return SC_ERR_UNSUPPORTED;
     if (c->B > 65535 || c->Hkv > 65535 || (int64_t)c->B * c->Hkv > (1 << 20)) return SC_ERR_UNSUPPORTED;
     const int R = c->page_rows;
     if (R < 16 || R > 1024 || (R & (R - 1))) return SC_ERR_INVALID_ARG;
     if (c->page_heads != (c->table_per_head ? 1 : c->Hkv)) return SC_ERR_INVALID_ARG;
     if ((int64_t)c->table_len * R > INT32_MAX) return SC_ERR_UNSUPPORTED;
-    const int64_t es = (int64_t)elem_size(c->dtype);
+    const int64_t es = code_bytes ? code_bytes : (int64_t)elem_size(c->dtype);
     // in any order of pages, heads and rows
     const int64_t size[3] = {c->num_pages, c->page_heads, R}, stride[3] = {c->stride_page, c->stride_head, c->stride_row};
     for (int i = 0; i < 3; ++i)
@@ -450,6 +450,23 @@ static sc_status paged_check(const sc_paged_cache *c, PagedView &v) {
     return SC_OK;
 }
 
+// the same for the cache of the sc_paged8_* calls
+static sc_status paged8_check(const sc_paged8_cache *c, PagedView &v, Paged8View &w) {
+    if (!c) return SC_ERR_INVALID_ARG;
+    const sc_paged_cache plain = {c->K, c->V, c->counts, nullptr, nullptr, c->table, c->stride_page, c->stride_head, c->stride_row, SC_F32,
+                                  c->num_pages, c->page_heads, c->page_rows, c->table_len, c->table_per_head, c->B, c->Hkv, c->d};
+    const sc_status st = paged_check(&plain, v, 1);
+    if (st != SC_OK) return st;
+    if (c->code != SC_E4M3 && c->code != SC_I8) return SC_ERR_UNSUPPORTED;
+    const int E = c->block_rows;
+    if (E < 16 || E > 128 || (E & (E - 1)) || E > c->page_rows) return SC_ERR_INVALID_ARG;
+    if (!c->k_scale || !c->v_scale || !aligned4(c->k_scale) || !aligned4(c->v_scale)) return SC_ERR_INVALID_ARG;
+    w.k_scale = c->k_scale; w.v_scale = c->v_scale;
+    w.log2_block = __builtin_ctz((unsigned)E);
+    w.code = c->code == SC_E4M3 ? 1 : 2;
+    return SC_OK;
+}
+
 // Rows [B, heads, N, d]: aligned, and, where the call writes them, none with a stride of less than a row.
 static bool rows_ok(const void *p, int64_t B, int64_t H, int64_t N, int64_t sb, int64_t sh, int64_t sn, int64_t d, int64_t es, bool written) {
     const int64_t size[3] = {B, H, N}, stride[3] = {sb, sh, sn};
@@ -464,18 +481,16 @@ static bool apart(const int32_t *a, int64_t na, const int32_t *b, int64_t nb) {
     return !b || x + na * sizeof(int32_t) <= y || y + nb * sizeof(int32_t) <= x;
 }
 
-sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *r, void *stream) {
-    PagedAppendArgs a;
-    const sc_status st = paged_check(cache, a.c);
-    if (st != SC_OK) return st;
+// the rows of sc_paged_append and sc_paged8_append (a.c is there already): K and V of elements of `es` bytes; a page, or a block, of `rows` rows is one workgroup's at most
+static sc_status append_check(const sc_paged_rows *r, int64_t es, int rows, PagedAppendArgs &a) {
+    const PagedView &c = a.c;
     if (!r || !r->K || !r->V || !r->base_lens || !r->lens || r->N <= 0) return SC_ERR_INVALID_ARG;
     if (!aligned4(r->base_lens) || !aligned4(r->lens) || !aligned4(r->new_lens) || !aligned4(r->positions) || !aligned4(r->counts)) return SC_ERR_INVALID_ARG;
-    if (!r->counts != !cache->counts) return SC_ERR_INVALID_ARG;
-    const int64_t es = (int64_t)elem_size(cache->dtype);
-    if (!rows_ok(r->K, cache->B, cache->Hkv, r->N, r->k_stride_b, r->k_stride_h, r->k_stride_n, cache->d, es, false)) return SC_ERR_INVALID_ARG;
-    if (!rows_ok(r->V, cache->B, cache->Hkv, r->N, r->v_stride_b, r->v_stride_h, r->v_stride_n, cache->d, es, false)) return SC_ERR_INVALID_ARG;
+    if (!r->counts != !c.counts) return SC_ERR_INVALID_ARG;
+    if (!rows_ok(r->K, c.B, c.H, r->N, r->k_stride_b, r->k_stride_h, r->k_stride_n, c.d, es, false)) return SC_ERR_INVALID_ARG;
+    if (!rows_ok(r->V, c.B, c.H, r->N, r->v_stride_b, r->v_stride_h, r->v_stride_n, c.d, es, false)) return SC_ERR_INVALID_ARG;
     if (r->cos_sin) {
-        if (r->rot <= 0 || r->rot > cache->d || r->rot % 16 || r->max_position <= 0 || !aligned16(r->cos_sin)) return SC_ERR_INVALID_ARG;
+        if (r->rot <= 0 || r->rot > c.d || r->rot % 16 || r->max_position <= 0 || !aligned16(r->cos_sin)) return SC_ERR_INVALID_ARG;
         if (!r->positions && r->per_head) return SC_ERR_INVALID_ARG;      // a token has one position
     } else if (r->rot != 0 || r->Q) {
         return SC_ERR_INVALID_ARG;
@@ -486,16 +501,16 @@ sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *r, v
         if (!dtype_ok(r->q_dtype)) return SC_ERR_UNSUPPORTED;
         if (r->Hq <= 0) return SC_ERR_INVALID_ARG;
         qs = (int64_t)elem_size(r->q_dtype);
-        if (!rows_ok(r->Q, cache->B, r->Hq, r->N, r->q_stride_b, r->q_stride_h, r->q_stride_n, cache->d, qs, false)) return SC_ERR_INVALID_ARG;
-        if (!rows_ok(r->Q_out, cache->B, r->Hq, r->N, r->o_stride_b, r->o_stride_h, r->o_stride_n, cache->d, qs, true)) return SC_ERR_INVALID_ARG;
+        if (!rows_ok(r->Q, c.B, r->Hq, r->N, r->q_stride_b, r->q_stride_h, r->q_stride_n, c.d, qs, false)) return SC_ERR_INVALID_ARG;
+        if (!rows_ok(r->Q_out, c.B, r->Hq, r->N, r->o_stride_b, r->o_stride_h, r->o_stride_n, c.d, qs, true)) return SC_ERR_INVALID_ARG;
         if (r->Hq > 65535) return SC_ERR_UNSUPPORTED;
     }
-    if (!paged_append_fits(cache->B, cache->Hkv, cache->page_rows, r->N, r->Q ? r->Hq : 0)) return SC_ERR_UNSUPPORTED;      // grid size
-    const int64_t q_size[3] = {cache->B, r->Hq, r->N}, o_stride[3] = {r->o_stride_b, r->o_stride_h, r->o_stride_n};
-    if (r->Q && !rows_apart(q_size, o_stride, cache->d)) return SC_ERR_INVALID_ARG;
+    if (!paged_append_fits(c.B, c.H, rows, r->N, r->Q ? r->Hq : 0)) return SC_ERR_UNSUPPORTED;      // grid size
+    const int64_t q_size[3] = {c.B, r->Hq, r->N}, o_stride[3] = {r->o_stride_b, r->o_stride_h, r->o_stride_n};
+    if (r->Q && !rows_apart(q_size, o_stride, c.d)) return SC_ERR_INVALID_ARG;
     // every workgroup reads the old lengths and the positions while one of them files the new lengths
-    const int64_t n = (int64_t)cache->B * (r->per_head ? cache->Hkv : 1);
-    if (!apart(r->lens, n, r->base_lens, n) || !apart(r->lens, n, r->new_lens, n) || !apart(r->lens, n, r->positions, cache->B)) return SC_ERR_INVALID_ARG;
+    const int64_t n = (int64_t)c.B * (r->per_head ? c.H : 1);
+    if (!apart(r->lens, n, r->base_lens, n) || !apart(r->lens, n, r->new_lens, n) || !apart(r->lens, n, r->positions, c.B)) return SC_ERR_INVALID_ARG;
     a.K = static_cast<const char *>(r->K); a.V = static_cast<const char *>(r->V);
     a.k_b = r->k_stride_b * es; a.k_h = r->k_stride_h * es; a.k_n = r->k_stride_n * es;
     a.v_b = r->v_stride_b * es; a.v_h = r->v_stride_h * es; a.v_n = r->v_stride_n * es;
@@ -508,7 +523,27 @@ sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *r, v
     a.q_b = r->q_stride_b * qs; a.q_h = r->q_stride_h * qs; a.q_n = r->q_stride_n * qs;
     a.o_b = r->o_stride_b * qs; a.o_h = r->o_stride_h * qs; a.o_n = r->o_stride_n * qs;
     a.q_dtype = r->Q ? static_cast<DType>(r->q_dtype) : a.c.dtype;
+    return SC_OK;
+}
+
+sc_status sc_paged_append(const sc_paged_cache *cache, const sc_paged_rows *r, void *stream) {
+    PagedAppendArgs a;
+    sc_status st = paged_check(cache, a.c);
+    if (st == SC_OK) st = append_check(r, (int64_t)elem_size(cache->dtype), cache->page_rows, a);
+    if (st != SC_OK) return st;
     return runtime_status(launch_paged_append(a, static_cast<hipStream_t>(stream)));
+}
+
+sc_status sc_paged8_append(const sc_paged8_cache *cache, const sc_paged_rows *r, sc_dtype kv_dtype, void *stream) {
+    PagedAppendArgs a;
+    Paged8View w;
+    sc_status st = paged8_check(cache, a.c, w);
+    if (st == SC_OK && !dtype_ok(kv_dtype)) st = SC_ERR_UNSUPPORTED;
+    if (st != SC_OK) return st;
+    a.c.dtype = static_cast<DType>(kv_dtype);
+    st = append_check(r, (int64_t)elem_size(kv_dtype), cache->block_rows, a);
+    if (st != SC_OK) return st;
+    return runtime_status(launch_paged8_append(a, w, static_cast<hipStream_t>(stream)));
 }
 
 size_t sc_paged_workspace_bytes(int B, int Hq, int Hkv, int d, int table_len) {
@@ -523,42 +558,73 @@ sc_status sc_paged_init_workspace(void *ws, size_t ws_bytes, void *stream) {
     return runtime_status(launch_decode_init_workspace(ws, state, static_cast<hipStream_t>(stream)));
 }
 
-// what sc_paged_decode_attn and sc_paged_select have in common
-static sc_status paged_query_check(const sc_paged_cache *cache, PagedView &v, const void *Q, sc_dtype q_dtype, int Hq, const int32_t *lens, const void *ws) {
-    const sc_status st = paged_check(cache, v);
+// what the calls with a query have in common
+static sc_status paged_query_check(sc_status st, const PagedView &v, const void *Q, sc_dtype q_dtype, int Hq, const int32_t *lens, const void *ws) {
     if (st != SC_OK) return st;
     if (!Q || !lens || Hq <= 0 || !aligned16(Q) || !aligned4(lens)) return SC_ERR_INVALID_ARG;
-    if (!dtype_ok(q_dtype) || Hq % cache->Hkv || Hq / cache->Hkv > 16) return SC_ERR_UNSUPPORTED;
+    if (!dtype_ok(q_dtype) || Hq % v.H || Hq / v.H > 16) return SC_ERR_UNSUPPORTED;
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SC_ERR_WORKSPACE;
     return SC_OK;
+}
+// ... and those that attend (a.c, a.sel, a.sel_lens, a.keep, a.window and a.sinks are there already)
+static sc_status paged_attend(sc_status st, PagedDecodeArgs &a, const void *Q, sc_dtype q_dtype, int Hq, const int32_t *lens, int lens_per_head, float scale,
+                              void *O, sc_dtype o_dtype, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    st = paged_query_check(st, a.c, Q, q_dtype, Hq, lens, ws);
+    if (st != SC_OK) return st;
+    if (!O || !aligned16(O) || !aligned4(lse) || !a.sel != !a.sel_lens || !aligned4(a.sel) || !aligned4(a.sel_lens)) return SC_ERR_INVALID_ARG;
+    if (!dtype_ok(o_dtype)) return SC_ERR_UNSUPPORTED;
+    if (scale != scale) return SC_ERR_INVALID_ARG;
+    if (a.sel && a.keep <= 0) return SC_ERR_CAPACITY;
+    if (a.sel && a.keep > (1 << 20)) return SC_ERR_UNSUPPORTED;
+    if (a.window < 0 || a.sinks < 0) return SC_ERR_INVALID_ARG;
+    const int64_t most = (int64_t)(a.sel ? a.keep : a.c.P) * a.c.R;
+    if ((most / 64 + 1) * a.c.B * a.c.H > (1 << 30)) return SC_ERR_UNSUPPORTED;      // the kernel counts stretches of 64 rows and more in 32 bits
+    if (ws_bytes < paged_state_bytes() + paged_decode_bytes(Hq / a.c.H, a.c.d)) return SC_ERR_WORKSPACE;
+    a.Q = Q; a.q_dtype = static_cast<DType>(q_dtype); a.Hq = Hq;
+    a.lens = lens; a.lens_per_head = lens_per_head != 0;
+    a.scale = (scale == 0.f) ? 1.0f / sqrtf((float)a.c.d) : scale;
+    a.O = O; a.o_dtype = static_cast<DType>(o_dtype); a.lse = lse; a.ws = ws;
+    return runtime_status(launch_paged_decode(a, static_cast<hipStream_t>(stream)));
 }
 
 sc_status sc_paged_decode_attn(const sc_paged_cache *cache, const void *Q, sc_dtype q_dtype, int Hq, const int32_t *lens,
                                int lens_per_head, const int32_t *sel, const int32_t *sel_lens, int keep, float scale, void *O,
                                sc_dtype o_dtype, float *lse, void *ws, size_t ws_bytes, void *stream) {
     PagedDecodeArgs a;
-    const sc_status st = paged_query_check(cache, a.c, Q, q_dtype, Hq, lens, ws);
-    if (st != SC_OK) return st;
-    if (!O || !aligned16(O) || !aligned4(lse) || !sel != !sel_lens || !aligned4(sel) || !aligned4(sel_lens)) return SC_ERR_INVALID_ARG;
-    if (!dtype_ok(o_dtype)) return SC_ERR_UNSUPPORTED;
-    if (scale != scale) return SC_ERR_INVALID_ARG;
-    if (sel && keep <= 0) return SC_ERR_CAPACITY;
-    if (sel && keep > (1 << 20)) return SC_ERR_UNSUPPORTED;
-    const int64_t most = (int64_t)(sel ? keep : cache->table_len) * cache->page_rows;
-    if ((most / 64 + 1) * cache->B * cache->Hkv > (1 << 30)) return SC_ERR_UNSUPPORTED;      // the kernel counts stretches of 64 rows and more in 32 bits
-    if (ws_bytes < paged_state_bytes() + paged_decode_bytes(Hq / cache->Hkv, cache->d)) return SC_ERR_WORKSPACE;
-    a.Q = Q; a.q_dtype = static_cast<DType>(q_dtype); a.Hq = Hq;
-    a.lens = lens; a.lens_per_head = lens_per_head != 0;
+    const sc_status st = paged_check(cache, a.c);
     a.sel = sel; a.sel_lens = sel_lens; a.keep = sel ? keep : 0;
-    a.scale = (scale == 0.f) ? 1.0f / sqrtf((float)cache->d) : scale;
-    a.O = O; a.o_dtype = static_cast<DType>(o_dtype); a.lse = lse; a.ws = ws;
-    return runtime_status(launch_paged_decode(a, static_cast<hipStream_t>(stream)));
+    return paged_attend(st, a, Q, q_dtype, Hq, lens, lens_per_head, scale, O, o_dtype, lse, ws, ws_bytes, stream);
+}
+
+sc_status sc_paged_window_attn(const sc_paged_cache *cache, const void *Q, sc_dtype q_dtype, int Hq, const int32_t *lens,
+                               int lens_per_head, int window, int sinks, float scale, void *O, sc_dtype o_dtype, float *lse,
+                               void *ws, size_t ws_bytes, void *stream) {
+    PagedDecodeArgs a;
+    const sc_status st = paged_check(cache, a.c);
+    a.sel = a.sel_lens = nullptr; a.keep = 0;
+    a.window = window; a.sinks = sinks;
+    return paged_attend(st, a, Q, q_dtype, Hq, lens, lens_per_head, scale, O, o_dtype, lse, ws, ws_bytes, stream);
+}
+
+sc_status sc_paged8_decode_attn(const sc_paged8_cache *cache, const void *Q, sc_dtype q_dtype, int Hq, const int32_t *lens,
+                                int lens_per_head, int window, int sinks, float scale, void *O, sc_dtype o_dtype, float *lse,
+                                void *ws, size_t ws_bytes, void *stream) {
+    PagedDecodeArgs a;
+    Paged8View w;
+    const sc_status st = paged8_check(cache, a.c, w);
+    a.sel = a.sel_lens = nullptr; a.keep = 0;
+    a.window = window; a.sinks = sinks;
+    if (st == SC_OK) {
+        a.code = w.code; a.log2_block = w.log2_block;
+        a.k_scale = w.k_scale; a.v_scale = w.v_scale;
+    }
+    return paged_attend(st, a, Q, q_dtype, Hq, lens, lens_per_head, scale, O, o_dtype, lse, ws, ws_bytes, stream);
 }
 
 sc_status sc_paged_select(const sc_paged_cache *cache, const void *Q, sc_dtype q_dtype, int Hq, const int32_t *lens, int lens_per_head,
                           int keep, int first, int recent, int32_t *sel, int32_t *sel_lens, void *ws, size_t ws_bytes, void *stream) {
     PagedSelectArgs a;
-    const sc_status st = paged_query_check(cache, a.c, Q, q_dtype, Hq, lens, ws);
+    const sc_status st = paged_query_check(paged_check(cache, a.c), a.c, Q, q_dtype, Hq, lens, ws);
     if (st != SC_OK) return st;
     if (!cache->k_min || !sel || !sel_lens || !aligned4(sel) || !aligned4(sel_lens) || first < 0 || recent < 0) return SC_ERR_INVALID_ARG;
     if (keep <= 0 || (int64_t)first + recent > keep) return SC_ERR_CAPACITY;
@@ -570,6 +636,27 @@ sc_status sc_paged_select(const sc_paged_cache *cache, const void *Q, sc_dtype q
     a.keep = keep; a.first = first; a.recent = recent;
     a.sel = sel; a.sel_lens = sel_lens; a.ws = ws;
     return runtime_status(launch_paged_select(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t sc_paged_reserve_workspace_bytes(int sequences, int table_len) {
+    if (sequences <= 0 || table_len <= 0 || sequences > (1 << 20) || (int64_t)sequences * table_len > (1 << 28)) return 0;
+    return paged_reserve_bytes(sequences, table_len);
+}
+
+sc_status sc_paged_reserve(int32_t *table, int sequences, int table_len, int num_pages, int page_rows, const int32_t *base_lens, const int32_t *new_lens, int N,
+                           int window, int sinks, int32_t *free_pages, int32_t *num_free, int32_t *lens, int32_t *slots, void *ws, size_t ws_bytes, void *stream) {
+    if (!table || !base_lens || !free_pages || !num_free || !lens) return SC_ERR_INVALID_ARG;
+    if (sequences <= 0 || table_len <= 0 || num_pages <= 0 || N < 0 || window < 0 || sinks < 0) return SC_ERR_INVALID_ARG;
+    if (!aligned4(table) || !aligned4(base_lens) || !aligned4(new_lens) || !aligned4(free_pages) || !aligned4(num_free) || !aligned4(lens) || !aligned4(slots)) return SC_ERR_INVALID_ARG;
+    if (page_rows < 16 || page_rows > 1024 || (page_rows & (page_rows - 1))) return SC_ERR_INVALID_ARG;
+    if (sequences > (1 << 20) || (int64_t)sequences * table_len > (1 << 28)) return SC_ERR_UNSUPPORTED;      // counted in 32 bits
+    if ((int64_t)table_len * page_rows > INT32_MAX || (int64_t)num_pages * page_rows > INT32_MAX) return SC_ERR_UNSUPPORTED;      // rows and slots are 32-bit
+    // the second of two launches reads the old lengths again
+    const int64_t S = sequences;
+    if (!apart(lens, S, base_lens, S) || !apart(lens, S, new_lens, S)) return SC_ERR_INVALID_ARG;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < paged_reserve_bytes(sequences, table_len)) return SC_ERR_WORKSPACE;
+    const PagedReserveArgs a = {table, sequences, table_len, num_pages, page_rows, base_lens, new_lens, N, window, sinks, free_pages, num_free, lens, N > 0 ? slots : nullptr};
+    return runtime_status(launch_paged_reserve(a, ws, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

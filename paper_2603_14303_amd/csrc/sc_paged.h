@@ -85,6 +85,15 @@ inline bool paged_append_fits(int64_t B, int64_t H, int64_t R, int64_t N, int64_
 }
 hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t stream);
 
+// ---- a cache of 8-bit codes: PagedView in bytes, and their scales
+struct Paged8View {
+    float *k_scale, *v_scale;      // [page][head][R >> log2_block]
+    int log2_block;
+    int code;                      // 1 e4m3, 2 int8
+};
+// c.dtype is the type of the rows that arrive
+hipError_t launch_paged8_append(const PagedAppendArgs &a, const Paged8View &v, hipStream_t stream);
+
 // ---- sc_paged_decode_attn
 struct PagedDecodeArgs {
     PagedView c;
@@ -100,6 +109,10 @@ struct PagedDecodeArgs {
     DType o_dtype;
     float *lse;
     void *ws;
+    int window = 0, sinks = 0;                                     // window 0: none (then sinks say nothing); not with sel
+    int code = 0;                                                  // 8-bit codes: 1 e4m3, 2 int8 (c.dtype says nothing then)
+    const float *k_scale = nullptr, *v_scale = nullptr;            // [page][head][R >> log2_block]
+    int log2_block = 0;
 };
 hipError_t launch_paged_decode(const PagedDecodeArgs &a, hipStream_t stream);
 
@@ -116,6 +129,17 @@ struct PagedSelectArgs {
     void *ws;
 };
 hipError_t launch_paged_select(const PagedSelectArgs &a, hipStream_t stream);
+
+// ---- sc_paged_reserve
+struct PagedReserveArgs {
+    int32_t *table;
+    int S, P, num_pages, R;
+    const int32_t *base_lens, *new_lens;
+    int N, window, sinks;
+    int32_t *free_pages, *num_free, *lens, *slots;
+};
+size_t paged_reserve_bytes(int S, int P);
+hipError_t launch_paged_reserve(const PagedReserveArgs &a, void *ws, hipStream_t stream);
 
 // ---- workspace: counters, then what the two calls need (they follow each other on a stream, so it is the same memory)
 size_t paged_state_bytes();

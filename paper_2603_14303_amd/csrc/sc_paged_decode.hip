@@ -23,7 +23,12 @@ namespace sc {
 
 constexpr int kPagWaves = 8;
 constexpr int kPagThreads = kPagWaves * kWave;
-constexpr int kStep = 16 * kPagWaves;        // rows of a step of all wavefronts: the unit of work
+// What a cache holds: T is float, bf16_t, or one of the 8-bit codes below.  A wavefront takes kSub times 16 rows a step: 8-bit rows are half as long as bf16's, and as
+// many bytes have to be under way.
+struct e4m3_t { uint8_t bits; };
+struct i8_t { int8_t value; };
+template <typename T> constexpr int kSub = sizeof(T) == 1 ? 2 : 1;
+template <typename T> constexpr int kStep = 16 * kSub<T> * kPagWaves;        // rows of a step of all wavefronts: the unit of work
 // steps up to which a head goes to one workgroup, if there is one for every head: 8 heads of 170 and 250 rows (two steps) 6.6 and 7.4 us, 8.2 and 8.3 split; of 400
 // and 512 rows (four) 8.8 and 10.5 alone, 8.4 and 8.7 split
 constexpr int kAlone = 2;
@@ -60,11 +65,15 @@ struct PagDecParams {
     int *counter;        // [2][2 * kMaxWgs] workgroups that have left their part of a head (of a group of parts), groups that have been joined; by the first one's place
     float *part;         // [2 * kMaxWgs][G][D + kPagPad]: a workgroup's first stretch and its last one
     int wgs;             // workgroups of the launch
+    int window, sinks;   // (WIN) rows from len - window on and rows below `sinks` attend
+    const float *k_scale, *v_scale;      // (8-bit codes) [page][head][R >> log2_block]
+    int log2_block;
 };
 
 // a value that all lanes agree on, kept in a scalar register (what a division or a conversion gives is in a vector register otherwise, and every
 // branch on it is one on lanes)
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float readlane(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
 __device__ __forceinline__ float inverse_of(int y) { return __builtin_amdgcn_rcpf((float)y); }
 __device__ __forceinline__ float pag_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -105,7 +114,9 @@ template <typename T, int D> __device__ __forceinline__ void load_values(Rows<T,
     constexpr int VW = Rows<T, D>::VW;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if constexpr (VW == 2) {
+        if constexpr (VW == 1) {
+            x.v[i][0] = __builtin_amdgcn_raw_buffer_load_b32(v, lane_offset + i * row_bytes, 0, kAuxNt);
+        } else if constexpr (VW == 2) {
             const pag_u32x2 t = __builtin_amdgcn_raw_buffer_load_b64(v, lane_offset + i * row_bytes, 0, kAuxNt);
             x.v[i][0] = t.x;
             x.v[i][1] = t.y;
@@ -122,11 +133,29 @@ template <typename T, int D> __device__ __forceinline__ void load_values(Rows<T,
     }
 }
 
+// ---- 8-bit codes as bf16, exactly (e4m3 has three bits behind the point, a whole number up to 128 seven): four codes of a dword in two dwords
+typedef __bf16 pag_bf16x2 __attribute__((ext_vector_type(2)));
+template <typename T> __device__ __forceinline__ uint2 widen4(uint32_t w) {
+    if constexpr (std::is_same_v<T, e4m3_t>) {
+        return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
+                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)));
+    } else {
+        const float x0 = (float)(int8_t)w, x1 = (float)(int8_t)(w >> 8), x2 = (float)(int8_t)(w >> 16), x3 = (float)((int32_t)w >> 24);
+        return make_uint2(pack_hi(__float_as_uint(x0), __float_as_uint(x1)), pack_hi(__float_as_uint(x2), __float_as_uint(x3)));
+    }
+}
+// four dwords (rows) of four codes -> four dwords (columns) of the rows' codes
+__device__ __forceinline__ void transpose4(const uint32_t (&r)[4], uint32_t (&c)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), b = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);      // rows 0, 1: columns 0 and 1, 2 and 3
+    const uint32_t d = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u), e = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+    c[0] = pack_lo(a, d); c[1] = pack_hi(a, d); c[2] = pack_lo(b, e); c[3] = pack_hi(b, e);
+}
+
 // The accumulators of lane (g, c): acc[a][i] is head 4 g + i, element acc_element(a, c).
 template <typename T, int D> struct Acc {
     static constexpr int N = D / 16;
     static __device__ __forceinline__ int element(int a, int c) {
-        if constexpr (sizeof(T) == 2) return (D / 16) * c + a;      // 2 VW neighbouring elements
+        if constexpr (sizeof(T) <= 2) return (D / 16) * c + a;      // neighbouring elements
         else return 64 * (a / 4) + 4 * c + a % 4;
     }
 };
@@ -246,10 +275,13 @@ __device__ __forceinline__ bool last_of(int *counter, int n, int tid, int *s_las
     return *s_last != 0;
 }
 
-// QP: parts of the queries (bf16 caches)
-template <typename T, int D, int QP>
+// QP: parts of the queries (bf16 caches and codes).  WIN: a window and first rows that stay (p.window, p.sinks; codes always have it); p.sel is NULL then
+template <typename T, int D, int QP, bool WIN>
 __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecParams p) {
-    constexpr bool kBf16 = sizeof(T) == 2;
+    constexpr bool kBf16 = sizeof(T) <= 2;     // products in bf16
+    constexpr bool kCodes = sizeof(T) == 1;
+    constexpr int NS = kSub<T>, kStep = sc::kStep<T>;
+    constexpr int NM = kBf16 ? D / 32 : Rows<T, D>::KL;               // first products a row, pieces of 16 bytes of a query
     constexpr int KL = Rows<T, D>::KL, VW = Rows<T, D>::VW, NA = Acc<T, D>::N;
     constexpr int PP = 3;                     // parts of the probabilities (bf16)
     constexpr int kStride = D + kPagPad;
@@ -269,11 +301,21 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     const bool per_head = p.sel != nullptr || p.lens_per_head != 0;
     const int entries = per_head ? cv.B * cv.H : cv.B, weight = per_head ? 1 : cv.H;
     int my_rows = 0, my_len = 0;      // of the lane's entry among the 64 at hand
+    // WIN: rows that no step visits, `gap` of them from row `gap_at` on, both multiples of 16
+    auto gap_of = [&](int len, int &gap_at) {
+        const PagedGap x = paged_gap(len, p.window, p.sinks);
+        gap_at = x.at;
+        return x.rows;
+    };
     auto entry = [&](int e) {
         my_rows = my_len = 0;
         if (e < entries) {
             my_len = min(max(p.lens[p.sel && !p.lens_per_head ? paged_quotient(e, cv.H, inverse_of(cv.H)) : e], 0), cv.P << cv.log2_R);
-            my_rows = p.sel ? min(max(p.sel_lens[e], 0), p.keep) << cv.log2_R : my_len;      // selected: the rows of whole pages; those behind the length are masked
+            my_rows = !WIN && p.sel ? min(max(p.sel_lens[e], 0), p.keep) << cv.log2_R : my_len;      // selected: the rows of whole pages; those behind the length are masked
+            if constexpr (WIN) {
+                int at;
+                my_rows -= gap_of(my_len, at);
+            }
         }
     };
     // Units of a head: its steps, rounded up to what a workgroup takes, so that no workgroup has parts of two heads (each costs it a start and a store,
@@ -338,6 +380,7 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     struct Stretch {
         int b, h, a, units, end;           // units [a, a + units) are the head's, the stretch goes to `end`
         int len, first, steps;             // rows of the sequence; the wavefront's first row, its steps (every kStep rows)
+        int gap, gap_at;                   // (WIN)
         const int32_t *table, *sel;
     };
     auto stretch_at = [&](int pos) {
@@ -348,32 +391,52 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
         t.units = uniform(units);
         t.end = uniform(min(a + units, stop));
         t.len = uniform(len);
-        t.first = uniform((pos - a) * kStep + 16 * wave);
+        t.first = uniform((pos - a) * kStep + 16 * NS * wave);
+        t.gap = t.gap_at = 0;
+        if constexpr (WIN) {
+            t.gap = uniform(gap_of(len, t.gap_at));
+            t.gap_at = uniform(t.gap_at);
+        }
         const int r1 = min((t.end - a) * kStep, rows);
         t.steps = uniform(t.first < r1 ? (r1 - t.first + kStep - 1) / kStep : 0);
         t.table = paged_table(cv, b, h);
-        t.sel = p.sel ? p.sel + ((int64_t)b * cv.H + h) * p.keep : nullptr;
+        t.sel = !WIN && p.sel ? p.sel + ((int64_t)b * cv.H + h) * p.keep : nullptr;
         return t;
     };
-    // Lane i knows the page of step s0 + i, how many of the step's rows are there, and whether anything is wrong with it
-    struct Pages { int page, left, bad; };
+    // Lane i knows the page of the i-th 16 rows from step s0 on, how many of them are there, and whether anything is wrong with it; of codes, their scales too
+    struct Pages { int page, left, bad; float ks, vs; };
+    auto row_of = [&](const Stretch &t, int s, int u) {      // of the sequence
+        const int r = t.first + s * kStep + 16 * u;
+        return WIN && r >= t.gap_at ? r + t.gap : r;
+    };
     auto look_up = [&](const Stretch &t, int s0) {
-        Pages x = {0, 0, 0};
-        if (s0 + lane < t.steps) {
-            const PagedStep y = paged_step(t.first + (s0 + lane) * kStep, cv.log2_R, t.len, cv.P, cv.num_pages, t.table, t.sel != nullptr, t.sel);
-            x = {y.page, y.left, y.bad};
+        Pages x = {0, 0, 0, 0.f, 0.f};
+        if (s0 + lane / NS < t.steps) {
+            const int row = row_of(t, s0 + lane / NS, lane % NS);
+            const PagedStep y = paged_step(row, cv.log2_R, WIN ? paged_window_len(row, t.len, p.window, p.sinks) : t.len, cv.P, cv.num_pages, t.table, !WIN && t.sel != nullptr, t.sel);
+            x.page = y.page;
+            x.left = y.left;
+            x.bad = y.bad;
+            if constexpr (kCodes) {
+                if (y.left > 0) {
+                    const int64_t at = (paged_index(cv, y.page, t.h) << (cv.log2_R - p.log2_block)) + ((row & (cv.R - 1)) >> p.log2_block);
+                    x.ks = p.k_scale[at];
+                    x.vs = p.v_scale[at];
+                }
+            }
         }
         return x;
     };
     // Queries: lane (g, c) holds of head c what meets its pieces of a key; heads beyond the group read as zeros
-    uint4 q[QP][KL];
+    uint4 q[QP][NM];
     auto load_queries = [&](const Stretch &t) {
         const int qs = p.q_is_bf16 ? 2 : 4;
         const pag_rsrc rows = rows_at(static_cast<const char *>(p.Q) + ((int64_t)t.b * cv.H + t.h) * G * D * qs, G * D * qs);
 #pragma unroll
-        for (int ks = 0; ks < KL; ++ks) {
+        for (int ks = 0; ks < NM; ++ks) {
+            const int el = kCodes ? 64 * (ks / 2) + 16 * g + 8 * (ks % 2) : 32 * ks + 8 * g;      // the lane's elements of a key in this product (bf16)
             if constexpr (kBf16 && QP > 1) {
-                const int at = (c * D + 32 * ks + 8 * g) * 4;
+                const int at = (c * D + el) * 4;
                 const pag_u32x4 y0 = __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, 0), y1 = __builtin_amdgcn_raw_buffer_load_b128(rows, at + 16, 0, 0);
                 uint32_t w[4][QP];
                 split_bf16<QP>(__uint_as_float(y0.x), __uint_as_float(y0.y), w[0]);
@@ -386,7 +449,7 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
                 const pag_u32x2 y = __builtin_amdgcn_raw_buffer_load_b64(rows, (c * D + 16 * ks + 4 * g) * 2, 0, 0);
                 q[0][ks] = make_uint4(y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u);
             } else {
-                const pag_u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(rows, c * D * (int)sizeof(T) + 64 * ks + 16 * g, 0, 0);
+                const pag_u32x4 y = __builtin_amdgcn_raw_buffer_load_b128(rows, kBf16 ? (c * D + el) * 2 : c * D * 4 + 64 * ks + 16 * g, 0, 0);
                 q[0][ks] = make_uint4(y.x, y.y, y.z, y.w);
             }
         }
@@ -394,26 +457,32 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     // The next step is on its way while one is worked on: the registers of the keys are requested anew as soon as the first product has used them, those of
     // the values behind the second, without asking whether there is another step (with a load that is issued or not, the compiler has the next step wait
     // for everything under way).  Two steps ahead were no faster anywhere, and 0.8 us slower with one or two steps (the requests beyond the last).
-    Rows<T, D> x;
-    const char *values = nullptr;
-    int left = 0;
-    const int k_lane = c * cv.row_bytes + 16 * g, v_lane = 4 * g * cv.row_bytes + (VW == 2 ? 8 : 16) * c;
+    Rows<T, D> x[NS];
+    const char *values[NS];
+    int left[NS];
+    const int k_lane = c * cv.row_bytes + 16 * g, v_lane = 4 * g * cv.row_bytes + (VW <= 2 ? 4 * VW : 16) * c;
     const int size_bytes = cv.counts ? 64 : 0;
     auto request_keys = [&](const Stretch &t, Pages &pages, int s) {
-        if (s % kWave == 0 && s != 0) {
+        if (NS * s % kWave == 0 && s != 0) {
             const Pages y = look_up(t, s);
-            pages = {y.page, y.left, pages.bad | y.bad};
+            pages = {y.page, y.left, pages.bad | y.bad, y.ks, y.vs};
         }
-        const int page = __builtin_amdgcn_readlane(pages.page, s % kWave), in_page = (t.first + s * kStep) & (cv.R - 1);
-        const int64_t off = paged_offset(cv, page, t.h) + (int64_t)in_page * cv.row_bytes;
-        left = __builtin_amdgcn_readlane(pages.left, s % kWave);
-        values = cv.V + off;
-        load_keys<T, D>(x, rows_at(cv.K + off, left * cv.row_bytes), k_lane);
-        const char *sizes = reinterpret_cast<const char *>(cv.counts) + (paged_index(cv, page, t.h) * cv.R + in_page) * (int64_t)sizeof(int32_t);
-        const pag_u32x4 n = __builtin_amdgcn_raw_buffer_load_b128(rows_at(sizes, left > 0 ? size_bytes : 0), 16 * g, 0, 0);
-        x.n[0] = (int)n.x; x.n[1] = (int)n.y; x.n[2] = (int)n.z; x.n[3] = (int)n.w;
+#pragma unroll
+        for (int u = 0; u < NS; ++u) {
+            const int page = __builtin_amdgcn_readlane(pages.page, (NS * s + u) % kWave), in_page = row_of(t, s, u) & (cv.R - 1);
+            const int64_t off = paged_offset(cv, page, t.h) + (int64_t)in_page * cv.row_bytes;
+            left[u] = __builtin_amdgcn_readlane(pages.left, (NS * s + u) % kWave);
+            values[u] = cv.V + off;
+            load_keys<T, D>(x[u], rows_at(cv.K + off, left[u] * cv.row_bytes), k_lane);
+            const char *sizes = reinterpret_cast<const char *>(cv.counts) + (paged_index(cv, page, t.h) * cv.R + in_page) * (int64_t)sizeof(int32_t);
+            const pag_u32x4 n = __builtin_amdgcn_raw_buffer_load_b128(rows_at(sizes, left[u] > 0 ? size_bytes : 0), 16 * g, 0, 0);
+            x[u].n[0] = (int)n.x; x[u].n[1] = (int)n.y; x[u].n[2] = (int)n.z; x[u].n[3] = (int)n.w;
+        }
     };
-    auto request_values = [&]() { load_values<T, D>(x, rows_at(values, left * cv.row_bytes), v_lane, cv.row_bytes); };
+    auto request_values = [&]() {
+#pragma unroll
+        for (int u = 0; u < NS; ++u) load_values<T, D>(x[u], rows_at(values[u], left[u] * cv.row_bytes), v_lane, cv.row_bytes);
+    };
 
     Stretch cur = stretch_at(pos);
     load_queries(cur);
@@ -427,55 +496,82 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
         for (int i = 0; i < NA; ++i) acc[i] = pag_f32x4{0.f, 0.f, 0.f, 0.f};
         float m_run = -INFINITY, l_run = 0.f;
         for (int s = 0; s < cur.steps; ++s) {
-            const int here = left;
-            pag_f32x4 sc = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (kBf16) {
-                pag_f32x4 rest = sc;      // of the queries' lower parts
-#pragma unroll
-                for (int ks = 0; ks < KL; ++ks) {
-                    sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, x.k[ks]), __builtin_bit_cast(pag_bf16x8, q[0][ks]), sc, 0, 0, 0);
-#pragma unroll
-                    for (int k = QP - 1; k > 0; --k)
-                        rest = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, x.k[ks]), __builtin_bit_cast(pag_bf16x8, q[k][ks]), rest, 0, 0, 0);
-                }
-                if constexpr (QP > 1) {      // a lower part that is zero meets an infinite key: the upper parts' sum is infinite, or no number, by itself then
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sc[i] += fabsf(rest[i]) < INFINITY ? rest[i] : 0.f;
-                }
-            } else {
-                // four sums side by side: one over all d has twice the error (3 x 2 heads of 500 to 1000 rows take 9.0 us with either)
-                pag_f32x4 part[4] = {sc, sc, sc, sc};
-#pragma unroll
-                for (int ks = 0; ks < KL; ++ks)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        part[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(dword_of(x.k[ks], i)), __uint_as_float(dword_of(q[0][ks], i)), part[i], 0, 0, 0);
-                sc = (part[0] + part[1]) + (part[2] + part[3]);
-            }
-            float sv[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sv[i] = sc[i] * p.scale_log2;
-                if (cv.counts) sv[i] = x.n[i] > 0 ? sv[i] + __log2f((float)x.n[i]) : -INFINITY;
-                if (4 * g + i >= here) sv[i] = -INFINITY;
-            }
-            // rows without weight: their values may be anything, and 0 times a NaN is one
+            int here[NS];
+            float sv[4 * NS], vs[NS];      // logits of the lane's rows: 4 g + i of every 16
             int nothing = 0;
-            if (cv.counts) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) nothing |= x.n[i] > 0 ? 0 : 1 << i;
+            for (int u = 0; u < NS; ++u) {
+                here[u] = left[u];
+                float factor = p.scale_log2;
+                vs[u] = 1.f;
+                if constexpr (kCodes) {
+                    factor *= readlane(pages.ks, (NS * s + u) % kWave);
+                    vs[u] = readlane(pages.vs, (NS * s + u) % kWave);
+                }
+                pag_f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+                if constexpr (kBf16) {
+                    pag_f32x4 rest = sc;      // of the queries' lower parts
+#pragma unroll
+                    for (int ks = 0; ks < NM; ++ks) {
+                        uint4 key;
+                        if constexpr (kCodes) {
+                            const uint2 lo = widen4<T>(dword_of(x[u].k[ks / 2], 2 * (ks % 2))), hi = widen4<T>(dword_of(x[u].k[ks / 2], 2 * (ks % 2) + 1));
+                            key = make_uint4(lo.x, lo.y, hi.x, hi.y);
+                        } else {
+                            key = x[u].k[ks];
+                        }
+                        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, key), __builtin_bit_cast(pag_bf16x8, q[0][ks]), sc, 0, 0, 0);
+#pragma unroll
+                        for (int k = QP - 1; k > 0; --k)
+                            rest = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, key), __builtin_bit_cast(pag_bf16x8, q[k][ks]), rest, 0, 0, 0);
+                    }
+                    if constexpr (QP > 1) {      // a lower part that is zero meets an infinite key: the upper parts' sum is infinite, or no number, by itself then
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sc[i] += fabsf(rest[i]) < INFINITY ? rest[i] : 0.f;
+                    }
+                } else {
+                    // four sums side by side: one over all d has twice the error (3 x 2 heads of 500 to 1000 rows take 9.0 us with either)
+                    pag_f32x4 part[4] = {sc, sc, sc, sc};
+#pragma unroll
+                    for (int ks = 0; ks < KL; ++ks)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            part[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(dword_of(x[u].k[ks], i)), __uint_as_float(dword_of(q[0][ks], i)), part[i], 0, 0, 0);
+                    sc = (part[0] + part[1]) + (part[2] + part[3]);
+                }
+                const int row = WIN ? row_of(cur, s, u) + 4 * g : 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float z = sc[i] * factor;
+                    if (cv.counts) z = x[u].n[i] > 0 ? z + __log2f((float)x[u].n[i]) : -INFINITY;
+                    if (4 * g + i >= here[u]) z = -INFINITY;
+                    if constexpr (WIN) {
+                        if (!paged_visible(row + i, cur.len, p.window, p.sinks)) {
+                            z = -INFINITY;
+                            nothing |= 1 << (4 * u + i);
+                        }
+                    }
+                    sv[4 * u + i] = z;
+                }
+                // rows without weight: their values may be anything, and 0 times a NaN is one
+                if (cv.counts) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) nothing |= x[u].n[i] > 0 ? 0 : 1 << (4 * u + i);
+                }
             }
             request_keys(cur, pages, s + 1);
             float m_loc = m_run;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) m_loc = fmaxf(m_loc, sv[i]);
+            for (int i = 0; i < 4 * NS; ++i) m_loc = fmaxf(m_loc, sv[i]);
             const float m_new = rows_allreduce_max(m_loc);
             const float m_safe = (m_new == -INFINITY) ? 0.f : m_new;
             const float alpha = pag_exp2(m_run - m_safe);
-            float pi[4];
+            float pi[4 * NS], sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pi[i] = pag_exp2(sv[i] - m_safe);
-            l_run = fmaf(l_run, alpha, (pi[0] + pi[1]) + (pi[2] + pi[3]));      // of the lane's own rows; added up behind the loop
+            for (int i = 0; i < 4 * NS; ++i) pi[i] = pag_exp2(sv[i] - m_safe);
+#pragma unroll
+            for (int u = 0; u < NS; ++u) sum = u == 0 ? (pi[0] + pi[1]) + (pi[2] + pi[3]) : sum + ((pi[4 * u] + pi[4 * u + 1]) + (pi[4 * u + 2] + pi[4 * u + 3]));
+            l_run = fmaf(l_run, alpha, sum);      // of the lane's own rows; added up behind the loop
             m_run = m_new;
             if (ballot64(alpha != 1.0f) != 0ull) {
                 float al[4];      // the factor of head 4 g + i is in the lanes (.., 4 g + i)
@@ -488,18 +584,44 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
             }
             if (ballot64(nothing != 0) != 0ull) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int u = 0; u < NS; ++u)
 #pragma unroll
-                    for (int k = 0; k < VW; ++k) x.v[i][k] = nothing >> i & 1 ? 0u : x.v[i][k];
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int k = 0; k < VW; ++k) x[u].v[i][k] = nothing >> (4 * u + i) & 1 ? 0u : x[u].v[i][k];
             }
-            if constexpr (kBf16) {
+            if constexpr (kCodes) {
+                // both 16 rows in one product: place 8 g + j of its inner dimension is row 4 g + j of the first 16, or 4 g + j - 4 of the second.  The values' scale
+                // goes to the probabilities, before they are split.
+                uint32_t part[4][PP];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) split_bf16<PP>(pi[2 * i] * vs[i / 2], pi[2 * i + 1] * vs[i / 2], part[i]);
+#pragma unroll
+                for (int w = 0; w < VW; ++w) {
+                    uint32_t col[NS][4];
+#pragma unroll
+                    for (int u = 0; u < NS; ++u) {
+                        const uint32_t r[4] = {x[u].v[0][w], x[u].v[1][w], x[u].v[2][w], x[u].v[3][w]};
+                        transpose4(r, col[u]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint2 lo = widen4<T>(col[0][j]), hi = widen4<T>(col[NS - 1][j]);
+                        const pag_bf16x8 bb = __builtin_bit_cast(pag_bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+#pragma unroll
+                        for (int t = PP - 1; t >= 0; --t)
+                            acc[4 * w + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pag_bf16x8, make_uint4(part[0][t], part[1][t], part[2][t], part[3][t])), bb,
+                                                                                     acc[4 * w + j], 0, 0, 0);
+                    }
+                }
+            } else if constexpr (kBf16) {
                 uint32_t p01[PP], p23[PP];
                 split_bf16<PP>(pi[0], pi[1], p01);
                 split_bf16<PP>(pi[2], pi[3], p23);
 #pragma unroll
                 for (int k = 0; k < NA; ++k) {
-                    const uint32_t lo = (k & 1) ? pack_hi(x.v[0][k / 2], x.v[1][k / 2]) : pack_lo(x.v[0][k / 2], x.v[1][k / 2]);
-                    const uint32_t hi = (k & 1) ? pack_hi(x.v[2][k / 2], x.v[3][k / 2]) : pack_lo(x.v[2][k / 2], x.v[3][k / 2]);
+                    const uint32_t lo = (k & 1) ? pack_hi(x[0].v[0][k / 2], x[0].v[1][k / 2]) : pack_lo(x[0].v[0][k / 2], x[0].v[1][k / 2]);
+                    const uint32_t hi = (k & 1) ? pack_hi(x[0].v[2][k / 2], x[0].v[3][k / 2]) : pack_lo(x[0].v[2][k / 2], x[0].v[3][k / 2]);
                     const pag_short4 bb = __builtin_bit_cast(pag_short4, make_uint2(lo, hi));
 #pragma unroll
                     for (int t = PP - 1; t >= 0; --t)
@@ -509,14 +631,14 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
 #pragma unroll
                 for (int k = 0; k < NA; ++k)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(pi[i], __uint_as_float(x.v[i][k]), acc[k], 0, 0, 0);
+                    for (int i = 0; i < 4; ++i) acc[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(pi[i], __uint_as_float(x[0].v[i][k]), acc[k], 0, 0, 0);
             }
             request_values();
         }
         // ---- the next head of the workgroup's stretch, if any: its first rows are on their way while the results of this one are stored
         const bool more = cur.end < stop;
         Stretch nxt = cur;
-        Pages nxt_pages = {0, 0, 0};
+        Pages nxt_pages = {0, 0, 0, 0.f, 0.f};
         if (more) {
             a += units;
             ++h;
@@ -617,12 +739,16 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
 size_t paged_state_bytes() { return align_up((size_t)4 * kMaxWgs * sizeof(int), 256); }
 size_t paged_decode_bytes(int G, int d) { return align_up((size_t)2 * kMaxWgs * G * (d + kPagPad) * sizeof(float), 256); }
 
-template <typename T, int D, int QP> static hipError_t launch_k(const PagDecParams &p, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_decode_kernel<T, D, QP>), dim3((unsigned)p.wgs), dim3(kPagThreads), 0, stream, p);
+template <typename T, int D, int QP, bool WIN> static hipError_t launch_k(const PagDecParams &p, hipStream_t stream) {
+    hipLaunchKernelGGL((paged_decode_kernel<T, D, QP, WIN>), dim3((unsigned)p.wgs), dim3(kPagThreads), 0, stream, p);
     return hipGetLastError();
 }
-template <typename T, int QP> static hipError_t launch_d(const PagDecParams &p, hipStream_t stream) {
-    return p.c.d == 128 ? launch_k<T, 128, QP>(p, stream) : launch_k<T, 64, QP>(p, stream);
+template <typename T, int QP, bool WIN> static hipError_t launch_d(const PagDecParams &p, hipStream_t stream) {
+    return p.c.d == 128 ? launch_k<T, 128, QP, WIN>(p, stream) : launch_k<T, 64, QP, WIN>(p, stream);
+}
+template <typename T, bool WIN> static hipError_t launch_q(const PagDecParams &p, hipStream_t stream) {
+    if constexpr (sizeof(T) > 2) return launch_d<T, 1, WIN>(p, stream);
+    else return p.q_is_bf16 ? launch_d<T, 1, WIN>(p, stream) : launch_d<T, 3, WIN>(p, stream);
 }
 
 hipError_t launch_paged_decode(const PagedDecodeArgs &a, hipStream_t stream) {
@@ -635,14 +761,20 @@ hipError_t launch_paged_decode(const PagedDecodeArgs &a, hipStream_t stream) {
     p.O = a.O; p.o_is_bf16 = a.o_dtype == DType::BF16; p.lse = a.lse;
     p.counter = reinterpret_cast<int *>(a.ws);
     p.part = reinterpret_cast<float *>(reinterpret_cast<char *>(a.ws) + paged_state_bytes());
-    // never more workgroups than the tables (the selections) have units for, nor than a head's partial results are worth
-    const int64_t heads = (int64_t)a.c.B * a.c.H;
-    const int64_t most = ((int64_t)(a.sel ? a.keep : a.c.P) * a.c.R + kStep - 1) / kStep * heads;
+    p.window = a.window; p.sinks = a.sinks;
+    p.k_scale = a.k_scale; p.v_scale = a.v_scale; p.log2_block = a.log2_block;
+    // never more workgroups than the tables (the selections, the windows) have units for, nor than a head's partial results are worth
+    const int64_t heads = (int64_t)a.c.B * a.c.H, unit = a.code ? kStep<e4m3_t> : kStep<float>;
+    int64_t rows = (int64_t)(a.sel ? a.keep : a.c.P) * a.c.R;
+    if (a.window > 0 && (int64_t)a.window + a.sinks + 48 < rows) rows = (int64_t)a.window + a.sinks + 48;      // (paged_gap: the ends of both stretches are rounded to 16)
+    const int64_t most = (rows + unit - 1) / unit * heads;
     int64_t wgs = kMaxWgs < heads * kMaxHeadWgs ? kMaxWgs : heads * kMaxHeadWgs;
     if (wgs > most) wgs = most;
     p.wgs = (int)wgs;
-    if (a.c.dtype == DType::BF16) return p.q_is_bf16 ? launch_d<bf16_t, 1>(p, stream) : launch_d<bf16_t, 3>(p, stream);
-    return launch_d<float, 1>(p, stream);
+    if (a.code == 1) return launch_q<e4m3_t, true>(p, stream);
+    if (a.code == 2) return launch_q<i8_t, true>(p, stream);
+    if (a.window > 0) return a.c.dtype == DType::BF16 ? launch_q<bf16_t, true>(p, stream) : launch_q<float, true>(p, stream);
+    return a.c.dtype == DType::BF16 ? launch_q<bf16_t, false>(p, stream) : launch_q<float, false>(p, stream);
 }
 
 }  // namespace sc

@@ -77,4 +77,26 @@ constexpr PagedStep paged_step(int row, int log2_R, int len, int P, int num_page
     return {page, left < 16 ? (int)left : 16, false};
 }
 
+// ---- a window of `window` rows (0: none) and the first `sinks` rows
+constexpr bool paged_visible(int row, int len, int window, int sinks) { return row < len && (window <= 0 || row >= len - window || row < sinks); }
+// Rows that no step visits: `rows` of them from row `at` on, both multiples of 16 (a step of 16 rows that begins at a multiple of 16 stays in one page)
+struct PagedGap {
+    int at, rows;
+};
+constexpr PagedGap paged_gap(int len, int window, int sinks) {
+    if (window <= 0 || len <= window) return {0, 0};
+    const int64_t at = ((int64_t)(sinks < len ? sinks : len) + 15) / 16 * 16, next = (int64_t)(len - window) / 16 * 16;
+    return at < next ? PagedGap{(int)at, (int)(next - at)} : PagedGap{0, 0};
+}
+// `len`, or 0 if none of the 16 rows from `row` (a multiple of 16) on is visible: their page is not looked up then
+constexpr int paged_window_len(int row, int len, int window, int sinks) {
+    return window <= 0 || (int64_t)row + 16 > (int64_t)len - window || row < sinks ? len : 0;
+}
+
+// ---- sc_paged_reserve: does place `place` of a table hold rows below base + fresh that a token from `base` on sees, or rows that arrive
+constexpr bool paged_wants(int place, int log2_R, int base, int fresh, int window, int sinks) {
+    const int64_t row = (int64_t)place << log2_R, end = row + (1 << log2_R);
+    return row < (int64_t)base + fresh && (window <= 0 || row < sinks || end > (int64_t)base + 1 - window);
+}
+
 }  // namespace sc
