@@ -565,6 +565,37 @@ sc_status sc_paged_reserve(int32_t *table, int sequences, int table_len, int num
                            void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * sc_prompt_attn — attention of a prompt's rows, or of a chunk of them behind a context, causal:
+ *     O[b,hq,i] = softmax_j( Q[b,hq,i] . K[b,h,j] * scale ) V[b,h,j],   h = hq / (Hq / Hkv),   pos = kv_lens[b] - q_lens[b] + i,
+ *     over j <= pos with  window = 0  or  j > pos - window  or  j < sinks.
+ * (The queries are the last q_lens tokens of kv_lens.)  bf16: products of bf16 in fp32, probabilities rounded to bf16, sums and statistics in fp32; fp32: everything in fp32.
+ *   Q, O            device [B, Hq, N, d] of dtype;  K, V  device [B, Hkv, M, d] of dtype; strides (b, h, n) of each in ELEMENTS, multiples of 16
+ *                   bytes, the last dimension contiguous, 16-byte aligned; the rows of O do not overlap and share nothing with the inputs
+ *   q_lens, kv_lens device i32 [B] or NULL (= N, = M), taken as 0 .. N and 0 .. M.  Rows of Q, K and V behind them are not looked at (they may hold anything), rows of O (and of
+ *                   lse) behind them are left as they were
+ *   window, sinks   as for sc_paged_window_attn
+ *   scale           0 selects 1/sqrt(d)
+ *   lse             device f32 [B, Hq, N], contiguous, or NULL.  A query that sees no key (pos < 0) gives O = 0 and lse = -inf
+ *   ws              sc_prompt_attn_workspace_bytes bytes; needs no initialisation
+ * A row that a query does not see may hold anything.  An element of V that is not finite, of a row that the query sees, makes that element of O infinite or NaN.
+ * Host errors: NULL or misaligned pointers, sizes <= 0, strides that are negative or no multiples, window or sinks < 0 (SC_ERR_INVALID_ARG); d not in {64, 128}, bad dtype, Hq no multiple of Hkv,
+ * B or Hq > 65535, N * Hq / Hkv > 2^30, rows of K or V 32 MiB apart (SC_ERR_UNSUPPORTED).
+ */
+typedef struct {
+    const void *Q, *K, *V;
+    void *O;
+    float *lse;
+    int64_t q_stride_b, q_stride_h, q_stride_n, k_stride_b, k_stride_h, k_stride_n;
+    int64_t v_stride_b, v_stride_h, v_stride_n, o_stride_b, o_stride_h, o_stride_n;
+    const int32_t *q_lens, *kv_lens;
+    int32_t dtype;             /* sc_dtype */
+    int32_t B, Hq, Hkv, N, M, d, window, sinks;
+    float scale;
+} sc_prompt;
+size_t sc_prompt_attn_workspace_bytes(int B, int Hq, int Hkv, int N, int M, int d);
+sc_status sc_prompt_attn(const sc_prompt *prompt, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
  * sc_stream_read_probe — a measuring aid for benchmarks, not a step of the method: reads the first
  * `bytes` bytes (rounded down to a multiple of 16) of a device buffer once, 16 bytes per lane, fully
  * coalesced, eight non-temporal loads in flight per lane, one workgroup of twelve wavefronts per CU on a

@@ -54,6 +54,12 @@ class _PagedRowsStruct(ctypes.Structure):       # sc_paged_rows
                [("q_dtype", ctypes.c_int32)]
 
 
+class _PromptStruct(ctypes.Structure):          # sc_prompt
+    _fields_ = [(x, ctypes.c_void_p) for x in ("Q", "K", "V", "O", "lse")] + \
+               [(x + "_stride_" + y, ctypes.c_int64) for x in "qkvo" for y in "bhn"] + [(x, ctypes.c_void_p) for x in ("q_lens", "kv_lens")] + \
+               [(x, ctypes.c_int32) for x in ("dtype", "B", "Hq", "Hkv", "N", "M", "d", "window", "sinks")] + [("scale", ctypes.c_float)]
+
+
 def load_library() -> ctypes.CDLL:
     """Load libsemanticache.so built in-tree (python -m paper_2603_14303_amd.build)."""
     global _lib, _native
@@ -146,6 +152,10 @@ def load_library() -> ctypes.CDLL:
     lib.sc_paged_reserve_workspace_bytes.argtypes = [i32, i32]
     lib.sc_paged_reserve.restype = i32
     lib.sc_paged_reserve.argtypes = [vp, i32, i32, i32, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.sc_prompt_attn_workspace_bytes.restype = sz
+    lib.sc_prompt_attn_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+    lib.sc_prompt_attn.restype = i32
+    lib.sc_prompt_attn.argtypes = [c.POINTER(_PromptStruct), vp, sz, vp]
     if torch is not None:
         _native = _load_native()
     _lib = lib
@@ -178,6 +188,7 @@ EXPORTED = [
     "sc_gsc_merge_global_workspace_bytes", "sc_gsc_merge_global",
     "sc_paged_append", "sc_paged_workspace_bytes", "sc_paged_init_workspace", "sc_paged_decode_attn", "sc_paged_select",
     "sc_paged_window_attn", "sc_paged8_append", "sc_paged8_decode_attn", "sc_paged_reserve_workspace_bytes", "sc_paged_reserve",
+    "sc_prompt_attn_workspace_bytes", "sc_prompt_attn",
 ]
 
 
@@ -852,6 +863,54 @@ def sc_paged_reserve(table, page_rows: int, base_lens, lens, free_pages, num_fre
                               _ptr(free_pages), _ptr(num_free), _ptr(lens), _ptr(slots), workspace.ptr, workspace.nbytes, _stream())
     _check(st, "sc_paged_reserve")
     return lens, slots
+
+
+# ------------------------------------------------------------------------------------------------ prompts
+def prompt_attn_workspace(B: int, Hq: int, Hkv: int, N: int, M: int, d: int, device) -> Workspace:
+    """Workspace of sc_prompt_attn for N queries and M keys a sequence at most."""
+    _c_ints(B=B, Hq=Hq, Hkv=Hkv, N=N, M=M, d=d)
+    nbytes = load_library().sc_prompt_attn_workspace_bytes(B, Hq, Hkv, N, M, d)
+    if nbytes == 0:
+        raise SemantiCacheError("no workspace for B=%d Hq=%d Hkv=%d N=%d M=%d d=%d" % (B, Hq, Hkv, N, M, d))
+    return Workspace(nbytes, device)
+
+
+def sc_prompt_attn(Q, K, V, q_lens=None, kv_lens=None, window: int = 0, sinks: int = 0, scale: float = 0.0, O=None, lse=None, want_lse: bool = False,
+                   workspace: Optional[Workspace] = None):
+    """Causal attention of Q [B, Hq, N, d] over K, V [B, Hkv, M, d] -> (O [B, Hq, N, d], lse [B, Hq, N] or None).
+
+    The queries are the last q_lens [B] (None: N) of kv_lens [B] (None: M) tokens; each sees itself and the tokens before it, with a window only the newest
+    `window` of them and the first `sinks` ones.  Rows behind the lengths are left as they were (an O that is made here holds anything there).
+    """
+    lib = load_library()
+    _require_cuda(Q, K, V, q_lens, kv_lens, O, lse)
+    for t in (Q, K):
+        _c_ints(**{"dimension %d" % i: n for i, n in enumerate(t.shape)})
+    _c_ints(window=window, sinks=sinks)
+    if Q.dim() != 4 or K.dim() != 4 or K.shape != V.shape or K.shape[0] != Q.shape[0] or K.shape[3] != Q.shape[3] or K.dtype != Q.dtype or V.dtype != Q.dtype:
+        raise SemantiCacheError("Q must be [B, Hq, N, d], K and V [B, Hkv, M, d] of its dtype")
+    B, Hq, N, d = Q.shape
+    Hkv, M = K.shape[1:3]
+    if not (q_lens is None or _is_i32(q_lens, (B,))) or not (kv_lens is None or _is_i32(kv_lens, (B,))):
+        raise SemantiCacheError("q_lens and kv_lens must be int32 [B], contiguous")
+    if O is None:      # a token's heads side by side, as the projection behind takes them
+        O = torch.empty((B, N, Hq, d), dtype=Q.dtype, device=Q.device).permute(0, 2, 1, 3)
+    if lse is None and want_lse:
+        lse = torch.empty((B, Hq, N), dtype=torch.float32, device=Q.device)
+    if O.shape != Q.shape or O.dtype != Q.dtype or (lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, N) or not lse.is_contiguous())):
+        raise SemantiCacheError("O must be [B, Hq, N, d] of Q's dtype and lse float32 [B, Hq, N], contiguous")
+    for t in (Q, K, V, O):
+        if t.stride(3) != 1:
+            raise SemantiCacheError("rows must be contiguous")
+    if workspace is None:
+        workspace = prompt_attn_workspace(B, Hq, Hkv, N, M, d, Q.device)
+    x = _PromptStruct(Q=_ptr(Q), K=_ptr(K), V=_ptr(V), O=_ptr(O), lse=_ptr(lse), q_lens=_ptr(q_lens), kv_lens=_ptr(kv_lens), dtype=_dtype_code(Q),
+                      B=B, Hq=Hq, Hkv=Hkv, N=N, M=M, d=d, window=int(window), sinks=int(sinks), scale=float(scale))
+    for name, t in (("q", Q), ("k", K), ("v", V), ("o", O)):
+        for axis, s in zip("bhn", t.stride()):
+            setattr(x, "%s_stride_%s" % (name, axis), s)
+    _check(lib.sc_prompt_attn(ctypes.byref(x), workspace.ptr, workspace.nbytes, _stream()), "sc_prompt_attn")
+    return O, lse
 
 
 def stream_read_probe(buf, sink) -> None:

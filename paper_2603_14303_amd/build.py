@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libsemanticache.so")
 NATIVE = os.path.join(HERE, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))      # (another Python looks for another name)
 NATIVE_FOR = os.path.join(OBJ, "native_torch_version")                               # the torch that it was built against
 SOURCES = ["sc_api.hip", "sc_segment.hip", "sc_gsc_merge.hip", "sc_gsc_fast.hip", "sc_gsc_global.hip", "sc_decode.hip", "sc_multi.hip", "sc_budget.hip", "sc_probe.hip",
-           "sc_paged_append.hip", "sc_paged_decode.hip", "sc_paged_select.hip", "sc_paged8_append.hip", "sc_paged_reserve.hip"]
+           "sc_paged_append.hip", "sc_paged_decode.hip", "sc_paged_select.hip", "sc_paged8_append.hip", "sc_paged_reserve.hip", "sc_prompt.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

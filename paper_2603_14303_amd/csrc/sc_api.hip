@@ -638,6 +638,42 @@ sc_status sc_paged_select(const sc_paged_cache *cache, const void *Q, sc_dtype q
     return runtime_status(launch_paged_select(a, static_cast<hipStream_t>(stream)));
 }
 
+size_t sc_prompt_attn_workspace_bytes(int B, int Hq, int Hkv, int N, int M, int d) {
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || N <= 0 || M <= 0 || Hq % Hkv || (d != 64 && d != 128)) return 0;
+    return prompt_workspace_bytes(B, Hq, Hkv, N, M, d);
+}
+
+sc_status sc_prompt_attn(const sc_prompt *x, void *ws, size_t ws_bytes, void *stream) {
+    if (!x || !x->Q || !x->K || !x->V || !x->O) return SC_ERR_INVALID_ARG;
+    if (x->B <= 0 || x->Hq <= 0 || x->Hkv <= 0 || x->N <= 0 || x->M <= 0 || x->window < 0 || x->sinks < 0 || x->scale != x->scale) return SC_ERR_INVALID_ARG;
+    if (!dtype_ok(x->dtype) || (x->d != 64 && x->d != 128) || x->Hq % x->Hkv) return SC_ERR_UNSUPPORTED;
+    if (x->B > 65535 || x->Hq > 65535 || (int64_t)x->N * (x->Hq / x->Hkv) > (1 << 30)) return SC_ERR_UNSUPPORTED;      // rows of a KV head are counted in 32 bits
+    if (!aligned4(x->lse) || !aligned4(x->q_lens) || !aligned4(x->kv_lens)) return SC_ERR_INVALID_ARG;
+    const int64_t es = (int64_t)elem_size(x->dtype);
+    if (!rows_ok(x->Q, x->B, x->Hq, x->N, x->q_stride_b, x->q_stride_h, x->q_stride_n, x->d, es, false)) return SC_ERR_INVALID_ARG;
+    if (!rows_ok(x->K, x->B, x->Hkv, x->M, x->k_stride_b, x->k_stride_h, x->k_stride_n, x->d, es, false)) return SC_ERR_INVALID_ARG;
+    if (!rows_ok(x->V, x->B, x->Hkv, x->M, x->v_stride_b, x->v_stride_h, x->v_stride_n, x->d, es, false)) return SC_ERR_INVALID_ARG;
+    if (!rows_ok(x->O, x->B, x->Hq, x->N, x->o_stride_b, x->o_stride_h, x->o_stride_n, x->d, es, true)) return SC_ERR_INVALID_ARG;
+    const int64_t size[3] = {x->B, x->Hq, x->N}, stride[3] = {x->o_stride_b, x->o_stride_h, x->o_stride_n};
+    if (!rows_apart(size, stride, x->d)) return SC_ERR_INVALID_ARG;
+    if (x->M > 1 && (x->k_stride_n * es > INT32_MAX / 64 || x->v_stride_n * es > INT32_MAX / 64)) return SC_ERR_UNSUPPORTED;      // offsets inside a tile of keys are 32-bit
+    if (!prompt_fits(x->B, x->Hq, x->Hkv, x->N, x->M, x->d, x->dtype == SC_BF16)) return SC_ERR_UNSUPPORTED;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < prompt_workspace_bytes(x->B, x->Hq, x->Hkv, x->N, x->M, x->d)) return SC_ERR_WORKSPACE;
+    PromptArgs a;
+    a.Q = static_cast<const char *>(x->Q); a.K = static_cast<const char *>(x->K); a.V = static_cast<const char *>(x->V);
+    a.O = static_cast<char *>(x->O); a.lse = x->lse;
+    a.q_b = x->q_stride_b * es; a.q_h = x->q_stride_h * es; a.q_n = x->q_stride_n * es;
+    a.k_b = x->k_stride_b * es; a.k_h = x->k_stride_h * es; a.k_n = x->M > 1 ? x->k_stride_n * es : 0;
+    a.v_b = x->v_stride_b * es; a.v_h = x->v_stride_h * es; a.v_n = x->M > 1 ? x->v_stride_n * es : 0;
+    a.o_b = x->o_stride_b * es; a.o_h = x->o_stride_h * es; a.o_n = x->o_stride_n * es;
+    a.q_lens = x->q_lens; a.kv_lens = x->kv_lens;
+    a.dtype = static_cast<DType>(x->dtype);
+    a.B = x->B; a.Hq = x->Hq; a.Hkv = x->Hkv; a.N = x->N; a.M = x->M; a.d = x->d; a.window = x->window; a.sinks = x->sinks;
+    a.scale = (x->scale == 0.f) ? 1.0f / sqrtf((float)x->d) : x->scale;
+    a.ws = ws;
+    return runtime_status(launch_prompt(a, static_cast<hipStream_t>(stream)));
+}
+
 size_t sc_paged_reserve_workspace_bytes(int sequences, int table_len) {
     if (sequences <= 0 || table_len <= 0 || sequences > (1 << 20) || (int64_t)sequences * table_len > (1 << 28)) return 0;
     return paged_reserve_bytes(sequences, table_len);

@@ -127,6 +127,22 @@ hipError_t launch_multi(const MultiArgs &a, hipStream_t stream);
 size_t multi_fast_workspace_bytes(int B, int Hq, int Hkv, int nq, int cap);
 hipError_t launch_multi_fast(const MultiArgs &a, hipStream_t stream);
 
+// ---- sc_prompt_attn
+struct PromptArgs {
+    const char *Q, *K, *V;    // [B, heads, N (M), d]
+    char *O;
+    float *lse;               // [B, Hq, N] or NULL
+    int64_t q_b, q_h, q_n, k_b, k_h, k_n, v_b, v_h, v_n, o_b, o_h, o_n;   // bytes
+    const int32_t *q_lens, *kv_lens;
+    DType dtype;
+    int B, Hq, Hkv, N, M, d, window, sinks;
+    float scale;
+    void *ws;
+};
+size_t prompt_workspace_bytes(int B, int Hq, int Hkv, int N, int M, int d);
+bool prompt_fits(int B, int Hq, int Hkv, int N, int M, int d, bool bf16);   // the grid
+hipError_t launch_prompt(const PromptArgs &a, hipStream_t stream);
+
 // ---- measuring aid: streaming read of a buffer
 hipError_t launch_stream_read_probe(const void *src, size_t bytes, void *sink, hipStream_t stream);
 
