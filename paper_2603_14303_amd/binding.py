@@ -588,6 +588,11 @@ class PagedCache:
         return (self.B,), (self.B, self.Hkv)
 
 
+def _keeps_numbers(cache) -> None:
+    if isinstance(cache, PagedCache8):      # (its description has another layout)
+        raise SemantiCacheError("a cache of 8-bit codes has calls of its own: sc_paged8_append, sc_paged8_decode_attn")
+
+
 def _paged_rows(cache, dtype, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved):
     """The rows of a call that appends, checked -> (their sc_paged_rows, Q_out)."""
     _require_cuda(K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions)
@@ -636,6 +641,7 @@ def sc_paged_append(cache: PagedCache, K, V, base_lens, lens, new_lens=None, cou
     positions [B] (None: base_lens) + n.  counts [B, Hkv, N]: sizes of the rows, for a cache with counts.
     """
     lib = load_library()
+    _keeps_numbers(cache)
     if _native is not None and K.is_cuda and (Q is None) == (Q_out is None):
         st = _native.paged_append(cache.ptr, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, _stream())
         if st >= 0:
@@ -687,6 +693,7 @@ def sc_paged_decode_attn(cache: PagedCache, Q, lens, scale: float = 0.0, O=None,
     With sel [B, Hkv, keep] and sel_lens [B, Hkv] (sc_paged_select) only the rows of those pages attend.
     """
     lib = load_library()
+    _keeps_numbers(cache)
     if _native is not None and Q.is_cuda and O is not None and workspace is not None and not (want_lse and lse is None):
         st = _native.paged_decode(cache.ptr, Q, lens, scale, O, lse, sel, sel_lens, workspace.ptr, workspace.nbytes, _stream())
         if st >= 0:
@@ -712,6 +719,7 @@ def sc_paged_select(cache: PagedCache, Q, lens, keep: int, first: int = 1, recen
     """The `keep` pages of every (sequence, KV head) with the largest bounds on the logits of Q [B, Hq, d], its first `first` and last `recent`
     ones in any case -> (sel [B, Hkv, keep] ascending, -1 behind the last, sel_lens [B, Hkv])."""
     lib = load_library()
+    _keeps_numbers(cache)
     if _native is not None and Q.is_cuda and sel is not None and sel_lens is not None and workspace is not None:
         st = _native.paged_select(cache.ptr, Q, lens, keep, first, recent, sel, sel_lens, workspace.ptr, workspace.nbytes, _stream())
         if st >= 0:
@@ -736,13 +744,18 @@ def sc_paged_select(cache: PagedCache, Q, lens, keep: int, first: int = 1, recen
 def sc_paged_window_attn(cache: PagedCache, Q, lens, window: int, sinks: int = 0, scale: float = 0.0, O=None, lse=None, want_lse: bool = False,
                          workspace: Optional[Workspace] = None):
     """sc_paged_decode_attn where only the newest `window` rows (0: all) and the first `sinks` rows of a sequence attend -> (O, lse or None)."""
-    return _windowed("sc_paged_window_attn", PagedCache, cache, Q, lens, window, sinks, scale, O, lse, want_lse, workspace)
+    return _windowed("sc_paged_window_attn", "paged_window", PagedCache, cache, Q, lens, window, sinks, scale, O, lse, want_lse, workspace)
 
 
-def _windowed(name, kind, cache, Q, lens, window, sinks, scale, O, lse, want_lse, workspace):
+def _windowed(name, native, kind, cache, Q, lens, window, sinks, scale, O, lse, want_lse, workspace):
     lib = load_library()
     if not isinstance(cache, kind):
         raise SemantiCacheError("%s takes a %s" % (name, kind.__name__))
+    if _native is not None and Q.is_cuda and O is not None and workspace is not None and not (want_lse and lse is None):
+        st = getattr(_native, native)(cache.ptr, Q, lens, window, sinks, scale, O, lse, workspace.ptr, workspace.nbytes, _stream())
+        if st >= 0:
+            _check(st, name)
+            return O, lse
     _c_ints(window=window, sinks=sinks)
     workspace = _paged_query(cache, Q, lens, workspace)
     O, lse = _paged_outputs(Q, O, lse, want_lse)
@@ -803,6 +816,11 @@ def sc_paged8_append(cache: PagedCache8, K, V, base_lens, lens, new_lens=None, c
     lib = load_library()
     if not isinstance(cache, PagedCache8):
         raise SemantiCacheError("sc_paged8_append takes a PagedCache8")
+    if _native is not None and K.is_cuda and (Q is None) == (Q_out is None):
+        st = _native.paged8_append(cache.ptr, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, _stream())
+        if st >= 0:
+            _check(st, "sc_paged8_append")
+            return lens, Q_out
     r, Q_out = _paged_rows(cache, None, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved)
     _check(lib.sc_paged8_append(ctypes.byref(cache.struct), ctypes.byref(r), _dtype_code(K), _stream()), "sc_paged8_append")
     return lens, Q_out
@@ -812,7 +830,7 @@ def sc_paged8_decode_attn(cache: PagedCache8, Q, lens, window: int = 0, sinks: i
                           workspace: Optional[Workspace] = None):
     """Q [B, Hq, d] over the first lens [B] (or [B, Hkv]) rows of a cache of 8-bit codes, or over the newest `window` and the first `sinks` of them
     -> (O [B, Hq, d], lse [B, Hq] or None).  Workspace: paged_workspace."""
-    return _windowed("sc_paged8_decode_attn", PagedCache8, cache, Q, lens, window, sinks, scale, O, lse, want_lse, workspace)
+    return _windowed("sc_paged8_decode_attn", "paged8_decode", PagedCache8, cache, Q, lens, window, sinks, scale, O, lse, want_lse, workspace)
 
 
 # ------------------------------------------------------------------------------------------------ pages handed out on the GPU
@@ -834,18 +852,19 @@ def sc_paged_reserve(table, page_rows: int, base_lens, lens, free_pages, num_fre
 
     table int32 [..., P] (-1: no page) and the stack free_pages int32 [pages] with num_free int32 [1] are changed; base_lens, lens and new_lens (None: N
     everywhere) are int32 [...] like the table's rows.  slots int32 [..., N]: page * page_rows + row of every new row, -1 for none.  N is the
-    slots' last dimension, else the argument (default 1; with new_lens and no slots it says nothing: any number goes).  lens: base_lens + new_lens, or -1.
+    slots' last dimension, or the argument (without both 1, or any number that new_lens say).  lens: base_lens + new_lens, or -1.
     """
     lib = load_library()
+    if N is None:
+        N = (slots.shape[-1] if slots.dim() else 0) if slots is not None else 1 if new_lens is None or want_slots else 2**31 - 1
+    if _native is not None and table.is_cuda and workspace is not None and (slots is not None or not want_slots):
+        st = _native.paged_reserve(table, page_rows, base_lens, lens, free_pages, num_free, new_lens, N, window, sinks, slots, workspace.ptr, workspace.nbytes, _stream())
+        if st >= 0:
+            _check(st, "sc_paged_reserve")
+            return lens, slots
     if table.dim() < 2 or table.dtype != torch.int32 or not table.is_contiguous():
         raise SemantiCacheError("table must be int32 [..., P], contiguous")
     rows = tuple(table.shape[:-1])
-    if slots is not None:
-        if slots.dim() != table.dim() or (N is not None and N != slots.shape[-1]):
-            raise SemantiCacheError("slots must be int32 [..., N], contiguous")
-        N = slots.shape[-1]
-    elif N is None:
-        N = 1 if new_lens is None or want_slots else 2**31 - 1
     _c_ints(page_rows=page_rows, N=N, window=window, sinks=sinks, **{"dimension %d" % i: n for i, n in enumerate(table.shape)})
     if not _is_i32(base_lens, rows) or not _is_i32(lens, rows) or not (new_lens is None or _is_i32(new_lens, rows)):
         raise SemantiCacheError("base_lens, lens and new_lens must be int32 like the table's rows, contiguous")
@@ -883,6 +902,11 @@ def sc_prompt_attn(Q, K, V, q_lens=None, kv_lens=None, window: int = 0, sinks: i
     `window` of them and the first `sinks` ones.  Rows behind the lengths are left as they were (an O that is made here holds anything there).
     """
     lib = load_library()
+    if _native is not None and Q.is_cuda and O is not None and workspace is not None and not (want_lse and lse is None):
+        st = _native.prompt(Q, K, V, q_lens, kv_lens, window, sinks, scale, O, lse, workspace.ptr, workspace.nbytes, _stream())
+        if st >= 0:
+            _check(st, "sc_prompt_attn")
+            return O, lse
     _require_cuda(Q, K, V, q_lens, kv_lens, O, lse)
     for t in (Q, K):
         _c_ints(**{"dimension %d" % i: n for i, n in enumerate(t.shape)})

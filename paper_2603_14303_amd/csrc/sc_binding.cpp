@@ -9,6 +9,8 @@
 #include <ATen/core/Tensor.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <type_traits>
+
 #include "../../include/semanticache.h"
 
 namespace {
@@ -184,26 +186,32 @@ PyObject *multi(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // ---- a cache held in pages: the first argument is the address of its sc_paged_cache, which the wrapper keeps
 inline bool is_i32(const at::Tensor *t) { return t->scalar_type() == at::kInt && t->is_contiguous(); }
 // lengths [B] or [B, Hkv]
-inline bool lengths(const at::Tensor *t, const sc_paged_cache *c, bool &per_head) {
+template <typename C> inline bool lengths(const at::Tensor *t, const C *c, bool &per_head) {
     if (!is_i32(t) || t->dim() < 1 || t->dim() > 2 || t->size(0) != c->B) return false;
     per_head = t->dim() == 2;
     return !per_head || t->size(1) == c->Hkv;
 }
 inline bool is_shape(const at::Tensor *t, int64_t a, int64_t b, int64_t c) { return t->dim() == 3 && t->size(0) == a && t->size(1) == b && t->size(2) == c; }
 
+inline int dtype_of(const sc_paged_cache *c) { return c->dtype; }
+inline int dtype_of(const sc_paged8_cache *) { return -1; }
+inline sc_status append_to(const sc_paged_cache *c, const sc_paged_rows *r, int, void *stream) { return sc_paged_append(c, r, stream); }
+inline sc_status append_to(const sc_paged8_cache *c, const sc_paged_rows *r, int code, void *stream) { return sc_paged8_append(c, r, (sc_dtype)code, stream); }
+
 // (cache, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, stream)
-PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+template <typename C> PyObject *append(PyObject *const *a, Py_ssize_t n) {
+    constexpr bool codes = std::is_same<C, sc_paged8_cache>::value;
     return guarded([&]() {
         const at::Tensor *K, *V, *base, *lens, *fresh, *counts, *Q, *Qo, *angles, *positions;
         if (n != 13 || !take_some(a[1], K) || !take_some(a[2], V) || !take_some(a[3], base) || !take_some(a[4], lens) || !take(a[5], fresh) || !take(a[6], counts)) return kNotTaken;
         if (!take(a[7], Q) || !take(a[8], Qo) || !take(a[9], angles) || !take(a[10], positions)) return kNotTaken;
-        const auto *c = static_cast<const sc_paged_cache *>(pointer(a[0]));
+        const auto *c = static_cast<const C *>(pointer(a[0]));
         const int turned = PyObject_IsTrue(a[11]);
         void *stream = pointer(a[12]);
         if (PyErr_Occurred() || !c) return kNotTaken;
         bool per_head, same;
         if (K->dim() != 4 || K->sizes() != V->sizes() || K->size(0) != c->B || K->size(1) != c->Hkv || K->size(3) != c->d) return kNotTaken;
-        if (code(*K) != c->dtype || code(*V) != c->dtype || K->stride(3) != 1 || V->stride(3) != 1) return kNotTaken;
+        if (code(*K) < 0 || code(*K) != code(*V) || (!codes && code(*K) != dtype_of(c)) || K->stride(3) != 1 || V->stride(3) != 1) return kNotTaken;
         if (!lengths(base, c, per_head) || !lengths(lens, c, same) || same != per_head) return kNotTaken;
         if (fresh && (!lengths(fresh, c, same) || same != per_head)) return kNotTaken;
         const int64_t N = K->size(2);
@@ -226,9 +234,11 @@ PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
             r.q_stride_b = Q->stride(0); r.q_stride_h = Q->stride(1); r.q_stride_n = Q->stride(2);
             r.o_stride_b = Qo->stride(0); r.o_stride_h = Qo->stride(1); r.o_stride_n = Qo->stride(2);
         }
-        return unlocked([&]() { return (int)sc_paged_append(c, &r, stream); });
+        return unlocked([&]() { return (int)append_to(c, &r, code(*K), stream); });
     });
 }
+PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) { return append<sc_paged_cache>(a, n); }
+PyObject *paged8_append(PyObject *, PyObject *const *a, Py_ssize_t n) { return append<sc_paged8_cache>(a, n); }
 
 // (cache, Q, lens, scale, O, lse, sel, sel_lens, workspace, bytes, stream)
 PyObject *paged_decode(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -280,6 +290,93 @@ PyObject *paged_select(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// (cache, Q, lens, window, sinks, scale, O, lse, workspace, bytes, stream)
+template <typename C, typename F> PyObject *windowed(PyObject *const *a, Py_ssize_t n, F attend) {
+    return guarded([&]() {
+        const at::Tensor *Q, *lens, *O, *lse;
+        if (n != 11 || !take_some(a[1], Q) || !take_some(a[2], lens) || !take_some(a[6], O) || !take(a[7], lse)) return kNotTaken;
+        const auto *c = static_cast<const C *>(pointer(a[0]));
+        const long window = PyLong_AsLong(a[3]), sinks = PyLong_AsLong(a[4]);
+        const double scale = PyFloat_AsDouble(a[5]);
+        const size_t bytes = PyLong_AsSize_t(a[9]);
+        void *w = pointer(a[8]), *stream = pointer(a[10]);
+        if (PyErr_Occurred() || !c || window != (int)window || sinks != (int)sinks) return kNotTaken;
+        bool per_head;
+        if (Q->dim() != 3 || Q->size(0) != c->B || Q->size(2) != c->d || !Q->is_contiguous() || Q->sizes() != O->sizes() || !O->is_contiguous()) return kNotTaken;
+        const int qc = code(*Q), oc = code(*O);
+        if (qc < 0 || oc < 0 || Q->size(1) != (int)Q->size(1) || !lengths(lens, c, per_head)) return kNotTaken;
+        if (lse && (lse->scalar_type() != at::kFloat || lse->dim() != 2 || lse->size(0) != c->B || lse->size(1) != Q->size(1) || !lse->is_contiguous())) return kNotTaken;
+        const void *q = data(Q);
+        const auto *l = data<const int32_t>(lens);
+        void *o = data(O);
+        auto *e = data<float>(lse);
+        return unlocked([&]() {
+            return (int)attend(c, q, (sc_dtype)qc, (int)Q->size(1), l, per_head, (int)window, (int)sinks, (float)scale, o, (sc_dtype)oc, e, w, bytes, stream);
+        });
+    });
+}
+PyObject *paged_window(PyObject *, PyObject *const *a, Py_ssize_t n) { return windowed<sc_paged_cache>(a, n, sc_paged_window_attn); }
+PyObject *paged8_decode(PyObject *, PyObject *const *a, Py_ssize_t n) { return windowed<sc_paged8_cache>(a, n, sc_paged8_decode_attn); }
+
+// (table, page_rows, base_lens, lens, free_pages, num_free, new_lens, N, window, sinks, slots, workspace, bytes, stream)
+PyObject *paged_reserve(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() {
+        const at::Tensor *table, *base, *lens, *free_pages, *num_free, *fresh, *slots;
+        if (n != 14 || !take_some(a[0], table) || !take_some(a[2], base) || !take_some(a[3], lens) || !take_some(a[4], free_pages) || !take_some(a[5], num_free)) return kNotTaken;
+        if (!take(a[6], fresh) || !take(a[10], slots)) return kNotTaken;
+        const long rows = PyLong_AsLong(a[1]), N = PyLong_AsLong(a[7]), window = PyLong_AsLong(a[8]), sinks = PyLong_AsLong(a[9]);
+        const size_t bytes = PyLong_AsSize_t(a[12]);
+        void *w = pointer(a[11]), *stream = pointer(a[13]);
+        if (PyErr_Occurred() || rows != (int)rows || N != (int)N || window != (int)window || sinks != (int)sinks) return kNotTaken;
+        const int64_t dims = table->dim();
+        if (dims < 2 || !is_i32(table) || !is_i32(base) || !is_i32(lens) || (fresh && !is_i32(fresh)) || (slots && !is_i32(slots))) return kNotTaken;
+        const auto shape = table->sizes().slice(0, dims - 1);
+        if (base->sizes() != shape || lens->sizes() != shape || (fresh && fresh->sizes() != shape)) return kNotTaken;
+        if (slots && (slots->dim() != dims || slots->sizes().slice(0, dims - 1) != shape || slots->size(dims - 1) != N)) return kNotTaken;
+        if (!is_i32(free_pages) || free_pages->dim() != 1 || !is_i32(num_free) || num_free->dim() != 1 || num_free->size(0) != 1) return kNotTaken;
+        const int64_t S = base->numel(), P = table->size(dims - 1), pages = free_pages->size(0);
+        if (S != (int)S || P != (int)P || pages != (int)pages) return kNotTaken;
+        auto *t = data<int32_t>(table), *l = data<int32_t>(lens), *f = data<int32_t>(free_pages), *m = data<int32_t>(num_free), *sl = data<int32_t>(slots);
+        const auto *b = data<const int32_t>(base), *nw = data<const int32_t>(fresh);
+        return unlocked([&]() {
+            return (int)sc_paged_reserve(t, (int)S, (int)P, (int)pages, (int)rows, b, nw, (int)N, (int)window, (int)sinks, f, m, l, sl, w, bytes, stream);
+        });
+    });
+}
+
+// (Q, K, V, q_lens, kv_lens, window, sinks, scale, O, lse, workspace, bytes, stream)
+PyObject *prompt(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() {
+        const at::Tensor *Q, *K, *V, *O, *ql, *kl, *lse;
+        if (n != 13 || !take_some(a[0], Q) || !take_some(a[1], K) || !take_some(a[2], V) || !take(a[3], ql) || !take(a[4], kl) || !take_some(a[8], O) || !take(a[9], lse)) return kNotTaken;
+        const long window = PyLong_AsLong(a[5]), sinks = PyLong_AsLong(a[6]);
+        const double scale = PyFloat_AsDouble(a[7]);
+        const size_t bytes = PyLong_AsSize_t(a[11]);
+        void *w = pointer(a[10]), *stream = pointer(a[12]);
+        if (PyErr_Occurred() || window != (int)window || sinks != (int)sinks) return kNotTaken;
+        if (Q->dim() != 4 || K->dim() != 4 || K->sizes() != V->sizes() || K->size(0) != Q->size(0) || K->size(3) != Q->size(3) || Q->sizes() != O->sizes()) return kNotTaken;
+        if (code(*Q) < 0 || code(*K) != code(*Q) || code(*V) != code(*Q) || code(*O) != code(*Q)) return kNotTaken;
+        if (Q->stride(3) != 1 || K->stride(3) != 1 || V->stride(3) != 1 || O->stride(3) != 1) return kNotTaken;
+        for (int i = 0; i < 4; ++i)
+            if (Q->size(i) != (int)Q->size(i) || K->size(i) != (int)K->size(i)) return kNotTaken;
+        const int64_t B = Q->size(0);
+        if (ql && (!is_i32(ql) || ql->dim() != 1 || ql->size(0) != B)) return kNotTaken;
+        if (kl && (!is_i32(kl) || kl->dim() != 1 || kl->size(0) != B)) return kNotTaken;
+        if (lse && (lse->scalar_type() != at::kFloat || !is_shape(lse, B, Q->size(1), Q->size(2)) || !lse->is_contiguous())) return kNotTaken;
+        sc_prompt x = {};
+        x.Q = data(Q); x.K = data(K); x.V = data(V); x.O = data(O); x.lse = data<float>(lse);
+        x.q_stride_b = Q->stride(0); x.q_stride_h = Q->stride(1); x.q_stride_n = Q->stride(2);
+        x.k_stride_b = K->stride(0); x.k_stride_h = K->stride(1); x.k_stride_n = K->stride(2);
+        x.v_stride_b = V->stride(0); x.v_stride_h = V->stride(1); x.v_stride_n = V->stride(2);
+        x.o_stride_b = O->stride(0); x.o_stride_h = O->stride(1); x.o_stride_n = O->stride(2);
+        x.q_lens = data<const int32_t>(ql); x.kv_lens = data<const int32_t>(kl);
+        x.dtype = code(*Q);
+        x.B = (int)B; x.Hq = (int)Q->size(1); x.Hkv = (int)K->size(1); x.N = (int)Q->size(2); x.M = (int)K->size(2); x.d = (int)Q->size(3);
+        x.window = (int)window; x.sinks = (int)sinks; x.scale = (float)scale;
+        return unlocked([&]() { return (int)sc_prompt_attn(&x, w, bytes, stream); });
+    });
+}
+
 PyMethodDef methods[] = {
     {"segment", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(segment)), METH_FASTCALL, nullptr},
     {"merge", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(merge)), METH_FASTCALL, nullptr},
@@ -288,6 +385,11 @@ PyMethodDef methods[] = {
     {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
     {"paged_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_decode)), METH_FASTCALL, nullptr},
     {"paged_select", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_select)), METH_FASTCALL, nullptr},
+    {"paged8_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged8_append)), METH_FASTCALL, nullptr},
+    {"paged_window", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_window)), METH_FASTCALL, nullptr},
+    {"paged8_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged8_decode)), METH_FASTCALL, nullptr},
+    {"paged_reserve", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_reserve)), METH_FASTCALL, nullptr},
+    {"prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(prompt)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
