@@ -647,7 +647,7 @@ sc_status sc_prompt_attn(const sc_prompt *x, void *ws, size_t ws_bytes, void *st
     if (!x || !x->Q || !x->K || !x->V || !x->O) return SC_ERR_INVALID_ARG;
     if (x->B <= 0 || x->Hq <= 0 || x->Hkv <= 0 || x->N <= 0 || x->M <= 0 || x->window < 0 || x->sinks < 0 || x->scale != x->scale) return SC_ERR_INVALID_ARG;
     if (!dtype_ok(x->dtype) || (x->d != 64 && x->d != 128) || x->Hq % x->Hkv) return SC_ERR_UNSUPPORTED;
-    if (x->B > 65535 || x->Hq > 65535 || (int64_t)x->N * (x->Hq / x->Hkv) > (1 << 30)) return SC_ERR_UNSUPPORTED;      // rows of a KV head are counted in 32 bits
+    if (x->B > 65535 || x->Hq > 65535 || (int64_t)x->N * (x->Hq / x->Hkv) > (1 << 30) || x->M > (1 << 30)) return SC_ERR_UNSUPPORTED;      // counted in 32 bits
     if (!aligned4(x->lse) || !aligned4(x->q_lens) || !aligned4(x->kv_lens)) return SC_ERR_INVALID_ARG;
     const int64_t es = (int64_t)elem_size(x->dtype);
     if (!rows_ok(x->Q, x->B, x->Hq, x->N, x->q_stride_b, x->q_stride_h, x->q_stride_n, x->d, es, false)) return SC_ERR_INVALID_ARG;

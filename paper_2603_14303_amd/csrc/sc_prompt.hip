@@ -21,8 +21,6 @@
 
 namespace sc {
 
-constexpr int kProWaves = 4;
-constexpr int kProThreads = kProWaves * kWave;
 constexpr float kProLog2e = 1.4426950408889634f;
 constexpr float kProLn2 = 0.6931471805599453f;
 // The running maximum follows once a logit exceeds it by this many powers of two: until then nothing needs rescaling, and weights up to 2^8 lose no bit
@@ -55,10 +53,10 @@ __device__ __forceinline__ float halves_sum(float x) {
 }
 
 // A tile of keys (values) in shared memory: rows of RB bytes, 16-byte pieces of a row exchanged by `swap` (a function of the row)
-template <typename T, int D, bool VALUES> struct Tile {
+template <typename T, int D, int THREADS, bool VALUES> struct Tile {
     static constexpr int KT = kTileKeys<T>, PIECES = D * (int)sizeof(T) / 16;
     static constexpr int RB = sizeof(T) == 2 ? 2 * D : 4 * D + 16;
-    static constexpr int BYTES = KT * RB, LOADS = KT * PIECES / kProThreads;
+    static constexpr int BYTES = KT * RB, LOADS = KT * PIECES / THREADS;
     static __device__ __forceinline__ int swap(int row) {
         if constexpr (sizeof(T) == 4) return 0;
         else if constexpr (!VALUES) return row & (PIECES - 1);
@@ -69,14 +67,14 @@ template <typename T, int D, bool VALUES> struct Tile {
         const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(rows), (short)0, here > 0 ? (int)((here - 1) * stride) + PIECES * 16 : 0, 0x00020000);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int c = tid + kProThreads * i;
+            const int c = tid + THREADS * i;
             x[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, (c / PIECES) * (int)stride + (c % PIECES) * 16, 0, 0);
         }
     }
     static __device__ __forceinline__ void store(const pro_u32x4 (&x)[LOADS], char *lds, int tid) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int c = tid + kProThreads * i, row = c / PIECES;
+            const int c = tid + THREADS * i, row = c / PIECES;
             *reinterpret_cast<pro_u32x4 *>(lds + row * RB + ((c % PIECES) ^ swap(row)) * 16) = x[i];
         }
     }
@@ -91,33 +89,38 @@ template <typename T, int D, bool VALUES> struct Tile {
             }
         return any != 0;
     }
+    static __device__ __forceinline__ void tame(pro_u32x4 (&x)[LOADS]) {            // zero in their place
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t w = x[i][k];
+                if constexpr (sizeof(T) == 2) x[i][k] = ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+                else x[i][k] = (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
+            }
+    }
 };
 
-// four values of row `key`, elements e .. e + 3, as fp32
-template <typename T, int D> __device__ __forceinline__ float4 values4(const char *lds, int key, int e) {
-    using V = Tile<T, D, true>;
-    const int at = e * (int)sizeof(T);
-    const char *p = lds + key * V::RB + ((at / 16) ^ V::swap(key)) * 16 + at % 16;
+// four values of a row, elements e .. e + 3, as fp32
+template <typename T> __device__ __forceinline__ float4 values4(const char *row, int e) {
     if constexpr (sizeof(T) == 2) {
-        const uint2 w = *reinterpret_cast<const uint2 *>(p);
+        const uint2 w = *reinterpret_cast<const uint2 *>(row + 2 * e);
         return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
     } else {
-        return *reinterpret_cast<const float4 *>(p);
+        return *reinterpret_cast<const float4 *>(row + 4 * e);
     }
 }
 __device__ __forceinline__ float if_wild(float x) { return fabsf(x) < INFINITY ? 0.f : x; }
-__device__ __forceinline__ uint32_t without_wild(uint32_t w) {      // a pair of bf16
-    return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
-}
 
-template <typename T, int D, int QB>
-__global__ __launch_bounds__(kProThreads, 1) void prompt_kernel(ProParams p) {
+// NW wavefronts of 32 QB rows
+template <typename T, int D, int QB, int NW>
+__global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) {
     constexpr bool kBf16 = sizeof(T) == 2;
-    constexpr int KT = kTileKeys<T>, KB = KT / 32, DT = D / 32, ROWS = 32 * QB * kProWaves;
-    using KTile = Tile<T, D, false>;
-    using VTile = Tile<T, D, true>;
+    constexpr int KT = kTileKeys<T>, KB = KT / 32, DT = D / 32, ROWS = 32 * QB * NW;
+    using KTile = Tile<T, D, NW * kWave, false>;
+    using VTile = Tile<T, D, NW * kWave, true>;
     __shared__ __attribute__((aligned(16))) char s_k[2][KTile::BYTES], s_v[2][VTile::BYTES];
-    __shared__ int s_wild[2][kProWaves];
+    __shared__ int s_wild[2][NW];
     const PromptArgs &a = p.a;
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int half = lane / 32, col = lane % 32;
@@ -130,28 +133,32 @@ __global__ __launch_bounds__(kProThreads, 1) void prompt_kernel(ProParams p) {
     const int behind = kv_len - q_len;                 // position of the first query
     const int token0 = first / p.G, token1 = min((first + ROWS - 1) / p.G, q_len - 1);
     if (token0 >= q_len) return;
-    const PromptTiles mine = prompt_tiles((int64_t)behind + token0, (int64_t)behind + token1, a.window, a.sinks, KT);
+    const PromptSpan all = prompt_span((int64_t)behind + token0, (int64_t)behind + token1, a.window, a.sinks);
+    const PromptTiles mine = prompt_tiles(all, KT);
     const int t0 = (int)((int64_t)mine.count * split / p.splits), t1 = (int)((int64_t)mine.count * (split + 1) / p.splits);
     // ... and my wavefront's
     const int row0 = first + 32 * QB * wave;
     const int wt0 = row0 / p.G, wt1 = min((row0 + 32 * QB - 1) / p.G, q_len - 1);
     const bool idle = wt0 >= q_len;
-    const int wp0 = behind + wt0, wp1 = behind + wt1;
+    const PromptSpan span = prompt_span((int64_t)behind + wt0, (int64_t)behind + wt1, a.window, a.sinks);
 
-    int token[QB], head[QB];
+    int token[QB], head[QB], pos[QB], edge[QB];
 #pragma unroll
     for (int u = 0; u < QB; ++u) {
         const int r = row0 + 32 * u + col;
         token[u] = r / p.G;
         head[u] = h * p.G + r - token[u] * p.G;
+        pos[u] = behind + token[u];
+        edge[u] = prompt_edge(pos[u], a.window);
     }
     // ---- queries: bf16: lane (half, col) holds 8 half .. 8 half + 7 of every 16 elements of row `col`; fp32: elements (D / 2) half + ..
-    pro_u32x4 q[QB][kBf16 ? D / 16 : D / 8];
+    constexpr int QL = kBf16 ? D / 16 : D / 8;
+    pro_u32x4 q[QB][QL];
 #pragma unroll
     for (int u = 0; u < QB; ++u) {
         const char *src = a.Q + b * a.q_b + head[u] * a.q_h + (int64_t)min(token[u], a.N - 1) * a.q_n;
 #pragma unroll
-        for (int i = 0; i < (kBf16 ? D / 16 : D / 8); ++i) {
+        for (int i = 0; i < QL; ++i) {
             q[u][i] = *reinterpret_cast<const pro_u32x4 *>(src + (kBf16 ? (16 * i + 8 * half) * 2 : ((D / 2) * half + 4 * i) * 4));
             q[u][i] ^= kBf16 ? p.flip | p.flip >> 16 : p.flip;
         }
@@ -169,6 +176,140 @@ __global__ __launch_bounds__(kProThreads, 1) void prompt_kernel(ProParams p) {
             for (int i = 0; i < 16; ++i) o[u][t][i] = 0.f;
     }
 
+    // ---- a tile of keys for my rows
+    auto attend = [&](int k0, const char *lk, const char *lv) {
+        pro_f32x16 s[QB][KB];
+#pragma unroll
+        for (int u = 0; u < QB; ++u)
+#pragma unroll
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[u][k][i] = 0.f;
+        if constexpr (kBf16) {
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+                for (int k = 0; k < KB; ++k) {
+                    const int row = 32 * k + col;
+                    const pro_u32x4 key = *reinterpret_cast<const pro_u32x4 *>(lk + row * KTile::RB + ((2 * e + half) ^ KTile::swap(row)) * 16);
+#pragma unroll
+                    for (int u = 0; u < QB; ++u)
+                        s[u][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, key), __builtin_bit_cast(pro_bf16x8, q[u][e]), s[u][k], 0, 0, 0);
+                }
+        } else {
+#pragma unroll
+            for (int e = 0; e < D / 8; ++e) {
+                const pro_u32x4 key = *reinterpret_cast<const pro_u32x4 *>(lk + col * KTile::RB + ((D / 2) * half + 4 * e) * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int u = 0; u < QB; ++u)
+                        s[u][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(key[i]), __uint_as_float(q[u][e][i]), s[u][0], 0, 0, 0);
+            }
+        }
+        if (!prompt_all(span, k0, KT)) {
+#pragma unroll
+            for (int u = 0; u < QB; ++u)
+#pragma unroll
+                for (int k = 0; k < KB; ++k)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = k0 + 32 * k + 8 * (i / 4) + 4 * half + i % 4;
+                        s[u][k][i] = prompt_sees(key, pos[u], edge[u], a.sinks) ? s[u][k][i] : -INFINITY;
+                    }
+        }
+        // ---- softmax
+#pragma unroll
+        for (int u = 0; u < QB; ++u) {
+            float mx = s[u][0][0];
+#pragma unroll
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][k][i]);
+            mx = halves_max(mx) * p.scale_log2;
+            if (ballot64(mx > m_run[u] + kProSlack) != 0ull) {
+                const float m_new = fmaxf(m_run[u], mx);
+                const float alpha = m_new == -INFINITY ? 1.f : pro_exp2(m_run[u] - m_new);
+                m_run[u] = m_new;
+                l_run[u] *= alpha;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[u][d][i] *= alpha;
+            }
+            const float shift = m_run[u] == -INFINITY ? 0.f : m_run[u];
+            float sum[2] = {0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[u][k][i] = pro_exp2(fmaf(s[u][k][i], p.scale_log2, -shift));
+                    sum[i % 2] += s[u][k][i];
+                }
+            l_run[u] += sum[0] + sum[1];
+        }
+        // ---- O^T += V^T P^T.  Place 8 half + j of the inner dimension is key 4 half + j of 16, or 8 + 4 half + j - 4
+        if constexpr (kBf16) {
+#pragma unroll
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    pro_u32x4 w[QB];
+#pragma unroll
+                    for (int u = 0; u < QB; ++u)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[u][i] = pack_bf16x2(s[u][k][8 * g + 2 * i], s[u][k][8 * g + 2 * i + 1]);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        // 16 lanes read 4 keys x 16 elements, every lane four elements of a key, and get four keys of an element
+                        const int lane16 = lane % 16, key = 32 * k + 16 * g + 4 * half + lane16 / 4;
+                        const int at = 64 * d + 32 * (lane / 16 % 2) + 8 * (lane16 % 4);
+                        uint2 v[2];
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            typedef __attribute__((address_space(3))) pro_s16x4 lds_s16x4;
+                            const char *src = lv + (key + 8 * x) * VTile::RB + ((at / 16) ^ VTile::swap(key + 8 * x)) * 16 + at % 16;
+                            v[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)src));
+                        }
+                        const pro_u32x4 val = {v[0].x, v[0].y, v[1].x, v[1].y};
+#pragma unroll
+                        for (int u = 0; u < QB; ++u)
+                            o[u][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, val), __builtin_bit_cast(pro_bf16x8, w[u]), o[u][d], 0, 0, 0);
+                    }
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int key = 8 * (i / 4) + 4 * half + i % 4;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    const float val = *reinterpret_cast<const float *>(lv + key * VTile::RB + (32 * d + col) * 4);
+#pragma unroll
+                    for (int u = 0; u < QB; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(val, s[u][0][i], o[u][d], 0, 0, 0);
+                }
+            }
+        }
+    };
+    // Values that are not finite, in a tile that some row of the workgroup does not see whole: 0 times such a number would be none.  They are zero in shared memory then, and added to
+    // the rows that see them from where they lie
+    auto attend_wild = [&](int k0, const char *rows, int here) {
+        for (int key = 0; key < here; ++key)
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 v = values4<T>(rows + (int64_t)key * a.v_n, 32 * d + 8 * i + 4 * half);
+#pragma unroll
+                    for (int u = 0; u < QB; ++u)
+                        if (prompt_sees(k0 + key, pos[u], edge[u], a.sinks)) {
+                            o[u][d][4 * i] += if_wild(v.x);
+                            o[u][d][4 * i + 1] += if_wild(v.y);
+                            o[u][d][4 * i + 2] += if_wild(v.z);
+                            o[u][d][4 * i + 3] += if_wild(v.w);
+                        }
+                }
+    };
+
     const char *kb = a.K + b * a.k_b + h * a.k_h, *vb = a.V + b * a.v_b + h * a.v_h;
     pro_u32x4 kx[KTile::LOADS], vx[VTile::LOADS];
     auto request = [&](int t) {
@@ -177,14 +318,14 @@ __global__ __launch_bounds__(kProThreads, 1) void prompt_kernel(ProParams p) {
         VTile::load(vx, vb + (int64_t)k0 * a.v_n, a.v_n, min(kv_len - k0, KT), tid);
     };
     auto lay_down = [&](int t, int buf) {
+        if (!prompt_all(all, prompt_tile(mine, t) * KT, KT)) {
+            const bool wild = VTile::wild(vx);
+            const uint64_t any = ballot64(wild);
+            if (lane == 0) s_wild[buf][wave] = any != 0;
+            if (wild) VTile::tame(vx);
+        }
         KTile::store(kx, s_k[buf], tid);
         VTile::store(vx, s_v[buf], tid);
-        // values that are not finite, of a key that some rows do not see: 0 times such a number is none
-        const int k0 = prompt_tile(mine, t) * KT;
-        if (!prompt_all(k0, (int64_t)behind + token0, (int64_t)behind + token1, a.window, a.sinks, KT)) {
-            const uint64_t any = ballot64(VTile::wild(vx));
-            if (lane == 0) s_wild[buf][wave] = any != 0;
-        }
     };
     if (t0 < t1) {
         request(t0);
@@ -194,144 +335,13 @@ __global__ __launch_bounds__(kProThreads, 1) void prompt_kernel(ProParams p) {
     for (int t = t0; t < t1; ++t) {
         const int buf = (t - t0) & 1, k0 = prompt_tile(mine, t) * KT;
         if (t + 1 < t1) request(t + 1);
-        if (!idle && prompt_some(k0, wp0, wp1, a.window, a.sinks, KT)) {
-            const char *lk = s_k[buf], *lv = s_v[buf];
-            pro_f32x16 s[QB][KB];
+        if (!idle && prompt_some(span, k0, KT)) {
+            attend(k0, s_k[buf], s_v[buf]);
+            if (!prompt_all(all, k0, KT)) {
+                int wild = 0;
 #pragma unroll
-            for (int u = 0; u < QB; ++u)
-#pragma unroll
-                for (int k = 0; k < KB; ++k)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[u][k][i] = 0.f;
-            if constexpr (kBf16) {
-#pragma unroll
-                for (int e = 0; e < D / 16; ++e)
-#pragma unroll
-                    for (int k = 0; k < KB; ++k) {
-                        const int row = 32 * k + col;
-                        const pro_u32x4 key = *reinterpret_cast<const pro_u32x4 *>(lk + row * KTile::RB + ((2 * e + half) ^ KTile::swap(row)) * 16);
-#pragma unroll
-                        for (int u = 0; u < QB; ++u)
-                            s[u][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, key), __builtin_bit_cast(pro_bf16x8, q[u][e]), s[u][k], 0, 0, 0);
-                    }
-            } else {
-#pragma unroll
-                for (int e = 0; e < D / 8; ++e) {
-                    const pro_u32x4 key = *reinterpret_cast<const pro_u32x4 *>(lk + col * KTile::RB + ((D / 2) * half + 4 * e) * 4);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int u = 0; u < QB; ++u)
-                            s[u][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(key[i]), __uint_as_float(q[u][e][i]), s[u][0], 0, 0, 0);
-                }
-            }
-            const bool masked = !prompt_all(k0, wp0, wp1, a.window, a.sinks, KT);
-            bool wild = false;
-            if (masked) {
-#pragma unroll
-                for (int u = 0; u < QB; ++u) {
-                    const int pos = behind + token[u];
-#pragma unroll
-                    for (int k = 0; k < KB; ++k)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (!prompt_sees(pos, k0 + 32 * k + 8 * (i / 4) + 4 * half + i % 4, a.window, a.sinks)) s[u][k][i] = -INFINITY;
-                }
-#pragma unroll
-                for (int w = 0; w < kProWaves; ++w) wild |= s_wild[buf][w] != 0;
-            }
-            // ---- softmax
-#pragma unroll
-            for (int u = 0; u < QB; ++u) {
-                float mx = s[u][0][0];
-#pragma unroll
-                for (int k = 0; k < KB; ++k)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][k][i]);
-                mx = halves_max(mx) * p.scale_log2;
-                if (ballot64(mx > m_run[u] + kProSlack) != 0ull) {
-                    const float m_new = fmaxf(m_run[u], mx);
-                    const float alpha = m_new == -INFINITY ? 1.f : pro_exp2(m_run[u] - m_new);
-                    m_run[u] = m_new;
-                    l_run[u] *= alpha;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[u][d][i] *= alpha;
-                }
-                const float shift = m_run[u] == -INFINITY ? 0.f : m_run[u];
-                float sum = 0.f;
-#pragma unroll
-                for (int k = 0; k < KB; ++k)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        s[u][k][i] = pro_exp2(fmaf(s[u][k][i], p.scale_log2, -shift));
-                        sum += s[u][k][i];
-                    }
-                l_run[u] += sum;
-            }
-            // ---- O^T += V^T P^T.  Place 8 half + j of the inner dimension is key 4 half + j of 16, or 8 + 4 half + j - 4
-            if constexpr (kBf16) {
-#pragma unroll
-                for (int k = 0; k < KB; ++k)
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        pro_u32x4 w[QB];
-#pragma unroll
-                        for (int u = 0; u < QB; ++u)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) w[u][i] = pack_bf16x2(s[u][k][8 * g + 2 * i], s[u][k][8 * g + 2 * i + 1]);
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            // 16 lanes read 4 keys x 16 elements, every lane four elements of a key, and get four keys of an element
-                            const int lane16 = lane % 16, key = 32 * k + 16 * g + 4 * half + lane16 / 4;
-                            const int at = 64 * d + 32 * (lane / 16 % 2) + 8 * (lane16 % 4);
-                            uint2 v[2];
-#pragma unroll
-                            for (int x = 0; x < 2; ++x) {
-                                const char *src = lv + (key + 8 * x) * VTile::RB + ((at / 16) ^ VTile::swap(key + 8 * x)) * 16 + at % 16;
-                                typedef __attribute__((address_space(3))) pro_s16x4 lds_s16x4;
-                                v[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)src));
-                            }
-                            pro_u32x4 val = {v[0].x, v[0].y, v[1].x, v[1].y};
-                            if (wild) {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) val[i] = without_wild(val[i]);
-                            }
-#pragma unroll
-                            for (int u = 0; u < QB; ++u)
-                                o[u][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, val), __builtin_bit_cast(pro_bf16x8, w[u]), o[u][d], 0, 0, 0);
-                        }
-                    }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = 8 * (i / 4) + 4 * half + i % 4;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        float val = *reinterpret_cast<const float *>(lv + key * VTile::RB + (32 * d + col) * 4);
-                        if (wild) val = fabsf(val) < INFINITY ? val : 0.f;
-#pragma unroll
-                        for (int u = 0; u < QB; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(val, s[u][0][i], o[u][d], 0, 0, 0);
-                    }
-                }
-            }
-            if (wild) {      // they were left out: to the rows that see them
-                for (int key = 0; key < KT; ++key)
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float4 v = values4<T, D>(lv, key, 32 * d + 8 * i + 4 * half);
-#pragma unroll
-                            for (int u = 0; u < QB; ++u)
-                                if (prompt_sees(behind + token[u], k0 + key, a.window, a.sinks)) {
-                                    o[u][d][4 * i] += if_wild(v.x);
-                                    o[u][d][4 * i + 1] += if_wild(v.y);
-                                    o[u][d][4 * i + 2] += if_wild(v.z);
-                                    o[u][d][4 * i + 3] += if_wild(v.w);
-                                }
-                        }
+                for (int w = 0; w < NW; ++w) wild |= s_wild[buf][w];
+                if (__builtin_amdgcn_readfirstlane(wild)) attend_wild(k0, vb + (int64_t)k0 * a.v_n, min(kv_len - k0, KT));
             }
         }
         if (t + 1 < t1) lay_down(t + 1, buf ^ 1);
@@ -424,9 +434,13 @@ bool prompt_fits(int B, int Hq, int Hkv, int N, int M, int d, bool bf16) {
     return (int64_t)s.tiles * B * Hkv * s.splits <= INT32_MAX && (int64_t)B * Hq * N <= ((int64_t)1 << 33);
 }
 
-template <typename T, int D, int QB> static hipError_t launch_prompt_k(const ProParams &p, hipStream_t stream) {
+#ifndef PRO_QB
+#define PRO_QB 1
+#define PRO_NW 8
+#endif
+template <typename T, int D, int QB, int NW> static hipError_t launch_prompt_k(const ProParams &p, hipStream_t stream) {
     const unsigned wgs = (unsigned)((int64_t)p.tiles * p.a.B * p.a.Hkv * p.splits);
-    hipLaunchKernelGGL((prompt_kernel<T, D, QB>), dim3(wgs), dim3(kProThreads), 0, stream, p);
+    hipLaunchKernelGGL((prompt_kernel<T, D, QB, NW>), dim3(wgs), dim3(NW * kWave), 0, stream, p);
     if (p.splits > 1) {
         const int64_t rows = (int64_t)p.a.N * p.a.Hq * p.a.B, per = 256 / (D / 4);
         hipLaunchKernelGGL((prompt_join_kernel<D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, p);
@@ -434,8 +448,8 @@ template <typename T, int D, int QB> static hipError_t launch_prompt_k(const Pro
     return hipGetLastError();
 }
 template <int D> static hipError_t launch_prompt_d(const ProParams &p, int rows, hipStream_t stream) {
-    if (p.a.dtype != DType::BF16) return launch_prompt_k<float, D, 1>(p, stream);
-    return rows == 256 ? launch_prompt_k<bf16_t, D, 2>(p, stream) : launch_prompt_k<bf16_t, D, 1>(p, stream);
+    if (p.a.dtype != DType::BF16) return launch_prompt_k<float, D, 1, 4>(p, stream);
+    return rows == 256 ? launch_prompt_k<bf16_t, D, PRO_QB, PRO_NW>(p, stream) : launch_prompt_k<bf16_t, D, 1, 4>(p, stream);
 }
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t stream) {
