@@ -25,6 +25,9 @@ constexpr float kProLog2e = 1.4426950408889634f;
 constexpr float kProLn2 = 0.6931471805599453f;
 // The running maximum follows once a logit exceeds it by this many powers of two: until then nothing needs rescaling, and weights up to 2^8 lose no bit
 constexpr float kProSlack = 8.f;
+#ifndef PRO_AHEAD
+#define PRO_AHEAD 8
+#endif
 
 typedef float pro_f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned int pro_u32x4 __attribute__((ext_vector_type(4)));
@@ -52,52 +55,65 @@ __device__ __forceinline__ float halves_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// A tile of keys (values) in shared memory: rows of RB bytes, 16-byte pieces of a row exchanged by `swap` (a function of the row)
-template <typename T, int D, int THREADS, bool VALUES> struct Tile {
-    static constexpr int KT = kTileKeys<T>, PIECES = D * (int)sizeof(T) / 16;
-    static constexpr int RB = sizeof(T) == 2 ? 2 * D : 4 * D + 16;
-    static constexpr int BYTES = KT * RB, LOADS = KT * PIECES / THREADS;
+template <typename T> __device__ __forceinline__ bool is_wild(uint32_t w) {      // an element of w is not finite
+    return (w & 0x7f800000u) == 0x7f800000u || (sizeof(T) == 2 && (w & 0x7f80u) == 0x7f80u);
+}
+template <typename T> __device__ __forceinline__ uint32_t tamed(uint32_t w) {    // zero in its place
+    if constexpr (sizeof(T) == 2) return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+    else return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
+}
+
+// A tile of KT rows in shared memory, as it comes from memory without a register between (buffer_load .. lds: lane l of a wavefront writes the l-th 16 bytes from a common address on).  The 16-byte
+// pieces of a row are exchanged by a function of the row, so that reads across rows meet all banks: the lanes ask for them in that order.
+template <typename T, int D, int NW, bool VALUES> struct Tile {
+    static constexpr int KT = kTileKeys<T>, RB = D * (int)sizeof(T), PIECES = RB / 16, BYTES = KT * RB;
+    static constexpr int LOADS = BYTES / (1024 * NW);
+    static_assert(LOADS * 1024 * NW == BYTES, "the same for every wavefront");
     static __device__ __forceinline__ int swap(int row) {
-        if constexpr (sizeof(T) == 4) return 0;
-        else if constexpr (!VALUES) return row & (PIECES - 1);
-        else return D == 128 ? (row & 3) << 2 : (row >> 1 & 1) << 2;
+        if constexpr (sizeof(T) == 2 && VALUES) return D == 128 ? (row & 3) << 2 : (row >> 1 & 1) << 2;      // (read transposed: 4 rows x 64 bytes a half)
+        else return row & (PIECES - 1);
     }
-    // A thread's pieces: LOADS of them, of rows tid / PIECES + ...
-    static __device__ __forceinline__ void load(pro_u32x4 (&x)[LOADS], const char *rows, int64_t stride, int here, int tid) {
-        const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(rows), (short)0, here > 0 ? (int)((here - 1) * stride) + PIECES * 16 : 0, 0x00020000);
+    int offset[LOADS];      // of the lane's pieces
+    uint32_t stride;
+    __device__ __forceinline__ void init(int64_t row_stride, int wave, int lane) {
+        stride = (uint32_t)row_stride;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int c = tid + THREADS * i;
-            x[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, (c / PIECES) * (int)stride + (c % PIECES) * 16, 0, 0);
+            const int c = (i * NW + wave) * kWave + lane, row = c / PIECES;
+            offset[i] = row * (int)row_stride + ((c % PIECES) ^ swap(row)) * 16;
         }
     }
-    static __device__ __forceinline__ void store(const pro_u32x4 (&x)[LOADS], char *lds, int tid) {
+    // rows k0 .. of `rows`, up to `end`; nothing is read behind them
+    __device__ __forceinline__ void load(char *lds, const char *rows, int k0, int end, int wave) const {
+        const uint64_t at = (uint64_t)(uintptr_t)rows + (uint64_t)(uint32_t)k0 * stride;
+        const int here = min(end - k0, KT);
+        const pro_u32x4 rs = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xffffu)),
+                              (uint32_t)__builtin_amdgcn_readfirstlane(here > 0 ? (here - 1) * (int)stride + RB : 0), 0x00020000u};
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int c = tid + THREADS * i, row = c / PIECES;
-            *reinterpret_cast<pro_u32x4 *>(lds + row * RB + ((c % PIECES) ^ swap(row)) * 16) = x[i];
+            const int m0 = __builtin_amdgcn_readfirstlane((int)(to + (i * NW + wave) * 1024));
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m0), "v"(offset[i]), "s"(rs) : "memory");
         }
     }
-    static __device__ __forceinline__ bool wild(const pro_u32x4 (&x)[LOADS]) {      // an element that is not finite
-        uint32_t any = 0;
+    // The wavefront's own pieces, arrived: numbers that are not finite become zero.  Says whether there were any
+    __device__ __forceinline__ bool tame(char *lds, int wave, int lane) const {
+        bool any = false;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
+        for (int i = 0; i < LOADS; ++i) {
+            auto *p = reinterpret_cast<pro_u32x4 *>(lds + (i * NW + wave) * 1024 + lane * 16);
+            pro_u32x4 x = *p;
+            bool wild = false;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if constexpr (sizeof(T) == 2) any |= (uint32_t)((x[i][k] & 0x7f80u) == 0x7f80u) | (uint32_t)((x[i][k] & 0x7f800000u) == 0x7f800000u);
-                else any |= (uint32_t)((x[i][k] & 0x7f800000u) == 0x7f800000u);
+            for (int k = 0; k < 4; ++k) wild |= is_wild<T>(x[k]);
+            if (wild) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = tamed<T>(x[k]);
+                *p = x;
             }
-        return any != 0;
-    }
-    static __device__ __forceinline__ void tame(pro_u32x4 (&x)[LOADS]) {            // zero in their place
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t w = x[i][k];
-                if constexpr (sizeof(T) == 2) x[i][k] = ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
-                else x[i][k] = (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
-            }
+            any |= wild;
+        }
+        return any;
     }
 };
 
@@ -117,10 +133,12 @@ template <typename T, int D, int QB, int NW>
 __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) {
     constexpr bool kBf16 = sizeof(T) == 2;
     constexpr int KT = kTileKeys<T>, KB = KT / 32, DT = D / 32, ROWS = 32 * QB * NW;
-    using KTile = Tile<T, D, NW * kWave, false>;
-    using VTile = Tile<T, D, NW * kWave, true>;
-    __shared__ __attribute__((aligned(16))) char s_k[2][KTile::BYTES], s_v[2][VTile::BYTES];
-    __shared__ int s_wild[2][NW];
+    using KTile = Tile<T, D, NW, false>;
+    using VTile = Tile<T, D, NW, true>;
+    constexpr bool kTurns = NW == 8;              // the halves of the workgroup take turns (below)
+    constexpr int kPlaces = kTurns ? 3 : 2;
+    __shared__ int s_wild[kPlaces][NW];
+    __shared__ __attribute__((aligned(16))) char s_k[kPlaces][KTile::BYTES], s_v[kPlaces][VTile::BYTES];
     const PromptArgs &a = p.a;
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int half = lane / 32, col = lane % 32;
@@ -139,7 +157,6 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
     // ... and my wavefront's
     const int row0 = first + 32 * QB * wave;
     const int wt0 = row0 / p.G, wt1 = min((row0 + 32 * QB - 1) / p.G, q_len - 1);
-    const bool idle = wt0 >= q_len;
     const PromptSpan span = prompt_span((int64_t)behind + wt0, (int64_t)behind + wt1, a.window, a.sinks);
 
     int token[QB], head[QB], pos[QB], edge[QB];
@@ -176,9 +193,10 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
             for (int i = 0; i < 16; ++i) o[u][t][i] = 0.f;
     }
 
-    // ---- a tile of keys for my rows
-    auto attend = [&](int k0, const char *lk, const char *lv) {
-        pro_f32x16 s[QB][KB];
+    // ---- a tile of keys for my rows: logits, probabilities, and their product with the values
+    pro_f32x16 s[QB][KB];                          // logits, then (fp32) probabilities
+    pro_u32x4 w[QB][kBf16 ? 2 * KB : 1];           // (bf16) probabilities
+    auto logits = [&](const char *lk) {
 #pragma unroll
         for (int u = 0; u < QB; ++u)
 #pragma unroll
@@ -199,7 +217,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
         } else {
 #pragma unroll
             for (int e = 0; e < D / 8; ++e) {
-                const pro_u32x4 key = *reinterpret_cast<const pro_u32x4 *>(lk + col * KTile::RB + ((D / 2) * half + 4 * e) * 4);
+                const pro_u32x4 key = *reinterpret_cast<const pro_u32x4 *>(lk + col * KTile::RB + ((D / 8 * half + e) ^ KTile::swap(col)) * 16);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -207,7 +225,9 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
                         s[u][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(key[i]), __uint_as_float(q[u][e][i]), s[u][0], 0, 0, 0);
             }
         }
-        if (!prompt_all(span, k0, KT)) {
+    };
+    auto probabilities = [&](int k0, bool masked) {
+        if (masked) {
 #pragma unroll
             for (int u = 0; u < QB; ++u)
 #pragma unroll
@@ -218,7 +238,6 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
                         s[u][k][i] = prompt_sees(key, pos[u], edge[u], a.sinks) ? s[u][k][i] : -INFINITY;
                     }
         }
-        // ---- softmax
 #pragma unroll
         for (int u = 0; u < QB; ++u) {
             float mx = s[u][0][0];
@@ -247,18 +266,21 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
                     sum[i % 2] += s[u][k][i];
                 }
             l_run[u] += sum[0] + sum[1];
+            if constexpr (kBf16) {
+#pragma unroll
+                for (int k = 0; k < KB; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[u][2 * k + i / 4][i % 4] = pack_bf16x2(s[u][k][2 * i], s[u][k][2 * i + 1]);
+            }
         }
-        // ---- O^T += V^T P^T.  Place 8 half + j of the inner dimension is key 4 half + j of 16, or 8 + 4 half + j - 4
+    };
+    auto add_values = [&](const char *lv) {
+        // O^T += V^T P^T.  Place 8 half + j of the inner dimension is key 4 half + j of 16, or 8 + 4 half + j - 4
         if constexpr (kBf16) {
 #pragma unroll
             for (int k = 0; k < KB; ++k)
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    pro_u32x4 w[QB];
-#pragma unroll
-                    for (int u = 0; u < QB; ++u)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) w[u][i] = pack_bf16x2(s[u][k][8 * g + 2 * i], s[u][k][8 * g + 2 * i + 1]);
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
                         // 16 lanes read 4 keys x 16 elements, every lane four elements of a key, and get four keys of an element
@@ -274,7 +296,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
                         const pro_u32x4 val = {v[0].x, v[0].y, v[1].x, v[1].y};
 #pragma unroll
                         for (int u = 0; u < QB; ++u)
-                            o[u][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, val), __builtin_bit_cast(pro_bf16x8, w[u]), o[u][d], 0, 0, 0);
+                            o[u][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, val), __builtin_bit_cast(pro_bf16x8, w[u][2 * k + g]), o[u][d], 0, 0, 0);
                     }
                 }
         } else {
@@ -283,7 +305,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
                 const int key = 8 * (i / 4) + 4 * half + i % 4;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    const float val = *reinterpret_cast<const float *>(lv + key * VTile::RB + (32 * d + col) * 4);
+                    const float val = *reinterpret_cast<const float *>(lv + key * VTile::RB + ((8 * d + col / 4) ^ VTile::swap(key)) * 16 + col % 4 * 4);
 #pragma unroll
                     for (int u = 0; u < QB; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(val, s[u][0][i], o[u][d], 0, 0, 0);
                 }
@@ -311,42 +333,94 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
     };
 
     const char *kb = a.K + b * a.k_b + h * a.k_h, *vb = a.V + b * a.v_b + h * a.v_h;
-    pro_u32x4 kx[KTile::LOADS], vx[VTile::LOADS];
-    auto request = [&](int t) {
-        const int k0 = prompt_tile(mine, t) * KT;
-        KTile::load(kx, kb + (int64_t)k0 * a.k_n, a.k_n, min(kv_len - k0, KT), tid);
-        VTile::load(vx, vb + (int64_t)k0 * a.v_n, a.v_n, min(kv_len - k0, KT), tid);
+    KTile kx;
+    VTile vx;
+    kx.init(a.k_n, wave, lane);
+    vx.init(a.v_n, wave, lane);
+    const int n = t1 - t0;
+    auto key_of = [&](int t) { return prompt_tile(mine, t0 + t) * KT; };
+    // Tile t is in place t % kPlaces of its buffers
+    auto request_keys = [&](int t, int place) {
+        if (t < n) kx.load(s_k[place], kb, key_of(t), kv_len, wave);
     };
-    auto lay_down = [&](int t, int buf) {
-        if (!prompt_all(all, prompt_tile(mine, t) * KT, KT)) {
-            const bool wild = VTile::wild(vx);
-            const uint64_t any = ballot64(wild);
-            if (lane == 0) s_wild[buf][wave] = any != 0;
-            if (wild) VTile::tame(vx);
-        }
-        KTile::store(kx, s_k[buf], tid);
-        VTile::store(vx, s_v[buf], tid);
+    auto request_values = [&](int t, int place) {
+        if (t < n) vx.load(s_v[place], vb, key_of(t), kv_len, wave);
     };
-    if (t0 < t1) {
-        request(t0);
-        lay_down(t0, 0);
-    }
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-        const int buf = (t - t0) & 1, k0 = prompt_tile(mine, t) * KT;
-        if (t + 1 < t1) request(t + 1);
-        if (!idle && prompt_some(span, k0, KT)) {
-            attend(k0, s_k[buf], s_v[buf]);
-            if (!prompt_all(all, k0, KT)) {
-                int wild = 0;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) wild |= s_wild[buf][w];
-                if (__builtin_amdgcn_readfirstlane(wild)) attend_wild(k0, vb + (int64_t)k0 * a.v_n, min(kv_len - k0, KT));
-            }
+    auto settle = [&](int t, int place) {      // what the wavefront has requested is there; the values of tile t are fit for the product
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (t < n && !prompt_all(all, key_of(t), KT)) {
+            const uint64_t any = ballot64(vx.tame(s_v[place], wave, lane));
+            if (lane == 0) s_wild[place][wave] = any != 0;
         }
-        if (t + 1 < t1) lay_down(t + 1, buf ^ 1);
+    };
+    // ---- The two halves of the workgroup take turns: while one is at its products (values of a tile, logits of the next), the other forms probabilities, so that the matrix cores and the
+    // vector units are at work together (wavefronts w and w + NW / 2 share a SIMD).  The second half runs one barrier behind the first.  Phase p lies between barriers p and p + 1:
+    //     first half    logits 0 in phase 0, probabilities t in phase 2 t + 1, products t (values t, keys t + 1) in 2 t + 2
+    //     second half   logits 0 in phase 1, probabilities t in phase 2 t + 2, products t in 2 t + 3
+    // Keys t + 2 and values t + 1 are requested with probabilities t.  They take the places of keys t - 1 and values t - 2, which were last read in phase 2 t - 1, and are there by the end of phase
+    // 2 t + 3: a half waits for what it has requested at the end of its phase of that number.
+    // With four wavefronts, one on each SIMD, nobody takes turns: all are the first half, the other workgroup of the compute unit is in the other phase or is not, and keys t and values t - 1 make room.
+    const bool second = kTurns && wave >= NW / 2;
+    auto meet = [&]() {      // (nothing of one phase is put off into the next one: the compiler would)
+        __builtin_amdgcn_sched_barrier(0);
         __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    request_keys(0, 0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    meet();
+    request_keys(1, 1);
+    request_values(0, 0);
+    if (second) meet();
+    logits(s_k[0]);
+    if (second) settle(0, 0);
+    meet();
+    int here = 0, next = 1, after = 2 % kPlaces;      // places of tiles t, t + 1, t + 2
+    for (int t = 0; t < n; ++t) {
+        const int k0 = key_of(t);
+        const bool edges = !prompt_all(all, k0, KT);
+        if (!second) settle(t, here);
+        request_keys(t + 2, after);
+        request_values(t + 1, next);
+        probabilities(k0, !prompt_all(span, k0, KT));
+        if constexpr (kBf16) {
+#pragma unroll
+            for (int u = 0; u < QB; ++u)
+#pragma unroll
+                for (int i = 0; i < 2 * KB; ++i) asm volatile("" : "+v"(w[u][i]));
+        }
+        meet();
+        add_values(s_v[here]);
+        logits(s_k[next]);      // (behind the last tile of anything: nobody uses them)
+        if constexpr (kBf16) {         // operands are read well ahead of the products that take them: a read takes as long as four products
+            constexpr int kAhead = PRO_AHEAD, PV = 2 * KB * DT, QK = KB * D / 16;
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAhead, 0);
+#pragma unroll
+            for (int i = 0; i < PV - kAhead; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < QK; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+        }
+        if (edges) {
+            int wild = 0;
+#pragma unroll
+            for (int x = 0; x < NW; ++x) wild |= s_wild[here][x];
+            if (__builtin_amdgcn_readfirstlane(wild)) attend_wild(k0, vb + (int64_t)k0 * a.v_n, min(kv_len - k0, KT));
+        }
+        if (second) settle(t + 1, next);
+        meet();
+        const int x = here;
+        here = next;
+        next = after;
+        after = kTurns ? x : here;
     }
+    if (kTurns && !second) meet();
     // ---- results
 #pragma unroll
     for (int u = 0; u < QB; ++u) {
