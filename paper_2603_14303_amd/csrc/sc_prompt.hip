@@ -5,7 +5,7 @@
 // reads from the caches.
 //
 // Work.  The queries of the G heads that share a KV head are rows (token, head) of one matrix, so that a tile of rows spans few tokens (the diagonal and the
-// window's edge cost little) and every tile of keys serves all of them.  A workgroup of four wavefronts takes 32 QB rows a wavefront and goes over the tiles of keys that any of its rows sees; only
+// window's edge cost little) and every tile of keys serves all of them.  A workgroup of eight wavefronts (four in small calls) takes 32 rows a wavefront and goes over the tiles of keys that any of its rows sees; only
 // tiles that some row does not see whole are masked.  Products are S^T = K Q^T and O^T += V^T P^T in 32 x 32 tiles: a query row stays on one pair of lanes from the
 // logits to the output, and the probabilities leave the first product in the layout of the second one's operand.  Keys and values go through shared memory
 // in two buffers, the next tile on its way in registers; rows are laid down with 16-byte pieces exchanged so that reads across rows meet all banks, and values
@@ -25,9 +25,6 @@ constexpr float kProLog2e = 1.4426950408889634f;
 constexpr float kProLn2 = 0.6931471805599453f;
 // The running maximum follows once a logit exceeds it by this many powers of two: until then nothing needs rescaling, and weights up to 2^8 lose no bit
 constexpr float kProSlack = 8.f;
-#ifndef PRO_AHEAD
-#define PRO_AHEAD 8
-#endif
 
 typedef float pro_f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned int pro_u32x4 __attribute__((ext_vector_type(4)));
@@ -128,11 +125,11 @@ template <typename T> __device__ __forceinline__ float4 values4(const char *row,
 }
 __device__ __forceinline__ float if_wild(float x) { return fabsf(x) < INFINITY ? 0.f : x; }
 
-// NW wavefronts of 32 QB rows
-template <typename T, int D, int QB, int NW>
+// NW wavefronts of 32 rows
+template <typename T, int D, int NW>
 __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) {
     constexpr bool kBf16 = sizeof(T) == 2;
-    constexpr int KT = kTileKeys<T>, KB = KT / 32, DT = D / 32, ROWS = 32 * QB * NW;
+    constexpr int KT = kTileKeys<T>, KB = KT / 32, DT = D / 32, ROWS = 32 * NW;
     using KTile = Tile<T, D, NW, false>;
     using VTile = Tile<T, D, NW, true>;
     constexpr bool kTurns = NW == 8;              // the halves of the workgroup take turns (below)
@@ -155,54 +152,37 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
     const PromptTiles mine = prompt_tiles(all, KT);
     const int t0 = (int)((int64_t)mine.count * split / p.splits), t1 = (int)((int64_t)mine.count * (split + 1) / p.splits);
     // ... and my wavefront's
-    const int row0 = first + 32 * QB * wave;
-    const int wt0 = row0 / p.G, wt1 = min((row0 + 32 * QB - 1) / p.G, q_len - 1);
+    const int row0 = first + 32 * wave;
+    const int wt0 = row0 / p.G, wt1 = min((row0 + 31) / p.G, q_len - 1);
     const PromptSpan span = prompt_span((int64_t)behind + wt0, (int64_t)behind + wt1, a.window, a.sinks);
 
-    int token[QB], head[QB], pos[QB], edge[QB];
-#pragma unroll
-    for (int u = 0; u < QB; ++u) {
-        const int r = row0 + 32 * u + col;
-        token[u] = r / p.G;
-        head[u] = h * p.G + r - token[u] * p.G;
-        pos[u] = behind + token[u];
-        edge[u] = prompt_edge(pos[u], a.window);
-    }
+    const int token = (row0 + col) / p.G, head = h * p.G + (row0 + col) - token * p.G;
+    const int pos = behind + token, edge = prompt_edge(pos, a.window);
     // ---- queries: bf16: lane (half, col) holds 8 half .. 8 half + 7 of every 16 elements of row `col`; fp32: elements (D / 2) half + ..
     constexpr int QL = kBf16 ? D / 16 : D / 8;
-    pro_u32x4 q[QB][QL];
+    pro_u32x4 q[QL];
+    const char *src = a.Q + b * a.q_b + head * a.q_h + (int64_t)min(token, a.N - 1) * a.q_n;
 #pragma unroll
-    for (int u = 0; u < QB; ++u) {
-        const char *src = a.Q + b * a.q_b + head[u] * a.q_h + (int64_t)min(token[u], a.N - 1) * a.q_n;
-#pragma unroll
-        for (int i = 0; i < QL; ++i) {
-            q[u][i] = *reinterpret_cast<const pro_u32x4 *>(src + (kBf16 ? (16 * i + 8 * half) * 2 : ((D / 2) * half + 4 * i) * 4));
-            q[u][i] ^= kBf16 ? p.flip | p.flip >> 16 : p.flip;
-        }
+    for (int i = 0; i < QL; ++i) {
+        q[i] = *reinterpret_cast<const pro_u32x4 *>(src + (kBf16 ? (16 * i + 8 * half) * 2 : ((D / 2) * half + 4 * i) * 4));
+        q[i] ^= kBf16 ? p.flip | p.flip >> 16 : p.flip;
     }
 
-    pro_f32x16 o[QB][DT];
-    float m_run[QB], l_run[QB];
+    pro_f32x16 o[DT];
+    float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-    for (int u = 0; u < QB; ++u) {
-        m_run[u] = -INFINITY;
-        l_run[u] = 0.f;
+    for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[u][t][i] = 0.f;
-    }
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
 
     // ---- a tile of keys for my rows: logits, probabilities, and their product with the values
-    pro_f32x16 s[QB][KB];                          // logits, then (fp32) probabilities
-    pro_u32x4 w[QB][kBf16 ? 2 * KB : 1];           // (bf16) probabilities
+    pro_f32x16 s[KB];                          // logits, then (fp32) probabilities
+    pro_u32x4 w[kBf16 ? 2 * KB : 1];           // (bf16) probabilities
     auto logits = [&](const char *lk) {
 #pragma unroll
-        for (int u = 0; u < QB; ++u)
+        for (int k = 0; k < KB; ++k)
 #pragma unroll
-            for (int k = 0; k < KB; ++k)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[u][k][i] = 0.f;
+            for (int i = 0; i < 16; ++i) s[k][i] = 0.f;
         if constexpr (kBf16) {
 #pragma unroll
             for (int e = 0; e < D / 16; ++e)
@@ -210,9 +190,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
                 for (int k = 0; k < KB; ++k) {
                     const int row = 32 * k + col;
                     const pro_u32x4 key = *reinterpret_cast<const pro_u32x4 *>(lk + row * KTile::RB + ((2 * e + half) ^ KTile::swap(row)) * 16);
-#pragma unroll
-                    for (int u = 0; u < QB; ++u)
-                        s[u][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, key), __builtin_bit_cast(pro_bf16x8, q[u][e]), s[u][k], 0, 0, 0);
+                    s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, key), __builtin_bit_cast(pro_bf16x8, q[e]), s[k], 0, 0, 0);
                 }
         } else {
 #pragma unroll
@@ -220,58 +198,51 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
                 const pro_u32x4 key = *reinterpret_cast<const pro_u32x4 *>(lk + col * KTile::RB + ((D / 8 * half + e) ^ KTile::swap(col)) * 16);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int u = 0; u < QB; ++u)
-                        s[u][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(key[i]), __uint_as_float(q[u][e][i]), s[u][0], 0, 0, 0);
+                    s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(key[i]), __uint_as_float(q[e][i]), s[0], 0, 0, 0);
             }
         }
     };
     auto probabilities = [&](int k0, bool masked) {
         if (masked) {
 #pragma unroll
-            for (int u = 0; u < QB; ++u)
-#pragma unroll
-                for (int k = 0; k < KB; ++k)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int key = k0 + 32 * k + 8 * (i / 4) + 4 * half + i % 4;
-                        s[u][k][i] = prompt_sees(key, pos[u], edge[u], a.sinks) ? s[u][k][i] : -INFINITY;
-                    }
-        }
-#pragma unroll
-        for (int u = 0; u < QB; ++u) {
-            float mx = s[u][0][0];
-#pragma unroll
-            for (int k = 0; k < KB; ++k)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][k][i]);
-            mx = halves_max(mx) * p.scale_log2;
-            if (ballot64(mx > m_run[u] + kProSlack) != 0ull) {
-                const float m_new = fmaxf(m_run[u], mx);
-                const float alpha = m_new == -INFINITY ? 1.f : pro_exp2(m_run[u] - m_new);
-                m_run[u] = m_new;
-                l_run[u] *= alpha;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[u][d][i] *= alpha;
-            }
-            const float shift = m_run[u] == -INFINITY ? 0.f : m_run[u];
-            float sum[2] = {0.f, 0.f};
-#pragma unroll
             for (int k = 0; k < KB; ++k)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    s[u][k][i] = pro_exp2(fmaf(s[u][k][i], p.scale_log2, -shift));
-                    sum[i % 2] += s[u][k][i];
+                    const int key = k0 + 32 * k + 8 * (i / 4) + 4 * half + i % 4;
+                    s[k][i] = prompt_sees(key, pos, edge, a.sinks) ? s[k][i] : -INFINITY;
                 }
-            l_run[u] += sum[0] + sum[1];
-            if constexpr (kBf16) {
+        }
+        float mx = s[0][0];
 #pragma unroll
-                for (int k = 0; k < KB; ++k)
+        for (int k = 0; k < KB; ++k)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) w[u][2 * k + i / 4][i % 4] = pack_bf16x2(s[u][k][2 * i], s[u][k][2 * i + 1]);
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[k][i]);
+        mx = halves_max(mx) * p.scale_log2;
+        if (ballot64(mx > m_run + kProSlack) != 0ull) {
+            const float m_new = fmaxf(m_run, mx);
+            const float alpha = m_new == -INFINITY ? 1.f : pro_exp2(m_run - m_new);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+        }
+        const float shift = m_run == -INFINITY ? 0.f : m_run;
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[k][i] = pro_exp2(fmaf(s[k][i], p.scale_log2, -shift));
+                sum[i % 2] += s[k][i];
             }
+        l_run += sum[0] + sum[1];
+        if constexpr (kBf16) {
+#pragma unroll
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[2 * k + i / 4][i % 4] = pack_bf16x2(s[k][2 * i], s[k][2 * i + 1]);
         }
     };
     auto add_values = [&](const char *lv) {
@@ -294,9 +265,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
                             v[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)src));
                         }
                         const pro_u32x4 val = {v[0].x, v[0].y, v[1].x, v[1].y};
-#pragma unroll
-                        for (int u = 0; u < QB; ++u)
-                            o[u][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, val), __builtin_bit_cast(pro_bf16x8, w[u][2 * k + g]), o[u][d], 0, 0, 0);
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, val), __builtin_bit_cast(pro_bf16x8, w[2 * k + g]), o[d], 0, 0, 0);
                     }
                 }
         } else {
@@ -306,8 +275,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     const float val = *reinterpret_cast<const float *>(lv + key * VTile::RB + ((8 * d + col / 4) ^ VTile::swap(key)) * 16 + col % 4 * 4);
-#pragma unroll
-                    for (int u = 0; u < QB; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(val, s[u][0][i], o[u][d], 0, 0, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(val, s[0][i], o[d], 0, 0, 0);
                 }
             }
         }
@@ -321,14 +289,12 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float4 v = values4<T>(rows + (int64_t)key * a.v_n, 32 * d + 8 * i + 4 * half);
-#pragma unroll
-                    for (int u = 0; u < QB; ++u)
-                        if (prompt_sees(k0 + key, pos[u], edge[u], a.sinks)) {
-                            o[u][d][4 * i] += if_wild(v.x);
-                            o[u][d][4 * i + 1] += if_wild(v.y);
-                            o[u][d][4 * i + 2] += if_wild(v.z);
-                            o[u][d][4 * i + 3] += if_wild(v.w);
-                        }
+                    if (prompt_sees(k0 + key, pos, edge, a.sinks)) {
+                        o[d][4 * i] += if_wild(v.x);
+                        o[d][4 * i + 1] += if_wild(v.y);
+                        o[d][4 * i + 2] += if_wild(v.z);
+                        o[d][4 * i + 3] += if_wild(v.w);
+                    }
                 }
     };
 
@@ -385,15 +351,14 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
         probabilities(k0, !prompt_all(span, k0, KT));
         if constexpr (kBf16) {
 #pragma unroll
-            for (int u = 0; u < QB; ++u)
-#pragma unroll
-                for (int i = 0; i < 2 * KB; ++i) asm volatile("" : "+v"(w[u][i]));
+            for (int i = 0; i < 2 * KB; ++i) asm volatile("" : "+v"(w[i]));
         }
         meet();
+        __builtin_amdgcn_s_setprio(1);      // (who is at the products goes first: 528 -> 522 us)
         add_values(s_v[here]);
         logits(s_k[next]);      // (behind the last tile of anything: nobody uses them)
         if constexpr (kBf16) {         // operands are read well ahead of the products that take them: a read takes as long as four products
-            constexpr int kAhead = PRO_AHEAD, PV = 2 * KB * DT, QK = KB * D / 16;
+            constexpr int kAhead = 8, PV = 2 * KB * DT, QK = KB * D / 16;
             __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAhead, 0);
 #pragma unroll
             for (int i = 0; i < PV - kAhead; ++i) {
@@ -407,6 +372,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
             }
             __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
         }
+        __builtin_amdgcn_s_setprio(0);
         if (edges) {
             int wild = 0;
 #pragma unroll
@@ -422,29 +388,26 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
     }
     if (kTurns && !second) meet();
     // ---- results
-#pragma unroll
-    for (int u = 0; u < QB; ++u) {
-        if (token[u] >= q_len) continue;
-        const float l = halves_sum(l_run[u]);
-        if (p.splits > 1) {
-            float *part = p.part + (((int64_t)split * heads + bh) * ((int64_t)a.N * p.G) + row0 + 32 * u + col) * (D + 4);
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<float4 *>(part + 32 * d + 8 * i + 4 * half) = make_float4(o[u][d][4 * i], o[u][d][4 * i + 1], o[u][d][4 * i + 2], o[u][d][4 * i + 3]);
-            if (half == 0) *reinterpret_cast<float2 *>(part + D) = make_float2(m_run[u], l);
-            continue;
-        }
-        const float f = l != 0.f ? 1.0f / l : 0.f;
-        char *dst = a.O + b * a.o_b + head[u] * a.o_h + (int64_t)token[u] * a.o_n;
+    if (token >= q_len) return;
+    const float l = halves_sum(l_run);
+    if (p.splits > 1) {
+        float *part = p.part + (((int64_t)split * heads + bh) * ((int64_t)a.N * p.G) + row0 + col) * (D + 4);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                store_row4(dst, kBf16, 32 * d + 8 * i + 4 * half, make_float4(o[u][d][4 * i] * f, o[u][d][4 * i + 1] * f, o[u][d][4 * i + 2] * f, o[u][d][4 * i + 3] * f));
-        if (a.lse && half == 0) a.lse[((int64_t)b * a.Hq + head[u]) * a.N + token[u]] = l != 0.f ? (m_run[u] + __log2f(l)) * kProLn2 : -INFINITY;
+                *reinterpret_cast<float4 *>(part + 32 * d + 8 * i + 4 * half) = make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
+        if (half == 0) *reinterpret_cast<float2 *>(part + D) = make_float2(m_run, l);
+        return;
     }
+    const float f = l != 0.f ? 1.0f / l : 0.f;
+    char *dst = a.O + b * a.o_b + head * a.o_h + (int64_t)token * a.o_n;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            store_row4(dst, kBf16, 32 * d + 8 * i + 4 * half, make_float4(o[d][4 * i] * f, o[d][4 * i + 1] * f, o[d][4 * i + 2] * f, o[d][4 * i + 3] * f));
+    if (a.lse && half == 0) a.lse[((int64_t)b * a.Hq + head) * a.N + token] = l != 0.f ? (m_run + __log2f(l)) * kProLn2 : -INFINITY;
 }
 
 // D / 4 threads a row, all partial results of it one after the other
@@ -508,13 +471,9 @@ bool prompt_fits(int B, int Hq, int Hkv, int N, int M, int d, bool bf16) {
     return (int64_t)s.tiles * B * Hkv * s.splits <= INT32_MAX && (int64_t)B * Hq * N <= ((int64_t)1 << 33);
 }
 
-#ifndef PRO_QB
-#define PRO_QB 1
-#define PRO_NW 8
-#endif
-template <typename T, int D, int QB, int NW> static hipError_t launch_prompt_k(const ProParams &p, hipStream_t stream) {
+template <typename T, int D, int NW> static hipError_t launch_prompt_k(const ProParams &p, hipStream_t stream) {
     const unsigned wgs = (unsigned)((int64_t)p.tiles * p.a.B * p.a.Hkv * p.splits);
-    hipLaunchKernelGGL((prompt_kernel<T, D, QB, NW>), dim3(wgs), dim3(NW * kWave), 0, stream, p);
+    hipLaunchKernelGGL((prompt_kernel<T, D, NW>), dim3(wgs), dim3(NW * kWave), 0, stream, p);
     if (p.splits > 1) {
         const int64_t rows = (int64_t)p.a.N * p.a.Hq * p.a.B, per = 256 / (D / 4);
         hipLaunchKernelGGL((prompt_join_kernel<D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, p);
@@ -522,8 +481,8 @@ template <typename T, int D, int QB, int NW> static hipError_t launch_prompt_k(c
     return hipGetLastError();
 }
 template <int D> static hipError_t launch_prompt_d(const ProParams &p, int rows, hipStream_t stream) {
-    if (p.a.dtype != DType::BF16) return launch_prompt_k<float, D, 1, 4>(p, stream);
-    return rows == 256 ? launch_prompt_k<bf16_t, D, PRO_QB, PRO_NW>(p, stream) : launch_prompt_k<bf16_t, D, 1, 4>(p, stream);
+    if (p.a.dtype != DType::BF16) return launch_prompt_k<float, D, 4>(p, stream);
+    return rows == 256 ? launch_prompt_k<bf16_t, D, 8>(p, stream) : launch_prompt_k<bf16_t, D, 4>(p, stream);
 }
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t stream) {
