@@ -576,7 +576,7 @@ sc_status sc_paged_reserve(int32_t *table, int sequences, int table_len, int num
  *   window, sinks   as for sc_paged_window_attn
  *   scale           0 selects 1/sqrt(d)
  *   lse             device f32 [B, Hq, N], contiguous, or NULL.  A query that sees no key (pos < 0) gives O = 0 and lse = -inf
- *   ws              sc_prompt_attn_workspace_bytes bytes; needs no initialisation
+ *   ws              sc_prompt_attn_workspace_bytes bytes, of this call or of one with more sequences, queries or keys; needs no initialisation
  * A row that a query does not see may hold anything.  An element of V that is not finite, of a row that the query sees, makes that element of O infinite or NaN.
  * Host errors: NULL or misaligned pointers, sizes <= 0, strides that are negative or no multiples, window or sinks < 0 (SC_ERR_INVALID_ARG); d not in {64, 128}, bad dtype, Hq no multiple of Hkv,
  * B or Hq > 65535, N * Hq / Hkv or M > 2^30, rows of K or V 32 MiB apart (SC_ERR_UNSUPPORTED).

@@ -423,17 +423,32 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(ProParams p) {
     if (token >= (a.q_lens ? min(max(a.q_lens[b], 0), a.N) : a.N)) return;
     const float *part = p.part + i * (D + 4);
     const int64_t next = all * (D + 4);
-    float m = -INFINITY;
-    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, part[s * next + D]);
-    const float shift = m == -INFINITY ? 0.f : m;
+    constexpr int PASS = 8;      // partial results whose loads are on their way together (those behind the last one read it again, and count for nothing)
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
-        const float2 ml = *reinterpret_cast<const float2 *>(part + s * next + D);
-        const float4 x = *reinterpret_cast<const float4 *>(part + s * next + e);
-        const float f = pro_exp2(ml.x - shift);
-        l = fmaf(ml.y, f, l);
-        o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+    float m = -INFINITY, l = 0.f;
+    for (int s0 = 0; s0 < p.splits; s0 += PASS) {
+        float2 ml[PASS];
+        float4 x[PASS];
+#pragma unroll
+        for (int t = 0; t < PASS; ++t) {
+            const float *from = part + min(s0 + t, p.splits - 1) * next;
+            ml[t] = *reinterpret_cast<const float2 *>(from + D);
+            x[t] = *reinterpret_cast<const float4 *>(from + e);
+        }
+        float m_new = m;
+#pragma unroll
+        for (int t = 0; t < PASS; ++t) m_new = fmaxf(m_new, ml[t].x);
+        const float shift = m_new == -INFINITY ? 0.f : m_new, keep = pro_exp2(m - shift);
+        o = make_float4(o.x * keep, o.y * keep, o.z * keep, o.w * keep);
+        l *= keep;
+        m = m_new;
+#pragma unroll
+        for (int t = 0; t < PASS; ++t) {
+            const float f = s0 + t < p.splits ? pro_exp2(ml[t].x - shift) : 0.f;
+            if (s0 + t >= p.splits) x[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+            l = fmaf(s0 + t < p.splits ? ml[t].y : 0.f, f, l);
+            o.x = fmaf(x[t].x, f, o.x); o.y = fmaf(x[t].y, f, o.y); o.z = fmaf(x[t].z, f, o.z); o.w = fmaf(x[t].w, f, o.w);
+        }
     }
     const float f = l != 0.f ? 1.0f / l : 0.f;
     store_row4(a.O + b * a.o_b + head * a.o_h + (int64_t)token * a.o_n, a.dtype == DType::BF16, e, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
@@ -447,24 +462,27 @@ struct ProShape {
 static ProShape prompt_shape(int B, int Hq, int Hkv, int N, int M, int d, bool bf16) {
     const int64_t G = Hq / Hkv, rows = (int64_t)N * G, heads = (int64_t)B * Hkv;
     ProShape s;
-    s.rows = bf16 && rows * heads >= 128 * 256 ? 256 : 128;
+    // Eight wavefronts take turns, four have a compute unit's other half for another workgroup.  512 tokens of 8 x 4 heads behind 16384 148 us with 256 rows, 219 with 128; 2048 tokens 61 and 69;
+    // but 64 tokens 12.5 and 9.5, 16 behind 32768 46 and 41
+    s.rows = bf16 && rows >= 1024 ? 256 : 128;
     s.tiles = (int)((rows + s.rows - 1) / s.rows);
-    // a workgroup for every compute unit, with eight tiles of keys each at least
-    const int64_t wgs = s.tiles * heads, most = (M + 511) / 512;
-    int64_t splits = wgs >= 192 ? 1 : 256 / wgs;
+    // A workgroup for every compute unit with eight tiles of keys each at least; fp32, whose products take eight times as long, two of them with two tiles (500 tokens of 2 x 2 heads 25.5 us, 88 with
+    // the former; the former with twice the splits: 1024 tokens of 8 x 4 heads 45 us, 33)
+    const int64_t wgs = s.tiles * heads, target = bf16 ? 256 : 512, most = bf16 ? (M + 511) / 512 : (M + 63) / 64;
+    int64_t splits = wgs >= target * 3 / 4 ? 1 : target / wgs;
     if (splits > most) splits = most;
     if (splits > 64) splits = 64;
     s.splits = splits < 1 ? 1 : (int)splits;
     return s;
 }
+// Enough for every call of up to so many sequences, queries and keys: splits x workgroups are no more than prompt_shape's targets, 256 of 256 rows or 512 of 128
 size_t prompt_workspace_bytes(int B, int Hq, int Hkv, int N, int M, int d) {
-    size_t most = 0;
-    for (int bf16 = 0; bf16 < 2; ++bf16) {
-        const ProShape s = prompt_shape(B, Hq, Hkv, N, M, d, bf16 != 0);
-        const size_t bytes = s.splits > 1 ? (size_t)s.splits * B * Hq * N * (d + 4) * sizeof(float) : 0;
-        if (bytes > most) most = bytes;
-    }
-    return align_up(most + 256, 256);
+    (void)Hkv;
+    const int64_t splits = (M + 63) / 64 < 64 ? (M + 63) / 64 : 64;
+    int64_t rows = (int64_t)B * Hq * N;
+    rows = rows < 65536 ? rows * splits : 65536;
+    if (rows > 65536) rows = 65536;
+    return align_up((size_t)rows * (d + 4) * sizeof(float), 256);
 }
 bool prompt_fits(int B, int Hq, int Hkv, int N, int M, int d, bool bf16) {
     const ProShape s = prompt_shape(B, Hq, Hkv, N, M, d, bf16);
