@@ -554,7 +554,7 @@ sc_status sc_paged8_decode_attn(const sc_paged8_cache *cache, const void *Q, sc_
  *                   with rows below base_lens that the table does not have (a sequence that is taken back behind its window): nothing is changed for these two.
  *                   No element in common with base_lens or new_lens (SC_ERR_INVALID_ARG)
  *   slots           device i32 [sequences, N] or NULL: page * page_rows + row of every new row, -1 behind new_lens and for sequences of length -1
- *   ws              sc_paged_reserve_workspace_bytes bytes, initialised ONCE with sc_paged_init_workspace
+ *   ws              sc_paged_reserve_workspace_bytes bytes; needs no initialisation
  * Host errors: NULL or misaligned pointers, sizes <= 0 (N < 0), window or sinks < 0, page_rows no power of two or out of range (SC_ERR_INVALID_ARG); sequences > 2^20, sequences * table_len > 2^28,
  * table_len * page_rows or num_pages * page_rows >= 2^31 (SC_ERR_UNSUPPORTED).
  */

@@ -835,15 +835,13 @@ def sc_paged8_decode_attn(cache: PagedCache8, Q, lens, window: int = 0, sinks: i
 
 # ------------------------------------------------------------------------------------------------ pages handed out on the GPU
 def paged_reserve_workspace(sequences: int, table_len: int, device) -> Workspace:
-    """Workspace of sc_paged_reserve for tables of `sequences` rows, initialised on the current stream."""
+    """Workspace of sc_paged_reserve for tables of `sequences` rows."""
     lib = load_library()
     _c_ints(sequences=sequences, table_len=table_len)
     nbytes = lib.sc_paged_reserve_workspace_bytes(int(sequences), int(table_len))
     if nbytes == 0:
         raise SemantiCacheError("no workspace for sequences=%d table_len=%d" % (sequences, table_len))
-    ws = Workspace(nbytes, device)
-    _check(lib.sc_paged_init_workspace(ws.ptr, ws.nbytes, _stream()), "sc_paged_init_workspace")
-    return ws
+    return Workspace(nbytes, device)
 
 
 def sc_paged_reserve(table, page_rows: int, base_lens, lens, free_pages, num_free, new_lens=None, N: Optional[int] = None, window: int = 0, sinks: int = 0,

@@ -6,9 +6,9 @@
 //     the k-th page taken, in the order of (s, p), is the k-th given back in that order, then the stack's top; what is given back and not taken goes on the stack, the last one
 //     first, so that a call that is followed by its opposite leaves the stack as it was.
 //
-// Two launches, bound by their chains of trips.  The first counts, a workgroup a sequence, and compacts what it gives back; the workgroup that ends last turns the counts into
-// places of all sequences.  The second applies them, a workgroup for 256 places, and writes the slots of the rows that lie in them.  The stack is only read where more is taken than
-// given back and only written where less is, so no workgroup waits for another.
+// Two launches, bound by their chains of trips.  The first counts, a workgroup a sequence, and compacts what it gives back.  The second applies, a workgroup for 256 places of a sequence: it adds up the
+// counts of the others by itself (of more than kResSelf sequences a launch between does, by one workgroup), knows the ranks of its places from them, and writes the slots of the rows that lie in them.  The stack is only
+// read where more is taken than given back and only written where less is, so no workgroup waits for another.
 #include "sc_paged.h"
 
 namespace sc {
@@ -16,12 +16,14 @@ namespace sc {
 constexpr int kResThreads = 256;      // places of a chunk
 constexpr int kResWaves = kResThreads / kWave;
 
-// workspace, behind the counters: per sequence {taken, given back} and their sums over the sequences before it (negative: the sequence is refused), per chunk the same within the sequence, the
-// pages given back by every sequence, and the call's totals
+constexpr int kResRows = 8;           // counts that a thread adds up
+constexpr int kResSelf = kResThreads * kResRows;
+
+// workspace: per sequence {taken, given back} (-1: refused) and, of many, their sums over the sequences before it; per chunk the same within the sequence; the call's totals (free pages at the start;
+// of many also given back and taken); the pages given back by every sequence
 struct ReserveSpace {
-    int *counter;
     int2 *count, *before, *chunk;
-    int *total;      // free pages at the start, given back, taken
+    int *total;
     int32_t *given;
 };
 static size_t reserve_layout(int S, int P, char *base, ReserveSpace &w) {
@@ -32,7 +34,6 @@ static size_t reserve_layout(int S, int P, char *base, ReserveSpace &w) {
         at = align_up(at + bytes, 256);
         return base + here;
     };
-    w.counter = reinterpret_cast<int *>(take(paged_state_bytes()));
     w.count = reinterpret_cast<int2 *>(take((size_t)S * sizeof(int2)));
     w.before = reinterpret_cast<int2 *>(take((size_t)S * sizeof(int2)));
     w.chunk = reinterpret_cast<int2 *>(take((size_t)S * chunks * sizeof(int2)));
@@ -79,25 +80,47 @@ __device__ __forceinline__ Ranks ranks(bool take, bool back, int lane, int wave,
     __syncthreads();
     return r;
 }
-__device__ __forceinline__ int2 load_agent(const int2 *p) {
-    const uint64_t x = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_int2((int)(uint32_t)x, (int)(uint32_t)(x >> 32));
+// Sums over the threads before this one, and over all of the workgroup
+struct Sums {
+    int2 before, all;
+};
+__device__ __forceinline__ Sums sums(int2 x, int lane, int wave, int2 *s_wave) {
+    const int2 incl = make_int2(wave_scan(x.x), wave_scan(x.y));
+    if (lane == kWave - 1) s_wave[wave] = incl;
+    __syncthreads();
+    Sums r = {make_int2(incl.x - x.x, incl.y - x.y), make_int2(0, 0)};
+#pragma unroll
+    for (int w = 0; w < kResWaves; ++w) {
+        const int2 n = s_wave[w];
+        if (w < wave) { r.before.x += n.x; r.before.y += n.y; }
+        r.all.x += n.x;
+        r.all.y += n.y;
+    }
+    __syncthreads();
+    return r;
 }
-__device__ __forceinline__ void store_agent(int2 *p, int2 x) {
-    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), (uint64_t)(uint32_t)x.y << 32 | (uint32_t)x.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ int wg_max(int x, int lane, int wave, int2 *s_wave) {      // x >= 0
+    x = wave_max(x);
+    if (lane == 0) s_wave[wave].x = x;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kResWaves; ++w) x = max(x, s_wave[w].x);
+    __syncthreads();
+    return x;
 }
 
 __global__ __launch_bounds__(kResThreads) void reserve_count_kernel(ReserveParams p) {
     const PagedReserveArgs &a = p.a;
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, s = blockIdx.x;
     __shared__ int2 s_wave[kResWaves];
-    __shared__ int s_last;
-    const Lengths n = lengths_of(a, s, p.log2_R);
     const int32_t *row = a.table + (int64_t)s * a.P;
+    int page = tid < a.P ? row[tid] : -1;      // (with the lengths)
+    const Lengths n = lengths_of(a, s, p.log2_R);
+    if (s == 0 && tid == 0) p.w.total[0] = min(max(a.num_free[0], 0), a.num_pages);
     int takes = 0, backs = 0, missing = 0;
     for (int c = 0; n.ok && c < p.chunks; ++c) {
         const int place = c * kResThreads + tid;
-        const int page = place < a.P ? row[place] : -1;
+        const int next = place + kResThreads < a.P ? row[place + kResThreads] : -1;
         const bool held = (unsigned)page < (unsigned)a.num_pages, want = place < a.P && paged_wants(place, p.log2_R, n.base, n.fresh, a.window, a.sinks);
         missing |= want && !held && ((int64_t)place << p.log2_R) < n.base;
         const Ranks r = ranks(want && !held, held && !want, lane, wave, s_wave);
@@ -105,96 +128,102 @@ __global__ __launch_bounds__(kResThreads) void reserve_count_kernel(ReserveParam
         if (held && !want) p.w.given[(int64_t)s * a.P + backs + r.back] = page;
         takes += r.takes;
         backs += r.backs;
+        page = next;
     }
     missing = __syncthreads_or(missing);
-    const bool fine = n.ok && !missing;
-    if (tid == 0) store_agent(p.w.count + s, fine ? make_int2(takes, backs) : make_int2(-1, 0));
-    // ---- the last workgroup: places of all sequences
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (its counts have arrived)
-    __syncthreads();
-    if (tid == 0) {
-        const int before = __hip_atomic_fetch_add(p.w.counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = before == a.S - 1;
-        if (s_last) __hip_atomic_store(p.w.counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __syncthreads();
-    if (!s_last) return;
-    __shared__ int2 s_sum[kResWaves];
-    const int free_pages = min(max(a.num_free[0], 0), a.num_pages);
-    int all_backs = 0;
+    if (tid == 0) p.w.count[s] = n.ok && !missing ? make_int2(takes, backs) : make_int2(-1, 0);
+}
+
+// more than kResSelf sequences: their places, by one workgroup
+__global__ __launch_bounds__(kResThreads) void reserve_scan_kernel(ReserveParams p) {
+    const PagedReserveArgs &a = p.a;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    __shared__ int2 s_wave[kResWaves];
+    int2 start = make_int2(0, 0);
     for (int s0 = 0; s0 < a.S; s0 += kResThreads) {
-        const int2 x = s0 + tid < a.S ? load_agent(p.w.count + s0 + tid) : make_int2(0, 0);
-        const int sum = __builtin_amdgcn_readlane(wave_scan(x.y), kWave - 1);
-        if (lane == 0) s_sum[wave].y = sum;
-        __syncthreads();
-        for (int w = 0; w < kResWaves; ++w) all_backs += s_sum[w].y;
-        __syncthreads();
+        const int s = s0 + tid;
+        const int2 x = s < a.S ? p.w.count[s] : make_int2(0, 0);
+        const Sums r = sums(make_int2(max(x.x, 0), x.y), lane, wave, s_wave);
+        if (s < a.S) p.w.before[s] = make_int2(start.x + r.before.x, start.y + r.before.y);
+        start.x += r.all.x;
+        start.y += r.all.y;
     }
-    const int available = (int)min((int64_t)free_pages + all_backs, (int64_t)INT32_MAX);
-    int taken = 0, given = 0, served = 0;      // of the sequences before; taken by those that are served
-    for (int s0 = 0; s0 < a.S; s0 += kResThreads) {
-        const int2 x = s0 + tid < a.S ? load_agent(p.w.count + s0 + tid) : make_int2(-1, 0);
-        const int mine = max(x.x, 0), t = wave_scan(mine), k = wave_scan(x.y);
-        if (lane == kWave - 1) s_sum[wave] = make_int2(t, k);
-        __syncthreads();
-        int2 start = make_int2(taken, given);
-        for (int w = 0; w < kResWaves; ++w) {
-            const int2 y = s_sum[w];
-            if (w < wave) { start.x += y.x; start.y += y.y; }
-            taken += y.x;
-            given += y.y;
-        }
-        const int through = start.x + t;
-        const bool gets = x.x == 0 || (x.x > 0 && through <= available);
-        if (gets && x.x > 0) served = max(served, through);
-        if (s0 + tid < a.S) {
-            const Lengths m = lengths_of(a, s0 + tid, p.log2_R);
-            // (pages go back all the same where there are none to take)
-            p.w.before[s0 + tid] = make_int2(x.x < 0 ? -1 : gets ? through - mine : -2, start.y + k - x.y);
-            a.lens[s0 + tid] = gets ? m.base + m.fresh : -1;
-        }
-        __syncthreads();
+    const int available = p.w.total[0] + start.y;
+    int taken = 0;
+    for (int s = tid; s < a.S; s += kResThreads) {
+        const int through = p.w.before[s].x + max(p.w.count[s].x, 0);      // (the thread's own)
+        if (through <= available) taken = max(taken, through);
     }
-    served = wave_max(served);
-    if (lane == 0) s_sum[wave].x = served;
-    __syncthreads();
+    taken = wg_max(taken, lane, wave, s_wave);
     if (tid == 0) {
-        for (int w = 0; w < kResWaves; ++w) served = max(served, s_sum[w].x);
-        p.w.total[0] = free_pages;
-        p.w.total[1] = all_backs;
-        p.w.total[2] = served;
-        a.num_free[0] = min(available - served, a.num_pages);      // (more only if tables name a page twice)
+        p.w.total[1] = start.y;
+        p.w.total[2] = taken;
     }
 }
 
-__global__ __launch_bounds__(kResThreads) void reserve_apply_kernel(ReserveParams p) {
+// SELF: the workgroup adds up the counts
+template <bool SELF> __global__ __launch_bounds__(kResThreads) void reserve_apply_kernel(ReserveParams p) {
     const PagedReserveArgs &a = p.a;
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const int s = blockIdx.x / p.chunks, c = blockIdx.x % p.chunks;
-    __shared__ int2 s_wave[kResWaves];
+    __shared__ int2 s_wave[kResWaves], s_mine;
     __shared__ int32_t s_page[kResThreads];
-    const Lengths n = lengths_of(a, s, p.log2_R);
-    const int2 before = p.w.before[s], chunk = p.w.chunk[(int64_t)s * p.chunks + c];
-    const int free_pages = p.w.total[0], backs = p.w.total[1], takes = p.w.total[2];
+    __shared__ int s_back[SELF ? kResSelf : 1];      // given back by the sequences before
     const int place = c * kResThreads + tid;
     int32_t *entry = a.table + (int64_t)s * a.P + place;
     const int page = place < a.P ? *entry : -1;
+    const Lengths n = lengths_of(a, s, p.log2_R);
+    const int2 count = p.w.count[s], chunk = p.w.chunk[(int64_t)s * p.chunks + c];
+    const int free_pages = p.w.total[0];
+    int2 before;
+    int backs, taken;
+    if constexpr (SELF) {
+        int2 x[kResRows], mine = make_int2(0, 0);
+#pragma unroll
+        for (int i = 0; i < kResRows; ++i) {
+            const int r = tid * kResRows + i;
+            x[i] = r < a.S ? p.w.count[r] : make_int2(0, 0);
+            x[i].x = max(x[i].x, 0);
+            mine.x += x[i].x;
+            mine.y += x[i].y;
+        }
+        const Sums r = sums(mine, lane, wave, s_wave);
+        backs = r.all.y;
+        int2 at = r.before;
+        taken = 0;
+#pragma unroll
+        for (int i = 0; i < kResRows; ++i) {
+            s_back[tid * kResRows + i] = at.y;
+            if (tid * kResRows + i == s) s_mine = at;
+            at.x += x[i].x;
+            at.y += x[i].y;
+            if (at.x <= free_pages + backs) taken = max(taken, at.x);
+        }
+        taken = wg_max(taken, lane, wave, s_wave);
+        before = s_mine;
+    } else {
+        before = p.w.before[s];
+        backs = p.w.total[1];
+        taken = p.w.total[2];
+    }
+    // (pages go back all the same where there are none to take)
+    const bool fine = count.x == 0 || (count.x > 0 && before.x + count.x <= free_pages + backs);
     int32_t now = page;
-    const bool fine = before.x >= 0;
-    if (n.ok && before.x != -1) {
+    if (count.x >= 0) {
         const bool held = (unsigned)page < (unsigned)a.num_pages, want = place < a.P && paged_wants(place, p.log2_R, n.base, n.fresh, a.window, a.sinks);
         const Ranks r = ranks(want && !held, held && !want, lane, wave, s_wave);
         if (want && !held && fine) {
             const int k = before.x + chunk.x + r.take;
             if (k < backs) {
                 // the sequence that gives the k-th back: the last one whose first is not behind it
+                auto first_of = [&](int q) { return SELF ? s_back[q] : p.w.before[q].y; };
                 int lo = 0, hi = a.S - 1;
                 while (lo < hi) {
                     const int mid = (lo + hi + 1) / 2;
-                    if (p.w.before[mid].y <= k) lo = mid;
+                    if (first_of(mid) <= k) lo = mid;
                     else hi = mid - 1;
                 }
-                now = p.w.given[(int64_t)lo * a.P + (k - p.w.before[lo].y)];
+                now = p.w.given[(int64_t)lo * a.P + (k - first_of(lo))];
             } else {
                 now = a.free_pages[free_pages - 1 - (k - backs)];
             }
@@ -202,23 +231,26 @@ __global__ __launch_bounds__(kResThreads) void reserve_apply_kernel(ReserveParam
         } else if (held && !want) {
             const int k = before.y + chunk.y + r.back;
             const int64_t to = (int64_t)free_pages + backs - 1 - k;
-            if (k >= takes && to < a.num_pages) a.free_pages[to] = page;
+            if (k >= taken && to < a.num_pages) a.free_pages[to] = page;      // (beyond the pool only if tables name a page twice)
             now = -1;
             *entry = -1;
         }
     }
+    if (c == 0 && tid == 0) {
+        a.lens[s] = fine ? n.base + n.fresh : -1;
+        if (s == 0) a.num_free[0] = (int)min((int64_t)free_pages + backs - taken, (int64_t)a.num_pages);
+    }
     if (!a.slots) return;
     s_page[tid] = now;
     __syncthreads();
-    const int total = fine && n.ok ? n.base + n.fresh : n.base;
     const int64_t first = (int64_t)c * kResThreads << p.log2_R, past = (int64_t)(c + 1) * kResThreads << p.log2_R;
     int32_t *slots = a.slots + (int64_t)s * a.N;
-    if (fine && n.ok) {
-        const int t1 = (int)min((int64_t)total, past);
+    if (fine) {
+        const int t1 = (int)min((int64_t)n.base + n.fresh, past);
         for (int64_t t = max((int64_t)n.base, first) + tid; t < t1; t += kResThreads)
             slots[t - n.base] = (s_page[(t >> p.log2_R) - c * kResThreads] << p.log2_R) + (int)(t & ((1 << p.log2_R) - 1));
     }
-    for (int64_t k = (fine && n.ok ? n.fresh : 0) + (int64_t)c * kResThreads + tid; k < a.N; k += (int64_t)p.chunks * kResThreads) slots[k] = -1;
+    for (int64_t k = (fine ? n.fresh : 0) + (int64_t)c * kResThreads + tid; k < a.N; k += (int64_t)p.chunks * kResThreads) slots[k] = -1;
 }
 
 hipError_t launch_paged_reserve(const PagedReserveArgs &a, void *ws, hipStream_t stream) {
@@ -228,7 +260,13 @@ hipError_t launch_paged_reserve(const PagedReserveArgs &a, void *ws, hipStream_t
     p.log2_R = __builtin_ctz((unsigned)a.R);
     p.chunks = (a.P + kResThreads - 1) / kResThreads;
     hipLaunchKernelGGL(reserve_count_kernel, dim3((unsigned)a.S), dim3(kResThreads), 0, stream, p);
-    hipLaunchKernelGGL(reserve_apply_kernel, dim3((unsigned)(a.S * p.chunks)), dim3(kResThreads), 0, stream, p);
+    const dim3 wgs((unsigned)(a.S * p.chunks));      // (at most S P <= 2^28)
+    if (a.S <= kResSelf) {
+        hipLaunchKernelGGL(reserve_apply_kernel<true>, wgs, dim3(kResThreads), 0, stream, p);
+    } else {
+        hipLaunchKernelGGL(reserve_scan_kernel, dim3(1), dim3(kResThreads), 0, stream, p);
+        hipLaunchKernelGGL(reserve_apply_kernel<false>, wgs, dim3(kResThreads), 0, stream, p);
+    }
     return hipGetLastError();
 }
 

@@ -97,6 +97,22 @@ def test_sequences_grow_step_by_step(S, P, R, window, sinks):
     assert len(both.stack) == S * P
 
 
+def test_more_sequences_than_a_workgroup_adds_up():
+    S = 2600
+    gen = torch.Generator().manual_seed(8)
+    both = Both(S, 3, 16, 3000, seed=8)
+    base = [0] * S
+    for step in range(4):      # growing, ending, some without room
+        new = torch.randint(0, 17, (S,), generator=gen).tolist()
+        gone = torch.rand(S, generator=gen) < 0.3
+        base = [0 if g else b for b, g in zip(base, gone.tolist())]
+        new = [min(n, 48 - b) for n, b in zip(new, base)]
+        lens = both.step(base, new, 16, slots=step % 2 == 1)
+        base = [b if n < 0 else n for b, n in zip(base, lens)]
+        # (a sequence that was not served and has given back everything keeps its rows' pages: base says which)
+    assert both.step([0] * S, [0] * S, 1) == [0] * S and len(both.stack) == 3000
+
+
 def test_a_call_and_its_opposite_leave_the_stack_as_it_was():
     both = Both(6, 30, 16, 100, seed=2)
     base = [100, 0, 37, 64, 5, 63]
