@@ -88,6 +88,12 @@ template <int NP> __device__ __forceinline__ void split_bf16(float x0, float x1,
     }
 }
 
+// Two rounded parts, off by 2^-17 of x: for numbers that end in a bf16 result
+__device__ __forceinline__ void split_bf16_rounded(float x0, float x1, uint32_t (&part)[2]) {
+    part[0] = pack_bf16x2(x0, x1);
+    part[1] = pack_bf16x2(x0 - bf16_lo(part[0]), x1 - bf16_hi(part[0]));
+}
+
 // What a wavefront holds of 16 rows: KL pieces of 16 bytes a lane of keys; VL registers of values per row of the lane.
 template <typename T, int D> struct Rows {
     static constexpr int KL = D * (int)sizeof(T) / 64;
@@ -275,15 +281,14 @@ __device__ __forceinline__ bool last_of(int *counter, int n, int tid, int *s_las
     return *s_last != 0;
 }
 
-// QP: parts of the queries (bf16 caches and codes).  WIN: a window and first rows that stay (p.window, p.sinks; codes always have it); p.sel is NULL then
-template <typename T, int D, int QP, bool WIN>
+// QP: parts of the queries (bf16 caches and codes).  WIN: a window and first rows that stay (p.window, p.sinks; codes always have it); p.sel is NULL then.  PP: parts of the probabilities (bf16 products)
+template <typename T, int D, int QP, bool WIN, int PP>
 __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecParams p) {
     constexpr bool kBf16 = sizeof(T) <= 2;     // products in bf16
     constexpr bool kCodes = sizeof(T) == 1;
     constexpr int NS = kSub<T>, kStep = sc::kStep<T>;
     constexpr int NM = kBf16 ? D / 32 : Rows<T, D>::KL;               // first products a row, pieces of 16 bytes of a query
     constexpr int KL = Rows<T, D>::KL, VW = Rows<T, D>::VW, NA = Acc<T, D>::N;
-    constexpr int PP = 3;                     // parts of the probabilities (bf16)
     constexpr int kStride = D + kPagPad;
     const PagedView &cv = p.c;
     const int G = p.G;
@@ -329,7 +334,7 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
     }
     const int most = paged_units(wave_max(longest), kStep);
     int per, multiple;
-    if (most <= kAlone && cv.B * cv.H <= p.wgs) {
+    if (most <= kAlone / NS && cv.B * cv.H <= p.wgs) {
         per = multiple = most;
         total = cv.B * cv.H * most;
     } else {
@@ -337,7 +342,7 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
         const int share = total <= p.wgs ? 1 : uniform((total + p.wgs - 1) / p.wgs);
         per = share;
         multiple = 1;
-        for (int t = share; share > 1 && t <= share + kMore; ++t) {
+        for (int t = share; share > 1 && t <= share + kMore / NS; ++t) {
             const float inverse = inverse_of(t);
             int parts = 0;
             for (int e0 = 0; e0 < entries; e0 += kWave) {
@@ -539,19 +544,25 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
                             part[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(dword_of(x[u].k[ks], i)), __uint_as_float(dword_of(q[0][ks], i)), part[i], 0, 0, 0);
                     sc = (part[0] + part[1]) + (part[2] + part[3]);
                 }
-                const int row = WIN ? row_of(cur, s, u) + 4 * g : 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float z = sc[i] * factor;
                     if (cv.counts) z = x[u].n[i] > 0 ? z + __log2f((float)x[u].n[i]) : -INFINITY;
-                    if (4 * g + i >= here[u]) z = -INFINITY;
-                    if constexpr (WIN) {
-                        if (!paged_visible(row + i, cur.len, p.window, p.sinks)) {
-                            z = -INFINITY;
-                            nothing |= 1 << (4 * u + i);
-                        }
+                    if constexpr (!WIN) {
+                        if (4 * g + i >= here[u]) z = -INFINITY;
                     }
                     sv[4 * u + i] = z;
+                }
+                if constexpr (WIN) {      // few steps have rows that do not attend
+                    const int row = row_of(cur, s, u);
+                    if (!paged_whole(row, cur.len, p.window, p.sinks)) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (4 * g + i >= here[u] || !paged_visible(row + 4 * g + i, cur.len, p.window, p.sinks)) {
+                                sv[4 * u + i] = -INFINITY;
+                                nothing |= 1 << (4 * u + i);
+                            }
+                    }
                 }
                 // rows without weight: their values may be anything, and 0 times a NaN is one
                 if (cv.counts) {
@@ -595,7 +606,11 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
                 // goes to the probabilities, before they are split.
                 uint32_t part[4][PP];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) split_bf16<PP>(pi[2 * i] * vs[i / 2], pi[2 * i + 1] * vs[i / 2], part[i]);
+                for (int i = 0; i < 4; ++i) {
+                    const float p0 = pi[2 * i] * vs[i / 2], p1 = pi[2 * i + 1] * vs[i / 2];
+                    if constexpr (PP == 2) split_bf16_rounded(p0, p1, part[i]);
+                    else split_bf16<PP>(p0, p1, part[i]);
+                }
 #pragma unroll
                 for (int w = 0; w < VW; ++w) {
                     uint32_t col[NS][4];
@@ -740,7 +755,14 @@ size_t paged_state_bytes() { return align_up((size_t)4 * kMaxWgs * sizeof(int), 
 size_t paged_decode_bytes(int G, int d) { return align_up((size_t)2 * kMaxWgs * G * (d + kPagPad) * sizeof(float), 256); }
 
 template <typename T, int D, int QP, bool WIN> static hipError_t launch_k(const PagDecParams &p, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_decode_kernel<T, D, QP, WIN>), dim3((unsigned)p.wgs), dim3(kPagThreads), 0, stream, p);
+    // codes, bf16 results: two parts instead of three 83 -> 79 us for 32 x 4 heads of 8192 to 16384 rows, G = 7
+    if constexpr (sizeof(T) == 1) {
+        if (p.o_is_bf16) {
+            hipLaunchKernelGGL((paged_decode_kernel<T, D, QP, WIN, 2>), dim3((unsigned)p.wgs), dim3(kPagThreads), 0, stream, p);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((paged_decode_kernel<T, D, QP, WIN, 3>), dim3((unsigned)p.wgs), dim3(kPagThreads), 0, stream, p);
     return hipGetLastError();
 }
 template <typename T, int QP, bool WIN> static hipError_t launch_d(const PagDecParams &p, hipStream_t stream) {

@@ -88,6 +88,10 @@ constexpr PagedGap paged_gap(int len, int window, int sinks) {
     const int64_t at = ((int64_t)(sinks < len ? sinks : len) + 15) / 16 * 16, next = (int64_t)(len - window) / 16 * 16;
     return at < next ? PagedGap{(int)at, (int)(next - at)} : PagedGap{0, 0};
 }
+// all 16 rows from `row` on attend
+constexpr bool paged_whole(int row, int len, int window, int sinks) {
+    return (int64_t)row + 16 <= len && (window <= 0 || row >= (int64_t)len - window || (int64_t)row + 16 <= sinks);
+}
 // `len`, or 0 if none of the 16 rows from `row` (a multiple of 16) on is visible: their page is not looked up then
 constexpr int paged_window_len(int row, int len, int window, int sinks) {
     return window <= 0 || (int64_t)row + 16 > (int64_t)len - window || row < sinks ? len : 0;

@@ -155,6 +155,10 @@ int main() {
             bool some_seen = false;
             for (int i = row; i < std::min(row + 16, len); ++i) some_seen |= paged_visible(i, len, window, sinks);
             CHECK((paged_window_len(row, len, window, sinks) > 0) == some_seen);
+            bool all_seen = true;
+            for (int i = row; i < row + 16; ++i) all_seen &= paged_visible(i, len, window, sinks);
+            CHECK(!paged_whole(row, len, window, sinks) || all_seen);
+            CHECK(paged_whole(row, len, window, sinks) || !all_seen || (window > 0 && row < sinks && sinks < row + 16));
         }
         // steps that a launch reckons with
         if (window > 0) CHECK((long long)len - gap.rows <= (long long)window + sinks + 48);
