@@ -589,7 +589,7 @@ class PagedCache:
 
 
 def _keeps_numbers(cache) -> None:
-    if isinstance(cache, PagedCache8):      # (its description has another layout)
+    if isinstance(cache, PagedCache8):
         raise SemantiCacheError("a cache of 8-bit codes has calls of its own: sc_paged8_append, sc_paged8_decode_attn")
 
 
@@ -641,12 +641,12 @@ def sc_paged_append(cache: PagedCache, K, V, base_lens, lens, new_lens=None, cou
     positions [B] (None: base_lens) + n.  counts [B, Hkv, N]: sizes of the rows, for a cache with counts.
     """
     lib = load_library()
-    _keeps_numbers(cache)
     if _native is not None and K.is_cuda and (Q is None) == (Q_out is None):
         st = _native.paged_append(cache.ptr, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, _stream())
         if st >= 0:
             _check(st, "sc_paged_append")
             return lens, Q_out
+    _keeps_numbers(cache)
     r, Q_out = _paged_rows(cache, cache.K.dtype, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved)
     _check(lib.sc_paged_append(ctypes.byref(cache.struct), ctypes.byref(r), _stream()), "sc_paged_append")
     return lens, Q_out
@@ -693,12 +693,12 @@ def sc_paged_decode_attn(cache: PagedCache, Q, lens, scale: float = 0.0, O=None,
     With sel [B, Hkv, keep] and sel_lens [B, Hkv] (sc_paged_select) only the rows of those pages attend.
     """
     lib = load_library()
-    _keeps_numbers(cache)
     if _native is not None and Q.is_cuda and O is not None and workspace is not None and not (want_lse and lse is None):
         st = _native.paged_decode(cache.ptr, Q, lens, scale, O, lse, sel, sel_lens, workspace.ptr, workspace.nbytes, _stream())
         if st >= 0:
             _check(st, "sc_paged_decode_attn")
             return O, lse
+    _keeps_numbers(cache)
     workspace = _paged_query(cache, Q, lens, workspace)
     _require_cuda(sel, sel_lens)
     O, lse = _paged_outputs(Q, O, lse, want_lse)
@@ -719,12 +719,12 @@ def sc_paged_select(cache: PagedCache, Q, lens, keep: int, first: int = 1, recen
     """The `keep` pages of every (sequence, KV head) with the largest bounds on the logits of Q [B, Hq, d], its first `first` and last `recent`
     ones in any case -> (sel [B, Hkv, keep] ascending, -1 behind the last, sel_lens [B, Hkv])."""
     lib = load_library()
-    _keeps_numbers(cache)
     if _native is not None and Q.is_cuda and sel is not None and sel_lens is not None and workspace is not None:
         st = _native.paged_select(cache.ptr, Q, lens, keep, first, recent, sel, sel_lens, workspace.ptr, workspace.nbytes, _stream())
         if st >= 0:
             _check(st, "sc_paged_select")
             return sel, sel_lens
+    _keeps_numbers(cache)
     _c_ints(keep=keep, first=first, recent=recent)
     workspace = _paged_query(cache, Q, lens, workspace)
     _require_cuda(sel, sel_lens)
@@ -752,7 +752,7 @@ def _windowed(name, native, kind, cache, Q, lens, window, sinks, scale, O, lse, 
     if not isinstance(cache, kind):
         raise SemantiCacheError("%s takes a %s" % (name, kind.__name__))
     if _native is not None and Q.is_cuda and O is not None and workspace is not None and not (want_lse and lse is None):
-        st = getattr(_native, native)(cache.ptr, Q, lens, window, sinks, scale, O, lse, workspace.ptr, workspace.nbytes, _stream())
+        st = getattr(_native, native)(cache.ptr8 if kind is PagedCache8 else cache.ptr, Q, lens, window, sinks, scale, O, lse, workspace.ptr, workspace.nbytes, _stream())
         if st >= 0:
             _check(st, name)
             return O, lse
@@ -798,8 +798,13 @@ class PagedCache8:
             K=_ptr(K), V=_ptr(V), k_scale=_ptr(k_scale), v_scale=_ptr(v_scale), counts=_ptr(counts), table=_ptr(table),
             stride_page=K.stride(0), stride_head=K.stride(1), stride_row=K.stride(2), code=codes[K.dtype], block_rows=R // blocks, num_pages=pages,
             page_heads=heads, page_rows=R, table_len=table.shape[-1], table_per_head=int(table.dim() == 3), B=self.B, Hkv=self.Hkv, d=d)
-        self.ptr = ctypes.addressof(self.struct)
+        self.ptr8 = ctypes.addressof(self.struct)
         self._made = True
+
+    @property
+    def ptr(self):
+        """Of a PagedCache: this one's description has another layout."""
+        _keeps_numbers(self)
 
     _fixed = PagedCache._fixed
     __setattr__ = __delattr__ = _fixed
@@ -817,7 +822,7 @@ def sc_paged8_append(cache: PagedCache8, K, V, base_lens, lens, new_lens=None, c
     if not isinstance(cache, PagedCache8):
         raise SemantiCacheError("sc_paged8_append takes a PagedCache8")
     if _native is not None and K.is_cuda and (Q is None) == (Q_out is None):
-        st = _native.paged8_append(cache.ptr, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, _stream())
+        st = _native.paged8_append(cache.ptr8, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, _stream())
         if st >= 0:
             _check(st, "sc_paged8_append")
             return lens, Q_out
