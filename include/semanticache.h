@@ -501,7 +501,7 @@ sc_status sc_paged_window_attn(const sc_paged_cache *cache, const void *Q, sc_dt
  *               counts   as in sc_paged_cache
  *   block_rows           a power of two, 16 .. 128, page_rows at most
  * Everything else as in sc_paged_cache (there are no k_min and k_max).  Host errors as there, code unknown: SC_ERR_UNSUPPORTED,
- * block_rows out of range: SC_ERR_INVALID_ARG.
+ * block_rows out of range, scales of keys and values that share elements: SC_ERR_INVALID_ARG.
  */
 typedef enum { SC_E4M3 = 0, SC_I8 = 1 } sc_code;
 typedef struct {
@@ -529,7 +529,7 @@ typedef struct {
 sc_status sc_paged8_append(const sc_paged8_cache *cache, const sc_paged_rows *rows, sc_dtype kv_dtype, void *stream);
 
 /* sc_paged8_decode_attn — sc_paged_window_attn over such a cache (window 0: all rows attend).  Codes and their products with bf16 are exact; queries of
- * fp32 and probabilities enter as three bf16 parts, scales and sums are fp32.  Workspace as for sc_paged_decode_attn.
+ * fp32 and probabilities enter as three bf16 parts (for a bf16 O the probabilities as two, 2^-17 off), scales and sums are fp32.  Workspace as for sc_paged_decode_attn.
  */
 sc_status sc_paged8_decode_attn(const sc_paged8_cache *cache, const void *Q, sc_dtype q_dtype, int Hq,
                                 const int32_t *lens, int lens_per_head, int window, int sinks, float scale,
@@ -552,10 +552,10 @@ sc_status sc_paged8_decode_attn(const sc_paged8_cache *cache, const void *Q, sc_
  *   free_pages      device i32 [num_pages]: the stack;   num_free  device i32 [1]: how many it holds (taken as 0 .. num_pages)
  *   lens            device i32 [sequences]: base_lens + new_lens, or -1: not served (its rows get no pages; what it does not need has gone back), or lengths that are not possible, or a needed page
  *                   with rows below base_lens that the table does not have (a sequence that is taken back behind its window): nothing is changed for these two.
- *                   No element in common with base_lens or new_lens (SC_ERR_INVALID_ARG)
  *   slots           device i32 [sequences, N] or NULL: page * page_rows + row of every new row, -1 behind new_lens and for sequences of length -1
  *   ws              sc_paged_reserve_workspace_bytes bytes; needs no initialisation
- * Host errors: NULL or misaligned pointers, sizes <= 0 (N < 0), window or sinks < 0, page_rows no power of two or out of range (SC_ERR_INVALID_ARG); sequences > 2^20, sequences * table_len > 2^28,
+ * Host errors: NULL or misaligned pointers, arrays that are written and share elements with another one, sizes <= 0 (N < 0), window or sinks < 0, page_rows no power of two or out of range
+ * (SC_ERR_INVALID_ARG); sequences > 2^20, sequences * table_len > 2^28,
  * table_len * page_rows or num_pages * page_rows >= 2^31 (SC_ERR_UNSUPPORTED).
  */
 size_t sc_paged_reserve_workspace_bytes(int sequences, int table_len);

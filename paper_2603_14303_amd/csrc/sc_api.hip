@@ -450,6 +450,12 @@ static sc_status paged_check(const sc_paged_cache *c, PagedView &v, int64_t code
     return SC_OK;
 }
 
+// whether two arrays have no element in common (b may be NULL)
+static bool apart(const int32_t *a, int64_t na, const int32_t *b, int64_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return !b || x + na * sizeof(int32_t) <= y || y + nb * sizeof(int32_t) <= x;
+}
+
 // the same for the cache of the sc_paged8_* calls
 static sc_status paged8_check(const sc_paged8_cache *c, PagedView &v, Paged8View &w) {
     if (!c) return SC_ERR_INVALID_ARG;
@@ -461,6 +467,8 @@ static sc_status paged8_check(const sc_paged8_cache *c, PagedView &v, Paged8View
     const int E = c->block_rows;
     if (E < 16 || E > 128 || (E & (E - 1)) || E > c->page_rows) return SC_ERR_INVALID_ARG;
     if (!c->k_scale || !c->v_scale || !aligned4(c->k_scale) || !aligned4(c->v_scale)) return SC_ERR_INVALID_ARG;
+    const int64_t scales = (int64_t)c->num_pages * c->page_heads * (c->page_rows / E);
+    if (!apart(reinterpret_cast<const int32_t *>(c->k_scale), scales, reinterpret_cast<const int32_t *>(c->v_scale), scales)) return SC_ERR_INVALID_ARG;
     w.k_scale = c->k_scale; w.v_scale = c->v_scale;
     w.log2_block = __builtin_ctz((unsigned)E);
     w.code = c->code == SC_E4M3 ? 1 : 2;
@@ -473,12 +481,6 @@ static bool rows_ok(const void *p, int64_t B, int64_t H, int64_t N, int64_t sb, 
     for (int i = 0; i < 3; ++i)
         if (size[i] > 1 && (stride[i] < 0 || (stride[i] * es) % 16 || (written && stride[i] < d))) return false;
     return aligned16(p);
-}
-
-// whether two arrays have no element in common (b may be NULL)
-static bool apart(const int32_t *a, int64_t na, const int32_t *b, int64_t nb) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return !b || x + na * sizeof(int32_t) <= y || y + nb * sizeof(int32_t) <= x;
 }
 
 // the rows of sc_paged_append and sc_paged8_append (a.c is there already): K and V of elements of `es` bytes; a page, or a block, of `rows` rows is one workgroup's at most
@@ -687,9 +689,13 @@ sc_status sc_paged_reserve(int32_t *table, int sequences, int table_len, int num
     if (page_rows < 16 || page_rows > 1024 || (page_rows & (page_rows - 1))) return SC_ERR_INVALID_ARG;
     if (sequences > (1 << 20) || (int64_t)sequences * table_len > (1 << 28)) return SC_ERR_UNSUPPORTED;      // counted in 32 bits
     if ((int64_t)table_len * page_rows > INT32_MAX || (int64_t)num_pages * page_rows > INT32_MAX) return SC_ERR_UNSUPPORTED;      // rows and slots are 32-bit
-    // the second of two launches reads the old lengths again
+    // what is written is nothing else (the second of two launches reads the lengths again)
     const int64_t S = sequences;
-    if (!apart(lens, S, base_lens, S) || !apart(lens, S, new_lens, S)) return SC_ERR_INVALID_ARG;
+    const int32_t *array[7] = {table, lens, free_pages, num_free, N > 0 ? slots : nullptr, base_lens, new_lens};
+    const int64_t size[7] = {S * table_len, S, num_pages, 1, S * N, S, S};
+    for (int i = 0; i < 5; ++i)
+        for (int k = i + 1; k < 7; ++k)
+            if (array[i] && !apart(array[i], size[i], array[k], size[k])) return SC_ERR_INVALID_ARG;
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < paged_reserve_bytes(sequences, table_len)) return SC_ERR_WORKSPACE;
     const PagedReserveArgs a = {table, sequences, table_len, num_pages, page_rows, base_lens, new_lens, N, window, sinks, free_pages, num_free, lens, N > 0 ? slots : nullptr};
     return runtime_status(launch_paged_reserve(a, ws, static_cast<hipStream_t>(stream)));

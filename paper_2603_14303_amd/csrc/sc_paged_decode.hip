@@ -593,7 +593,15 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[k][i] *= al[i];
             }
+            // codes: with the values' scale, before they are split (a scale that is no number must not show where no row of its block attends)
+            float pv[4 * NS];
+#pragma unroll
+            for (int i = 0; i < 4 * NS; ++i) pv[i] = kCodes ? pi[i] * vs[i / 4] : pi[i];
             if (ballot64(nothing != 0) != 0ull) {
+                if constexpr (kCodes) {
+#pragma unroll
+                    for (int i = 0; i < 4 * NS; ++i) pv[i] = nothing >> i & 1 ? 0.f : pv[i];
+                }
 #pragma unroll
                 for (int u = 0; u < NS; ++u)
 #pragma unroll
@@ -602,14 +610,12 @@ __global__ __launch_bounds__(kPagThreads, 2) void paged_decode_kernel(PagDecPara
                         for (int k = 0; k < VW; ++k) x[u].v[i][k] = nothing >> (4 * u + i) & 1 ? 0u : x[u].v[i][k];
             }
             if constexpr (kCodes) {
-                // both 16 rows in one product: place 8 g + j of its inner dimension is row 4 g + j of the first 16, or 4 g + j - 4 of the second.  The values' scale
-                // goes to the probabilities, before they are split.
+                // both 16 rows in one product: place 8 g + j of its inner dimension is row 4 g + j of the first 16, or 4 g + j - 4 of the second
                 uint32_t part[4][PP];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float p0 = pi[2 * i] * vs[i / 2], p1 = pi[2 * i + 1] * vs[i / 2];
-                    if constexpr (PP == 2) split_bf16_rounded(p0, p1, part[i]);
-                    else split_bf16<PP>(p0, p1, part[i]);
+                    if constexpr (PP == 2) split_bf16_rounded(pv[2 * i], pv[2 * i + 1], part[i]);
+                    else split_bf16<PP>(pv[2 * i], pv[2 * i + 1], part[i]);
                 }
 #pragma unroll
                 for (int w = 0; w < VW; ++w) {

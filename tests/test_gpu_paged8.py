@@ -209,6 +209,26 @@ def test_a_block_whose_scale_is_no_number_shows_where_it_attends(code):
     assert O.isnan().all() and lse.isnan().all()
 
 
+@pytest.mark.parametrize("code", [E4, I8])
+def test_a_scale_that_is_no_number_does_not_show_where_no_row_of_its_block_has_weight(code):
+    """Rows of size 0 or less weigh nothing, whatever is theirs; rows outside the window neither."""
+    pc = Paged8(1, 1, 8, 32, 128, code, 16, per_head_table=True, counts=True, seed=15)
+    pc.fill([[200]])
+    t = torch.arange(48, 64)
+    page, head, row = pc.place(0, 0, t)
+    pc.counts[page, head, row] = torch.arange(16, dtype=torch.int32, device=DEV) % 3 - 2
+    Q, lens = torch.randn((1, 3, 128), device=DEV).to(BF), torch.tensor([[200]], dtype=torch.int32, device=DEV)
+    want = sc.sc_paged8_decode_attn(pc.cache(), Q, lens)[0]
+    pc.ks[page, head, row // 16] = math.nan
+    pc.vs[page, head, row // 16] = math.nan
+    assert want.isfinite().all() and (sc.sc_paged8_decode_attn(pc.cache(), Q, lens)[0] == want).all()
+    # a block whose last rows are behind the window, and the visible ones without weight
+    want = sc.sc_paged8_decode_attn(pc.cache(), Q, lens, window=200 - 56, sinks=8)[0]
+    pc.counts[page, head, row] = 1
+    pc.counts[page[8:], head, row[8:]] = 0
+    assert want.isfinite().all() and (sc.sc_paged8_decode_attn(pc.cache(), Q, lens, window=200 - 56, sinks=8)[0] == want).all()
+
+
 # ------------------------------------------------------------------------------------------------ appending
 def turned(x, cos, sin, rot, interleaved):
     """fp32, rounded product by product; x [N, d], cos and sin [N, rot / 2]."""

@@ -11,14 +11,14 @@ from test_paged_host import ARG, FAKE, ROWS, UNSUPPORTED, WORKSPACE, lib  # noqa
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
-CACHE8 = dict(K=FAKE, V=FAKE, k_scale=FAKE, v_scale=FAKE, counts=None, table=FAKE, stride_page=4 * 32 * 128, stride_head=32 * 128, stride_row=128, code=0,
+CACHE8 = dict(K=FAKE, V=FAKE, k_scale=FAKE, v_scale=FAKE + (1 << 20), counts=None, table=FAKE, stride_page=4 * 32 * 128, stride_head=32 * 128, stride_row=128, code=0,
               block_rows=16, num_pages=100, page_heads=4, page_rows=32, table_len=20, table_per_head=0, B=2, Hkv=4, d=128)
 BAD8 = [
     (dict(K=None), ARG), (dict(V=None), ARG), (dict(table=None), ARG), (dict(k_scale=None), ARG), (dict(v_scale=None), ARG), (dict(k_scale=FAKE + 2), ARG), (dict(K=FAKE + 8), ARG),
     (dict(B=0), ARG), (dict(Hkv=0), ARG), (dict(num_pages=0), ARG), (dict(table_len=0), ARG), (dict(page_rows=8), ARG), (dict(page_rows=48), ARG), (dict(page_rows=2048), ARG),
     (dict(page_heads=2), ARG), (dict(table_per_head=1), ARG), (dict(stride_row=64), ARG), (dict(stride_row=136), ARG), (dict(stride_head=128), ARG), (dict(stride_head=32 * 128 - 16), ARG),
     (dict(stride_page=3 * 32 * 128), ARG), (dict(block_rows=8), ARG), (dict(block_rows=24), ARG), (dict(block_rows=64), ARG), (dict(block_rows=0), ARG), (dict(block_rows=256, page_rows=256), ARG),
-    (dict(code=2), UNSUPPORTED), (dict(code=-1), UNSUPPORTED), (dict(d=96), UNSUPPORTED), (dict(B=70000), UNSUPPORTED), (dict(table_len=2**27), UNSUPPORTED),
+    (dict(v_scale=FAKE), ARG), (dict(v_scale=FAKE + 3196), ARG), (dict(code=2), UNSUPPORTED), (dict(code=-1), UNSUPPORTED), (dict(d=96), UNSUPPORTED), (dict(B=70000), UNSUPPORTED), (dict(table_len=2**27), UNSUPPORTED),
 ]
 
 
@@ -79,6 +79,8 @@ def test_reserve_rejects_bad_arguments(lib):  # noqa: F811
         assert call(**{name: -1}) == ARG, name
     assert call(page_rows=8) == ARG and call(page_rows=48) == ARG and call(page_rows=2048) == ARG
     assert call(lens=FAKE + 4096) == ARG and call(lens=FAKE + 8192) == ARG and call(lens=FAKE + 4096 + 36) == ARG
+    for a, b in (("many", "free"), ("many", "table"), ("free", "table"), ("lens", "many"), ("slots", "lens"), ("slots", "free"), ("base", "table"), ("new", "slots"), ("base", "many")):
+        assert call(**{a: good[b]}) == ARG, (a, b)
     assert call(sequences=(1 << 20) + 1) == UNSUPPORTED and call(sequences=1 << 20, table_len=1 << 9) == UNSUPPORTED
     assert call(table_len=1 << 26) == UNSUPPORTED and call(num_pages=1 << 26) == UNSUPPORTED
     assert call(ws=None) == WORKSPACE and call(ws=FAKE + 8) == WORKSPACE and call(nbytes=1000) == WORKSPACE
