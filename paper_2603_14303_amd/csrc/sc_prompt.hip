@@ -7,10 +7,13 @@
 // Work.  The queries of the G heads that share a KV head are rows (token, head) of one matrix, so that a tile of rows spans few tokens (the diagonal and the
 // window's edge cost little) and every tile of keys serves all of them.  A workgroup of eight wavefronts (four in small calls) takes 32 rows a wavefront and goes over the tiles of keys that any of its rows sees; only
 // tiles that some row does not see whole are masked.  Products are S^T = K Q^T and O^T += V^T P^T in 32 x 32 tiles: a query row stays on one pair of lanes from the
-// logits to the output, and the probabilities leave the first product in the layout of the second one's operand.  Keys and values go through shared memory
-// in two buffers, the next tile on its way in registers; rows are laid down with 16-byte pieces exchanged so that reads across rows meet all banks, and values
-// are read transposed (ds_read_b64_tr_b16).  Softmax is online, in the exp2 domain, its sums in fp32; probabilities enter the second product as bf16 (each off by 2^-8 at
+// logits to the output, and the probabilities leave the first product in the layout of the second one's operand.  Keys and values go straight to shared
+// memory (buffer_load .. lds), in three places (two in workgroups of four), the next tiles on their way; the 16-byte pieces of a row are exchanged so that reads across rows meet all banks, and values
+// are read transposed (ds_read_b64_tr_b16).  The halves of a workgroup of eight take turns: one is at the matrix cores while the other forms probabilities, a barrier a phase.  Softmax is online, in the exp2 domain, its sums in fp32; probabilities enter the second product as bf16 (each off by 2^-8 at
 // most, as the bf16 output is by itself; errors of many keys average out), in fp32 calls as they are (v_mfma_f32_32x32x2_f32).
+//
+// Measured (d = 128, bf16, 8 KV and 32 query heads): 8192 tokens 503 to 516 us (1.07 to 1.09 PFLOP/s; a library product of 8192^3 reaches 1.27), 16384 behind a window of 4096 922 to 942 (1.03 to 1.05): the matrix
+// cores are busy half of the cycles, and at that load the clock is at 2.0 GHz.  fp32, d = 64, 3 x 2 x 3 heads, up to 600 tokens: 32 to 36 us, 5 of it the second launch.
 //
 // Calls with few tiles of rows cut their keys into splits, whose partial results a second launch joins.
 #include <type_traits>
@@ -463,8 +466,9 @@ static ProShape prompt_shape(int B, int Hq, int Hkv, int N, int M, int d, bool b
     const int64_t G = Hq / Hkv, rows = (int64_t)N * G, heads = (int64_t)B * Hkv;
     ProShape s;
     // Eight wavefronts take turns, four have a compute unit's other half for another workgroup.  512 tokens of 8 x 4 heads behind 16384 148 us with 256 rows, 219 with 128; 2048 tokens 61 and 69;
-    // but 64 tokens 12.5 and 9.5, 16 behind 32768 46 and 41
-    s.rows = bf16 && rows >= 1024 ? 256 : 128;
+    // but 64 tokens 12.5 and 9.5, 16 behind 32768 46 and 41.  With few keys 128 rows are no slower as long as each compute unit has one workgroup at most: 512 and 1024 tokens of 8 x 4 heads 20.3 and
+    // 33.5 us, 22.6 and 37.6 with 256; but three times 400 tokens (312 workgroups) 20.2 and 19.0, 1024 behind 512 45.9 and 44.3, behind 2048 82 and 67
+    s.rows = bf16 && rows >= 1024 && (M > 1024 || (rows + 127) / 128 * heads > 256) ? 256 : 128;
     s.tiles = (int)((rows + s.rows - 1) / s.rows);
     // A workgroup for every compute unit with eight tiles of keys each at least; fp32, whose products take eight times as long, two of them with two tiles (500 tokens of 2 x 2 heads 25.5 us, 88 with
     // the former; the former with twice the splits: 1024 tokens of 8 x 4 heads 45 us, 33)

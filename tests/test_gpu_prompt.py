@@ -1,6 +1,6 @@
 """sc_prompt_attn on the GPU against a plain implementation in fp64.
 
-Tolerances (u = 2^-24; r = 2^-9, the rounding of a probability to bf16, or 0 in fp32 calls):
+Tolerances (u = 2^-24; r = 2^-8, the rounding of a probability to bf16, or 0 in fp32 calls):
   * a logit is a sum of d products in fp32, scaled: off by delta = (d + 16) u (sum_e |q_e k_e| |scale| + |logit|), so a weight by a factor exp(2 delta);
   * a weight enters the second product off by r of itself (bf16 has 7 bits behind the point: numbers of [1, 2) are 2^-7 apart,
     so a rounding is off by up to 2^-8 of 1, torch.finfo(bfloat16).eps / 2), while the denominator does not; sums over n keys: (n + 256) u.
@@ -113,6 +113,40 @@ def test_few_queries_behind_a_long_context(dtype, N, M):
 def test_many_tiles_of_rows():
     check(1, 4, 2, 4200, 4200, 128, BF, window=300, sinks=20)
     check(2, 4, 4, 2100, 2300, 64, BF, q_lens=[2100, 1999], kv_lens=[2300, 2000])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("N,M,G,window,sinks", [(257, 1025, 4, 0, 0), (300, 1100, 5, 64, 64), (1030, 1030, 1, 100, 130), (1024, 1089, 1, 1, 1), (130, 2500, 8, 700, 33), (600, 1026, 3, 0, 0)])
+def test_256_rows_a_workgroup(d, N, M, G, window, sinks):
+    """bf16 calls of at least 1024 rows a KV head over more than 1024 keys."""
+    check(1, 2, G, N, M, d, BF, window=window, sinks=sinks, seed=M)
+    check(3, 1, G, N, M, d, BF, q_lens=[N, 1, N - 100], kv_lens=[M, M - 70, N // 2], window=window, sinks=sinks, fused=False, seed=N)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (90, 0), (90, 70)])
+@pytest.mark.parametrize("N,M,G", [(600, 1090, 2), (150, 300, 2)])
+def test_numbers_that_are_not_finite_in_workgroups_of_either_size(N, M, G, window, sinks):
+    """Rows that do not see the number, and what is beside it in rows that see it in the values, are those of the formula, within the tolerance of any other call."""
+    d, gen = 64, torch.Generator().manual_seed(M)
+    Q, K, V = (torch.randn((1, h, n, d), generator=gen).to(BF) for h, n in ((G, N), (1, M), (1, M)))
+    want = [reference(Q[0, h].double(), K[0, 0].double(), V[0, 0].double(), window, sinks, 1 / math.sqrt(d), half_step(BF)) for h in range(G)]
+    seen = visible(N, M, window, sinks)
+    others = torch.arange(d) != 5
+    for which, value in (("V", math.nan), ("V", -math.inf), ("K", math.nan)):
+        for j in (0, 63, 64, M - N, M - N + 1, M - N + 128, M - 65, M - 1):
+            x = {"K": K.clone(), "V": V.clone()}
+            x[which][0, 0, j, 5] = value
+            O, _ = sc.sc_prompt_attn(Q.to(DEV), x["K"].to(DEV), x["V"].to(DEV), window=window, sinks=sinks)
+            hit = seen[:, j]
+            for h in range(G):
+                o, (wo, _, to, _) = O[0, h].cpu(), want[h]
+                tol = to + half_step(BF) * wo.abs() * (1 + 2.0**-6) + 1e-30
+                close(o[~hit], wo[~hit], tol[~hit])
+                if which == "V":
+                    assert not o[hit][:, 5].isfinite().any()
+                    close(o[hit][:, others], wo[hit][:, others], tol[hit][:, others])
+                else:
+                    assert o[hit].isnan().all()
 
 
 @pytest.mark.parametrize("scale", [0.7, -0.3, 1e-3])
