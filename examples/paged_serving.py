@@ -2,7 +2,7 @@
 
 Every layer keeps its keys and values in pages of a pool that all sequences share.
   prompt   sc_paged_append takes the fused projection as it is, rotates keys and queries and files the rows; attention inside the prompt is not
-           shown (any prefill kernel does it).
+           shown (sc_prompt_attn does it).
   token    sc_paged_append for the new token of every sequence, sc_paged_select keeps the pages that the query can attend to most, and
            sc_paged_decode_attn attends to those; or to all of them (--keep 0).
   merged   with --merge the prompt's cache is compressed first (sc_segment, sc_gsc_merge): every KV head of a sequence then has its own number of

@@ -15,6 +15,7 @@
 //
 // Measured (d = 128, bf16): 8 heads x 32768 rows, G = 4: 27.4 us (4.9 TB/s; 18 us of it the rows, 7.4 TB/s); 128 heads of 8192 to 16384 rows, G = 7: 128 us
 // from a graph (6.3 TB/s), 131 called one after another; 8 heads x 170 rows: 6.6 us, x 1 row 5.5, of which the launch is 1.8: arguments, lengths, page numbers, rows and the results' store follow each other.
+// 8-bit codes, the same ragged heads (4 of 32 sequences), G = 7, pages of 64 rows: e4m3 74 us (5.5 TB/s), int8 78, with fp32 queries 82; bound by instructions as much as by bytes.  A window of 4096 of bf16 rows, 256 heads, G = 4: 85 us (6.3 TB/s).
 #include <type_traits>
 
 #include "sc_paged.h"
@@ -761,7 +762,7 @@ size_t paged_state_bytes() { return align_up((size_t)4 * kMaxWgs * sizeof(int), 
 size_t paged_decode_bytes(int G, int d) { return align_up((size_t)2 * kMaxWgs * G * (d + kPagPad) * sizeof(float), 256); }
 
 template <typename T, int D, int QP, bool WIN> static hipError_t launch_k(const PagDecParams &p, hipStream_t stream) {
-    // codes, bf16 results: two parts instead of three 83 -> 79 us for 32 x 4 heads of 8192 to 16384 rows, G = 7
+    // codes, bf16 results: two parts instead of three and masks only in steps that are not whole: 81 -> 77 us together for 32 x 4 heads of 8192 to 16384 rows, G = 7
     if constexpr (sizeof(T) == 1) {
         if (p.o_is_bf16) {
             hipLaunchKernelGGL((paged_decode_kernel<T, D, QP, WIN, 2>), dim3((unsigned)p.wgs), dim3(kPagThreads), 0, stream, p);
