@@ -224,6 +224,15 @@ def _stream() -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _stream_of(*tensors) -> int:
+    """The current stream of the current device, for a call on tensors that have to live there: it is that device that launches."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise SemantiCacheError("all tensors must live on the current device (cuda:%d)" % device)
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def _require_cuda(*tensors) -> None:
     for t in tensors:
         if t is not None and not t.is_cuda:
@@ -752,15 +761,18 @@ def _windowed(name, native, kind, cache, Q, lens, window, sinks, scale, O, lse, 
     if not isinstance(cache, kind):
         raise SemantiCacheError("%s takes a %s" % (name, kind.__name__))
     if _native is not None and Q.is_cuda and O is not None and workspace is not None and not (want_lse and lse is None):
-        st = getattr(_native, native)(cache.ptr8 if kind is PagedCache8 else cache.ptr, Q, lens, window, sinks, scale, O, lse, workspace.ptr, workspace.nbytes, _stream())
+        st = getattr(_native, native)(cache.ptr8 if kind is PagedCache8 else cache.ptr, Q, lens, window, sinks, scale, O, lse, workspace.ptr, workspace.nbytes,
+                                      _stream_of(Q, cache.K, workspace.buf))
         if st >= 0:
             _check(st, name)
             return O, lse
     _c_ints(window=window, sinks=sinks)
+    _require_cuda(Q)
+    _stream_of(Q)      # (before a workspace is made)
     workspace = _paged_query(cache, Q, lens, workspace)
     O, lse = _paged_outputs(Q, O, lse, want_lse)
     st = getattr(lib, name)(ctypes.byref(cache.struct), _ptr(Q), _dtype_code(Q), Q.shape[1], _ptr(lens), int(lens.dim() == 2), int(window), int(sinks),
-                            float(scale), _ptr(O), _dtype_code(O), _ptr(lse), workspace.ptr, workspace.nbytes, _stream())
+                            float(scale), _ptr(O), _dtype_code(O), _ptr(lse), workspace.ptr, workspace.nbytes, _stream_of(Q, cache.K, cache.table, lens, O, lse, workspace.buf))
     _check(st, name)
     return O, lse
 
@@ -792,6 +804,8 @@ class PagedCache8:
                 k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or not k_scale.is_contiguous() or not v_scale.is_contiguous():
             raise SemantiCacheError("k_scale and v_scale must be float32 [pages, heads, R / block], contiguous")
         _require_cuda(K, V, k_scale, v_scale, table, counts)
+        if any(t is not None and t.get_device() != K.get_device() for t in (V, k_scale, v_scale, table, counts)):
+            raise SemantiCacheError("the tensors of a cache must live on one device")
         self.K, self.V, self.k_scale, self.v_scale, self.table, self.counts = K, V, k_scale, v_scale, table, counts
         self.B, self.Hkv, self.d = table.shape[0], table.shape[1] if table.dim() == 3 else heads, d
         self.struct = _Paged8CacheStruct(
@@ -822,12 +836,13 @@ def sc_paged8_append(cache: PagedCache8, K, V, base_lens, lens, new_lens=None, c
     if not isinstance(cache, PagedCache8):
         raise SemantiCacheError("sc_paged8_append takes a PagedCache8")
     if _native is not None and K.is_cuda and (Q is None) == (Q_out is None):
-        st = _native.paged8_append(cache.ptr8, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, _stream())
+        st = _native.paged8_append(cache.ptr8, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved, _stream_of(K, cache.K))
         if st >= 0:
             _check(st, "sc_paged8_append")
             return lens, Q_out
     r, Q_out = _paged_rows(cache, None, K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions, interleaved)
-    _check(lib.sc_paged8_append(ctypes.byref(cache.struct), ctypes.byref(r), _dtype_code(K), _stream()), "sc_paged8_append")
+    stream = _stream_of(K, cache.K, V, base_lens, lens, new_lens, counts, Q, Q_out, cos_sin, positions)
+    _check(lib.sc_paged8_append(ctypes.byref(cache.struct), ctypes.byref(r), _dtype_code(K), stream), "sc_paged8_append")
     return lens, Q_out
 
 
@@ -861,7 +876,7 @@ def sc_paged_reserve(table, page_rows: int, base_lens, lens, free_pages, num_fre
     if N is None:
         N = (slots.shape[-1] if slots.dim() else 0) if slots is not None else 1 if new_lens is None or want_slots else 2**31 - 1
     if _native is not None and table.is_cuda and workspace is not None and (slots is not None or not want_slots):
-        st = _native.paged_reserve(table, page_rows, base_lens, lens, free_pages, num_free, new_lens, N, window, sinks, slots, workspace.ptr, workspace.nbytes, _stream())
+        st = _native.paged_reserve(table, page_rows, base_lens, lens, free_pages, num_free, new_lens, N, window, sinks, slots, workspace.ptr, workspace.nbytes, _stream_of(table, workspace.buf))
         if st >= 0:
             _check(st, "sc_paged_reserve")
             return lens, slots
@@ -882,7 +897,8 @@ def sc_paged_reserve(table, page_rows: int, base_lens, lens, free_pages, num_fre
     if workspace is None:
         workspace = paged_reserve_workspace(S, P, table.device)
     st = lib.sc_paged_reserve(_ptr(table), S, P, free_pages.numel(), int(page_rows), _ptr(base_lens), _ptr(new_lens), int(N), int(window), int(sinks),
-                              _ptr(free_pages), _ptr(num_free), _ptr(lens), _ptr(slots), workspace.ptr, workspace.nbytes, _stream())
+                              _ptr(free_pages), _ptr(num_free), _ptr(lens), _ptr(slots), workspace.ptr, workspace.nbytes,
+                              _stream_of(table, base_lens, lens, new_lens, free_pages, num_free, slots, workspace.buf))
     _check(st, "sc_paged_reserve")
     return lens, slots
 
@@ -906,7 +922,7 @@ def sc_prompt_attn(Q, K, V, q_lens=None, kv_lens=None, window: int = 0, sinks: i
     """
     lib = load_library()
     if _native is not None and Q.is_cuda and O is not None and workspace is not None and not (want_lse and lse is None):
-        st = _native.prompt(Q, K, V, q_lens, kv_lens, window, sinks, scale, O, lse, workspace.ptr, workspace.nbytes, _stream())
+        st = _native.prompt(Q, K, V, q_lens, kv_lens, window, sinks, scale, O, lse, workspace.ptr, workspace.nbytes, _stream_of(Q, workspace.buf))
         if st >= 0:
             _check(st, "sc_prompt_attn")
             return O, lse
@@ -936,7 +952,7 @@ def sc_prompt_attn(Q, K, V, q_lens=None, kv_lens=None, window: int = 0, sinks: i
     for name, t in (("q", Q), ("k", K), ("v", V), ("o", O)):
         for axis, s in zip("bhn", t.stride()):
             setattr(x, "%s_stride_%s" % (name, axis), s)
-    _check(lib.sc_prompt_attn(ctypes.byref(x), workspace.ptr, workspace.nbytes, _stream()), "sc_prompt_attn")
+    _check(lib.sc_prompt_attn(ctypes.byref(x), workspace.ptr, workspace.nbytes, _stream_of(Q, K, V, q_lens, kv_lens, O, lse, workspace.buf)), "sc_prompt_attn")
     return O, lse
 
 

@@ -26,6 +26,11 @@ inline bool take(PyObject *o, const at::Tensor *&t) {
     return t->is_cuda();
 }
 inline bool take_some(PyObject *o, const at::Tensor *&t) { return take(o, t) && t != nullptr; }
+// whether the others live where `t` does
+template <typename... T> inline bool beside(const at::Tensor *t, const T *...others) {
+    const auto d = t->get_device();
+    return ((!others || others->get_device() == d) && ...);
+}
 inline int code(const at::Tensor &t) {
     switch (t.scalar_type()) {
         case at::kFloat: return SC_F32;
@@ -205,6 +210,7 @@ template <typename C> PyObject *append(PyObject *const *a, Py_ssize_t n) {
         const at::Tensor *K, *V, *base, *lens, *fresh, *counts, *Q, *Qo, *angles, *positions;
         if (n != 13 || !take_some(a[1], K) || !take_some(a[2], V) || !take_some(a[3], base) || !take_some(a[4], lens) || !take(a[5], fresh) || !take(a[6], counts)) return kNotTaken;
         if (!take(a[7], Q) || !take(a[8], Qo) || !take(a[9], angles) || !take(a[10], positions)) return kNotTaken;
+        if (codes && !beside(K, V, base, lens, fresh, counts, Q, Qo, angles, positions)) return kNotTaken;
         const auto *c = static_cast<const C *>(pointer(a[0]));
         const int turned = PyObject_IsTrue(a[11]);
         void *stream = pointer(a[12]);
@@ -294,7 +300,7 @@ PyObject *paged_select(PyObject *, PyObject *const *a, Py_ssize_t n) {
 template <typename C, typename F> PyObject *windowed(PyObject *const *a, Py_ssize_t n, F attend) {
     return guarded([&]() {
         const at::Tensor *Q, *lens, *O, *lse;
-        if (n != 11 || !take_some(a[1], Q) || !take_some(a[2], lens) || !take_some(a[6], O) || !take(a[7], lse)) return kNotTaken;
+        if (n != 11 || !take_some(a[1], Q) || !take_some(a[2], lens) || !take_some(a[6], O) || !take(a[7], lse) || !beside(Q, lens, O, lse)) return kNotTaken;
         const auto *c = static_cast<const C *>(pointer(a[0]));
         const long window = PyLong_AsLong(a[3]), sinks = PyLong_AsLong(a[4]);
         const double scale = PyFloat_AsDouble(a[5]);
@@ -323,7 +329,7 @@ PyObject *paged_reserve(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&]() {
         const at::Tensor *table, *base, *lens, *free_pages, *num_free, *fresh, *slots;
         if (n != 14 || !take_some(a[0], table) || !take_some(a[2], base) || !take_some(a[3], lens) || !take_some(a[4], free_pages) || !take_some(a[5], num_free)) return kNotTaken;
-        if (!take(a[6], fresh) || !take(a[10], slots)) return kNotTaken;
+        if (!take(a[6], fresh) || !take(a[10], slots) || !beside(table, base, lens, free_pages, num_free, fresh, slots)) return kNotTaken;
         const long rows = PyLong_AsLong(a[1]), N = PyLong_AsLong(a[7]), window = PyLong_AsLong(a[8]), sinks = PyLong_AsLong(a[9]);
         const size_t bytes = PyLong_AsSize_t(a[12]);
         void *w = pointer(a[11]), *stream = pointer(a[13]);
@@ -349,6 +355,7 @@ PyObject *prompt(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&]() {
         const at::Tensor *Q, *K, *V, *O, *ql, *kl, *lse;
         if (n != 13 || !take_some(a[0], Q) || !take_some(a[1], K) || !take_some(a[2], V) || !take(a[3], ql) || !take(a[4], kl) || !take_some(a[8], O) || !take(a[9], lse)) return kNotTaken;
+        if (!beside(Q, K, V, ql, kl, O, lse)) return kNotTaken;
         const long window = PyLong_AsLong(a[5]), sinks = PyLong_AsLong(a[6]);
         const double scale = PyFloat_AsDouble(a[7]);
         const size_t bytes = PyLong_AsSize_t(a[11]);

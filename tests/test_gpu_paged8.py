@@ -409,3 +409,29 @@ def test_append_reports_what_the_device_finds(code):
         a, b = got.cpu()[changed], was.cpu()[changed]
         assert ((a == b) | ((a != a) & (b != b))).all()
     assert (pc.K[page, 0, 14:].cpu() != before[0][page, 0, 14:].cpu()).any()
+
+
+def test_tensors_on_another_device_than_the_current_one_are_refused(monkeypatch):
+    """(The current device is said to be another one.)  With and without outputs and workspaces of the caller's; nothing is changed."""
+    pc, B, H, G, d = Paged8(2, 2, 3, 16, 64, E4, 16, seed=3), 2, 2, 2, 64
+    lens, one = torch.tensor([20, 5], dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV)
+    Q, X, P = torch.randn((B, H * G, d), device=DEV), torch.randn((B, H, 1, d), device=DEV), torch.randn((B, H * G, 3, d), device=DEV)
+    O, OP, out, slots = torch.full_like(Q, 7), torch.full_like(P, 7), torch.full_like(lens, 7), torch.full((2, 1), 7, dtype=torch.int32, device=DEV)
+    plain = sc.PagedCache(torch.zeros((pc.n, H, 16, d), device=DEV), torch.zeros((pc.n, H, 16, d), device=DEV), pc.table.to(DEV))
+    table, free = torch.full((2, 3), -1, dtype=torch.int32, device=DEV), torch.arange(4, dtype=torch.int32, device=DEV)
+    ws, wr, wp = sc.paged_workspace(B, H * G, H, d, 3, DEV), sc.paged_reserve_workspace(2, 3, DEV), sc.prompt_attn_workspace(B, H * G, H, 3, 1, d, DEV)
+    cache = pc.cache()
+    kept = [t.clone() for t in (pc.K, pc.ks.view(torch.int32), table, free)]
+    torch.cuda.synchronize()
+    with monkeypatch.context() as m:
+        m.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+        for call in (lambda: sc.sc_paged8_append(cache, X, X, lens, out), lambda: sc.sc_paged8_append(cache, X, X, lens, out, Q=X, cos_sin=torch.zeros((64, 64), device=DEV)),
+                     lambda: sc.sc_paged8_decode_attn(cache, Q, lens, O=O, workspace=ws), lambda: sc.sc_paged8_decode_attn(cache, Q, lens, want_lse=True, workspace=ws),
+                     lambda: sc.sc_paged_window_attn(plain, Q, lens, 4, O=O, workspace=ws), lambda: sc.sc_paged_window_attn(plain, Q, lens, 4, workspace=ws), lambda: sc.sc_paged_window_attn(plain, Q, lens, 4),
+                     lambda: sc.sc_paged_reserve(table, 16, lens, out, free, one, slots=slots, workspace=wr), lambda: sc.sc_paged_reserve(table, 16, lens, out, free, one),
+                     lambda: sc.sc_prompt_attn(P, X, X, O=OP, workspace=wp), lambda: sc.sc_prompt_attn(P, X, X)):
+            with pytest.raises(sc.SemantiCacheError, match="current device"):
+                call()
+    torch.cuda.synchronize()
+    assert all((t == 7).all() for t in (O, OP, out, slots)) and one.item() == 1
+    assert all(torch.equal(a, b) for a, b in zip(kept, (pc.K, pc.ks.view(torch.int32), table, free)))

@@ -267,3 +267,21 @@ def test_the_wrappers_refuse_what_does_not_fit(monkeypatch):
                 dict(Q=X.transpose(2, 3).contiguous().transpose(2, 3))):
         with pytest.raises(sc.SemantiCacheError):
             sc.sc_prompt_attn(**dict(dict(Q=X, K=K, V=K), **bad))
+
+
+def test_streams_are_those_of_the_device_that_holds_the_tensors(monkeypatch):
+    """Launches go to the current device: tensors anywhere else are refused (stand-ins, as there may be one device or none)."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device)
+
+    class On:
+        def __init__(self, device):
+            self.device = device
+
+        def get_device(self):
+            return self.device
+    assert sc._stream_of(On(1), None, On(1)) == 101
+    for tensors in ((On(0),), (On(1), On(0)), (On(1), None, On(-1))):
+        with pytest.raises(sc.SemantiCacheError, match="cuda:1"):
+            sc._stream_of(*tensors)
