@@ -12,7 +12,7 @@
 // are read transposed (ds_read_b64_tr_b16).  The halves of a workgroup of eight take turns: one is at the matrix cores while the other forms probabilities, a barrier a phase.  Softmax is online, in the exp2 domain, its sums in fp32; probabilities enter the second product as bf16 (each off by 2^-8 at
 // most, as the bf16 output is by itself; errors of many keys average out), in fp32 calls as they are (v_mfma_f32_32x32x2_f32).
 //
-// Measured (d = 128, bf16, 8 KV and 32 query heads): 8192 tokens 503 to 516 us (1.07 to 1.09 PFLOP/s; a library product of 8192^3 reaches 1.27), 16384 behind a window of 4096 922 to 942 (1.03 to 1.05): the matrix
+// Measured (d = 128, bf16, 8 KV and 32 query heads): 8192 tokens 503 to 524 us (1.05 to 1.09 PFLOP/s; a library product of 8192^3 reaches 1.27), 16384 behind a window of 4096 922 to 958 (1.01 to 1.05): the matrix
 // cores are busy half of the cycles, and at that load the clock is at 2.0 GHz.  fp32, d = 64, 3 x 2 x 3 heads, up to 600 tokens: 32 to 36 us, 5 of it the second launch.
 //
 // Calls with few tiles of rows cut their keys into splits, whose partial results a second launch joins.
