@@ -568,7 +568,7 @@ sc_status sc_paged_reserve(int32_t *table, int sequences, int table_len, int num
  * sc_prompt_attn — attention of a prompt's rows, or of a chunk of them behind a context, causal:
  *     O[b,hq,i] = softmax_j( Q[b,hq,i] . K[b,h,j] * scale ) V[b,h,j],   h = hq / (Hq / Hkv),   pos = kv_lens[b] - q_lens[b] + i,
  *     over j <= pos with  window = 0  or  j > pos - window  or  j < sinks.
- * (The queries are the last q_lens tokens of kv_lens.)  bf16: products of bf16 in fp32, probabilities rounded to bf16, sums and statistics in fp32; fp32: everything in fp32.
+ * (The queries are the last q_lens tokens of kv_lens.)  bf16: products of bf16 in fp32, probabilities as two bf16 parts (2^-17 off), sums and statistics in fp32; fp32: everything in fp32.
  *   Q, O            device [B, Hq, N, d] of dtype;  K, V  device [B, Hkv, M, d] of dtype; strides (b, h, n) of each in ELEMENTS, multiples of 16
  *                   bytes, the last dimension contiguous, 16-byte aligned; the rows of O do not overlap and share nothing with the inputs
  *   q_lens, kv_lens device i32 [B] or NULL (= N, = M), taken as 0 .. N and 0 .. M.  Rows of Q, K and V behind them are not looked at (they may hold anything), rows of O (and of

@@ -9,11 +9,11 @@
 // tiles that some row does not see whole are masked.  Products are S^T = K Q^T and O^T += V^T P^T in 32 x 32 tiles: a query row stays on one pair of lanes from the
 // logits to the output, and the probabilities leave the first product in the layout of the second one's operand.  Keys and values go straight to shared
 // memory (buffer_load .. lds), in three places (two in workgroups of four), the next tiles on their way; the 16-byte pieces of a row are exchanged so that reads across rows meet all banks, and values
-// are read transposed (ds_read_b64_tr_b16).  The halves of a workgroup of eight take turns: one is at the matrix cores while the other forms probabilities, a barrier a phase.  Softmax is online, in the exp2 domain, its sums in fp32; probabilities enter the second product as bf16 (each off by 2^-8 at
-// most, as the bf16 output is by itself; errors of many keys average out), in fp32 calls as they are (v_mfma_f32_32x32x2_f32).
+// are read transposed (ds_read_b64_tr_b16).  The halves of a workgroup of eight take turns: one is at the matrix cores while the other forms probabilities, a barrier a phase.  Softmax is online, in the exp2 domain, its sums in fp32; probabilities enter the second product as two
+// rounded bf16 parts, 2^-17 off, in fp32 calls as they are (v_mfma_f32_32x32x2_f32).  One part (the products take two thirds then, 8192 tokens 526 us instead of 690 to 705) would be 2^-8 off: that is a bf16 output's own rounding once more, 0.0020 of its norm instead of
+// 0.0016, and where many keys have one weight, all of them are rounded the same way and the output is no mean of the values any more.
 //
-// Measured (d = 128, bf16, 8 KV and 32 query heads): 8192 tokens 503 to 524 us (1.05 to 1.09 PFLOP/s; a library product of 8192^3 reaches 1.27), 16384 behind a window of 4096 922 to 958 (1.01 to 1.05): the matrix
-// cores are busy half of the cycles, and at that load the clock is at 2.0 GHz.  fp32, d = 64, 3 x 2 x 3 heads, up to 600 tokens: 32 to 36 us, 5 of it the second launch.
+// Measured (d = 128, bf16, 8 KV and 32 query heads): 8192 tokens 690 to 705 us (1.17 to 1.20 PFLOP/s with the products of the second part; a library product of 8192^3 reaches 1.27), 16384 behind a window of 4096 1270 (1.14).  fp32, d = 64, 3 x 2 x 3 heads, up to 600 tokens: 32 to 36 us, 5 of it the second launch.
 //
 // Calls with few tiles of rows cut their keys into splits, whose partial results a second launch joins.
 #include <type_traits>
@@ -132,7 +132,7 @@ __device__ __forceinline__ float if_wild(float x) { return fabsf(x) < INFINITY ?
 template <typename T, int D, int NW>
 __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) {
     constexpr bool kBf16 = sizeof(T) == 2;
-    constexpr int KT = kTileKeys<T>, KB = KT / 32, DT = D / 32, ROWS = 32 * NW;
+    constexpr int KT = kTileKeys<T>, KB = KT / 32, DT = D / 32, ROWS = 32 * NW, kParts = kBf16 ? 2 : 1;
     using KTile = Tile<T, D, NW, false>;
     using VTile = Tile<T, D, NW, true>;
     constexpr bool kTurns = NW == 8;              // the halves of the workgroup take turns (below)
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
 
     // ---- a tile of keys for my rows: logits, probabilities, and their product with the values
     pro_f32x16 s[KB];                          // logits, then (fp32) probabilities
-    pro_u32x4 w[kBf16 ? 2 * KB : 1];           // (bf16) probabilities
+    pro_u32x4 w[kParts][kBf16 ? 2 * KB : 1];   // (bf16) probabilities, in two parts
     auto logits = [&](const char *lk) {
 #pragma unroll
         for (int k = 0; k < KB; ++k)
@@ -245,7 +245,11 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
 #pragma unroll
             for (int k = 0; k < KB; ++k)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[2 * k + i / 4][i % 4] = pack_bf16x2(s[k][2 * i], s[k][2 * i + 1]);
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t hi = pack_bf16x2(s[k][2 * i], s[k][2 * i + 1]);
+                    w[0][2 * k + i / 4][i % 4] = hi;
+                    w[1][2 * k + i / 4][i % 4] = pack_bf16x2(s[k][2 * i] - bf16_lo(hi), s[k][2 * i + 1] - bf16_hi(hi));
+                }
         }
     };
     auto add_values = [&](const char *lv) {
@@ -268,7 +272,9 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
                             v[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)src));
                         }
                         const pro_u32x4 val = {v[0].x, v[0].y, v[1].x, v[1].y};
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, val), __builtin_bit_cast(pro_bf16x8, w[2 * k + g]), o[d], 0, 0, 0);
+#pragma unroll
+                        for (int x = kParts - 1; x >= 0; --x)
+                            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pro_bf16x8, val), __builtin_bit_cast(pro_bf16x8, w[x][2 * k + g]), o[d], 0, 0, 0);
                     }
                 }
         } else {
@@ -358,7 +364,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
         if (some) probabilities(k0, !prompt_all(span, k0, KT));
         if constexpr (kBf16) {
 #pragma unroll
-            for (int i = 0; i < 2 * KB; ++i) asm volatile("" : "+v"(w[i]));
+            for (int i = 0; i < 2 * KB; ++i) asm volatile("" : "+v"(w[0][i]), "+v"(w[1][i]));
         }
         meet();
         __builtin_amdgcn_s_setprio(1);      // (who is at the products goes first: 528 -> 522 us)
@@ -369,11 +375,16 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
             __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAhead, 0);
 #pragma unroll
             for (int i = 0; i < PV - kAhead; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, kParts, 0);
                 __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             }
 #pragma unroll
-            for (int i = 0; i < QK; ++i) {
+            for (int i = 0; i < kAhead; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, kParts, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < QK - kAhead; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
@@ -469,9 +480,9 @@ struct ProShape {
 static ProShape prompt_shape(int B, int Hq, int Hkv, int N, int M, int d, bool bf16) {
     const int64_t G = Hq / Hkv, rows = (int64_t)N * G, heads = (int64_t)B * Hkv;
     ProShape s;
-    // Eight wavefronts take turns, four have a compute unit's other half for another workgroup.  512 tokens of 8 x 4 heads behind 16384 148 us with 256 rows, 219 with 128; 2048 tokens 61 and 69;
-    // but 64 tokens 12.5 and 9.5, 16 behind 32768 46 and 41.  With few keys 128 rows are no slower as long as each compute unit has one workgroup at most: 512 and 1024 tokens of 8 x 4 heads 20.3 and
-    // 33.5 us, 22.6 and 37.6 with 256; but three times 400 tokens (312 workgroups) 20.2 and 19.0, 1024 behind 512 45.9 and 44.3, behind 2048 82 and 67
+    // Eight wavefronts take turns, four have a compute unit's other half for another workgroup.  512 tokens of 8 x 4 heads behind 16384 195 us with 256 rows, 277 with 128; 2048 tokens 78 and 79;
+    // but 64 tokens 13.0 and 9.8, 16 behind 32768 56 and 47.  With few keys 128 rows are no slower as long as each compute unit has one workgroup at most: 512 and 1024 tokens of 8 x 4 heads 23.1 and
+    // 38.8 us, 26.2 and 42.5 with 256; but 1024 behind 512 53.7 and 52.3, behind 2048 98 and 82 (three times 400 tokens, 312 workgroups, 23.3 and 23.5)
     s.rows = bf16 && rows >= 1024 && (M > 1024 || (rows + 127) / 128 * heads > 256) ? 256 : 128;
     s.tiles = (int)((rows + s.rows - 1) / s.rows);
     // A workgroup for every compute unit with eight tiles of keys each at least; fp32, whose products take eight times as long, two of them with two tiles (500 tokens of 2 x 2 heads 24 us, 88 with
