@@ -169,6 +169,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
     for (int i = 0; i < QL; ++i) {
         q[i] = *reinterpret_cast<const pro_u32x4 *>(src + (kBf16 ? (16 * i + 8 * half) * 2 : ((D / 2) * half + 4 * i) * 4));
         q[i] ^= kBf16 ? p.flip | p.flip >> 16 : p.flip;
+        if (token >= q_len) q[i] = pro_u32x4{0, 0, 0, 0};      // (the maxima of all rows of a wavefront follow together: what lies behind the last query must not say when)
     }
 
     pro_f32x16 o[DT];

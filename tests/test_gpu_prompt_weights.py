@@ -1,4 +1,4 @@
-"""The weights of sc_prompt_attn in bf16 calls keep 16 bits.
+"""The weights of sc_prompt_attn in bf16 calls keep 16 bits, and nothing of them depends on what lies behind the last query.
 
 Tolerances are those of test_gpu_prompt.py, with other numbers for a weight: it enters the second product as two bf16 numbers.  Of a weight of [1, 2) the first is off by 2^-8 at most (half
 of bf16's 2^-7 there); what is left, below 2^-8, by half of that range's 2^-16: r = 2^-17.  Two products a key are n more roundings of a sum: u each.
@@ -45,3 +45,22 @@ def test_equal_weights_that_are_no_power_of_two(N, d):
     V = numbers.repeat(d // 4).expand(1, H, N, d)
     O, _ = sc.sc_prompt_attn(*(x.to(BF).to(DEV) for x in (Q, K, V)), scale=1.0)
     assert (O.cpu().float() == V).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+@pytest.mark.parametrize("N,M,G", [(40, 600, 1), (330, 1200, 4)])
+def test_rows_behind_the_last_query_change_nothing(dtype, N, M, G):
+    """A wavefront has queries on both sides of the length: the same bits for those before it, whatever lies behind."""
+    gen = torch.Generator().manual_seed(N)
+    Q, K, V = (torch.randn((2, h, n, 128), generator=gen).to(dtype).to(DEV) for h, n in ((G, N), (1, M), (1, M)))
+    junk = torch.randn(Q.shape, generator=gen).to(dtype).to(DEV)
+    lens = (N - 20, N // 2 + 1)
+    q_lens = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    results = []
+    for factor in (0.0, 1.0, 50.0, math.inf, math.nan):
+        for b, n in enumerate(lens):
+            Q[b, :, n:] = junk[b, :, n:] * factor
+        O, L = sc.sc_prompt_attn(Q, K, V, q_lens=q_lens, O=torch.zeros_like(Q), lse=torch.zeros(Q.shape[:3], device=DEV))
+        results.append((O, L))
+    for O, L in results[1:]:
+        assert (O == results[0][0]).all() and (L == results[0][1]).all()
