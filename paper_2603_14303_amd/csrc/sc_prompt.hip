@@ -93,7 +93,8 @@ template <typename T, int D, int NW, bool VALUES> struct Tile {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int m0 = __builtin_amdgcn_readfirstlane((int)(to + (i * NW + wave) * 1024));
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m0), "v"(offset[i]), "s"(rs) : "memory");
+            // (m0 is the compiler's to write; five wait states for a descriptor that v_readfirstlane has just written, which it does not count into the text)
+            asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(m0), "v"(offset[i]), "s"(rs) : "memory");
         }
     }
     // The wavefront's own pieces, arrived: numbers that are not finite become zero.  Says whether there were any
