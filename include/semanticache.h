@@ -570,7 +570,7 @@ sc_status sc_paged_reserve(int32_t *table, int sequences, int table_len, int num
  *     over j <= pos with  window = 0  or  j > pos - window  or  j < sinks.
  * (The queries are the last q_lens tokens of kv_lens.)  bf16: products of bf16 in fp32, probabilities as two bf16 parts (2^-17 off), sums and statistics in fp32; fp32: everything in fp32.
  *   Q, O            device [B, Hq, N, d] of dtype;  K, V  device [B, Hkv, M, d] of dtype; strides (b, h, n) of each in ELEMENTS, multiples of 16
- *                   bytes, the last dimension contiguous, 16-byte aligned; the rows of O do not overlap and share nothing with the inputs
+ *                   bytes, the last dimension contiguous, 16-byte aligned; the rows of O do not overlap; O and lse share nothing with each other or with the inputs
  *   q_lens, kv_lens device i32 [B] or NULL (= N, = M), taken as 0 .. N and 0 .. M.  Rows of Q, K and V behind them are not looked at (they may hold anything), rows of O (and of
  *                   lse) behind them are left as they were
  *   window, sinks   as for sc_paged_window_attn
@@ -578,7 +578,7 @@ sc_status sc_paged_reserve(int32_t *table, int sequences, int table_len, int num
  *   lse             device f32 [B, Hq, N], contiguous, or NULL.  A query that sees no key (pos < 0) gives O = 0 and lse = -inf
  *   ws              sc_prompt_attn_workspace_bytes bytes, of this call or of one with more sequences, queries or keys; needs no initialisation
  * A row that a query does not see may hold anything.  An element of V that is not finite, of a row that the query sees, makes that element of O infinite or NaN.
- * Host errors: NULL or misaligned pointers, sizes <= 0, strides that are negative or no multiples, window or sinks < 0 (SC_ERR_INVALID_ARG); d not in {64, 128}, bad dtype, Hq no multiple of Hkv,
+ * Host errors: NULL or misaligned pointers, sizes <= 0, strides that are negative or no multiples, window or sinks < 0, rows that meet where they must not (SC_ERR_INVALID_ARG); d not in {64, 128}, bad dtype, Hq no multiple of Hkv,
  * B or Hq > 65535, N * Hq / Hkv or M > 2^30, rows of K or V 32 MiB apart (SC_ERR_UNSUPPORTED).
  */
 typedef struct {

@@ -6,6 +6,7 @@
 
 #include "sc_host.h"
 #include "sc_paged.h"
+#include "sc_rows_meet.h"
 #include <algorithm>
 #include <vector>
 
@@ -661,6 +662,15 @@ sc_status sc_prompt_attn(const sc_prompt *x, void *ws, size_t ws_bytes, void *st
     if (x->M > 1 && (x->k_stride_n * es > INT32_MAX / 64 || x->v_stride_n * es > INT32_MAX / 64)) return SC_ERR_UNSUPPORTED;      // offsets inside a tile of keys are 32-bit
     if (!prompt_fits(x->B, x->Hq, x->Hkv, x->N, x->M, x->d, x->dtype == SC_BF16)) return SC_ERR_UNSUPPORTED;
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < prompt_workspace_bytes(x->B, x->Hq, x->Hkv, x->N, x->M, x->d)) return SC_ERR_WORKSPACE;
+    // O and lse are nothing else (a workgroup reads queries, keys and values while others write)
+    auto rows = [&](const void *p, int heads, int n, int64_t sb, int64_t sh, int64_t sn) { return RowsAt{(uint64_t)(uintptr_t)p, {x->B, heads, n}, {sb * es, sh * es, sn * es}, x->d * es}; };
+    auto array = [](const void *p, int64_t bytes) { return RowsAt{(uint64_t)(uintptr_t)p, {1, 1, 1}, {0, 0, 0}, bytes}; };
+    const RowsAt O = rows(x->O, x->Hq, x->N, x->o_stride_b, x->o_stride_h, x->o_stride_n), lse = array(x->lse, (int64_t)x->B * x->Hq * x->N * 4);
+    const RowsAt inputs[5] = {rows(x->Q, x->Hq, x->N, x->q_stride_b, x->q_stride_h, x->q_stride_n), rows(x->K, x->Hkv, x->M, x->k_stride_b, x->k_stride_h, x->k_stride_n),
+                              rows(x->V, x->Hkv, x->M, x->v_stride_b, x->v_stride_h, x->v_stride_n), array(x->q_lens, (int64_t)x->B * 4), array(x->kv_lens, (int64_t)x->B * 4)};
+    if (x->lse && rows_meet(O, lse)) return SC_ERR_INVALID_ARG;
+    for (const RowsAt &i : inputs)
+        if (i.at && (rows_meet(O, i) || (x->lse && rows_meet(lse, i)))) return SC_ERR_INVALID_ARG;
     PromptArgs a;
     a.Q = static_cast<const char *>(x->Q); a.K = static_cast<const char *>(x->K); a.V = static_cast<const char *>(x->V);
     a.O = static_cast<char *>(x->O); a.lse = x->lse;
