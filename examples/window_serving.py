@@ -2,7 +2,7 @@
 
 Every layer attends to the newest `window` tokens and the first `sinks` ones, so a sequence holds a bounded number of pages however long it gets.
   pages    sc_paged_reserve gives every sequence the pages for the rows that arrive and takes back those that left its window; a request that ends
-           gives back all of them.  One table serves all layers.
+           gives back all of them.  A sequence that there is no page for waits with what it has, until a request ends.  One table serves all layers.
   prompt   sc_paged_append rotates keys and queries (filing the keys in an array of their own), sc_prompt_attn attends, and sc_paged8_append files the
            rows as 8-bit codes.
   token    sc_paged8_append and sc_paged8_decode_attn for the new token of every sequence.  The step is captured into a graph once: lengths, tables
@@ -41,11 +41,20 @@ class Pages:
         self.free = torch.arange(pages, dtype=torch.int32, device=device)
         self.many = torch.full((1,), pages, dtype=torch.int32, device=device)
         self.lens = torch.zeros(B, dtype=torch.int32, device=device)       # rows that the cache holds
-        self.next = torch.zeros_like(self.lens)                            # and will hold after the step; -1: no room for it
+        self.next = torch.zeros_like(self.lens)                            # and will hold after the step; -1: there is no page for it
         self.ws = sc.paged_reserve_workspace(B, P, device)
 
     def reserve(self, new):
         sc.sc_paged_reserve(self.table, R, self.lens, self.next, self.free, self.many, new_lens=new, window=self.window, sinks=self.sinks, workspace=self.ws)
+
+    def step(self, new):
+        """Pages for the step's rows -> which sequences there are some for, and for the layers the rows that the cache holds and those that arrive: none of one that waits."""
+        self.reserve(new)
+        served = self.next >= 0
+        return served, torch.where(served, self.lens, 0), torch.where(served, new, 0)
+
+    def done(self, served):
+        self.lens.copy_(torch.where(served, self.next, self.lens))
 
     def held(self) -> int:
         return int((self.table >= 0).sum())
@@ -88,10 +97,10 @@ class Layer:
         sc.sc_paged8_append(self.cache, K, V, zero, self.written, new_lens=new)
         return O.permute(0, 2, 1, 3).flatten(2) @ self.out
 
-    def token(self, x, new, cos_sin):
-        """x [B, 1, width] -> attention output [B, 1, width]; sequences with new = 0 are left alone."""
+    def token(self, x, base, new, cos_sin):
+        """x [B, 1, width] -> attention output [B, 1, width] of a token behind base [B] rows; sequences with new = 0 are left alone."""
         q, k, v = self.split(x)
-        _, q = sc.sc_paged8_append(self.cache, k, v, self.pages.lens, self.written, new_lens=new, Q=q, cos_sin=cos_sin)
+        _, q = sc.sc_paged8_append(self.cache, k, v, base, self.written, new_lens=new, Q=q, cos_sin=cos_sin)
         sc.sc_paged8_decode_attn(self.cache, q.flatten(1).unflatten(1, (-1, D)), self.written, window=self.pages.window, sinks=self.pages.sinks, O=self.O, workspace=self.ws)
         return (self.O.flatten(1) @ self.out)[:, None]
 
@@ -101,14 +110,19 @@ def normal(x):
 
 
 def serve(layers: int = 2, lens=(900, 200, 400, 31), tokens: int = 16, window: int = 128, sinks: int = 4, code: str = "e4m3", ends=None, width: int = 512, Hkv: int = 4,
-          G: int = 4, seed: int = 0, graph: bool = True, watch=None):
+          G: int = 4, seed: int = 0, graph: bool = True, watch=None, pool=None):
     """Prompts of the given lengths, then `tokens` steps; `ends` {step: sequence}: that request ends before the step.  watch(pages, step) is called after
-    the prompts (step -1) and every step.  Returns pages, layers and the last hidden states."""
+    the prompts (step -1) and every step.  pool: pages in all (None: as many as the sequences can need).  Returns pages, layers and the last hidden states."""
     dev = torch.device("cuda")
     gen = torch.Generator(dev).manual_seed(seed)
     B, N = len(lens), max(lens)
-    # the prompts' pages are held until the first token; from then on, what a window, the first tokens and a page at either edge need
-    pages = Pages(B, N + tokens, sum(-(-n // R) for n in lens) + B, window, sinks, dev)
+    # the prompts' pages are held until the first token; from then on all rows', or what the first tokens, a window and a page at its edge need
+    prompts, ends_at = sum(-(-n // R) for n in lens), [-(-(n + tokens) // R) for n in lens]
+    if pool is None:
+        pool = max(prompts, sum(min(n, -(-sinks // R) - (-window // R) + 1) if window else n for n in ends_at))
+    if pool < prompts:
+        raise ValueError("the prompts fill %d pages, the pool has %d" % (prompts, pool))
+    pages = Pages(B, N + tokens, pool, window, sinks, dev)
     cos_sin = angles(N + tokens, D, dev)
     model = [Layer(width, Hkv, G, pages, code, gen) for _ in range(layers)]
     new = torch.tensor(lens, dtype=torch.int32, device=dev)
@@ -123,12 +137,12 @@ def serve(layers: int = 2, lens=(900, 200, 400, 31), tokens: int = 16, window: i
     new.fill_(1)
 
     def step():
-        pages.reserve(new)
+        served, base, rows = pages.step(new)
         y = x
         for layer in model:
-            y = normal(y + layer.token(y, new, cos_sin))
-        x.copy_(y)
-        pages.lens.copy_(pages.next)
+            y = normal(y + layer.token(y, base, rows, cos_sin))
+        x.copy_(torch.where(served[:, None, None], y, x))
+        pages.done(served)
 
     captured = None
     for s in range(tokens):
