@@ -530,6 +530,7 @@ sc_status sc_paged8_append(const sc_paged8_cache *cache, const sc_paged_rows *ro
 
 /* sc_paged8_decode_attn — sc_paged_window_attn over such a cache (window 0: all rows attend).  Codes and their products with bf16 are exact; queries of
  * fp32 and probabilities enter as three bf16 parts (for a bf16 O the probabilities as two, 2^-17 off), scales and sums are fp32.  Workspace as for sc_paged_decode_attn.
+ * Products of a probability and a scale of values below 2^-126 lose bits: values below 1e-33 in all of a sequence are less exact (1e-5 of an fp32 O there, 2e-2 at 1e-37).
  */
 sc_status sc_paged8_decode_attn(const sc_paged8_cache *cache, const void *Q, sc_dtype q_dtype, int Hq,
                                 const int32_t *lens, int lens_per_head, int window, int sinks, float scale,

@@ -9,7 +9,7 @@
 // Bound by bytes: a row is read once, in its own type, and written as one byte an element.  One to four wavefronts take one block of one KV head and keep its new rows in
 // registers between the search for the largest number and the rounding.  No other workgroup touches the block, so nothing waits and nothing depends on an order.
 //
-// Measured (d = 128, from bf16): a prompt of 32768 tokens, 8 KV and 32 query heads: 145 to 153 us (5.2 TB/s; a copy: 5.3); a token of each of 64 sequences 5.3 us, of which the launch is 1.8: lengths, page, scale and store
+// Measured (d = 128, from bf16): a prompt of 32768 tokens, 8 KV and 32 query heads: 145 to 153 us by card (5.2 to 4.9 TB/s; a copy of 4 GiB: 5.3 to 4.9); a token of each of 64 sequences 5.3 us, of which the launch is 1.8: lengths, page, scale and store
 // follow each other.
 #include "sc_paged_rows.h"
 

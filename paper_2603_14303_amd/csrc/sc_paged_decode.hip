@@ -141,7 +141,6 @@ template <typename T, int D> __device__ __forceinline__ void load_values(Rows<T,
 }
 
 // ---- 8-bit codes as bf16, exactly (e4m3 has three bits behind the point, a whole number up to 128 seven): four codes of a dword in two dwords
-typedef __bf16 pag_bf16x2 __attribute__((ext_vector_type(2)));
 template <typename T> __device__ __forceinline__ uint2 widen4(uint32_t w) {
     if constexpr (std::is_same_v<T, e4m3_t>) {
         return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),

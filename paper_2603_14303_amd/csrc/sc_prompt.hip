@@ -5,15 +5,16 @@
 // reads from the caches.
 //
 // Work.  The queries of the G heads that share a KV head are rows (token, head) of one matrix, so that a tile of rows spans few tokens (the diagonal and the
-// window's edge cost little) and every tile of keys serves all of them.  A workgroup of eight wavefronts (four in small calls) takes 32 rows a wavefront and goes over the tiles of keys that any of its rows sees; only
+// window's edge cost little) and every tile of keys serves all of them.  A workgroup of eight wavefronts (four in small calls, and in fp32) takes 32 rows a wavefront and goes over the tiles of keys that any of its rows sees; only
 // tiles that some row does not see whole are masked.  Products are S^T = K Q^T and O^T += V^T P^T in 32 x 32 tiles: a query row stays on one pair of lanes from the
 // logits to the output, and the probabilities leave the first product in the layout of the second one's operand.  Keys and values go straight to shared
 // memory (buffer_load .. lds), in three places (two in workgroups of four), the next tiles on their way; the 16-byte pieces of a row are exchanged so that reads across rows meet all banks, and values
 // are read transposed (ds_read_b64_tr_b16).  The halves of a workgroup of eight take turns: one is at the matrix cores while the other forms probabilities, a barrier a phase.  Softmax is online, in the exp2 domain, its sums in fp32; probabilities enter the second product as two
-// rounded bf16 parts, 2^-17 off, in fp32 calls as they are (v_mfma_f32_32x32x2_f32).  One part (the products take two thirds then, 8192 tokens 526 us instead of 690 to 705) would be 2^-8 off: that is a bf16 output's own rounding once more, 0.0020 of its norm instead of
+// rounded bf16 parts, 2^-17 off, in fp32 calls as they are (v_mfma_f32_32x32x2_f32).  One part (the products take two thirds then, 8192 tokens 526 us instead of 705 on one card) would be 2^-8 off: that is a bf16 output's own rounding once more, 0.0020 of its norm instead of
 // 0.0016, and where many keys have one weight, all of them are rounded the same way and the output is no mean of the values any more.
 //
-// Measured (d = 128, bf16, 8 KV and 32 query heads): 8192 tokens 690 to 705 us (1.17 to 1.20 PFLOP/s with the products of the second part; a library product of 8192^3 reaches 1.27), 16384 behind a window of 4096 1270 (1.14).  fp32, d = 64, 3 x 2 x 3 heads, up to 600 tokens: 32 to 36 us, 5 of it the second launch.
+// Measured (d = 128, bf16, 8 KV and 32 query heads): 8192 tokens 690 to 730 us by card (1.13 to 1.20 PFLOP/s with the products of the second part; a library product of 8192^3 reaches 1.25 to 1.27), 16384 behind a window of 4096 1250 to 1310 (1.11 to 1.17): the matrix
+// cores are busy 60 % of the cycles, and at that load the clock is at 1.9 GHz.  d = 64: 8192 tokens 450, 2048 59.  fp32, d = 64, 3 x 2 x 3 heads, up to 600 tokens: 33 to 36 us, 5 of it the second launch.
 //
 // Calls with few tiles of rows cut their keys into splits, whose partial results a second launch joins.
 #include <type_traits>
@@ -336,7 +337,8 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
     //     second half   logits 0 in phase 1, probabilities t in phase 2 t + 2, products t in 2 t + 3
     // Keys t + 2 and values t + 1 are requested with probabilities t.  They take the places of keys t - 1 and values t - 2, which were last read in phase 2 t - 1, and are there by the end of phase
     // 2 t + 3: a half waits for what it has requested at the end of its phase of that number.
-    // With four wavefronts, one on each SIMD, nobody takes turns: all are the first half, the other workgroup of the compute unit is in the other phase or is not, and keys t and values t - 1 make room.
+    // With four wavefronts, one on each SIMD, nobody takes turns: all are the first half, and keys t and values t - 1 make room.  With d = 64 a second workgroup fits beside them, in the other phase or not; with d = 128 the
+    // compiler takes 290 registers (fp32: 348), and they are alone on a compute unit.
     const bool second = kTurns && wave >= NW / 2;
     auto meet = [&]() {      // (nothing of one phase is put off into the next one: the compiler would)
         __builtin_amdgcn_sched_barrier(0);
@@ -369,7 +371,7 @@ __global__ __launch_bounds__(NW *kWave, NW / 4) void prompt_kernel(ProParams p) 
             for (int i = 0; i < 2 * KB; ++i) asm volatile("" : "+v"(w[0][i]), "+v"(w[1][i]));
         }
         meet();
-        __builtin_amdgcn_s_setprio(1);      // (who is at the products goes first: 528 -> 522 us)
+        __builtin_amdgcn_s_setprio(1);      // (who is at the products goes first: 8192 tokens 528 -> 522 us, with probabilities in one part)
         if (some) add_values(s_v[here]);
         if (sees(t + 1)) logits(s_k[next]);      // (bf16: behind the last tile of anything: nobody uses them)
         if constexpr (kBf16) {         // operands are read well ahead of the products that take them: a read takes as long as four products
@@ -482,13 +484,13 @@ struct ProShape {
 static ProShape prompt_shape(int B, int Hq, int Hkv, int N, int M, int d, bool bf16) {
     const int64_t G = Hq / Hkv, rows = (int64_t)N * G, heads = (int64_t)B * Hkv;
     ProShape s;
-    // Eight wavefronts take turns, four have a compute unit's other half for another workgroup.  512 tokens of 8 x 4 heads behind 16384 195 us with 256 rows, 277 with 128; 2048 tokens 78 and 79;
-    // but 64 tokens 13.0 and 9.8, 16 behind 32768 56 and 47.  With few keys 128 rows are no slower as long as each compute unit has one workgroup at most: 512 and 1024 tokens of 8 x 4 heads 23.1 and
-    // 38.8 us, 26.2 and 42.5 with 256; but 1024 behind 512 53.7 and 52.3, behind 2048 98 and 82 (three times 400 tokens, 312 workgroups, 23.3 and 23.5)
+    // Eight wavefronts take turns, four do not, and have a compute unit to themselves with d = 128.  512 tokens of 8 x 4 heads behind 16384 198 us with 256 rows, 282 with 128; 2048 tokens 77 and 83;
+    // but 64 tokens 13.0 and 9.9, 16 behind 32768 52 and 49.  With few keys 128 rows are no slower as long as each compute unit has one workgroup at most: 512 and 1024 tokens of 8 x 4 heads 23.7 and
+    // 40.6 us, 25.8 and 42.3 with 256; but 1024 behind 512 56 and 52, behind 2048 103 and 82 (three times 400 tokens, 312 workgroups, 23.5 with either)
     s.rows = bf16 && rows >= 1024 && (M > 1024 || (rows + 127) / 128 * heads > 256) ? 256 : 128;
     s.tiles = (int)((rows + s.rows - 1) / s.rows);
     // A workgroup for every compute unit with eight tiles of keys each at least; fp32, whose products take eight times as long, two of them with two tiles (500 tokens of 2 x 2 heads 24 us, 88 with
-    // the former; with three or four chunks of a small model 40 to 43 us instead of 36; the former with twice the splits: 1024 tokens of 8 x 4 heads 45 us, 33)
+    // the former; with three or four chunks of a small model 40 to 43 us instead of 36; the former with twice the splits, when probabilities were in one part: 1024 tokens of 8 x 4 heads 45 us, 33)
     const int64_t wgs = s.tiles * heads, target = bf16 ? 256 : 512, most = bf16 ? (M + 511) / 512 : (M + 63) / 64;
     int64_t splits = wgs >= target * 3 / 4 ? 1 : target / wgs;
     if (splits > most) splits = most;
